@@ -1,0 +1,506 @@
+"""Operators that hold a longer context in the same memory, for timing: what they are, their inputs, one pass in elementary torch
+operations and one through the library, and the same in 64 bits.
+
+``quantise``  tokens of the cache to 4-bit records (E2M1 codes, a power-of-two scale for every 32 channels) and back
+``restore``   whole sequences from their records, as a prefill over an earlier context needs them
+``attend``    attention of one new token over the records, every page or a list of pages for each KV head
+``weigh``     attention over every page of a full-precision cache, which adds each page's share of it to an account
+``evict``     pages with the smallest account leave the page table, which closes up
+
+Layout of a page's record, for each KV head one after the other: K codes [S][D] two to a byte, even channel low; V codes
+[S/8][16][8][D/16]: in groups of eight tokens, and of D/16 channels; K scales [D/32][S]; V scales [D/32][S], both with the
+eight tokens of a group in the order 0 4 1 5 2 6 3 7.
+"""
+from __future__ import annotations
+
+import math
+import random
+import zlib
+
+import torch
+
+own = False
+
+DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+ORDER = (0, 4, 1, 5, 2, 6, 3, 7)
+LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _case(name, op, *, dtype="bf16", batch=1, q_heads=32, kv_heads=8, head_dim=128, page_size=16, context=32768, min_context=0,
+          tokens=0, top_k=0, budget=0, sinks=0, recent=1, decay=1.0):
+    case = dict(op=op, dtype=dtype, batch=batch, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page_size=page_size,
+                context=context, min_context=min_context or context, tokens=tokens, top_k=top_k, budget=budget, sinks=sinks,
+                recent=recent, decay=decay)
+    return dict(case, name=name) if name else case
+
+
+def listed():
+    return [
+        # the token that every sequence of a serving batch has just got
+        _case("quantise_append", "quantise", batch=32, context=32768, min_context=4096, tokens=1),
+        # a piece of a chunked prefill
+        _case("quantise_chunk", "quantise", batch=4, context=24_000, min_context=9_000, tokens=2048),
+        # an fp32 toy model's sessions of odd lengths
+        _case("restore_fp32", "restore", dtype="fp32", batch=3, q_heads=8, kv_heads=2, head_dim=64, page_size=8, context=2047, min_context=301),
+        # one session of 32K tokens that is to be prefilled further
+        _case("restore_32k", "restore"),
+        # a toy model: launch latency
+        _case("attend_tiny_fp32", "attend", dtype="fp32", q_heads=8, kv_heads=2, head_dim=64, context=2048),
+        # the headline batch, every page
+        _case("attend_batch_128k", "attend", batch=16, context=131072),
+        # the headline batch, the pages that a selection has found
+        _case("attend_list_128k", "attend", batch=16, context=131072, top_k=256),
+        # a 70B-shaped model (eight query heads to a KV head), mixed lengths, pages of 32 tokens
+        _case("attend_ragged", "attend", batch=12, q_heads=64, page_size=32, context=50_001, min_context=2_000),
+        # one chat session of 32K tokens
+        _case("weigh_one_32k", "weigh"),
+        # a serving batch of mixed lengths
+        _case("weigh_ragged", "weigh", batch=8, context=60_000, min_context=2_000, decay=0.95),
+        # a decode loop in which every sequence has just begun the page that is one too many
+        _case("evict_steady", "evict", batch=32, context=16 * 2049, budget=2048, sinks=1, recent=16),
+        # long prompts cut to an eighth
+        _case("evict_prompt", "evict", batch=16, context=131_001, budget=1024, sinks=4, recent=32),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng: random.Random):
+    """One more case of the ranges above. Padded to its longest sequence it holds at most the tokens of its kind's largest."""
+    most = {"quantise": 1 << 27, "restore": 1 << 27, "attend": 1 << 30, "weigh": 1 << 29, "evict": 1 << 31}  # K elements
+    largest = max(work(c)["bytes"] for c in listed())
+    while True:
+        op = rng.choice(sorted(most))
+        kv_heads = rng.choices([1, 2, 4, 8, 16, 32], [1, 1, 2, 5, 1, 1])[0]
+        group = rng.choices([1, 2, 4, 8], [2, 2, 4, 3])[0]
+        page = rng.choice([8, 16, 32])
+        context = _log_int(rng, 100, 200_000)
+        ragged = rng.random() < 0.6
+        pages = -(-context // page)
+        budget = _log_int(rng, 8, max(9, pages)) if op == "evict" else 0
+        case = _case(None, op, dtype=rng.choices(["bf16", "fp32"], [3, 1])[0], batch=_log_int(rng, 1, 64), q_heads=kv_heads * group,
+                     kv_heads=kv_heads, head_dim=rng.choices([64, 128], [1, 3])[0], page_size=page, context=context,
+                     min_context=max(1, int(context * rng.uniform(0.02, 0.9))) if ragged else context,
+                     tokens=_log_int(rng, 1, 4096) if op == "quantise" else 0,
+                     top_k=_log_int(rng, 4, 1024) if op == "attend" and rng.random() < 0.4 else 0, budget=budget,
+                     sinks=rng.choice([0, 1, 4]) if budget else 0, recent=rng.choice([1, 4]) if budget else 1,
+                     decay=rng.choice([1.0, 0.9]) if op == "weigh" else 1.0)
+        held = case["tokens"] + 2 * page if op == "quantise" else context
+        if case["q_heads"] > 128 or work(case)["bytes"] > largest:
+            continue
+        if case["batch"] * held * kv_heads * case["head_dim"] > most[op]:
+            continue
+        return case
+
+
+def _lengths(case):
+    """Sequence lengths, log-uniform between the case's bounds; they belong to the case, not to the seed."""
+    lo, hi, n = case["min_context"], case["context"], case["batch"]
+    if lo == hi:
+        return [hi] * n
+    r = random.Random(zlib.crc32(repr((lo, hi, n)).encode()))
+    lens = [min(hi, max(lo, round(math.exp(r.uniform(math.log(lo), math.log(hi)))))) for _ in range(n)]
+    lens[r.randrange(n)] = hi
+    return lens
+
+
+def _shape(case):
+    return tuple(case[k] for k in ("batch", "q_heads", "kv_heads", "head_dim", "page_size"))
+
+
+def work(case):
+    e = 2 if case["dtype"] == "bf16" else 4
+    B, H, Hkv, D, S = _shape(case)
+    lens = _lengths(case)
+    pages = [-(-n // S) for n in lens]
+    q_out = B * H * (2 * D * e + 4)
+    full, held = Hkv * D * 2 * e, Hkv * D * 2 * 17 // 32  # bytes of a token
+    if case["op"] == "quantise":
+        t = sum(min(n, case["tokens"]) for n in lens)
+        return {"bytes": t * (2 * full + held), "flops": 0}
+    if case["op"] == "restore":
+        return {"bytes": sum(lens) * (held + full), "flops": 0}
+    if case["op"] == "attend":
+        t = sum(min(n, case["top_k"] * S) if case["top_k"] else n for n in lens)
+        lists = sum(min(p, case["top_k"]) * Hkv if case["top_k"] else p for p in pages) * 4
+        return {"bytes": t * held + lists + q_out, "flops": t * H * 4 * D}
+    if case["op"] == "weigh":
+        return {"bytes": sum(lens) * full + sum(pages) * (Hkv * 8 + 4) + q_out, "flops": sum(lens) * H * 4 * D}
+    kept = sum(min(p, case["budget"]) for p in pages)
+    return {"bytes": sum(pages) * (Hkv * 8 + 8) + (sum(pages) - kept) * 4, "flops": sum(pages) * Hkv}
+
+
+# ---- the number format ----------------------------------------------------------------------------------------------
+
+def _codes(x):
+    """fp32 [..., D] -> codes uint8 [..., D] and scale bytes uint8 [..., D/32]."""
+    x = x.unflatten(-1, (-1, 32))
+    top = x.abs().amax(-1, keepdim=True)
+    e = torch.where(top > 0, (torch.frexp(top)[1] - 3).clamp(-126, 125), -126)
+    scale = ((127 - e) << 23).view(torch.float32)  # 2^-e
+    y = x * scale
+    a = y.abs()
+    level = ((a > 0.25).byte() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5.0)).byte()
+    code = level + 8 * (y < 0).byte()
+    return code.flatten(-2), (e + 127).squeeze(-1).byte()
+
+
+def _values(code, scale):
+    """The inverse: codes [..., D], bytes [..., D/32] -> fp32 [..., D]."""
+    lut = torch.tensor(LEVELS + tuple(-v for v in LEVELS), device=code.device)
+    s = (scale.int() << 23).view(torch.float32)
+    return (lut[code.int()].unflatten(-1, (-1, 32)) * s[..., None]).flatten(-2)
+
+
+def _pack(code):
+    return code[..., 0::2] | (code[..., 1::2] << 4)
+
+
+def _unpack(b):
+    return torch.stack((b & 15, b >> 4), -1).flatten(-2)
+
+
+def _record(k, v):
+    """Keys and values fp32 [pages, Hkv, S, D] -> records uint8 [pages, Hkv, bytes]."""
+    n, Hkv, S, D = k.shape
+    (kc, ks), (vc, vs) = _codes(k), _codes(v)
+    order = torch.tensor(ORDER, device=k.device)
+    vp = _pack(vc).view(n, Hkv, S // 8, 8, 16, D // 32).permute(0, 1, 2, 4, 3, 5)
+    sc = [s.view(n, Hkv, S // 8, 8, D // 32)[:, :, :, order].permute(0, 1, 4, 2, 3).reshape(n, Hkv, -1) for s in (ks, vs)]
+    return torch.cat([_pack(kc).reshape(n, Hkv, -1), vp.reshape(n, Hkv, -1), *sc], -1)
+
+
+def _from_record(rec, S, D):
+    """uint8 [..., bytes of a (page, head)] -> keys and values fp32 [..., S, D]."""
+    lead = rec.shape[:-1]
+    kc, vc, ks, vs = rec.split([S * D // 2, S * D // 2, S * D // 32, S * D // 32], -1)
+    back = torch.tensor(ORDER, device=rec.device).argsort()
+    vc = vc.reshape(*lead, S // 8, 16, 8, D // 32).transpose(-3, -2).reshape(*lead, S, D // 2)
+    ks, vs = (s.reshape(*lead, D // 32, S // 8, 8)[..., back].flatten(-2).transpose(-1, -2) for s in (ks, vs))
+    return _values(_unpack(kc.reshape(*lead, S, D // 2)), ks), _values(_unpack(vc), vs)
+
+
+# ---- inputs ---------------------------------------------------------------------------------------------------------
+
+def _kv(n, Hkv, S, D, dtype, q_b, g):
+    """Keys with a mean vector per (page, head), a few channels ten times as large and now and then a key that points
+    along the query of its head; values iid normal. As rounded to the cache's type."""
+    dev = g.device
+    k = torch.randn((n, Hkv, S, D), generator=g, device=dev)
+    k += 0.5 * torch.randn((n, Hkv, 1, D), generator=g, device=dev)
+    k[..., ::37] *= 10.0
+    if q_b is not None:
+        first = q_b.float().view(Hkv, -1, D)[:, 0]
+        along = torch.rand((n, Hkv, S, 1), generator=g, device=dev) < 0.001
+        k = torch.where(along, 0.25 * k + 1.0 * first[:, None], k)
+    return k.to(dtype), torch.randn((n, Hkv, S, D), generator=g, device=dev).to(dtype)
+
+
+def _inputs(case, seed):
+    """Everything that a pass reads, as a dict of tensors."""
+    dev, dtype, op = torch.device("cuda"), DTYPES[case["dtype"]], case["op"]
+    B, H, Hkv, D, S = _shape(case)
+    g = torch.Generator(device=dev)
+    g.manual_seed(int(seed))
+    lens = _lengths(case)
+    pages = [-(-n // S) for n in lens]
+    ids = torch.randperm(sum(pages), generator=g, device=dev).to(torch.int32)  # a pool that has been in use for a while
+    table = torch.full((B, max(pages)), -1, dtype=torch.int32, device=dev)
+    at = 0
+    for b, n in enumerate(pages):
+        table[b, :n] = ids[at:at + n]
+        at += n
+    s = {"case": case, "table": table, "seq_lens": torch.tensor(lens, dtype=torch.int32, device=dev), "num_pages": at, "longest": max(lens)}
+    if op == "evict":
+        s["weights"] = torch.zeros((B, Hkv, max(pages)), device=dev)
+        for b, n in enumerate(pages):  # an early page has been attended more often, a few of them much
+            age = 1.0 - torch.arange(n, device=dev) / n
+            s["weights"][b, :, :n] = age * torch.exp(2.0 * torch.randn((Hkv, n), generator=g, device=dev))
+        return s
+    if op == "quantise":  # full-precision pages exist for the tokens that are being written only
+        s["begin"] = (s["seq_lens"] - case["tokens"]).clamp(min=0)
+        s["end"] = s["seq_lens"].clone()
+        s["touched"] = -(-case["tokens"] // S) + 1
+        first = [max(0, n - case["tokens"]) // S for n in lens]
+        count = [p - f for p, f in zip(pages, first)]
+        stage = torch.randperm(sum(count), generator=g, device=dev).to(torch.int32)
+        s["stage"] = torch.full_like(table, -1)
+        at = 0
+        for b, (f, n) in enumerate(zip(first, count)):
+            s["stage"][b, f:f + n] = stage[at:at + n]
+            at += n
+        s["k"], s["v"] = _kv(at, Hkv, S, D, dtype, None, g)
+        return s
+    q = torch.randn((B, H, D), generator=g, device=dev).to(dtype)
+    if op == "weigh":
+        s["k"] = torch.zeros((at, Hkv, S, D), dtype=dtype, device=dev)
+        s["v"] = torch.zeros_like(s["k"])
+        s["weights"] = torch.rand((B, Hkv, max(pages)), generator=g, device=dev)
+    else:
+        s["records"] = torch.zeros((at, Hkv, S * D * 17 // 16), dtype=torch.uint8, device=dev)
+    at = 0
+    for b, n in enumerate(pages):
+        mine = ids[at:at + n].long()
+        at += n
+        for i in range(0, n, 1 << 13):
+            part = mine[i:i + (1 << 13)]
+            k, v = _kv(part.numel(), Hkv, S, D, dtype, q[b], g)
+            if op == "weigh":
+                s["k"][part], s["v"][part] = k, v
+            else:
+                s["records"][part] = _record(k.float(), v.float())
+    if op != "restore":
+        s["q"] = q
+    if case["top_k"]:
+        top = case["top_k"]
+        s["list"] = torch.full((B, Hkv, top), -1, dtype=torch.int32, device=dev)
+        s["count"] = torch.tensor([min(top, p) for p in pages], dtype=torch.int32, device=dev)[:, None].expand(B, Hkv).contiguous()
+        for b, p in enumerate(pages):
+            n = min(top, p)
+            best = torch.rand((Hkv, p), generator=g, device=dev).topk(n, -1)[1]
+            s["list"][b, :, :n] = best.sort(-1)[0].int()
+    return s
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    dev, dtype, op = torch.device("cuda"), DTYPES[case["dtype"]], case["op"]
+    B, H, Hkv, D, S = _shape(case)
+    if op == "quantise":
+        s["records"] = torch.zeros((s["num_pages"], Hkv, S * D * 17 // 16), dtype=torch.uint8, device=dev)
+        s["k_out"], s["v_out"] = torch.zeros_like(s["k"]), torch.zeros_like(s["v"])
+    elif op == "restore":
+        s["k_out"] = torch.zeros((s["num_pages"], Hkv, S, D), dtype=dtype, device=dev)
+        s["v_out"] = torch.zeros_like(s["k_out"])
+    elif op == "weigh":
+        s["weights_out"] = s["weights"].clone()
+    elif op == "evict":
+        s["weights_out"], s["table_out"], s["seq_lens_out"] = torch.zeros_like(s["weights"]), torch.full_like(s["table"], -1), torch.zeros_like(s["seq_lens"])
+    if own:  # the handles that a program keeps
+        from paper_2605_27740_amd.session import DecodeSession, PageAccounts, QuantisedCache
+        from paper_2605_27740_amd.workloads import Workload
+        geometry = dict(q_heads=H, kv_heads=Hkv, head_dim=D, page_size=S, dtype=dtype, num_pages=s["num_pages"], page_table=s["table"],
+                        seq_lens=s["seq_lens"], max_seq_len=s["longest"])
+        if op == "weigh":
+            s["session"] = DecodeSession(Workload(name="operators", dtype=dtype, B=B, H=H, Hkv=Hkv, D=D, S=S, top_k=1, lam=0.5, q=s["q"], k_cache=s["k"],
+                                                  v_cache=s["v"], page_table=s["table"], seq_lens=s["seq_lens"]), track_weights=True)
+        elif op == "evict":
+            s["accounts"] = PageAccounts(budget_pages=case["budget"], sink_pages=case["sinks"], recent_pages=case["recent"], **geometry)
+        else:
+            s["cache"] = QuantisedCache(records=s["records"], top_k=case["top_k"], **geometry)
+    return s
+
+
+# ---- one pass -------------------------------------------------------------------------------------------------------
+
+def _plain_quantise(s):
+    S = s["case"]["page_size"]
+    lp = s["begin"][:, None] // S + torch.arange(s["touched"], device=s["begin"].device)
+    page = s["stage"].gather(1, lp.clamp(max=s["stage"].shape[1] - 1).long())
+    tok = lp[..., None] * S + torch.arange(S, device=lp.device)
+    mine = (tok >= s["begin"][:, None, None]) & (tok < s["end"][:, None, None]) & (page >= 0)[..., None]
+    page = torch.where(mine.any(-1), page, s["k"].shape[0]).long()  # the others go to a page behind the last
+    got = {}
+    for name in ("k", "v"):
+        x = s[name][page.clamp(max=s["k"].shape[0] - 1)].float()
+        y = _values(*_codes(x)) * mine[:, :, None, :, None]
+        out = torch.zeros((s["k"].shape[0] + 1, *s["k"].shape[1:]), dtype=s["k"].dtype, device=x.device)
+        out[page] = y.to(out.dtype)
+        got[name] = out[:-1]
+    return got
+
+
+def _plain_restore(s):
+    S, D = s["case"]["page_size"], s["case"]["head_dim"]
+    n_tok = (s["seq_lens"][:, None] - S * torch.arange(s["table"].shape[1], device=s["table"].device)).clamp(0, S)
+    here = s["table"] >= 0
+    of_page = torch.zeros(s["num_pages"], dtype=n_tok.dtype, device=n_tok.device)
+    of_page[s["table"][here].long()] = n_tok[here]
+    mine = (torch.arange(S, device=n_tok.device) < of_page[:, None])[:, None, :, None]
+    k, v = _from_record(s["records"], S, D)
+    dtype = s["k_out"].dtype
+    return {"k": (k * mine).to(dtype), "v": (v * mine).to(dtype)}
+
+
+def _softmax(q, k, valid):
+    """q [B, Hkv, G, D], k [B, Hkv, T, D], valid [B, Hkv, T] -> probabilities [B, Hkv, G, T] and the log of the sum."""
+    x = torch.matmul(q, k.transpose(-1, -2)) / math.sqrt(q.shape[-1])
+    x = x.masked_fill(~valid[:, :, None], -math.inf)
+    top = x.amax(-1, keepdim=True)
+    p = torch.exp(x - top)
+    total = p.sum(-1, keepdim=True)
+    return p / total, (top + torch.log(total)).squeeze(-1)
+
+
+def _plain_attend(s):
+    B, H, Hkv, D, S = _shape(s["case"])
+    if "list" in s:
+        lp, used = s["list"].clamp(min=0), s["list"] >= 0
+    else:
+        lp = torch.arange(s["table"].shape[1], device=s["table"].device, dtype=torch.int32).expand(B, Hkv, -1)
+        used = lp * S < s["seq_lens"][:, None, None]
+    page = s["table"].gather(1, lp.reshape(B, -1).long()).view(lp.shape).clamp(min=0).long()
+    k, v = _from_record(s["records"][page, torch.arange(Hkv, device=page.device)[:, None]], S, D)
+    tok = lp[..., None] * S + torch.arange(S, device=page.device)
+    valid = (used[..., None] & (tok < s["seq_lens"][:, None, None, None])).flatten(-2)
+    p, lse = _softmax(s["q"].float().view(B, Hkv, -1, D), k.flatten(2, 3), valid)
+    out = torch.matmul(p, v.flatten(2, 3)).reshape(B, H, D).to(s["q"].dtype)
+    return {"out": out, "lse": lse.reshape(B, H)}
+
+
+def _plain_weigh(s):
+    B, H, Hkv, D, S = _shape(s["case"])
+    page = s["table"].clamp(min=0).long()
+    k, v = (s[n][page].transpose(1, 2).flatten(2, 3).float() for n in ("k", "v"))
+    P = page.shape[1]
+    valid = (torch.arange(P * S, device=page.device) < s["seq_lens"][:, None])[:, None].expand(B, Hkv, -1)
+    p, lse = _softmax(s["q"].float().view(B, Hkv, -1, D), k, valid)
+    out = torch.matmul(p, v).reshape(B, H, D).to(s["q"].dtype)
+    share = p.sum(2).unflatten(-1, (P, S)).sum(-1)
+    mine = torch.arange(P, device=page.device) * S < s["seq_lens"][:, None]
+    weights = torch.where(mine[:, None], s["case"]["decay"] * s["weights"] + share, s["weights"])
+    return {"out": out, "lse": lse.reshape(B, H), "weights": weights}
+
+
+def _plain_evict(s):
+    c, table, lens = s["case"], s["table"], s["seq_lens"]
+    S, P_max = c["page_size"], table.shape[1]
+    P = ((lens + S - 1) // S)[:, None]
+    i = torch.arange(P_max, device=table.device)[None]
+    rank = s["weights"].double().sum(1).float()
+    rank = torch.where((i < c["sinks"]) | (i >= P - c["recent"]), math.inf, rank).masked_fill(i >= P, -math.inf)
+    place = torch.sort(rank, dim=-1, descending=True, stable=True)[1].argsort(-1)
+    keep = (place < torch.clamp(P, max=c["budget"])) & (i < P)
+    gone = ~keep & (i < P)
+    kept = torch.where(keep, i, P_max).sort(-1)[0]
+    used = kept < P_max
+    kept = kept.clamp(max=P_max - 1)
+    freed = torch.where(gone, i, P_max).sort(-1)[0][:, :max(P_max - c["budget"], 1)]
+    n_freed = gone.sum(-1).int()
+    weights = s["weights"].gather(2, kept[:, None].expand(s["weights"].shape)) * used[:, None]
+    return {"table": torch.where(used, table.gather(1, kept), -1), "weights": weights, "seq_lens": lens - n_freed * S,
+            "freed": torch.where(freed < P_max, table.gather(1, freed.clamp(max=P_max - 1)), -1), "freed_count": n_freed}
+
+
+def run(state):
+    s, op = state, state["case"]["op"]
+    if not own:
+        return {"quantise": _plain_quantise, "restore": _plain_restore, "attend": _plain_attend, "weigh": _plain_weigh,
+                "evict": _plain_evict}[op](s)
+    if op == "quantise":
+        s["cache"].quantise_pages(s["k"], s["v"], s["stage"], s["begin"], s["end"], s["touched"])
+        s["cache"].restore_pages(s["k_out"], s["v_out"], s["stage"], s["begin"], s["end"], s["touched"])
+        return {"k": s["k_out"], "v": s["v_out"]}
+    if op == "restore":
+        s["cache"].restore_pages(s["k_out"], s["v_out"])
+        return {"k": s["k_out"], "v": s["v_out"]}
+    if op == "attend":
+        out, lse = s["cache"].paged_decode(s["q"], s.get("list"), s.get("count"))
+        return {"out": out, "lse": lse}
+    if op == "weigh":
+        session = s["session"]
+        session.weighted_paged_decode(decay=s["case"]["decay"], weights_in=s["weights"], weights_out=s["weights_out"])
+        return {"out": session.out_dense, "lse": session.lse_dense, "weights": s["weights_out"]}
+    accounts = s["accounts"]
+    accounts.evict_pages(weights_in=s["weights"], weights_out=s["weights_out"], page_table_out=s["table_out"], seq_lens_out=s["seq_lens_out"])
+    return {"table": s["table_out"], "weights": s["weights_out"], "seq_lens": s["seq_lens_out"], "freed": accounts.freed_pages,
+            "freed_count": accounts.freed_count}
+
+
+# ---- the same in 64 bits --------------------------------------------------------------------------------------------
+
+def _nearest(x):
+    """float64 [n, 32] -> the multiples of their block's power of two that they are rounded to."""
+    top = x.abs().max(-1, keepdim=True).values
+    e = torch.floor(torch.log2(top)) - 2
+    e = e + (torch.pow(2.0, e + 3) <= top).double() - (torch.pow(2.0, e + 2) > top).double()  # log2 of a number just below a power may be rounded up to it
+    e = torch.where(top > 0, e, torch.full_like(e, -126.0)).clamp(-126, 125)
+    y = x / torch.pow(2.0, e)
+    step = torch.pow(2.0, torch.floor(torch.log2(y.abs().clamp(min=1.0))).clamp(max=2) - 1)
+    return (torch.round(y / step) * step).clamp(-6, 6) * torch.pow(2.0, e)
+
+
+def _decoded(rec, S, D):
+    """One (page, head)'s records uint8 [n, bytes] -> keys and values float64 [n, S, D]."""
+    n, half, dev = rec.shape[0], S * D // 2, rec.device
+    t = torch.arange(S, device=dev)[:, None]
+    c = torch.arange(D, device=dev)[None]
+    unit = D // 16
+    at_k = t * (D // 2) + c // 2
+    at_v = half + (t // 8 * 128 + c // unit * 8 + t % 8) * (unit // 2) + c % unit // 2
+    spot = t // 8 * 8 + 2 * (t % 4) + t % 8 // 4
+    got = []
+    for at, base in ((at_k, 2 * half), (at_v, 2 * half + S * D // 32)):
+        code = (rec[:, at.reshape(-1)] >> (c % 2 * 4).expand(S, D).reshape(-1).byte()) & 15
+        m = (code & 7).double()
+        mag = torch.where(m < 4, m / 2, torch.where(m < 6, m - 2, 2 * m - 8))
+        e = rec[:, (base + c // 32 * S + spot).reshape(-1)].double() - 127
+        got.append((mag * (1 - 2 * (code >> 3).double()) * torch.pow(2.0, e)).view(n, S, D))
+    return got
+
+
+def exact(case, seed):
+    s = _inputs(case, seed)
+    op = case["op"]
+    B, H, Hkv, D, S = _shape(case)
+    lens = s["seq_lens"].tolist()
+    dev = s["table"].device
+    if op in ("quantise", "restore"):
+        pool = s["k"].shape[0] if op == "quantise" else s["num_pages"]
+        k, v = (torch.zeros((pool, Hkv, S, D), dtype=torch.float64, device=dev) for _ in range(2))
+        for b, n in enumerate(lens):
+            first = max(0, n - case["tokens"]) if op == "quantise" else 0
+            ids = s["stage" if op == "quantise" else "table"][b, first // S:-(-n // S)].long()
+            if op == "quantise":
+                vals = [_nearest(s[name][ids].double().reshape(-1, 32)).view(-1, Hkv, S, D) for name in ("k", "v")]
+            else:
+                vals = [x.view(-1, Hkv, S, D) for x in _decoded(s["records"][ids].flatten(0, 1), S, D)]
+            tok = first // S * S + torch.arange(ids.numel() * S, device=dev).view(-1, 1, S, 1)
+            mine = ((tok >= first) & (tok < n)).double()
+            k[ids], v[ids] = vals[0] * mine, vals[1] * mine
+        return {"k": k, "v": v}
+    if op == "evict":
+        P_max, budget = s["table"].shape[1], case["budget"]
+        table = torch.full_like(s["table"], -1).cpu()
+        weights = torch.zeros(s["weights"].shape, dtype=torch.float64)
+        freed = torch.full((B, max(P_max - budget, 1)), -1, dtype=torch.int32)
+        counts, left = [], []
+        for b, n in enumerate(lens):
+            P = -(-n // S)
+            w = s["weights"][b, :, :P].double().cpu()
+            total = w.sum(0).float().tolist()  # pages are ranked by 32-bit numbers
+            fixed = set(range(min(case["sinks"], P))) | set(range(max(P - case["recent"], 0), P))
+            others = sorted((p for p in range(P) if p not in fixed), key=lambda p: (-total[p], p))
+            keep = sorted(fixed | set(others[:max(budget - len(fixed), 0)])) if P > budget else list(range(P))
+            out = sorted(set(range(P)) - set(keep))
+            row = s["table"][b].cpu()
+            table[b, :len(keep)] = row[keep]
+            weights[b, :, :len(keep)] = w[:, keep]
+            freed[b, :len(out)] = row[out]
+            counts.append(len(out))
+            left.append(n - len(out) * S)
+        return {"table": table, "weights": weights, "seq_lens": torch.tensor(left, dtype=torch.int32), "freed": freed,
+                "freed_count": torch.tensor(counts, dtype=torch.int32)}
+    out = torch.zeros((B, Hkv, H // Hkv, D), dtype=torch.float64, device=dev)
+    lse = torch.full((B, Hkv, H // Hkv), -math.inf, dtype=torch.float64, device=dev)
+    q = s["q"].double().view(B, Hkv, -1, D)
+    weights = s["weights"].double().clone() if op == "weigh" else None
+    for b, n in enumerate(lens):
+        P = -(-n // S)
+        for h in range(Hkv):
+            lp = s["list"][b, h, :int(s["count"][b, h])].long() if "list" in s else torch.arange(P, device=dev)
+            ids = s["table"][b, lp].long()
+            k, v = (s["k"][ids, h].double(), s["v"][ids, h].double()) if op == "weigh" else _decoded(s["records"][ids, h], S, D)
+            tok = (lp[:, None] * S + torch.arange(S, device=dev)).reshape(-1) < n
+            x = (q[b, h] @ k.reshape(-1, D).T / math.sqrt(D))[:, tok]
+            lse[b, h] = torch.logsumexp(x, -1)
+            p = torch.exp(x - lse[b, h][:, None])
+            out[b, h] = p @ v.reshape(-1, D)[tok]
+            if op == "weigh":
+                share = torch.zeros(P * S, dtype=torch.float64, device=dev)
+                share[:n] = p.sum(0)
+                weights[b, h, :P] = case["decay"] * weights[b, h, :P] + share.view(P, S).sum(-1)
+    got = {"out": out.view(B, H, D), "lse": lse.view(B, H)}
+    return dict(got, weights=weights) if op == "weigh" else got
