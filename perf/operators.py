@@ -8,8 +8,7 @@ operations and one through the library, and the same in 64 bits.
 ``evict``     pages with the smallest account leave the page table, which closes up
 
 Layout of a page's record, for each KV head one after the other: K codes [S][D] two to a byte, even channel low; V codes
-[S/8][16][8][D/16]: in groups of eight tokens, and of D/16 channels; K scales [D/32][S]; V scales [D/32][S], both with the
-eight tokens of a group in the order 0 4 1 5 2 6 3 7.
+[S/8][16][8][D/16]: in groups of eight tokens, and of D/16 channels; K scales [D/32][S]; V scales [D/32][S].
 """
 from __future__ import annotations
 
@@ -22,7 +21,6 @@ import torch
 own = False
 
 DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
-ORDER = (0, 4, 1, 5, 2, 6, 3, 7)
 LEVELS = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 
 
@@ -166,9 +164,8 @@ def _record(k, v):
     """Keys and values fp32 [pages, Hkv, S, D] -> records uint8 [pages, Hkv, bytes]."""
     n, Hkv, S, D = k.shape
     (kc, ks), (vc, vs) = _codes(k), _codes(v)
-    order = torch.tensor(ORDER, device=k.device)
     vp = _pack(vc).view(n, Hkv, S // 8, 8, 16, D // 32).permute(0, 1, 2, 4, 3, 5)
-    sc = [s.view(n, Hkv, S // 8, 8, D // 32)[:, :, :, order].permute(0, 1, 4, 2, 3).reshape(n, Hkv, -1) for s in (ks, vs)]
+    sc = [s.transpose(-1, -2).reshape(n, Hkv, -1) for s in (ks, vs)]
     return torch.cat([_pack(kc).reshape(n, Hkv, -1), vp.reshape(n, Hkv, -1), *sc], -1)
 
 
@@ -176,9 +173,8 @@ def _from_record(rec, S, D):
     """uint8 [..., bytes of a (page, head)] -> keys and values fp32 [..., S, D]."""
     lead = rec.shape[:-1]
     kc, vc, ks, vs = rec.split([S * D // 2, S * D // 2, S * D // 32, S * D // 32], -1)
-    back = torch.tensor(ORDER, device=rec.device).argsort()
     vc = vc.reshape(*lead, S // 8, 16, 8, D // 32).transpose(-3, -2).reshape(*lead, S, D // 2)
-    ks, vs = (s.reshape(*lead, D // 32, S // 8, 8)[..., back].flatten(-2).transpose(-1, -2) for s in (ks, vs))
+    ks, vs = (s.reshape(*lead, D // 32, S).transpose(-1, -2) for s in (ks, vs))
     return _values(_unpack(kc.reshape(*lead, S, D // 2)), ks), _values(_unpack(vc), vs)
 
 
@@ -430,13 +426,12 @@ def _decoded(rec, S, D):
     unit = D // 16
     at_k = t * (D // 2) + c // 2
     at_v = half + (t // 8 * 128 + c // unit * 8 + t % 8) * (unit // 2) + c % unit // 2
-    spot = t // 8 * 8 + 2 * (t % 4) + t % 8 // 4
     got = []
     for at, base in ((at_k, 2 * half), (at_v, 2 * half + S * D // 32)):
         code = (rec[:, at.reshape(-1)] >> (c % 2 * 4).expand(S, D).reshape(-1).byte()) & 15
         m = (code & 7).double()
         mag = torch.where(m < 4, m / 2, torch.where(m < 6, m - 2, 2 * m - 8))
-        e = rec[:, (base + c // 32 * S + spot).reshape(-1)].double() - 127
+        e = rec[:, (base + c // 32 * S + t).reshape(-1)].double() - 127
         got.append((mag * (1 - 2 * (code >> 3).double()) * torch.pow(2.0, e)).view(n, S, D))
     return got
 
