@@ -215,6 +215,79 @@ int unique_decode_step_static(const unique_cache_desc* desc, const void* d_q, in
 int unique_dense_paged_decode(const unique_cache_desc* desc, const void* d_q, float sm_scale, void* d_out,
                               float* d_lse_out, void* d_workspace, size_t workspace_bytes, void* stream);
 
+/* ---- A longer context in the same memory: pages as 4-bit records, and pages that nobody attends to given back ----
+ *
+ * A page's record holds its K and V in a microscaled 4-bit format: the 32 channels [32 i, 32 i + 32) of a token and KV head share a scale
+ * 2^e, e = clamp(floor(log2(max |x|)) - 2, -126, 125), kept as the byte e + 127, and each is one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} times it (codes
+ * 0 to 7, bit 3 the sign): the nearest to x / 2^e, ties to the even code, what is above 6 as 6. A block of which an
+ * element is infinite or NaN gets the byte 255, which stands for NaN. 17/32 of a byte per element instead of 2 or 4.
+ *   record : for each KV head one after the other, S = page_size, D = head_dim:
+ *              S*D/2 bytes     K codes [S][D], two to a byte, the even channel in the low four bits
+ *              S*D/2 bytes     V codes [S/8][16][8][D/16]: groups of eight tokens, then of D/16 channels, then the tokens of the group
+ *              D/32 * S bytes  K scales [D/32][S]
+ *              D/32 * S bytes  V scales [D/32][S]
+ *            unique_page_record_bytes in all; a pool of them is [num_records][record], 16-byte aligned.
+ * The pool has a page table of its own (d_record_table, shaped like the descriptor's), so that full-precision pages need exist only where
+ * tokens are being written: entries outside a pool (-1) are skipped. One table for both is allowed. */
+
+/* Bytes of a page's record for this descriptor's num_kv_heads, head_dim and page_size; 0 if desc is NULL or they are not supported. */
+int64_t unique_page_record_bytes(const unique_cache_desc* desc);
+
+/* Tokens [d_tok_begin[b], d_tok_end[b]) (clamped to [0, seq_lens[b])) of every sequence from desc's k_cache and v_cache into records; the
+ * other tokens of a record are left as they are.
+ *   d_tok_begin, d_tok_end, max_pages_touched_per_seq : as in unique_update_page_stats; both NULL = every token.
+ *   d_records, num_records : the pool and its size.  d_record_table : its page table; NULL = desc->page_table. */
+int unique_quantise_pages(const unique_cache_desc* desc, const int32_t* d_tok_begin, const int32_t* d_tok_end,
+                          int32_t max_pages_touched_per_seq, void* d_records, const int32_t* d_record_table, int64_t num_records,
+                          void* stream);
+
+/* The way back, for a prefill over an earlier context or pages that leave the pool: the values of the records' tokens, exactly, into
+ * d_k_out and d_v_out, which have the layout, table and strides that desc gives (its k_cache and v_cache are not used and may be NULL). Slots
+ * outside the token range are left as they are. */
+int unique_restore_pages(const unique_cache_desc* desc, const int32_t* d_tok_begin, const int32_t* d_tok_end,
+                         int32_t max_pages_touched_per_seq, const void* d_records, const int32_t* d_record_table, int64_t num_records,
+                         void* d_k_out, void* d_v_out, void* stream);
+
+/* unique_sparse_paged_decode, or with d_sel_pages and d_sel_count NULL unique_dense_paged_decode, over a pool of records. desc->page_table
+ * and desc->num_phys_pages are the pool's; k_cache and v_cache are not used and may be NULL. d_q and d_out have desc->dtype. Slots of a page behind
+ * seq_lens[b] may be read but never count. The workspace needs unique_workspace_bytes(desc, sel_stride), any top_k without lists.
+ * The result of a head that attends a NaN scale is unspecified. */
+int unique_quantised_paged_decode(const unique_cache_desc* desc, const void* d_records, const void* d_q, const int32_t* d_sel_pages,
+                                  const int32_t* d_sel_count, int32_t sel_stride, float sm_scale, void* d_out, float* d_lse_out,
+                                  void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace that either of the two calls below may need for this descriptor (256-byte aligned, nothing carried between
+ * calls, one for each stream that may overlap another). */
+int unique_account_workspace_bytes(const unique_cache_desc* desc, size_t* out_bytes);
+
+/* unique_dense_paged_decode that also keeps an account of what each page is worth: for every sequence, KV head and page
+ *   d_weights_out[p] = decay * d_weights_in[p] + sum over the group's query heads and the page's tokens of the attention weights,
+ * float, row (b, h_kv) at (b*H_kv + h_kv)*weight_stride, weight_stride >= max_pages_per_seq (or the page bound implied by
+ * max_seq_len_hint). Entries at and beyond the pages of a sequence are left as they are (0 is what they should hold
+ * when the sequence grows into them).
+ *   decay        : in [0, 1]; 1 = the plain sum of the steps.
+ *   d_weights_in : NULL = nothing so far (and decay does not count); may be d_weights_out. */
+int unique_weighted_paged_decode(const unique_cache_desc* desc, const void* d_q, float sm_scale, float decay, const float* d_weights_in,
+                                 float* d_weights_out, int32_t weight_stride, void* d_out, float* d_lse_out, void* d_workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* Evicts pages by their accounts. A sequence of more than budget_pages pages keeps its first sink_pages, its last recent_pages (>= 1: the last
+ * page is being written) and of the others those with the largest accounts, budget_pages in all: a page's accounts are summed over the
+ * KV heads in 64 bits and ranked as one float; ties keep the earlier page, a NaN ranks lowest. Its row of the page table
+ * and its rows of accounts close up in the old order, vacated entries become -1 and 0, and seq_lens loses page_size tokens for each
+ * page evicted. (Keys keep the positions that they were given before they were cached.) The other sequences stay as they are.
+ * Statistics and 4-bit records go by physical page and need nothing.
+ *   d_weights_out, d_page_table_out, d_seq_lens_out : d_weights_in, desc->page_table and desc->seq_lens again (in place), or arrays like them
+ *                   that do not overlap them; entries at and beyond the pages that the sequence had are left as they are.
+ *   d_freed_pages : out, int32 [batch][freed_stride], the PHYSICAL ids of the evicted pages in their order in the sequence, -1 behind them;
+ *                   freed_stride >= 1 and >= max_pages_per_seq (or the page bound implied by max_seq_len_hint) - budget_pages.
+ *   d_freed_count : out, int32 [batch].
+ * desc's k_cache and v_cache are not used and may be NULL. */
+int unique_evict_pages(const unique_cache_desc* desc, int32_t budget_pages, int32_t sink_pages, int32_t recent_pages,
+                       const float* d_weights_in, float* d_weights_out, int32_t weight_stride, int32_t* d_page_table_out,
+                       int32_t* d_seq_lens_out, int32_t* d_freed_pages, int32_t* d_freed_count, int32_t freed_stride, void* d_workspace,
+                       size_t workspace_bytes, void* stream);
+
 /* Static strings; never NULL. */
 const char* unique_status_string(int status);
 const char* unique_last_error(void); /* thread-local detail of the last non-OK return on this thread */

@@ -18,7 +18,9 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, 1, 2, 3, 4
 DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1}
 
 EXPORTS = ("unique_workspace_bytes", "unique_page_stats_record_bytes", "unique_update_page_stats", "unique_score_select_topk",
-           "unique_page_scores", "unique_select_topk", "unique_decode_step", "unique_decode_step_static", "unique_sparse_paged_decode", "unique_dense_paged_decode", "unique_status_string",
+           "unique_page_scores", "unique_select_topk", "unique_decode_step", "unique_decode_step_static", "unique_sparse_paged_decode", "unique_dense_paged_decode",
+           "unique_page_record_bytes", "unique_quantise_pages", "unique_restore_pages", "unique_quantised_paged_decode",
+           "unique_account_workspace_bytes", "unique_weighted_paged_decode", "unique_evict_pages", "unique_status_string",
            "unique_last_error", "unique_version")
 
 
@@ -89,6 +91,16 @@ class Library:
         self.c.unique_dense_paged_decode.argtypes = [C.POINTER(CacheDesc), C.c_void_p, C.c_float, C.c_void_p,
                                                      C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
 
+        desc, ptr, i32 = C.POINTER(CacheDesc), C.c_void_p, C.c_int32
+        self.c.unique_page_record_bytes.argtypes = [desc]
+        self.c.unique_page_record_bytes.restype = C.c_int64
+        self.c.unique_quantise_pages.argtypes = [desc, ptr, ptr, i32, ptr, ptr, C.c_int64, ptr]
+        self.c.unique_restore_pages.argtypes = [desc, ptr, ptr, i32, ptr, ptr, C.c_int64, ptr, ptr, ptr]
+        self.c.unique_quantised_paged_decode.argtypes = [desc, ptr, ptr, ptr, ptr, i32, C.c_float, ptr, ptr, ptr, C.c_size_t, ptr]
+        self.c.unique_account_workspace_bytes.argtypes = [desc, C.POINTER(C.c_size_t)]
+        self.c.unique_weighted_paged_decode.argtypes = [desc, ptr, C.c_float, C.c_float, ptr, ptr, i32, ptr, ptr, ptr, C.c_size_t, ptr]
+        self.c.unique_evict_pages.argtypes = [desc, i32, i32, i32, ptr, ptr, i32, ptr, ptr, ptr, ptr, i32, ptr, C.c_size_t, ptr]
+
     # -- helpers -----------------------------------------------------------------------------
     def check(self, rc: int) -> None:
         if rc != OK:
@@ -151,6 +163,45 @@ class Library:
                                                     _p(workspace), workspace.numel() * workspace.element_size(),
                                                     _stream()))
 
+    def page_record_bytes(self, desc: CacheDesc) -> int:
+        return int(self.c.unique_page_record_bytes(C.byref(desc)))
+
+    def quantise_pages(self, desc: CacheDesc, records, record_table=None, tok_begin=None, tok_end=None,
+                       max_pages_touched_per_seq: int = 0):
+        self.check(self.c.unique_quantise_pages(C.byref(desc), _p(tok_begin), _p(tok_end), max_pages_touched_per_seq,
+                                                _p(records), _p(record_table), int(records.shape[0]), _stream()))
+
+    def restore_pages(self, desc: CacheDesc, records, k_out, v_out, record_table=None, tok_begin=None, tok_end=None,
+                      max_pages_touched_per_seq: int = 0):
+        self.check(self.c.unique_restore_pages(C.byref(desc), _p(tok_begin), _p(tok_end), max_pages_touched_per_seq,
+                                               _p(records), _p(record_table), int(records.shape[0]), _p(k_out), _p(v_out),
+                                               _stream()))
+
+    def quantised_paged_decode(self, desc: CacheDesc, records, q, sel_pages, sel_count, sm_scale: float, out, lse_out,
+                               workspace):
+        self.check(self.c.unique_quantised_paged_decode(C.byref(desc), _p(records), _p(q), _p(sel_pages), _p(sel_count),
+                                                        0 if sel_pages is None else int(sel_pages.shape[-1]), sm_scale,
+                                                        _p(out), _p(lse_out), _p(workspace),
+                                                        workspace.numel() * workspace.element_size(), _stream()))
+
+    def account_workspace_bytes(self, desc: CacheDesc) -> int:
+        n = C.c_size_t(0)
+        self.check(self.c.unique_account_workspace_bytes(C.byref(desc), C.byref(n)))
+        return int(n.value)
+
+    def weighted_paged_decode(self, desc: CacheDesc, q, sm_scale: float, decay: float, weights_in, weights_out, out, lse_out,
+                              workspace):
+        self.check(self.c.unique_weighted_paged_decode(C.byref(desc), _p(q), sm_scale, decay, _p(weights_in),
+                                                       _p(weights_out), int(weights_out.shape[-1]), _p(out), _p(lse_out),
+                                                       _p(workspace), workspace.numel() * workspace.element_size(), _stream()))
+
+    def evict_pages(self, desc: CacheDesc, budget_pages: int, sink_pages: int, recent_pages: int, weights_in, weights_out,
+                    page_table_out, seq_lens_out, freed_pages, freed_count, workspace):
+        self.check(self.c.unique_evict_pages(C.byref(desc), budget_pages, sink_pages, recent_pages, _p(weights_in),
+                                             _p(weights_out), int(weights_in.shape[-1]), _p(page_table_out), _p(seq_lens_out),
+                                             _p(freed_pages), _p(freed_count), int(freed_pages.shape[-1]), _p(workspace),
+                                             workspace.numel() * workspace.element_size(), _stream()))
+
 
 _lib: Library | None = None
 
@@ -193,3 +244,12 @@ def make_desc(*, q_heads: int, k_cache, v_cache, page_stats, page_table, seq_len
                      0 if page_stats is None else page_stats.data_ptr(),
                      page_table.data_ptr(), seq_lens.data_ptr(), DTYPE_CODE[stats_dtype], int(force_recent_pages),
                      k_cache.stride(0), k_cache.stride(1), int(min_seq_len_hint), 0)
+
+
+def make_shape_desc(*, q_heads: int, kv_heads: int, head_dim: int, page_size: int, dtype, num_pages: int, page_table, seq_lens,
+                    max_seq_len_hint: int = 0) -> CacheDesc:
+    """A ``unique_cache_desc`` without full-precision pages, for the calls on 4-bit records and on page accounts."""
+    assert page_table.dtype == torch.int32 and page_table.is_contiguous() and page_table.dim() == 2
+    assert seq_lens.dtype == torch.int32 and seq_lens.is_contiguous() and seq_lens.shape == (page_table.shape[0],)
+    return CacheDesc(DTYPE_CODE[dtype], q_heads, kv_heads, head_dim, page_size, page_table.shape[0], page_table.shape[1],
+                     max_seq_len_hint, num_pages, 0, 0, 0, page_table.data_ptr(), seq_lens.data_ptr(), 0, 0, 0, 0, 0, 0)

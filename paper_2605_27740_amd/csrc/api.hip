@@ -10,7 +10,9 @@
 #include <mutex>
 
 #include "kernels.hpp"
+#include "quant.hpp"
 #include "step_rule.hpp"
+#include "weigh.hpp"
 
 namespace {
 
@@ -240,6 +242,32 @@ int decode_step_launch(const unique::CacheView& v, const void* d_q, int32_t top_
   return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "sparse decode launch");
 }
 
+// The descriptor of a call that takes its pages from elsewhere: k_cache may be NULL.
+int make_shape_view(const unique_cache_desc* desc, unique::CacheView* v) {
+  if (!desc) return fail(UNIQUE_ERR_INVALID_ARG, "desc is NULL");
+  alignas(16) static const int dummy[4] = {0, 0, 0, 0};
+  unique_cache_desc d = *desc;
+  d.k_cache = dummy;
+  d.v_cache = nullptr;
+  d.page_stats = nullptr;
+  return make_view(&d, v, false, false);
+}
+
+// What the two calls between pages and records share.
+int record_call(const unique::CacheView& v, const void* d_records, const int32_t* d_record_table, int64_t num_records,
+                const int32_t* d_tok_begin, const int32_t* d_tok_end, int32_t max_pages_touched_per_seq, unique::QuantPool* pool, int* touched) {
+  if (!d_records) return fail(UNIQUE_ERR_INVALID_ARG, "d_records is NULL");
+  if ((uintptr_t)d_records & 15u) return fail(UNIQUE_ERR_INVALID_ARG, "d_records must be 16-byte aligned");
+  if (num_records < 1) return fail(UNIQUE_ERR_INVALID_ARG, "num_records must be >= 1 (got %lld)", (long long)num_records);
+  if ((d_tok_begin == nullptr) != (d_tok_end == nullptr))
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_tok_begin and d_tok_end must both be NULL or both be set");
+  if (d_tok_begin && max_pages_touched_per_seq < 0)
+    return fail(UNIQUE_ERR_INVALID_ARG, "max_pages_touched_per_seq must be >= 0 (got %d)", max_pages_touched_per_seq);
+  *pool = {reinterpret_cast<char*>(const_cast<void*>(d_records)), d_record_table ? d_record_table : v.page_table, num_records};
+  *touched = std::min(max_pages_touched_per_seq, v.max_pages);
+  return UNIQUE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -418,6 +446,124 @@ int unique_dense_paged_decode(const unique_cache_desc* desc, const void* d_q, fl
                                              d_out, d_lse_out, reinterpret_cast<float*>(d_workspace),
                                              (hipStream_t)stream);
   return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "dense decode launch");
+}
+
+int64_t unique_page_record_bytes(const unique_cache_desc* desc) {
+  if (!desc || desc->num_kv_heads < 1 || (desc->head_dim != 64 && desc->head_dim != 128) ||
+      (desc->page_size != 8 && desc->page_size != 16 && desc->page_size != 32))
+    return 0;
+  return (int64_t)desc->num_kv_heads * unique::QuantTile{desc->page_size, desc->head_dim}.bytes();
+}
+
+int unique_quantise_pages(const unique_cache_desc* desc, const int32_t* d_tok_begin, const int32_t* d_tok_end,
+                          int32_t max_pages_touched_per_seq, void* d_records, const int32_t* d_record_table, int64_t num_records,
+                          void* stream) {
+  unique::CacheView v;
+  int rc = make_view(desc, &v, false, true);
+  if (rc != UNIQUE_OK) return rc;
+  unique::QuantPool pool;
+  int touched;
+  rc = record_call(v, d_records, d_record_table, num_records, d_tok_begin, d_tok_end, max_pages_touched_per_seq, &pool, &touched);
+  if (rc != UNIQUE_OK) return rc;
+  const hipError_t e = unique::launch_quantise(v, pool, d_tok_begin, d_tok_end, touched, (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "quantise launch");
+}
+
+int unique_restore_pages(const unique_cache_desc* desc, const int32_t* d_tok_begin, const int32_t* d_tok_end,
+                         int32_t max_pages_touched_per_seq, const void* d_records, const int32_t* d_record_table, int64_t num_records,
+                         void* d_k_out, void* d_v_out, void* stream) {
+  unique::CacheView v;
+  int rc = make_shape_view(desc, &v);
+  if (rc != UNIQUE_OK) return rc;
+  if (!d_k_out || !d_v_out) return fail(UNIQUE_ERR_INVALID_ARG, "d_k_out and d_v_out must be non-NULL");
+  if (((uintptr_t)d_k_out | (uintptr_t)d_v_out) & 15u) return fail(UNIQUE_ERR_INVALID_ARG, "d_k_out and d_v_out must be 16-byte aligned");
+  unique::QuantPool pool;
+  int touched;
+  rc = record_call(v, d_records, d_record_table, num_records, d_tok_begin, d_tok_end, max_pages_touched_per_seq, &pool, &touched);
+  if (rc != UNIQUE_OK) return rc;
+  const hipError_t e = unique::launch_restore(v, pool, d_k_out, d_v_out, d_tok_begin, d_tok_end, touched, (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "restore launch");
+}
+
+int unique_quantised_paged_decode(const unique_cache_desc* desc, const void* d_records, const void* d_q, const int32_t* d_sel_pages,
+                                  const int32_t* d_sel_count, int32_t sel_stride, float sm_scale, void* d_out, float* d_lse_out,
+                                  void* d_workspace, size_t workspace_bytes, void* stream) {
+  unique::CacheView v;
+  int rc = make_shape_view(desc, &v);
+  if (rc != UNIQUE_OK) return rc;
+  if (!d_records || !d_q || !d_out) return fail(UNIQUE_ERR_INVALID_ARG, "d_records, d_q and d_out must be non-NULL");
+  if (((uintptr_t)d_records | (uintptr_t)d_q | (uintptr_t)d_out) & 15u)
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_records, d_q and d_out must be 16-byte aligned");
+  if ((d_sel_pages == nullptr) != (d_sel_count == nullptr))
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_sel_pages and d_sel_count must both be NULL or both be set");
+  if (d_sel_pages && sel_stride < 1) return fail(UNIQUE_ERR_INVALID_ARG, "sel_stride must be >= 1 (got %d)", sel_stride);
+  if (!(sm_scale == sm_scale)) return fail(UNIQUE_ERR_INVALID_ARG, "sm_scale is NaN");
+  const int list_len = d_sel_pages ? sel_stride : v.max_pages_hint;
+  rc = check_workspace(d_workspace, workspace_bytes, decode_bytes(v, list_len));
+  if (rc != UNIQUE_OK) return rc;
+  const hipError_t e = unique::launch_quant_decode(v, d_records, d_q, d_sel_pages, d_sel_count, list_len, list_len, sm_scale, d_out, d_lse_out,
+                                                   reinterpret_cast<float*>(d_workspace), (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "quantised decode launch");
+}
+
+int unique_account_workspace_bytes(const unique_cache_desc* desc, size_t* out_bytes) {
+  if (!out_bytes) return fail(UNIQUE_ERR_INVALID_ARG, "out_bytes is NULL");
+  if (!desc) return fail(UNIQUE_ERR_INVALID_ARG, "desc is NULL");
+  static const int32_t dummy = 0;
+  unique_cache_desc d = *desc;  // the size depends on dimensions only
+  if (!d.page_table) d.page_table = &dummy;
+  if (!d.seq_lens) d.seq_lens = &dummy;
+  unique::CacheView v;
+  const int rc = make_shape_view(&d, &v);
+  if (rc != UNIQUE_OK) return rc;
+  *out_bytes = round_up(std::max(unique::weigh_floats(v) * sizeof(float), unique::evict_bytes(v)), kAlign);
+  return UNIQUE_OK;
+}
+
+int unique_weighted_paged_decode(const unique_cache_desc* desc, const void* d_q, float sm_scale, float decay, const float* d_weights_in,
+                                 float* d_weights_out, int32_t weight_stride, void* d_out, float* d_lse_out, void* d_workspace,
+                                 size_t workspace_bytes, void* stream) {
+  unique::CacheView v;
+  int rc = make_view(desc, &v, false, true);
+  if (rc != UNIQUE_OK) return rc;
+  if (!d_q || !d_out || !d_weights_out) return fail(UNIQUE_ERR_INVALID_ARG, "d_q, d_out and d_weights_out must be non-NULL");
+  if (((uintptr_t)d_q | (uintptr_t)d_out) & 15u)
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_q and d_out must be 16-byte aligned");
+  if (!(sm_scale == sm_scale)) return fail(UNIQUE_ERR_INVALID_ARG, "sm_scale is NaN");
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(UNIQUE_ERR_INVALID_ARG, "decay must lie in [0, 1]");
+  if (weight_stride < v.max_pages_hint)
+    return fail(UNIQUE_ERR_INVALID_ARG, "weight_stride %d must be >= %d pages", weight_stride, v.max_pages_hint);
+  rc = check_workspace(d_workspace, workspace_bytes, unique::weigh_floats(v) * sizeof(float));
+  if (rc != UNIQUE_OK) return rc;
+  const unique::WeighArgs a = {d_q, unique::decode_scale_log2(v, sm_scale), decay, d_weights_in, d_weights_out, weight_stride,
+                               d_out, d_lse_out, reinterpret_cast<float*>(d_workspace)};
+  const hipError_t e = unique::launch_weigh(v, a, (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "weighted decode launch");
+}
+
+int unique_evict_pages(const unique_cache_desc* desc, int32_t budget_pages, int32_t sink_pages, int32_t recent_pages,
+                       const float* d_weights_in, float* d_weights_out, int32_t weight_stride, int32_t* d_page_table_out,
+                       int32_t* d_seq_lens_out, int32_t* d_freed_pages, int32_t* d_freed_count, int32_t freed_stride, void* d_workspace,
+                       size_t workspace_bytes, void* stream) {
+  unique::CacheView v;
+  int rc = make_shape_view(desc, &v);
+  if (rc != UNIQUE_OK) return rc;
+  if (!d_weights_in || !d_weights_out || !d_page_table_out || !d_seq_lens_out || !d_freed_pages || !d_freed_count)
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_weights_in, d_weights_out, d_page_table_out, d_seq_lens_out, d_freed_pages and d_freed_count must be "
+                "non-NULL");
+  if (sink_pages < 0 || recent_pages < 1 || (int64_t)sink_pages + recent_pages > budget_pages)
+    return fail(UNIQUE_ERR_INVALID_ARG, "need sink_pages >= 0, recent_pages >= 1 and sink_pages + recent_pages <= budget_pages (got %d, %d, %d)",
+                sink_pages, recent_pages, budget_pages);
+  if (weight_stride < v.max_pages_hint)
+    return fail(UNIQUE_ERR_INVALID_ARG, "weight_stride %d must be >= %d pages", weight_stride, v.max_pages_hint);
+  if (freed_stride < 1 || freed_stride < v.max_pages_hint - budget_pages)
+    return fail(UNIQUE_ERR_INVALID_ARG, "freed_stride %d must be >= 1 and >= %d pages - the budget", freed_stride, v.max_pages_hint);
+  rc = check_workspace(d_workspace, workspace_bytes, unique::evict_bytes(v));
+  if (rc != UNIQUE_OK) return rc;
+  const unique::EvictArgs a = {budget_pages, sink_pages, recent_pages, d_weights_in, d_weights_out, weight_stride, d_page_table_out,
+                               d_seq_lens_out, d_freed_pages, d_freed_count, freed_stride, d_workspace};
+  const hipError_t e = unique::launch_evict(v, a, (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "evict launch");
 }
 
 const char* unique_status_string(int status) {

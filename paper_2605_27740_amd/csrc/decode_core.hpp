@@ -75,9 +75,9 @@ struct DecodeShared {  // the waves' results, merged at the end; bf16 caches: ou
 // 128 channels (a step of 32K tokens 18.5 / 18.3 us, 12 x 50K with eight heads 61.3 / 60.8, the toy model 10.8 / 10.6). It is written as a loop of one
 // turn all the same: with an early return in its place every instance becomes longer, and one-kernel steps of two heads took 9.7 us for 9.6 (10 x 40 pages) and
 // 9.9 for 9.8 (25 x 81), the step of 32K tokens 16.1 for 15.9 to 16.1.
-template <typename T, int D, int G>
-__device__ __forceinline__ void finish_chunk(const CacheView& c, const Chunk& k, const ChunkOut<T>& to, const DecodeShared<T, D, G>& sh) {
-  constexpr int kSlots = DecodeShared<T, D, G>::kSlots;
+template <typename T, int D, int G, typename Shared>
+__device__ __forceinline__ void finish_chunk(const CacheView& c, const Chunk& k, const ChunkOut<T>& to, const Shared& sh) {
+  constexpr int kSlots = Shared::kSlots;
   constexpr int kPer = G * D <= kDecWaves * kWave ? 1 : G * D / (kDecWaves * kWave);
   static_assert(kPer <= 4, "a 16-byte access");
   typedef float vec_t __attribute__((ext_vector_type(kPer)));
@@ -115,14 +115,26 @@ __device__ __forceinline__ void finish_chunk(const CacheView& c, const Chunk& k,
   }
 }
 
+// What a chunk also tells of each of its pages: nothing, or, for every head g of the group, the log2 of the sum of the page's
+// exponentials (a page without tokens: -inf), written by one lane as entry e of the chunk's list is done.
+struct NoShares {
+  static constexpr bool kOn = false;
+};
+template <int G>
+struct PageShares {
+  static constexpr bool kOn = true;
+  float* at;  // [pages][G] of the row
+  __device__ __forceinline__ void put(int e, int g, float sum, float m) const { at[(int64_t)e * G + g] = m + log2f(sum); }
+};
+
 // ---- fp32 caches: vector ALUs ----
 // kNT: K and V are read with non-temporal loads (a launch that streams more than the caches hold). It is a template
 // parameter because the compiler merges the two loads of a run-time choice into a plain one.
 // us before (predicated loads, run-time choice) and now: 128 rows x 128 pages of 16 KB, G = 4 62.9 / 45.8 (5.9 TB/s);
 // all of 4 x 32768 tokens, G = 8 224 / 197; 2 rows x 16 pages of 8 KB 7.8 / 6.4.
-template <int D, int S, int G, bool kNT, typename Lookup>
+template <int D, int S, int G, bool kNT, typename Lookup, typename Shares = NoShares>
 __device__ __forceinline__ void decode_chunk(const CacheView& c, const float* __restrict__ q, const Chunk& k, int wave, int lane, Lookup lookup,
-                                             float scale_log2, const ChunkOut<float>& to, DecodeShared<float, D, G>& sh) {
+                                             float scale_log2, const ChunkOut<float>& to, DecodeShared<float, D, G>& sh, Shares shares = {}) {
   using T = float;
   constexpr int kVec = Elem<T>::kVec;
   constexpr int kLanesPerTok = D / kVec;
@@ -191,7 +203,8 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const float* __
         vd[j] = load_raw_stream(valid ? vc + off + j * kTokPerLoad * D : q_row, kNT);
       }
     };
-    auto consume = [&](const Raw16(&kr)[kTileLoads], Raw16(&vr)[kTileLoads], int rest) {
+    float page_sum[Shares::kOn ? G : 1];  // of this lane group, relative to m
+    auto consume = [&](int it, const Raw16(&kr)[kTileLoads], Raw16(&vr)[kTileLoads], int rest) {
       // logits of this lane group's tokens for the G heads
       float s[kTileLoads][G];
 #pragma unroll
@@ -224,8 +237,19 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const float* __
           psum += p[j][g];
         }
         l[g] = fmaf(l[g], alpha, psum);
+        if constexpr (Shares::kOn) page_sum[g] = it % kTilesPerPage == 0 ? psum : fmaf(page_sum[g], alpha, psum);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) acc[g][i] *= alpha;
+      }
+      if constexpr (Shares::kOn) {
+        if (it % kTilesPerPage == kTilesPerPage - 1) {  // the lane groups' sums, each relative to its own m
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const float M = cross_group_allreduce<kLanesPerTok, kLds>(m[g], OpMax());
+            const float sum = cross_group_allreduce<kLanesPerTok, kLds>(page_sum[g] * fast_exp2(m[g] - M), OpSum());
+            if (lane == g) shares.put(e0 + it / kTilesPerPage * kDecWaves, g, sum, M);
+          }
+        }
       }
       // A filler's value counts as zero: a query that is infinite or NaN must not reach the outputs of the other heads.
       if (__any(rest <= (kTileLoads - 1) * kTokPerLoad)) {
@@ -248,7 +272,7 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const float* __
     // x 64 pages, D = 64 8.2 / 7.7). With 8 heads the loop suffers from the second copy of the arithmetic (4 x 32768 tokens 97 / 121).
     if (G < 8 && n_tiles == 1) {
       issue(0, kb[0], vb[0], left[0]);
-      consume(kb[0], vb[0], left[0]);
+      consume(0, kb[0], vb[0], left[0]);
       continue;
     }
 #pragma unroll
@@ -258,7 +282,7 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const float* __
       for (int u = 0; u < kBuffers; ++u) {
         constexpr int kAhead = kBuffers - 1;
         issue(t0 + u + kAhead, kb[(u + kAhead) % kBuffers], vb[(u + kAhead) % kBuffers], left[(u + kAhead) % kBuffers]);
-        if (u == 0 || t0 + u < n_tiles) consume(kb[u], vb[u], left[u]);  // uniform
+        if (u == 0 || t0 + u < n_tiles) consume(t0 + u, kb[u], vb[u], left[u]);  // uniform
       }
     }
   }
@@ -376,9 +400,9 @@ __device__ __forceinline__ void load_v(const bf16_t* p, uint32_t (&out)[kVB / 2]
 constexpr int kDecBuffers = 2;
 
 // kNT: K and V are read with non-temporal loads (a launch that streams more than the caches hold).
-template <int D, int S, int G, bool kNT, typename Lookup>
+template <int D, int S, int G, bool kNT, typename Lookup, typename Shares = NoShares>
 __device__ __forceinline__ void decode_chunk(const CacheView& c, const bf16_t* __restrict__ q, const Chunk& k, int wave, int lane, Lookup lookup,
-                                             float scale_log2, const ChunkOut<bf16_t>& to, DecodeShared<bf16_t, D, G>& sh) {
+                                             float scale_log2, const ChunkOut<bf16_t>& to, DecodeShared<bf16_t, D, G>& sh, Shares shares = {}) {
   constexpr int kVec = 8;
   constexpr int kTile = 16;                          // token slots per MFMA tile
   constexpr int kSteps = D / 32;                     // q.k steps (and K loads per lane) per tile
@@ -461,7 +485,8 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const bf16_t* _
 #pragma unroll
       for (int j = 0; j < 4; ++j) load_v<kVB, kNT>(j < valid ? vp + j * D : q_row, vd[j]);
     };
-    auto consume = [&](const Raw16(&kr)[kSteps], const uint32_t(&vr)[4][kVB / 2], int valid) {
+    float page_sum = 0.f;  // this lane's, relative to m
+    auto consume = [&](int tile, const Raw16(&kr)[kSteps], const uint32_t(&vr)[4][kVB / 2], int valid) {
       f32x4_t sacc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
@@ -480,6 +505,7 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const bf16_t* _
         const float alpha = fast_exp2(m - mnew);
         m = mnew;
         l *= alpha;
+        if constexpr (Shares::kOn && S > kTile) page_sum *= alpha;
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[j] = j < valid ? fmaf(sacc[j], scale_log2, -m) : -INFINITY;
         // output row 4 * kg + i belongs to head (4 * kg + i) % G, whose alpha lane (4 * kg + i) % G holds
@@ -502,12 +528,24 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const bf16_t* _
       for (int j = 0; j < 4; ++j) {
         const float p = fast_exp2(x[j]);
         l += p;
+        if constexpr (Shares::kOn) page_sum = (S <= kTile || tile % (S / kTile) == 0) && j == 0 ? p : page_sum + p;
         const float r1 = p - bf16_part(p), r2 = r1 - bf16_part(r1);
         if constexpr (G == 8) {
           pa[j] = __float_as_uint(part == 0 ? p : r1);
           pb[j] = part == 0 ? __float_as_uint(r2) : 0u;
         } else {
           pa[j] = __float_as_uint(part == 0 ? p : (part == 1 ? r1 : r2));
+        }
+      }
+      if constexpr (Shares::kOn) {
+        if constexpr (S >= kTile) {
+          if (tile % (S / kTile) == S / kTile - 1) {
+            const float sum = rows_allreduce(page_sum, OpSum());
+            if (lane < G) shares.put(e0 + tile / (S / kTile) * kDecWaves, lane, sum, m);
+          }
+        } else {  // two pages, of lane groups 0 and 1 and of 2 and 3
+          const float sum = with_lane_xor16(page_sum, OpSum());
+          if (kg % 2 == 0 && kt < G && tile * 2 + kg / 2 < n_ent) shares.put(e0 + (tile * 2 + kg / 2) * kDecWaves, kt, sum, m);
         }
       }
       const s16x4_t a0 = as_s16x4(pack_hi(pa[0], pa[1]), pack_hi(pa[2], pa[3]));
@@ -530,7 +568,7 @@ __device__ __forceinline__ void decode_chunk(const CacheView& c, const bf16_t* _
       for (int u = 0; u < kDecBuffers; ++u) {
         constexpr int kAhead = kDecBuffers - 1;
         issue(t0 + u + kAhead, kb[(u + kAhead) % kDecBuffers], vb[(u + kAhead) % kDecBuffers], kv[(u + kAhead) % kDecBuffers]);
-        if (u == 0 || t0 + u < n_tiles) consume(kb[u], vb[u], kv[u]);  // uniform
+        if (u == 0 || t0 + u < n_tiles) consume(t0 + u, kb[u], vb[u], kv[u]);  // uniform
         if (t0 + u == 0) DEC_STAMP_AFTER(2, acc[0][0]);  // first tile consumed (first K/V data arrived)
 #ifdef UNIQUE_DEC_STAMPS
         if (t0 + u < n_tiles && t0 + u < kStampSlots - 6) DEC_STAMP_AFTER(6 + t0 + u, acc[0][0]);  // tile t0 + u consumed

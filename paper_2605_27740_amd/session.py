@@ -12,7 +12,7 @@ from .workloads import Workload
 class DecodeSession:
     def __init__(self, wl: Workload, top_k: int | None = None, max_seq_len_hint: int | None = None,
                  want_scores: bool = True, lib: binding.Library | None = None, stats_dtype=torch.float32,
-                 force_recent_pages: int = 0, min_seq_len_hint: int | None = None):
+                 force_recent_pages: int = 0, min_seq_len_hint: int | None = None, track_weights: bool = False):
         assert wl.k_cache.is_cuda, "the workload must live on the GPU"
         self.lib = lib or binding.load()
         self.wl = wl
@@ -48,6 +48,9 @@ class DecodeSession:
         self.lse_dense = torch.zeros_like(self.lse)
         assert self.lib.page_stats_record_bytes(self.desc) == self.page_stats.shape[1]
         self.workspace_bytes = self.lib.workspace_bytes(self.desc, self.top_k)
+        if track_weights:  # accounts of the pages for weighted_paged_decode
+            self.page_weights = torch.zeros((wl.B, wl.Hkv, wl.max_pages), device=dev, dtype=torch.float32)
+            self.workspace_bytes = max(self.workspace_bytes, self.lib.account_workspace_bytes(self.desc))
         self.workspace = torch.empty((max(self.workspace_bytes, 256),), device=dev, dtype=torch.uint8)
         assert self.workspace.data_ptr() % 256 == 0
 
@@ -82,7 +85,105 @@ class DecodeSession:
     def dense_paged_decode(self, sm_scale: float = 0.0):
         self.lib.dense_paged_decode(self.desc, self.wl.q, sm_scale, self.out_dense, self.lse_dense, self.workspace)
 
+    def weighted_paged_decode(self, sm_scale: float = 0.0, decay: float = 1.0, weights_in=None, weights_out=None):
+        """``dense_paged_decode`` that adds each page's share to its account: ``page_weights``, or from one array to another."""
+        if weights_out is None:
+            weights_in = weights_out = self.page_weights
+        _check_accounts(self.wl.B, self.wl.Hkv, weights_in, weights_out)
+        self.lib.weighted_paged_decode(self.desc, self.wl.q, sm_scale, decay, weights_in, weights_out, self.out_dense,
+                                       self.lse_dense, self.workspace)
+
     def sparse_step(self):
         """score + select + sparse decode (statistics assumed current)."""
         self.score_select_topk()
         self.sparse_paged_decode()
+
+
+def _check_accounts(batch: int, kv_heads: int, weights_in, weights_out):
+    for w in (weights_in, weights_out):
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.shape[:2] == (batch, kv_heads))
+    assert weights_in is None or weights_in.shape == weights_out.shape
+
+
+class QuantisedCache:
+    """A pool of 4-bit page records with its page table: tokens go in from full-precision pages, come back out of it, and are
+    attended to in it. ``records`` may be given (uint8, ``num_pages`` records in all); ``top_k`` is the longest list of
+    pages that ``paged_decode`` will be given."""
+
+    def __init__(self, *, q_heads: int, kv_heads: int, head_dim: int, page_size: int, dtype, num_pages: int, page_table, seq_lens,
+                 max_seq_len: int = 0, top_k: int = 0, records=None, lib: binding.Library | None = None):
+        self.lib = lib or binding.load()
+        dev = page_table.device
+        self.page_table, self.seq_lens, self.dtype = page_table, seq_lens, dtype
+        self.desc = binding.make_shape_desc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page_size=page_size, dtype=dtype,
+                                            num_pages=num_pages, page_table=page_table, seq_lens=seq_lens, max_seq_len_hint=max_seq_len)
+        record = self.lib.page_record_bytes(self.desc)
+        if records is None:
+            records = torch.zeros((num_pages, record), device=dev, dtype=torch.uint8)
+        assert records.dtype == torch.uint8 and records.is_contiguous() and records.shape[0] == num_pages
+        assert records.numel() == num_pages * record
+        self.records = records
+        B = page_table.shape[0]
+        self.out = torch.zeros((B, q_heads, head_dim), device=dev, dtype=dtype)
+        self.lse = torch.zeros((B, q_heads), device=dev, dtype=torch.float32)
+        self.workspace = torch.empty((max(self.lib.workspace_bytes(self.desc, max(top_k, 1)), 256),), device=dev, dtype=torch.uint8)
+
+    def _full_desc(self, k, v, table):
+        table = self.page_table if table is None else table
+        assert k.dtype == self.dtype and k.shape[1:] == (self.desc.num_kv_heads, self.desc.page_size, self.desc.head_dim)
+        assert table.shape == self.page_table.shape
+        return binding.make_desc(q_heads=self.desc.num_q_heads, k_cache=k, v_cache=v, page_stats=None, page_table=table,
+                                 seq_lens=self.seq_lens, max_seq_len_hint=self.desc.max_seq_len_hint)
+
+    def quantise_pages(self, k_cache, v_cache, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int = 0):
+        """Tokens of full-precision pages, found by ``page_table`` (default: the pool's own), into records."""
+        self.lib.quantise_pages(self._full_desc(k_cache, v_cache, page_table), self.records, self.page_table, tok_begin, tok_end,
+                                max_pages_touched_per_seq)
+
+    def restore_pages(self, k_out, v_out, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int = 0):
+        """The values of the records' tokens into full-precision pages."""
+        self.lib.restore_pages(self._full_desc(k_out, v_out, page_table), self.records, k_out, v_out, self.page_table, tok_begin,
+                               tok_end, max_pages_touched_per_seq)
+
+    def paged_decode(self, q, sel_pages=None, sel_count=None, sm_scale: float = 0.0):
+        """Attention over every page, or over the pages of a selection. -> ``out``, ``lse`` (the same tensors every time)."""
+        assert q.dtype == self.dtype and q.is_contiguous() and q.shape == self.out.shape
+        if sel_pages is not None:
+            assert sel_pages.dtype == sel_count.dtype == torch.int32 and sel_pages.is_contiguous() and sel_count.is_contiguous()
+            assert sel_pages.shape[:2] == sel_count.shape == (q.shape[0], self.desc.num_kv_heads)
+        self.lib.quantised_paged_decode(self.desc, self.records, q, sel_pages, sel_count, sm_scale, self.out, self.lse, self.workspace)
+        return self.out, self.lse
+
+
+class PageAccounts:
+    """Accounts of a paged cache's pages, and the policy by which pages with small ones are evicted: a sequence of more than
+    ``budget_pages`` keeps its first ``sink_pages``, its last ``recent_pages`` and the best of the others. ``page_table`` and
+    ``seq_lens`` are the cache's own, which ``evict_pages`` changes; the ids that it frees are in ``freed_pages`` (-1 behind the
+    ``freed_count`` of a sequence)."""
+
+    def __init__(self, *, budget_pages: int, sink_pages: int = 0, recent_pages: int = 1, q_heads: int, kv_heads: int, head_dim: int,
+                 page_size: int, dtype, num_pages: int, page_table, seq_lens, max_seq_len: int = 0, weights=None,
+                 lib: binding.Library | None = None):
+        self.lib = lib or binding.load()
+        dev, (B, max_pages) = page_table.device, page_table.shape
+        self.page_table, self.seq_lens = page_table, seq_lens
+        self.policy = (int(budget_pages), int(sink_pages), int(recent_pages))
+        self.desc = binding.make_shape_desc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page_size=page_size, dtype=dtype,
+                                            num_pages=num_pages, page_table=page_table, seq_lens=seq_lens, max_seq_len_hint=max_seq_len)
+        self.weights = torch.zeros((B, kv_heads, max_pages), device=dev, dtype=torch.float32) if weights is None else weights
+        self.freed_pages = torch.full((B, max(max_pages - self.policy[0], 1)), -1, device=dev, dtype=torch.int32)
+        self.freed_count = torch.zeros((B,), device=dev, dtype=torch.int32)
+        self.workspace = torch.empty((self.lib.account_workspace_bytes(self.desc),), device=dev, dtype=torch.uint8)
+
+    def evict_pages(self, weights_in=None, weights_out=None, page_table_out=None, seq_lens_out=None):
+        """In place by default; outputs that are given are written instead of the cache's own arrays."""
+        weights_in = self.weights if weights_in is None else weights_in
+        weights_out = weights_in if weights_out is None else weights_out
+        page_table_out = self.page_table if page_table_out is None else page_table_out
+        seq_lens_out = self.seq_lens if seq_lens_out is None else seq_lens_out
+        _check_accounts(self.page_table.shape[0], self.desc.num_kv_heads, weights_in, weights_out)
+        assert page_table_out.dtype == seq_lens_out.dtype == torch.int32
+        assert page_table_out.is_contiguous() and page_table_out.shape == self.page_table.shape
+        assert seq_lens_out.is_contiguous() and seq_lens_out.shape == self.seq_lens.shape
+        self.lib.evict_pages(self.desc, *self.policy, weights_in, weights_out, page_table_out, seq_lens_out, self.freed_pages,
+                             self.freed_count, self.workspace)

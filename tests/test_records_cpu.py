@@ -1,0 +1,157 @@
+"""The calls on 4-bit records, page accounts and eviction without a GPU: refusals, sizes, and the plain 64-bit counterparts themselves."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2605_27740_amd import binding
+from tests import records_ref as R
+from tests.test_boundary_cpu import good_desc
+
+BAD, UNSUPPORTED, WORKSPACE = binding.ERR_INVALID_ARG, binding.ERR_UNSUPPORTED, binding.ERR_WORKSPACE
+A, NWS = 0x10000, 1 << 30
+
+
+@pytest.fixture(scope="module")
+def c():
+    return binding.load().c
+
+
+def test_record_bytes(c):
+    assert c.unique_page_record_bytes(C.byref(good_desc())) == 8 * (16 * 128 + 2 * 16 * 4)
+    assert c.unique_page_record_bytes(C.byref(good_desc(head_dim=64, page_size=8, num_kv_heads=2))) == 2 * 544
+    for over in (dict(head_dim=96), dict(page_size=12), dict(num_kv_heads=0)):
+        assert c.unique_page_record_bytes(C.byref(good_desc(**over))) == 0
+    assert c.unique_page_record_bytes(None) == 0
+
+
+SHAPES = [(dict(dtype=2), BAD), (dict(batch=0), BAD), (dict(num_q_heads=30), BAD), (dict(head_dim=96), UNSUPPORTED), (dict(page_size=12), UNSUPPORTED),
+          (dict(num_q_heads=24), UNSUPPORTED), (dict(page_table=0), BAD), (dict(seq_lens=0), BAD), (dict(max_seq_len_hint=-1), BAD),
+          (dict(kv_head_stride=1024), BAD)]
+
+
+@pytest.mark.parametrize("over,code", SHAPES)
+def test_descriptors_are_refused(c, over, code):
+    d = C.byref(good_desc(**over))
+    n = C.c_size_t()
+    assert c.unique_quantise_pages(d, None, None, 0, A, None, 9, None) == code
+    assert c.unique_restore_pages(d, None, None, 0, A, None, 9, A, A, None) == code
+    assert c.unique_quantised_paged_decode(d, A, A, None, None, 0, 0.0, A, None, A, NWS, None) == code
+    assert c.unique_weighted_paged_decode(d, A, 0.0, 1.0, None, A, 64, A, None, A, NWS, None) == code
+    assert c.unique_evict_pages(d, 8, 0, 1, A, A, 64, A, A, A, A, 64, A, NWS, None) == code
+    if not any(k in over for k in ("page_table", "seq_lens")):  # a size needs no pointers
+        assert c.unique_account_workspace_bytes(d, C.byref(n)) == code
+
+
+def test_quantise_and_restore_refuse(c):
+    d = C.byref(good_desc())
+    f = c.unique_quantise_pages
+    assert f(None, None, None, 0, A, None, 9, None) == BAD
+    assert f(C.byref(good_desc(k_cache=0)), None, None, 0, A, None, 9, None) == BAD
+    assert f(C.byref(good_desc(v_cache=0)), None, None, 0, A, None, 9, None) == BAD
+    assert f(d, None, None, 0, None, None, 9, None) == BAD
+    assert f(d, None, None, 0, A + 8, None, 9, None) == BAD
+    assert f(d, None, None, 0, A, None, 0, None) == BAD
+    assert f(d, A, None, 1, A, None, 9, None) == BAD
+    assert f(d, None, A, 1, A, None, 9, None) == BAD
+    assert f(d, A, A, -1, A, None, 9, None) == BAD
+    g = c.unique_restore_pages
+    assert g(None, None, None, 0, A, None, 9, A, A, None) == BAD
+    assert g(d, None, None, 0, A, None, 9, None, A, None) == BAD
+    assert g(d, None, None, 0, A, None, 9, A, None, None) == BAD
+    assert g(d, None, None, 0, A, None, 9, A + 8, A, None) == BAD
+    assert g(d, None, None, 0, None, None, 9, A, A, None) == BAD
+    assert g(d, None, None, 0, A, None, -1, A, A, None) == BAD
+    assert g(d, A, None, 0, A, None, 9, A, A, None) == BAD
+    assert binding.load().last_error() != ""
+
+
+def test_decode_over_records_refuses(c):
+    d = C.byref(good_desc(k_cache=0, v_cache=0))
+    f = c.unique_quantised_paged_decode
+    assert f(None, A, A, None, None, 0, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, None, A, None, None, 0, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, A, None, None, None, 0, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, A, A, None, None, 0, 0.0, None, None, A, NWS, None) == BAD
+    assert f(d, A + 8, A, None, None, 0, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, A, A + 4, None, None, 0, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, A, A, A, None, 4, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, A, A, None, A, 4, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, A, A, A, A, 0, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, A, A, None, None, 0, float("nan"), A, None, A, NWS, None) == BAD
+    assert f(d, A, A, None, None, 0, 0.0, A, None, None, NWS, None) == WORKSPACE
+    assert f(d, A, A, None, None, 0, 0.0, A, None, A + 8, NWS, None) == WORKSPACE
+    assert f(d, A, A, None, None, 0, 0.0, A, None, A, 16, None) == WORKSPACE
+    assert f(d, A, A, A, A, 4, 0.0, A, None, A, 16, None) == WORKSPACE
+
+
+def test_weighted_decode_refuses(c):
+    d = C.byref(good_desc())
+    f = c.unique_weighted_paged_decode
+    assert f(C.byref(good_desc(k_cache=0)), A, 0.0, 1.0, None, A, 64, A, None, A, NWS, None) == BAD
+    assert f(C.byref(good_desc(v_cache=0)), A, 0.0, 1.0, None, A, 64, A, None, A, NWS, None) == BAD
+    assert f(d, None, 0.0, 1.0, None, A, 64, A, None, A, NWS, None) == BAD
+    assert f(d, A, 0.0, 1.0, None, None, 64, A, None, A, NWS, None) == BAD
+    assert f(d, A, 0.0, 1.0, None, A, 64, None, None, A, NWS, None) == BAD
+    assert f(d, A + 4, 0.0, 1.0, None, A, 64, A, None, A, NWS, None) == BAD
+    for decay in (-0.1, 1.1, float("nan")):
+        assert f(d, A, 0.0, decay, None, A, 64, A, None, A, NWS, None) == BAD
+    assert f(d, A, float("nan"), 1.0, None, A, 64, A, None, A, NWS, None) == BAD
+    assert f(d, A, 0.0, 1.0, None, A, 63, A, None, A, NWS, None) == BAD
+    assert f(d, A, 0.0, 1.0, None, A, 64, A, None, None, NWS, None) == WORKSPACE
+    n = C.c_size_t()
+    assert c.unique_account_workspace_bytes(d, C.byref(n)) == 0 and n.value % 256 == 0
+    assert c.unique_account_workspace_bytes(C.byref(good_desc(k_cache=0, page_table=0, seq_lens=0)), C.byref(n)) == 0
+    assert c.unique_account_workspace_bytes(d, None) == BAD and c.unique_account_workspace_bytes(None, C.byref(n)) == BAD
+    assert f(d, A, 0.0, 1.0, None, A, 64, A, None, A, 256, None) == WORKSPACE
+
+
+def test_evict_refuses(c):
+    d = C.byref(good_desc(k_cache=0, v_cache=0))
+    f = c.unique_evict_pages
+    good = [8, 2, 1, A, A, 64, A, A, A, A, 64, A, NWS, None]
+    for at in (3, 4, 6, 7, 8, 9):
+        assert f(d, *[None if i == at else v for i, v in enumerate(good)]) == BAD
+    for budget, sinks, recent in ((8, -1, 1), (8, 0, 0), (8, 5, 4), (0, 0, 1), (2 ** 31 - 1, 2 ** 31 - 1, 1)):
+        assert f(d, budget, sinks, recent, *good[3:]) == BAD
+    assert f(d, *good[:5], 63, *good[6:]) == BAD                  # weight_stride below the pages
+    assert f(d, *good[:10], 55, *good[11:]) == BAD                # 64 - 8 pages may be freed
+    assert f(d, 100, *good[1:10], 0, *good[11:]) == BAD
+    assert f(d, *good[:11], None, NWS, None) == WORKSPACE
+    assert f(d, *good[:11], A + 8, NWS, None) == WORKSPACE
+    assert f(d, *good[:12], 256, None) == WORKSPACE
+
+
+def test_the_number_format():
+    x = torch.zeros(64)
+    x[:16] = torch.tensor([6.0, 5.0, 5.01, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25, 0.26, -0.75, -5.0, -3.5, 0.0, -0.2, 7.9])
+    code, scale = R.encode(x)
+    assert code[:16].tolist() == [7, 6, 7, 6, 4, 4, 2, 2, 0, 1, 10, 14, 14, 0, 8, 7] and scale.tolist() == [127, 1]
+    assert R.values(code, scale)[:5].tolist() == [6, 4, 6, 4, 2]
+    x[40] = float("inf")
+    assert R.encode(x)[1].tolist() == [127, 255]
+    assert R.encode(torch.full((32,), 3.0e38))[1].tolist() == [252] and R.encode(torch.full((32,), 1e-44))[1].tolist() == [1]
+
+
+@pytest.mark.parametrize("S,D", [(8, 64), (16, 128), (32, 64), (32, 128)])
+def test_the_layout_is_a_permutation_and_its_own_inverse(S, D):
+    at = [R.k_byte(S, D, t, ch) for t in range(S) for ch in range(0, D, 2)] + [R.v_byte(S, D, t, ch) for t in range(S) for ch in range(0, D, 2)]
+    assert sorted(at) == list(range(S * D))
+    g = torch.Generator().manual_seed(3)
+    k, v = torch.randn((2, S, D), generator=g), torch.randn((2, S, D), generator=g)
+    tiles = R.tiles_of(k, v)
+    one = torch.zeros((R.tile_bytes(S, D),), dtype=torch.uint8)
+    for t in range(S):
+        (kc, ks), (vc, vs) = R.encode(k[1, t]), R.encode(v[1, t])
+        R.write_token(one, S, D, t, kc, ks, vc, vs)
+    assert torch.equal(one, tiles[1])
+    for x, y in zip(R.values_of(tiles, S, D), (k, v)):
+        assert torch.equal(x, R.values(*R.encode(y)))
+
+
+def test_evict_counterpart():
+    table = torch.arange(10).view(1, 10).int()
+    w = torch.tensor([[[0.0, 5, 1, 1, 9, 1, 2, 0, 0, 0]]])
+    (keep, freed, n), = R.evict(table, torch.tensor([73]), w, 8, 5, 1, 2)   # ten pages, the last of one token
+    assert keep == [0, 1, 4, 8, 9] and freed == [2, 3, 5, 6, 7] and n == 73 - 40
+    assert R.evict(table, torch.tensor([40]), w, 8, 5, 1, 2) == [(list(range(5)), [], 40)]
