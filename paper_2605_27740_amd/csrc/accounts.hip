@@ -49,60 +49,331 @@ __global__ __launch_bounds__(kAccountThreads) void account_kernel(CacheView c, S
   weights_out[at] = weights_in ? fmaf(decay, weights_in[at], w) : w;
 }
 
-// What a page is ranked by: the sum of its accounts over the KV heads in 64 bits, rounded once. First pages: +inf.
-__global__ __launch_bounds__(kAccountThreads) void rank_kernel(CacheView c, const float* weights, int weight_stride, int sinks, float* rank,
-                                                               int rank_stride, int32_t* pages) {
-  const int b = blockIdx.y, p = blockIdx.x * kAccountThreads + threadIdx.x;
-  const int P = min((c.seq_lens[b] + c.S - 1) / c.S, c.max_pages_hint);
-  if (p == 0) pages[b] = max(P, 0);
-  if (p >= P) return;
-  double sum = 0.0;
-  for (int h = 0; h < c.Hkv; ++h) sum += (double)weights[((int64_t)b * c.Hkv + h) * weight_stride + p];
-  rank[(int64_t)b * rank_stride + p] = p < sinks ? INFINITY : (float)sum;
+// A row of words behind a buffer descriptor: an access is one instruction with a 32-bit offset, where a pointer makes it a 64-bit
+// sum per lane; a load behind the row's end gives 0, and a store there, to kNowhere for instance, is dropped, so that nothing
+// branches. With sixteen waves on a compute unit an instruction costs sixteen cycles, and the kernels below are made of little else.
+constexpr uint32_t kNowhere = 0xfffffff0u;
+struct Row {
+  __amdgpu_buffer_rsrc_t at;
+  __device__ __forceinline__ Row(const void* p, int words)
+      : at(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, words * 4, 0x27000)) {}
+  __device__ __forceinline__ uint32_t word(uint32_t off) const { return __builtin_amdgcn_raw_buffer_load_b32(at, (int)off, 0, 0); }
+  __device__ __forceinline__ float real(uint32_t off) const { return __uint_as_float(word(off)); }
+  __device__ __forceinline__ void put(uint32_t off, uint32_t v) const { __builtin_amdgcn_raw_buffer_store_b32(v, at, (int)off, 0, 0); }
+};
+
+// What a page is ranked by: the sum of its accounts over the KV heads in 64 bits, rounded once. kAhead heads are requested at a
+// time, whether there are so many or not; w: the last of them.
+template <int kPer, int kAhead>
+__device__ __forceinline__ void page_ranks(const float* weights, int heads, int weight_stride, int P, const uint32_t (&off)[kPer],
+                                           float (&w)[kAhead][kPer], float (&rank)[kPer]) {
+  double sum[kPer];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) sum[j] = 0.0;
+  for (int h0 = 0; h0 < heads; h0 += kAhead) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const Row row(weights + (int64_t)min(h0 + u, heads - 1) * weight_stride, P);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) w[u][j] = row.real(off[j]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (h0 + u < heads) {  // uniform
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) sum[j] += (double)w[u][j];
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) rank[j] = (float)sum[j];
 }
 
-constexpr int kCloseThreads = 1024;
+// The ranks of all pages, for sequences that a workgroup does not sum up itself; the first pages are kept: +inf.
+__global__ __launch_bounds__(kAccountThreads) void rank_kernel(CacheView c, const float* weights, int weight_stride, int sinks, float* rank,
+                                                               int rank_stride) {
+  const int b = blockIdx.y, p = blockIdx.x * kAccountThreads + threadIdx.x;
+  const int P = min((c.seq_lens[b] + c.S - 1) / c.S, c.max_pages_hint);
+  if (p >= P) return;
+  const uint32_t off[1] = {(uint32_t)p * 4};
+  float w[8][1], r[1];
+  page_ranks<1, 8>(weights + (int64_t)b * c.Hkv * weight_stride, c.Hkv, weight_stride, P, off, w, r);
+  rank[(int64_t)b * rank_stride + p] = p < sinks ? INFINITY : r[0];
+}
 
-// Closes a sequence's rows up to the kept pages, in place or not: kept[] ascends, so that entry i comes from kept[i] >= i and
-// a round of the workgroup, which reads before it writes, leaves what later rounds read. blockIdx.x < Hkv: the accounts of a KV
-// head; else the page table, the length and the list of freed pages.
-__global__ __launch_bounds__(kCloseThreads) void close_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept, int kept_stride,
-                                                              const int32_t* __restrict__ kept_count, const int32_t* __restrict__ pages) {
+constexpr int kEvictMost = 16384;       // pages of the longest sequence that a workgroup holds
+constexpr int64_t kSumsHere = 24576;    // accounts of a sequence up to which its workgroup sums them up and closes their rows
+constexpr int kFew = 4;                 // pages that are sought one by one
+constexpr int kGathered = 256;            // keys that one wave searches
+constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
+
+// How many lanes for which pred(j) holds come before each of a wave's kPer rows of 64 lanes, in the order j, wave, lane of the workgroup;
+// counts: LDS. -> the rows' masks and what comes before them.
+template <int kPer, typename Pred>
+__device__ __forceinline__ void rows_before(Pred pred, int* counts, int wave, int lane, unsigned long long (&mask)[kPer], int (&before)[kPer]) {
+  int mine = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    mask[j] = __ballot(pred(j));
+    mine = lane == j ? __popcll(mask[j]) : mine;
+  }
+  __syncthreads();  // everyone is done with the previous contents
+  if (lane < kPer) counts[lane * kEvictWaves + wave] = mine;
+  __syncthreads();
+  if (wave == 0) {
+    int sum = 0;
+#pragma unroll
+    for (int i0 = 0; i0 < kPer * kEvictWaves; i0 += kWave) {
+      const int i = i0 + lane, n = i < kPer * kEvictWaves ? counts[i] : 0;
+      const int upto = wave_inclusive_scan(n);
+      if (i < kPer * kEvictWaves) counts[i] = sum + upto - n;
+      sum += __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+  }
+  __syncthreads();
+  mine = counts[min(lane, kPer - 1) * kEvictWaves + wave];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) before[j] = __builtin_amdgcn_readlane(mine, j);
+}
+__device__ __forceinline__ int lanes_below(unsigned long long mask, int acc) {
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, (uint32_t)acc));
+}
+
+// Chooses the pages of a sequence that stay and closes its row of the table, a workgroup a sequence with kPer keys a thread. The key
+// that separates them is found two bits at a time from the number of keys above three candidates, with comparisons and ballots only, as
+// histograms would be of a few exponents; done as soon as a candidate has exactly as many above it as stay, or few keys are
+// left, which one wave finishes. kSums: the pages'
+// sums are formed here and the rows of accounts closed, too; else they are in `rank`, and `kept` is for close_kernel.
+template <int kPer, bool kSums>
+__global__ __launch_bounds__(kEvictThreads) void evict_kernel(CacheView c, EvictArgs a, const float* __restrict__ rank, int rank_stride,
+                                                              int32_t* __restrict__ kept, int32_t* __restrict__ pages,
+                                                              int32_t* __restrict__ kept_count) {
+  constexpr int kAhead = kPer >= 8 ? 4 : 8;
+  __shared__ unsigned long long s_least[kFew];
+  __shared__ int s_sums[16][4], s_held, s_from;
+  __shared__ uint32_t s_key[kGathered];
+  __shared__ int s_counts[kPer * kEvictWaves];
+  const int b = blockIdx.x, t = threadIdx.x, lane = t % kWave, wave = __builtin_amdgcn_readfirstlane(t / kWave);
+  const int N = c.seq_lens[b];
+  const int P = max(min((N + c.S - 1) / c.S, c.max_pages_hint), 0), keep = min(P, a.budget);
+  uint32_t key[kPer], off[kPer];
+  int32_t id[kPer];
+  float w[kAhead][kPer];
+  const int64_t rows = (int64_t)b * c.Hkv * a.weight_stride;
+  {
+    const Row table(c.page_table + (int64_t)b * c.max_pages, P);
+    float r[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      off[j] = (uint32_t)(j * kEvictThreads + t) * 4;
+      id[j] = (int32_t)table.word(off[j]);
+    }
+    if constexpr (kSums) {
+      page_ranks<kPer, kAhead>(a.weights_in + rows, c.Hkv, a.weight_stride, P, off, w, r);
+    } else {
+      const Row row(rank + (int64_t)b * rank_stride, P);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) r[j] = row.real(off[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int p = j * kEvictThreads + t;
+      key[j] = p < a.sinks || p >= P - a.recent ? 0xffffffffu : score_key(r[j]);
+      key[j] = p < P ? key[j] : 0u;
+    }
+  }
+  if (t < 64) s_sums[t / 4][t % 4] = 0;
+  if (t < kFew) s_least[t] = 0;
+  if (t == 0) s_held = 0;
+  __syncthreads();
+  // Those above `last` stay, and of those that equal it the first few. One page too many, or a few, as in a decode loop: the smallest
+  // keys one after the other, the last page of equal ones, instead of the search.
+  uint32_t last = 0;
+  bool exact = P - keep <= kFew;  // every key of a page is at least 1
+  if (exact) {
+    for (int i = 0; i < P - keep; ++i) {
+      uint32_t least = ~0u, page = 0;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const uint32_t k = key[j] - 1;  // no page: the largest
+        page = k <= least ? j : page;
+        least = min(k, least);
+      }
+      const uint32_t top = wave_allreduce_minmax<false>(least);
+      const uint32_t at = wave_allreduce_minmax<true>(least == top ? page * kEvictThreads + t : 0u);
+      if (lane == 0) atomicMax(&s_least[i], (unsigned long long)~top << 32 | at);
+      __syncthreads();
+      const int gone = (int)(uint32_t)s_least[i];
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) key[j] = j * kEvictThreads + t == gone ? 0u : key[j];
+    }
+  }
+  int shift = 32, upper = 0, here = P;  // keys above the window of 2^shift from `last` on, and in it
+  while (!exact && shift > 0 && here > kGathered) {
+    shift -= 2;
+    int m[5] = {upper + here, 0, 0, 0, upper};  // keys from the d-th quarter of the window on
+#pragma unroll
+    for (int d = 1; d <= 3; ++d) {
+      const uint32_t cand = last | ((uint32_t)d << shift);
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) m[d] += __popcll(__ballot(key[j] >= cand));
+    }
+    int* sum = s_sums[shift / 2];
+    if (lane < 3) atomicAdd(&sum[lane], lane == 0 ? m[1] : (lane == 1 ? m[2] : m[3]));
+    __syncthreads();
+#pragma unroll
+    for (int d = 1; d <= 3; ++d) m[d] = __builtin_amdgcn_readfirstlane(sum[d - 1]);
+    const int d = m[3] >= keep ? 3 : (m[2] >= keep ? 2 : (m[1] >= keep ? 1 : 0));
+    const int from = d == 3 ? m[3] : (d == 2 ? m[2] : (d == 1 ? m[1] : m[0]));
+    upper = d == 3 ? m[4] : (d == 2 ? m[3] : (d == 1 ? m[2] : m[1]));
+    here = from - upper;
+    last |= (uint32_t)d << shift;
+    exact = from == keep;
+  }
+  if (!exact && shift > 0) {  // what is left is few enough for one wave, bit by bit
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (((unsigned long long)(key[j] - last) >> shift) == 0 && key[j] != 0) s_key[atomicAdd(&s_held, 1)] = key[j];
+    __syncthreads();
+    if (wave == 0) {
+      uint32_t k[kGathered / kWave];
+#pragma unroll
+      for (int i = 0; i < kGathered / kWave; ++i) k[i] = i * kWave + lane < here ? s_key[i * kWave + lane] : 0u;
+      while (shift > 0 && !exact) {
+        const uint32_t cand = last | 1u << --shift;
+        int m = upper;
+#pragma unroll
+        for (int i = 0; i < kGathered / kWave; ++i) m += __popcll(__ballot(k[i] >= cand));
+        last = m >= keep ? cand : last;
+        exact = m == keep;
+      }
+      if (lane == 0) {
+        s_key[0] = last;
+        s_held = exact;
+      }
+    }
+    __syncthreads();
+    last = s_key[0];
+    exact = s_held != 0;
+  }
+  if (P - keep > kFew && exact) last -= 1;  // the smallest that stays
+  unsigned long long mask[kPer];
+  int before[kPer];
+  if (!exact) {  // equal keys: the first few are raised above the others
+    rows_before<kPer>([&](int j) { return key[j] > last; }, s_counts, wave, lane, mask, before);
+    if (t == kEvictThreads - 1) s_from = before[kPer - 1] + __popcll(mask[kPer - 1]);
+    rows_before<kPer>([&](int j) { return key[j] == last; }, s_counts, wave, lane, mask, before);
+    const int from_same = keep - s_from;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) key[j] = key[j] == last && lanes_below(mask[j], before[j]) < from_same ? ~0u : key[j];
+  }
+  rows_before<kPer>([&](int j) { return key[j] > last; }, s_counts, wave, lane, mask, before);
+  int32_t* freed = a.freed_pages + (int64_t)b * a.freed_stride;
+  const Row table_out(a.page_table_out + (int64_t)b * c.max_pages, P), freed_row(freed, P - keep), kept_row(kept + (int64_t)b * a.budget, keep);
+  uint32_t to[kPer], vacant[kPer];  // where a page that stays goes; the place, if none will
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int p = j * kEvictThreads + t, at = lanes_below(mask[j], before[j]);  // pages before p that stay
+    to[j] = key[j] > last ? (uint32_t)at * 4 : kNowhere;
+    vacant[j] = p >= keep ? off[j] : kNowhere;
+    table_out.put(to[j], (uint32_t)id[j]);
+    table_out.put(vacant[j], ~0u);
+    freed_row.put(key[j] > last ? kNowhere : (uint32_t)(p - at) * 4, (uint32_t)id[j]);
+    if constexpr (!kSums) kept_row.put(to[j], (uint32_t)p);
+  }
+  if constexpr (kSums) {  // some heads are read before they are written, as it may be in place; few heads are here already
+    for (int h0 = 0; h0 < c.Hkv; h0 += kAhead) {
+      if (c.Hkv > kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const Row in(a.weights_in + rows + (int64_t)min(h0 + u, c.Hkv - 1) * a.weight_stride, P);
+#pragma unroll
+          for (int j = 0; j < kPer; ++j) w[u][j] = in.real(off[j]);
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (h0 + u >= c.Hkv) break;  // uniform
+        const Row out(a.weights_out + rows + (int64_t)(h0 + u) * a.weight_stride, P);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          out.put(to[j], __float_as_uint(w[u][j]));
+          out.put(vacant[j], 0u);
+        }
+      }
+    }
+  }
+  for (int i = P - keep + t; i < a.freed_stride; i += kEvictThreads) freed[i] = -1;
+  if (t == 0) {
+    a.freed_count[b] = P - keep;
+    a.seq_lens_out[b] = N - (P - keep) * c.S;
+    if constexpr (!kSums) {
+      pages[b] = P;
+      kept_count[b] = keep;
+    }
+  }
+}
+
+constexpr int kCloseThreads = 512, kCloseBatch = 8;
+
+// Closes rows of accounts up to the kept pages, in place or not: kept[] ascends, so that entry i comes from kept[i] >= i and a round
+// of the workgroup, which reads before it writes, leaves what later rounds read.
+__global__ __launch_bounds__(kCloseThreads) void close_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept,
+                                                              const int32_t* __restrict__ pages, const int32_t* __restrict__ kept_count) {
   const int b = blockIdx.y, t = threadIdx.x;
   const int P = pages[b], n = kept_count[b];
-  const int32_t* from = kept + (int64_t)b * kept_stride;
-  auto close = [&](const auto* in, auto* out, auto vacant) {
-    for (int i0 = 0; i0 < P; i0 += kCloseThreads) {
-      const int i = i0 + t;
-      auto v = vacant;
-      if (i < n) v = in[from[i]];
-      __syncthreads();
-      if (i < P) out[i] = v;
-    }
-  };
-  if ((int)blockIdx.x < c.Hkv) {
-    const int64_t row = ((int64_t)b * c.Hkv + blockIdx.x) * a.weight_stride;
-    close(a.weights_in + row, a.weights_out + row, 0.f);
-    return;
+  const int32_t* from = kept + (int64_t)b * a.budget;
+  const int64_t row = ((int64_t)b * c.Hkv + blockIdx.x) * a.weight_stride;
+  const float* in = a.weights_in + row;
+  float* out = a.weights_out + row;
+  for (int i0 = 0; i0 < n; i0 += kCloseThreads * kCloseBatch) {
+    int at[kCloseBatch];
+    float v[kCloseBatch];
+#pragma unroll
+    for (int u = 0; u < kCloseBatch; ++u) at[u] = from[min(i0 + u * kCloseThreads + t, n - 1)];
+#pragma unroll
+    for (int u = 0; u < kCloseBatch; ++u) v[u] = in[at[u]];
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kCloseBatch; ++u)
+      if (i0 + u * kCloseThreads + t < n) out[i0 + u * kCloseThreads + t] = v[u];
   }
+  __syncthreads();
+  for (int i = n + t; i < P; i += kCloseThreads) out[i] = 0.f;
+}
+
+// The table of a sequence whose pages launch_select has chosen (evict_kernel's end, for rows that no workgroup holds).
+__global__ __launch_bounds__(kEvictThreads) void close_table_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept,
+                                                                    const int32_t* __restrict__ kept_count, int32_t* __restrict__ pages) {
+  const int b = blockIdx.x, t = threadIdx.x;
+  const int N = c.seq_lens[b];
+  const int P = max(min((N + c.S - 1) / c.S, c.max_pages_hint), 0), n = kept_count[b];
+  const int32_t* from = kept + (int64_t)b * a.budget;
   const int32_t* table = c.page_table + (int64_t)b * c.max_pages;
+  int32_t* table_out = a.page_table_out + (int64_t)b * c.max_pages;
   int32_t* freed = a.freed_pages + (int64_t)b * a.freed_stride;
-  for (int p = t; p < P; p += kCloseThreads) {  // kept pages below p
+  for (int p = t; p < P; p += kEvictThreads) {  // kept pages below p
     int lo = 0, hi = n;
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (from[mid] < p) lo = mid + 1;
       else hi = mid;
     }
-    if ((lo == n || from[lo] != p) && p - lo < a.freed_stride) freed[p - lo] = table[p];
+    if (lo == n || from[lo] != p) freed[p - lo] = table[p];
   }
-  for (int i = P - n + t; i < a.freed_stride; i += kCloseThreads) freed[i] = -1;
-  const int N = c.seq_lens[b];
+  for (int i = P - n + t; i < a.freed_stride; i += kEvictThreads) freed[i] = -1;
   __syncthreads();
-  close(table, a.page_table_out + (int64_t)b * c.max_pages, (int32_t)-1);
+  for (int i0 = 0; i0 < P; i0 += kEvictThreads) {
+    const int i = i0 + t;
+    int32_t v = -1;
+    if (i < n) v = table[from[i]];
+    __syncthreads();
+    if (i < P) table_out[i] = v;
+  }
   if (t == 0) {
     a.freed_count[b] = P - n;
     a.seq_lens_out[b] = N - (P - n) * c.S;
+    pages[b] = P;
   }
 }
 
@@ -156,16 +427,37 @@ hipError_t launch_evict(const CacheView& c, const EvictArgs& args, hipStream_t s
   ws += aligned((size_t)c.B * c.max_pages_hint * sizeof(int32_t));
   int32_t* pages = reinterpret_cast<int32_t*>(ws);
   int32_t* kept_count = reinterpret_cast<int32_t*>(ws + aligned((size_t)c.B * sizeof(int32_t)));
-  const dim3 grid((c.max_pages_hint + kAccountThreads - 1) / kAccountThreads, c.B);
-  rank_kernel<<<grid, dim3(kAccountThreads), 0, stream>>>(c, a.weights_in, a.weight_stride, a.sinks, rank, rank_stride, pages);
-  hipError_t e = hipGetLastError();
+  hipError_t e = hipSuccess;
+  const bool sums = (int64_t)c.Hkv * c.max_pages_hint <= kSumsHere && c.max_pages_hint <= kEvictMost;
+  if (!sums) {
+    const dim3 grid((c.max_pages_hint + kAccountThreads - 1) / kAccountThreads, c.B);
+    rank_kernel<<<grid, dim3(kAccountThreads), 0, stream>>>(c, a.weights_in, a.weight_stride, a.sinks, rank, rank_stride);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess) return e;
-  CacheView one = c;  // a row per sequence
-  one.Hkv = one.H = 1;
-  one.force_recent = a.recent;
-  e = launch_select(one, rank, nullptr, rank_stride, a.budget, kept, kept_count, stream);
-  if (e != hipSuccess) return e;
-  close_kernel<<<dim3(c.Hkv + 1, c.B), dim3(kCloseThreads), 0, stream>>>(c, a, kept, a.budget, kept_count, pages);
+  auto go = [&](auto kernel) {
+    kernel<<<dim3(c.B), dim3(kEvictThreads), 0, stream>>>(c, a, rank, rank_stride, kept, pages, kept_count);
+    return hipGetLastError();
+  };
+  auto held = [&](auto per) {
+    constexpr int kPer = decltype(per)::value;
+    return sums ? go(evict_kernel<kPer, true>) : go(evict_kernel<kPer, false>);
+  };
+  if (c.max_pages_hint <= 1024) e = held(std::integral_constant<int, 1>());
+  else if (c.max_pages_hint <= 4096) e = held(std::integral_constant<int, 4>());
+  else if (c.max_pages_hint <= 8192) e = held(std::integral_constant<int, 8>());
+  else if (c.max_pages_hint <= kEvictMost) e = held(std::integral_constant<int, 16>());
+  else {
+    CacheView one = c;  // a row per sequence
+    one.Hkv = one.H = 1;
+    one.force_recent = a.recent;
+    e = launch_select(one, rank, nullptr, rank_stride, a.budget, kept, kept_count, stream);
+    if (e != hipSuccess) return e;
+    close_table_kernel<<<dim3(c.B), dim3(kEvictThreads), 0, stream>>>(c, a, kept, kept_count, pages);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || sums) return e;
+  close_kernel<<<dim3(c.Hkv, c.B), dim3(kCloseThreads), 0, stream>>>(c, a, kept, pages, kept_count);
   return hipGetLastError();
 }
 

@@ -11,7 +11,7 @@
 // k are the two halves' four slots --, as parts of 8 bits in rows parts times heads; B = the values of those slots, channels
 // D/16 * (L % 16) + e: 16 bytes of a half at D = 128, with a scale for each slot.
 // fp32 queries are taken as three bf16 numbers (24 bits, exactly), three products instead of one. The probabilities are three parts
-// (24 bits), two for eight heads of a bf16 output: what is left out is below 2^-16 of a probability, the output's own rounding 2^-9.
+// (24 bits) for fp32 outputs, two for bf16: what is left out is below 2^-16 of a probability, the output's own rounding 2^-9.
 #include <type_traits>
 
 #include "decode_core.hpp"
@@ -22,7 +22,8 @@ namespace {
 
 template <typename T, int D, int G>
 struct QuantShared {  // the waves' results; output rows are parts times heads
-  static constexpr int kSlots = G == 8 ? 16 : 3 * G;
+  static constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
+  static constexpr int kSlots = kParts * G > 16 ? 16 : kParts * G;
   __attribute__((aligned(16))) float acc[kDecWaves][kSlots][D];
   float m[kDecWaves][G], l[kDecWaves][G];
 };
@@ -66,6 +67,7 @@ struct QuantHalf {
   uint32_t v[4 * D / 128]; // D/16 channels of four slots
   uint32_t ks, vs;         // a byte; four bytes
   int valid;               // how many of the slots 4 * (L / 16) + i hold a token (any value <= 0: none)
+  bool full;               // all 16 slots do (uniform)
 };
 
 template <int D, int S, int G, bool kNT, typename T, typename Lookup>
@@ -113,6 +115,13 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
 
   const int64_t page_bytes = (int64_t)c.Hkv * kT.bytes();
   const char* mine = records + (int64_t)hkv * kT.bytes();
+  // where this lane's bytes lie behind the first slot of a half (S = 8: of its page)
+  const int kslot = S == 8 ? kt % 8 : kt, vslot = S == 8 ? 4 * kg % 8 : 4 * kg;
+  const uint32_t k_off = kT.k_codes() + kslot * (D / 2) + kg * (D / 8), v_off = kT.v_at(vslot, kt);
+  const uint32_t ks_off = kT.k_scales() + kg * (D / 4) / kQuantBlock * S + kslot;
+  const uint32_t vs_off = kT.v_scales() + kt * kVB / kQuantBlock * S + vslot;
+  // bits of a probability that this lane's part of it is without: those of the parts before
+  const uint32_t not_first = part >= 1 ? 0xffff0000u : 0u, not_second = part >= 2 ? 0xffff0000u : 0u;
 
   for (int e0 = begin + wave; e0 < end; e0 += kDecWaves * kWave) {
     int my_phys = 0, my_ntok = 0;
@@ -126,39 +135,38 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         QuantHalf<D>& x = half[h];
-        const char *kp, *vp;  // the record of this lane's key slot and of its value slots
-        int k_slot, v_slot;
-        if constexpr (S >= 16) {  // one page: scalar
-          const int gs = tile * kSlots32 + h * 16, ent = min(gs / S, kWave - 1);
+        const char *kp, *vp;  // the records of this lane's key slot and of its value slots
+        constexpr int kHalf = S == 32 ? 16 : 0;
+        const int first = h * kHalf;  // slot of the page that the half begins with
+        if constexpr (S >= 16) {      // one page: scalar
+          const int ent = min((tile * kSlots32 + h * 16) / S, kWave - 1);
           const int phys = __builtin_amdgcn_readlane(my_phys, ent);
           const int ntok = tile < n_tiles ? __builtin_amdgcn_readlane(my_ntok, ent) : 0;
           kp = vp = mine + phys * page_bytes;
-          k_slot = gs % S + kt;
-          v_slot = gs % S + 4 * kg;
-          x.valid = ntok - v_slot;
+          x.valid = ntok - first - vslot;
+          x.full = ntok >= first + 16;
         } else {  // two pages
           const int e1 = min(tile * 4 + h * 2, kWave - 1), e2 = min(e1 + 1, kWave - 1);
           const int p1 = __builtin_amdgcn_readlane(my_phys, e1), p2 = __builtin_amdgcn_readlane(my_phys, e2);
           const int n1 = __builtin_amdgcn_readlane(my_ntok, e1), n2 = __builtin_amdgcn_readlane(my_ntok, e2);
           kp = mine + (kt < 8 ? p1 : p2) * page_bytes;
           vp = mine + (kg < 2 ? p1 : p2) * page_bytes;
-          k_slot = kt % 8;
-          v_slot = 4 * kg % 8;
-          x.valid = (tile < n_tiles ? (kg < 2 ? n1 : n2) : 0) - v_slot;
+          x.valid = (tile < n_tiles ? (kg < 2 ? n1 : n2) : 0) - vslot;
+          x.full = tile < n_tiles && n1 >= 8 && n2 >= 8;
         }
         if constexpr (D == 128) {
-          const u32x4_t kw = load_as<kNT, u32x4_t>(kp + kT.k_codes() + k_slot * 64 + kg * 16);
-          const u32x4_t vw = load_as<kNT, u32x4_t>(vp + kT.v_at(v_slot, kt));
+          const u32x4_t kw = load_as<kNT, u32x4_t>(kp + first * (D / 2) + k_off);
+          const u32x4_t vw = load_as<kNT, u32x4_t>(vp + first * (D / 2) + v_off);
 #pragma unroll
           for (int i = 0; i < 4; ++i) { x.k[i] = kw[i]; x.v[i] = vw[i]; }
         } else {
-          const u32x2_t kw = load_as<kNT, u32x2_t>(kp + kT.k_codes() + k_slot * 32 + kg * 8);
-          const u32x2_t vw = load_as<kNT, u32x2_t>(vp + kT.v_at(v_slot, kt));
+          const u32x2_t kw = load_as<kNT, u32x2_t>(kp + first * (D / 2) + k_off);
+          const u32x2_t vw = load_as<kNT, u32x2_t>(vp + first * (D / 2) + v_off);
 #pragma unroll
           for (int i = 0; i < 2; ++i) { x.k[i] = kw[i]; x.v[i] = vw[i]; }
         }
-        x.ks = load_as<kNT, uint8_t>(kp + kT.k_scales() + kg * (D / 4) / kQuantBlock * S + k_slot);
-        x.vs = load_as<kNT, uint32_t>(vp + kT.v_scales() + kt * kVB / kQuantBlock * S + v_slot);
+        x.ks = load_as<kNT, uint8_t>(kp + first + ks_off);
+        x.vs = load_as<kNT, uint32_t>(vp + first + vs_off);
       }
     };
     auto consume = [&](QuantHalf<D>(&half)[2]) {
@@ -166,10 +174,9 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
       float x[8];
       auto relative = [&] {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[4 * h + i] = i < half[h].valid ? fmaf(logits[h][i], scale_log2, -m) : -INFINITY;
+        for (int i = 0; i < 8; ++i) x[i] = fmaf(logits[i / 4][i % 4], scale_log2, -m);
       };
+      const bool full = half[0].full && half[1].full;  // uniform
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const float sk = scale_at<0>(half[h].ks);
@@ -183,6 +190,15 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
         }
         logits[h] = sacc;
       }
+      if (!full) {  // a slot without a token may hold any scale, also the one that stands for NaN: that of its value becomes the smallest
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int n = half[h].valid;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) logits[h][i] = i < n ? logits[h][i] : -INFINITY;
+          half[h].vs &= n >= 4 ? ~0u : (n <= 0 ? 0u : (1u << (8 * n)) - 1u);
+        }
+      }
       relative();
       float top = x[0];
 #pragma unroll
@@ -192,7 +208,7 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) t = i < half[h].valid ? fmaxf(t, logits[h][i] * scale_log2) : t;
+          for (int i = 0; i < 4; ++i) t = fmaxf(t, logits[h][i] * scale_log2);
         const float mnew = fmaxf(m, rows_allreduce(t, OpMax()) + kRoom);
         const float alpha = fast_exp2(m - mnew);
         m = mnew;
@@ -218,21 +234,18 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
       for (int i = 0; i < 8; ++i) {
         const float p = fast_exp2(x[i]);
         l += p;
-        const float r1 = p - bf16_part(p);
-        if constexpr (G == 8) {
-          pa[i] = __float_as_uint(part == 0 ? p : r1);
-          if constexpr (kThird) pb[i] = part == 0 ? __float_as_uint(r1 - bf16_part(r1)) : 0u;
-        } else {
-          pa[i] = __float_as_uint(part == 0 ? p : (part == 1 ? r1 : r1 - bf16_part(r1)));
+        float r = p - __uint_as_float(__float_as_uint(p) & not_first);
+        if constexpr (kThird) {
+          const float r1 = p - bf16_part(p);
+          pb[i] = __float_as_uint(r1 - bf16_part(r1)) & ~not_first;
+        } else if constexpr (sizeof(T) == 4) {
+          r -= __uint_as_float(__float_as_uint(r) & not_second);
         }
+        pa[i] = __float_as_uint(r);
       }
       const bf16x8_t a0 = as_bf16x8(pack_hi(pa[0], pa[1]), pack_hi(pa[2], pa[3]), pack_hi(pa[4], pa[5]), pack_hi(pa[6], pa[7]));
       bf16x8_t a1 = a0;
       if constexpr (kThird) a1 = as_bf16x8(pack_hi(pb[0], pb[1]), pack_hi(pb[2], pb[3]), pack_hi(pb[4], pb[5]), pack_hi(pb[6], pb[7]));
-      // A slot without a token may hold any scale, also the one that stands for NaN: it becomes the smallest.
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (__any(half[h].valid < 4)) half[h].vs &= half[h].valid >= 4 ? ~0u : (half[h].valid <= 0 ? 0u : (1u << (8 * half[h].valid)) - 1u);
       uint32_t v[8][kVB / 2];  // two channels of a slot
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -290,7 +303,7 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
 }
 
 template <typename T, int D, int S, int G, bool kNT>
-__global__ __launch_bounds__(kDecWaves* kWave) void quant_partial_kernel(CacheView c, QuantDecodeArgs a, SplitPlan plan) {
+__global__ __launch_bounds__(kDecWaves* kWave, sizeof(T) == 4 ? 2 : 3) void quant_partial_kernel(CacheView c, QuantDecodeArgs a, SplitPlan plan) {
   __shared__ QuantShared<T, D, G> sh;
   int split, hkv, b;
   locate_chunk(c, plan, split, hkv, b);

@@ -89,7 +89,7 @@ class DecodeSession:
         """``dense_paged_decode`` that adds each page's share to its account: ``page_weights``, or from one array to another."""
         if weights_out is None:
             weights_in = weights_out = self.page_weights
-        _check_accounts(self.wl.B, self.wl.Hkv, weights_in, weights_out)
+        _check_accounts(self.page_weights.shape, weights_in, weights_out)
         self.lib.weighted_paged_decode(self.desc, self.wl.q, sm_scale, decay, weights_in, weights_out, self.out_dense,
                                        self.lse_dense, self.workspace)
 
@@ -99,10 +99,9 @@ class DecodeSession:
         self.sparse_paged_decode()
 
 
-def _check_accounts(batch: int, kv_heads: int, weights_in, weights_out):
-    for w in (weights_in, weights_out):
-        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.shape[:2] == (batch, kv_heads))
-    assert weights_in is None or weights_in.shape == weights_out.shape
+def _check_accounts(shape, *weights):
+    for w in weights:
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.shape == shape)
 
 
 class QuantisedCache:
@@ -123,17 +122,22 @@ class QuantisedCache:
         assert records.dtype == torch.uint8 and records.is_contiguous() and records.shape[0] == num_pages
         assert records.numel() == num_pages * record
         self.records = records
+        self._tile = (kv_heads, page_size, head_dim)
         B = page_table.shape[0]
         self.out = torch.zeros((B, q_heads, head_dim), device=dev, dtype=dtype)
         self.lse = torch.zeros((B, q_heads), device=dev, dtype=torch.float32)
         self.workspace = torch.empty((max(self.lib.workspace_bytes(self.desc, max(top_k, 1)), 256),), device=dev, dtype=torch.uint8)
 
     def _full_desc(self, k, v, table):
-        table = self.page_table if table is None else table
-        assert k.dtype == self.dtype and k.shape[1:] == (self.desc.num_kv_heads, self.desc.page_size, self.desc.head_dim)
-        assert table.shape == self.page_table.shape
-        return binding.make_desc(q_heads=self.desc.num_q_heads, k_cache=k, v_cache=v, page_stats=None, page_table=table,
-                                 seq_lens=self.seq_lens, max_seq_len_hint=self.desc.max_seq_len_hint)
+        """The descriptor with full-precision pages instead of the pool (a copy: 2 us where ``binding.make_desc`` takes 5)."""
+        d, stride = binding.CacheDesc.from_buffer_copy(self.desc), k.stride()
+        assert k.dtype == v.dtype == self.dtype and k.shape[1:] == self._tile and k.shape == v.shape
+        assert stride == v.stride() and stride[2:] == (self._tile[2], 1)
+        d.num_phys_pages, d.k_cache, d.v_cache, d.kv_page_stride, d.kv_head_stride = k.shape[0], k.data_ptr(), v.data_ptr(), *stride[:2]
+        if table is not None:
+            assert table.dtype == torch.int32 and table.is_contiguous() and table.shape == self.page_table.shape
+            d.page_table = table.data_ptr()
+        return d
 
     def quantise_pages(self, k_cache, v_cache, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int = 0):
         """Tokens of full-precision pages, found by ``page_table`` (default: the pool's own), into records."""
@@ -150,7 +154,7 @@ class QuantisedCache:
         assert q.dtype == self.dtype and q.is_contiguous() and q.shape == self.out.shape
         if sel_pages is not None:
             assert sel_pages.dtype == sel_count.dtype == torch.int32 and sel_pages.is_contiguous() and sel_count.is_contiguous()
-            assert sel_pages.shape[:2] == sel_count.shape == (q.shape[0], self.desc.num_kv_heads)
+            assert sel_pages.shape[:2] == sel_count.shape == (q.shape[0], self._tile[0])
         self.lib.quantised_paged_decode(self.desc, self.records, q, sel_pages, sel_count, sm_scale, self.out, self.lse, self.workspace)
         return self.out, self.lse
 
@@ -171,6 +175,7 @@ class PageAccounts:
         self.desc = binding.make_shape_desc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page_size=page_size, dtype=dtype,
                                             num_pages=num_pages, page_table=page_table, seq_lens=seq_lens, max_seq_len_hint=max_seq_len)
         self.weights = torch.zeros((B, kv_heads, max_pages), device=dev, dtype=torch.float32) if weights is None else weights
+        _check_accounts((B, kv_heads, max_pages), self.weights)
         self.freed_pages = torch.full((B, max(max_pages - self.policy[0], 1)), -1, device=dev, dtype=torch.int32)
         self.freed_count = torch.zeros((B,), device=dev, dtype=torch.int32)
         self.workspace = torch.empty((self.lib.account_workspace_bytes(self.desc),), device=dev, dtype=torch.uint8)
@@ -178,12 +183,10 @@ class PageAccounts:
     def evict_pages(self, weights_in=None, weights_out=None, page_table_out=None, seq_lens_out=None):
         """In place by default; outputs that are given are written instead of the cache's own arrays."""
         weights_in = self.weights if weights_in is None else weights_in
-        weights_out = weights_in if weights_out is None else weights_out
-        page_table_out = self.page_table if page_table_out is None else page_table_out
-        seq_lens_out = self.seq_lens if seq_lens_out is None else seq_lens_out
-        _check_accounts(self.page_table.shape[0], self.desc.num_kv_heads, weights_in, weights_out)
-        assert page_table_out.dtype == seq_lens_out.dtype == torch.int32
-        assert page_table_out.is_contiguous() and page_table_out.shape == self.page_table.shape
-        assert seq_lens_out.is_contiguous() and seq_lens_out.shape == self.seq_lens.shape
-        self.lib.evict_pages(self.desc, *self.policy, weights_in, weights_out, page_table_out, seq_lens_out, self.freed_pages,
-                             self.freed_count, self.workspace)
+        if weights_out is None:
+            weights_out = weights_in
+        _check_accounts(self.weights.shape, weights_in, weights_out)
+        for given, mine in ((page_table_out, self.page_table), (seq_lens_out, self.seq_lens)):
+            assert given is None or (given.dtype == torch.int32 and given.is_contiguous() and given.shape == mine.shape)
+        self.lib.evict_pages(self.desc, *self.policy, weights_in, weights_out, self.page_table if page_table_out is None else page_table_out,
+                             self.seq_lens if seq_lens_out is None else seq_lens_out, self.freed_pages, self.freed_count, self.workspace)
