@@ -1,53 +1,15 @@
-// Accounts of pages from the shares that weigh.hip's kernels write, and the eviction of pages by them.
+// Eviction of the pages with the smallest accounts.
 #include <algorithm>
 #include <type_traits>
 
 #include "decode_core.hpp"
+#include "dense_plan.hpp"
 #include "weigh.hpp"
 
 namespace unique {
 namespace {
 
 constexpr int kAccountThreads = 256;
-
-// The weights of a row's pages: the maximum M and the sum L of its chunks' (m, l) for every head, then, a thread a page,
-// sum over the heads of 2^(share - M) / L.
-template <int G>
-__global__ __launch_bounds__(kAccountThreads) void account_kernel(CacheView c, SplitPlan plan, const float* __restrict__ part_ml,
-                                                                  const float* __restrict__ shares, const float* weights_in, float* weights_out,
-                                                                  int weight_stride, float decay) {
-  __shared__ float s_m[G], s_r[G];
-  const int b = blockIdx.z, row = b * c.Hkv + blockIdx.y;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int P = min((c.seq_lens[b] + c.S - 1) / c.S, c.max_pages_hint);
-  if ((int)blockIdx.x * kAccountThreads >= P) return;
-  const int ns = (P + plan.pages_per_split - 1) / plan.pages_per_split;
-  for (int g = wave; g < G; g += kAccountThreads / kWave) {
-    const float2* ml = reinterpret_cast<const float2*>(part_ml) + (int64_t)row * plan.num_splits * G + g;
-    float M = kNegBig;
-    for (int s = lane; s < ns; s += kWave) M = fmaxf(M, ml[(int64_t)s * G].x);
-    M = group_allreduce<kWave>(M, OpMax());
-    float L = 0.f;
-    for (int s = lane; s < ns; s += kWave) {
-      const float2 p = ml[(int64_t)s * G];
-      L = fmaf(p.y, fast_exp2(p.x - M), L);
-    }
-    L = group_allreduce<kWave>(L, OpSum());
-    if (lane == 0) {
-      s_m[g] = M;
-      s_r[g] = L > 0.f ? 1.f / L : 0.f;
-    }
-  }
-  __syncthreads();
-  const int p = blockIdx.x * kAccountThreads + threadIdx.x;
-  if (p >= P) return;
-  const float* share = shares + ((int64_t)row * c.max_pages_hint + p) * G;
-  float w = 0.f;
-#pragma unroll
-  for (int g = 0; g < G; ++g) w = fmaf(fast_exp2(share[g] - s_m[g]), s_r[g], w);
-  const int64_t at = (int64_t)row * weight_stride + p;
-  weights_out[at] = weights_in ? fmaf(decay, weights_in[at], w) : w;
-}
 
 // A row of words behind a buffer descriptor: an access is one instruction with a 32-bit offset, where a pointer makes it a 64-bit
 // sum per lane; a load behind the row's end gives 0, and a store there, to kNowhere for instance, is dropped, so that nothing
@@ -387,28 +349,15 @@ size_t weigh_floats(const CacheView& c) {
 }
 
 hipError_t launch_weigh(const CacheView& c, const WeighArgs& a, hipStream_t stream) {
-  const SplitPlan plan = most_splits(c.B * c.Hkv, c.max_pages_hint);
-  const int G = c.H / c.Hkv;
-  float* part_ml = a.partials + (size_t)c.B * c.Hkv * plan.num_splits * G * c.D;
-  float* shares = a.partials + plan_partial_floats(c, plan);
-  auto run = [&](auto launch) { return launch(c, a, plan, part_ml, shares, stream); };
-  hipError_t e = c.dtype == 0 ? (c.D == 64 ? run(launch_weigh_partial<float, 64>) : run(launch_weigh_partial<float, 128>))
-                              : (c.D == 64 ? run(launch_weigh_partial<bf16_t, 64>) : run(launch_weigh_partial<bf16_t, 128>));
-  if (e != hipSuccess) return e;
-  e = launch_merge(c, nullptr, c.max_pages_hint, plan, a.partials, a.out, a.lse_out, stream);
-  if (e != hipSuccess) return e;
-  const dim3 grid((c.max_pages_hint + kAccountThreads - 1) / kAccountThreads, c.Hkv, c.B);
-  auto account = [&](auto kernel) {
-    kernel<<<grid, dim3(kAccountThreads), 0, stream>>>(c, plan, part_ml, shares, a.weights_in, a.weights_out, a.weight_stride, a.decay);
-    return hipGetLastError();
-  };
-  switch (G) {
-    case 1: return account(account_kernel<1>);
-    case 2: return account(account_kernel<2>);
-    case 4: return account(account_kernel<4>);
-    case 8: return account(account_kernel<8>);
-    default: return hipErrorInvalidValue;
-  }
+  const int rows = c.B * c.Hkv;
+  WeighCut cut = {most_splits(rows, c.max_pages_hint), 0};
+  if (dense_balances(c.B, c.Hkv, c.max_pages_hint, c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2))) cut.max_chunks = dense_max_chunks(rows, c.max_pages_hint);
+  const size_t slots = cut.max_chunks > 0 ? cut.max_chunks : (size_t)rows * cut.plan.num_splits;
+  float* part_ml = a.partials + slots * (c.H / c.Hkv) * c.D;
+  float* shares = a.partials + decode_partial_floats(c, c.max_pages_hint);
+  auto run = [&](auto launch) { return launch(c, a, cut, part_ml, shares, stream); };
+  return c.dtype == 0 ? (c.D == 64 ? run(launch_weigh_of<float, 64>) : run(launch_weigh_of<float, 128>))
+                      : (c.D == 64 ? run(launch_weigh_of<bf16_t, 64>) : run(launch_weigh_of<bf16_t, 128>));
 }
 
 size_t evict_bytes(const CacheView& c) {

@@ -8,41 +8,10 @@
 // to 131K tokens (5.7 GB) 1832 before, 911 now. Other sizes: dense_plan.hpp.
 #include <type_traits>
 
-#include "decode_core.hpp"
-#include "dense_plan.hpp"
+#include "dense_cut.hpp"
 
 namespace unique {
 namespace {
-
-// The chunks of a batch, the same in every wave that asks: lane b holds those of sequence b.
-struct BatchChunks {
-  int len;     // tokens of sequence `lane`
-  int pages;
-  int chunks;  // per row of that sequence
-  int before;  // chunks per head of the sequences before it
-};
-
-__device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_inclusive_scan(x), kWave - 1); }
-
-// false: no chunk has the index w, or a larger one
-__device__ __forceinline__ bool cut_batch(const CacheView& c, int S, int max_chunks, int w, BatchChunks& bc) {
-  const int lane = threadIdx.x % kWave;
-  bc.len = lane < c.B ? c.seq_lens[lane] : 0;
-  bc.pages = max(0, min((bc.len + S - 1) / S, c.max_pages_hint));
-  const int rows = c.B * c.Hkv;
-  const int total = wave_sum(bc.pages) * c.Hkv, slots = dense_slots(total, max_chunks);
-  const bool room = dense_has_room(rows, slots, max_chunks);
-  if (w >= (room ? slots + rows : slots)) return false;  // most workgroups of a launch whose bound is far above the lengths
-  if (__ballot(lane < c.B && bc.pages != __builtin_amdgcn_readfirstlane(bc.pages)) == 0) {
-    bc.chunks = lane < c.B ? dense_even_chunks(bc.pages, rows, slots) : 0;
-  } else {
-    bc.chunks = dense_row_chunks(bc.pages, dense_rate(total, rows, slots, [&](uint32_t rate) {
-      return wave_sum(dense_row_weight(bc.pages, rate, room)) * c.Hkv;
-    }));
-  }
-  bc.before = wave_inclusive_scan(bc.chunks) - bc.chunks;
-  return true;
-}
 
 template <typename T, int D, int S, int G, bool kNT>
 __global__ __launch_bounds__(kDecWaves* kWave) void paged_decode_dense_kernel(CacheView c, const T* __restrict__ q, int max_chunks,
@@ -53,16 +22,11 @@ __global__ __launch_bounds__(kDecWaves* kWave) void paged_decode_dense_kernel(Ca
   const int w = blockIdx.x;
   BatchChunks bc;
   if (!cut_batch(c, S, max_chunks, w, bc)) return;
-  const unsigned long long here = __ballot(w >= bc.before * c.Hkv && w < (bc.before + bc.chunks) * c.Hkv);
-  if (here == 0) return;  // beyond the last chunk
-  const int b = __ffsll(here) - 1;
-  const int P = __builtin_amdgcn_readlane(bc.pages, b), n = __builtin_amdgcn_readlane(bc.chunks, b);
-  const int i = w - __builtin_amdgcn_readlane(bc.before, b) * c.Hkv;  // chunk `split` of head hkv
-  const int hkv = i / n, split = i % n, len = (P + n - 1) / n;
-  const int begin = split * len, end = min(begin + len, P);
-  const int N = __builtin_amdgcn_readlane(bc.len, b);
+  const unsigned long long here = sequence_of(c, bc, w);
+  if (here == 0) return;
+  const Chunk chunk = chunk_of(c, bc, here, w);
+  const int b = chunk.b, N = chunk.N;
   const ChunkOut<T> to = {part_o, part_ml, nullptr, nullptr, 2};
-  const Chunk chunk = {hkv, b, begin, max(begin, end), N, w};
   auto lookup = [&](int e, bool, int& phys, int& ntok) {
     const int ph = c.page_table[(int64_t)b * c.max_pages + e];
     if (ph >= 0 && (int64_t)ph < c.num_phys) {
@@ -79,12 +43,7 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_decode_dense_merge_kernel
                                                                                   const float* __restrict__ part_ml, T* __restrict__ out,
                                                                                   float* __restrict__ lse_out) {
   __shared__ MergeShared<kWaves, D> sh;
-  const int h = blockIdx.x, b = blockIdx.y, hkv = h / G;
-  BatchChunks bc;
-  cut_batch(c, c.S, max_chunks, 0, bc);
-  const int n = __builtin_amdgcn_readlane(bc.chunks, b);
-  const int64_t base = (int64_t)__builtin_amdgcn_readlane(bc.before, b) * c.Hkv + (int64_t)hkv * n;
-  merge_chunks<T, D, G, kWaves>(c, b, h, base, n, [&] { return n; }, part_o, part_ml, out, lse_out, sh);
+  merge_cut<T, D, G, kWaves>(c, blockIdx.y, blockIdx.x, max_chunks, {}, part_o, part_ml, out, lse_out, sh);
 }
 
 template <typename T, int D, int S, int G>

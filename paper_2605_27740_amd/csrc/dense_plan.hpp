@@ -10,13 +10,16 @@ namespace unique {
 
 constexpr int kDenseSlots = 512;    // workgroups that run at the same time: two on each of the 256 compute units
 constexpr int kDensePages = 256;    // pages of a chunk from which on twice the workgroups are used
+struct DenseRound {  // workgroups at a time, and the pages of a chunk from which on there are more rounds of them
+  int slots = kDenseSlots, pages = kDensePages;
+};
 constexpr int64_t kDenseLeastBytes = 96ll << 20;
 constexpr int kDenseMaxBatch = 64;  // a lane per sequence
 
 // Chunks of the whole batch, at most as many as the partial results of most_splits hold.
-inline int dense_max_chunks(int rows, int max_pages) {
+inline int dense_max_chunks(int rows, int max_pages, DenseRound round = {}) {
   const int64_t all = (int64_t)rows * most_splits(rows, max_pages).num_splits;
-  const int64_t wanted = std::max<int64_t>((int64_t)rows * max_pages / (kDenseSlots * kDensePages), 1) * kDenseSlots;
+  const int64_t wanted = std::max<int64_t>((int64_t)rows * max_pages / (round.slots * round.pages), 1) * round.slots;
   return (int)std::min(all, wanted);
 }
 
@@ -25,10 +28,10 @@ inline int dense_max_chunks(int rows, int max_pages) {
 // 8 KV heads, G = 4, D = 128, pages of 16): 4 sequences of 6K to 30K tokens 66.4 / 43.2; 8 of 2K to 60K, 1012 MB 205 / 163; 16 of 1K
 // to 16K 128 / 70; even ones 8 x 16384 86.6 / 86.5, 16 x 30000 312 / 299, 5 x 7000 31.3 / 30.1. More rows than half the slots, and a
 // single sequence, have nothing to gain.
-inline bool dense_balances(int batch, int kv_heads, int max_pages, int page_bytes) {
+inline bool dense_balances(int batch, int kv_heads, int max_pages, int page_bytes, int64_t least_bytes = kDenseLeastBytes) {
   const int64_t rows = (int64_t)batch * kv_heads;
   if (batch < 2 || batch > kDenseMaxBatch || rows > kDenseSlots / 2 || rows * max_pages > INT32_MAX) return false;
-  return most_splits((int)rows, max_pages).num_splits > 1 && rows * max_pages * page_bytes >= kDenseLeastBytes;
+  return most_splits((int)rows, max_pages).num_splits > 1 && rows * max_pages * page_bytes >= least_bytes;
 }
 
 // One wave merges a head's chunks where the slots are four or fewer to a row, on average: every wave finds the cut for itself, which costs more
@@ -37,9 +40,9 @@ inline bool dense_balances(int batch, int kv_heads, int max_pages, int page_byte
 constexpr bool dense_merge_alone(int rows) { return rows >= kDenseSlots / 4; }
 
 // Workgroups that share the pages of a batch, `total` of them over all rows: those that run at the same time, or a multiple.
-constexpr int dense_slots(int total, int max_chunks) {
-  const int rounds = total / (kDenseSlots * kDensePages);
-  return std::min((rounds > 1 ? rounds : 1) * kDenseSlots, max_chunks);
+constexpr int dense_slots(int total, int max_chunks, DenseRound round = {}) {
+  const int rounds = total / (round.slots * round.pages);
+  return std::min((rounds > 1 ? rounds : 1) * round.slots, max_chunks);
 }
 // Where there is room for a chunk per row beside the slots, rows of less than a quarter of a chunk take only an eighth or two of a slot
 // each, as they are soon done: one sequence of 100000 tokens beside 30 of 50, whose 240 rows would leave it half of the slots, 104 / 76

@@ -202,14 +202,19 @@ hipError_t launch_quant_decode(const CacheView& c, const void* records, const vo
                                int sel_stride, int max_list_len, float sm_scale, void* d_out, float* d_lse_out, float* d_partials,
                                hipStream_t stream) {
   const int rows = c.B * c.Hkv, page_bytes = QuantTile{c.S, c.D}.bytes();
-  const SplitPlan plan = d_sel_pages ? plan_splits(c.B, c.Hkv, max_list_len, c.max_pages_hint, page_bytes, false) : most_splits(rows, max_list_len);
+  SplitPlan plan = d_sel_pages ? plan_splits(c.B, c.Hkv, max_list_len, c.max_pages_hint, page_bytes, false) : most_splits(rows, max_list_len);
+  size_t slots = (size_t)rows * plan.num_splits;
+  if (!d_sel_pages && dense_balances(c.B, c.Hkv, max_list_len, page_bytes, kQuantLeastBytes)) {
+    plan = SplitPlan{dense_max_chunks(rows, max_list_len, kQuantRound), 0, 0};
+    slots = plan.pages_per_split;
+  }
   const bool nt = (int64_t)rows * max_list_len * page_bytes > kStreamNtBytes;
   const QuantDecodeArgs a = {reinterpret_cast<const char*>(records), d_q, d_sel_pages, d_sel_count, sel_stride, decode_scale_log2(c, sm_scale),
-                             d_partials, d_partials + (size_t)rows * plan.num_splits * (c.H / c.Hkv) * c.D, d_out, d_lse_out};
+                             d_partials, d_partials + slots * (c.H / c.Hkv) * c.D, d_out, d_lse_out};
   auto run = [&](auto launch) { return launch(c, a, plan, nt, stream); };
   const hipError_t e = c.dtype == 0 ? (c.D == 64 ? run(launch_quant_partial<float, 64>) : run(launch_quant_partial<float, 128>))
                                     : (c.D == 64 ? run(launch_quant_partial<bf16_t, 64>) : run(launch_quant_partial<bf16_t, 128>));
-  if (e != hipSuccess || plan.num_splits == 1) return e;
+  if (e != hipSuccess || plan.num_splits <= 1) return e;
   return launch_merge(c, d_sel_pages ? d_sel_count : nullptr, sel_stride, plan, d_partials, d_out, d_lse_out, stream);
 }
 

@@ -1,5 +1,6 @@
 // Pages of 4-bit numbers: the layout of a page's record and the launches that write, read back and attend over records.
 #pragma once
+#include "dense_plan.hpp"
 #include "kernels.hpp"
 
 namespace unique {
@@ -39,6 +40,11 @@ hipError_t launch_quant_decode(const CacheView& c, const void* records, const vo
                                int sel_stride, int max_list_len, float sm_scale, void* d_out, float* d_lse_out, float* d_partials,
                                hipStream_t stream);
 
+// Every page of a batch whose sequences may differ in length is cut by the lengths on the device, as for full-precision pages
+// (dense_plan.hpp). Three workgroups run on a compute unit, and a page of records is a quarter of the bytes.
+constexpr DenseRound kQuantRound = {768, 512};
+constexpr int64_t kQuantLeastBytes = 24ll << 20;
+
 struct QuantDecodeArgs {
   const char* records;
   const void* q;
@@ -51,6 +57,7 @@ struct QuantDecodeArgs {
   void* out;
   float* lse_out;
 };
+// plan.num_splits == 0: cut by the lengths into at most plan.pages_per_split chunks, and merged.
 template <typename T, int D>
 hipError_t launch_quant_partial(const CacheView& c, const QuantDecodeArgs& a, const SplitPlan& plan, bool stream_nt, hipStream_t stream);
 template <> hipError_t launch_quant_partial<float, 64>(const CacheView&, const QuantDecodeArgs&, const SplitPlan&, bool, hipStream_t);

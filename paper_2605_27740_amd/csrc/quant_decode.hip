@@ -14,7 +14,7 @@
 // (24 bits) for fp32 outputs, two for bf16: what is left out is below 2^-16 of a probability, the output's own rounding 2^-9.
 #include <type_traits>
 
-#include "decode_core.hpp"
+#include "dense_cut.hpp"
 #include "quant.hpp"
 
 namespace unique {
@@ -338,8 +338,45 @@ __global__ __launch_bounds__(kDecWaves* kWave, sizeof(T) == 4 ? 2 : 3) void quan
   quant_chunk<D, S, G, kNT>(c, a.records, reinterpret_cast<const T*>(a.q), chunk, wave, lane, lookup, a.scale_log2, to, sh);
 }
 
+// Every page of sequences that are cut by their lengths.
+template <typename T, int D, int S, int G, bool kNT>
+__global__ __launch_bounds__(kDecWaves* kWave, sizeof(T) == 4 ? 2 : 3) void quant_dense_kernel(CacheView c, QuantDecodeArgs a, int max_chunks) {
+  __shared__ QuantShared<T, D, G> sh;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, w = blockIdx.x;
+  BatchChunks bc;
+  if (!cut_batch(c, S, max_chunks, w, bc, kQuantRound)) return;
+  const unsigned long long here = sequence_of(c, bc, w);
+  if (here == 0) return;
+  const Chunk chunk = chunk_of(c, bc, here, w);
+  const ChunkOut<T> to = {a.part_o, a.part_ml, nullptr, nullptr, 2};
+  auto lookup = [&](int e, bool, int& phys, int& ntok) {
+    const int ph = c.page_table[(int64_t)chunk.b * c.max_pages + e];
+    if (ph >= 0 && (int64_t)ph < c.num_phys) {
+      phys = ph;
+      ntok = min(S, chunk.N - e * S);
+    }
+  };
+  quant_chunk<D, S, G, kNT>(c, a.records, reinterpret_cast<const T*>(a.q), chunk, wave, lane, lookup, a.scale_log2, to, sh);
+}
+
+template <typename T, int D, int G, int kWaves>
+__global__ __launch_bounds__(kWaves* kWave) void quant_merge_kernel(CacheView c, QuantDecodeArgs a, int max_chunks) {
+  __shared__ MergeShared<kWaves, D> sh;
+  merge_cut<T, D, G, kWaves>(c, blockIdx.y, blockIdx.x, max_chunks, kQuantRound, a.part_o, a.part_ml, reinterpret_cast<T*>(a.out), a.lse_out, sh);
+}
+
 template <typename T, int D, int S, int G>
 hipError_t launch_t(const CacheView& c, const QuantDecodeArgs& a, const SplitPlan& plan, bool stream_nt, hipStream_t st) {
+  if (plan.num_splits == 0) {
+    const int max_chunks = plan.pages_per_split;
+    if (stream_nt) quant_dense_kernel<T, D, S, G, true><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks);
+    else quant_dense_kernel<T, D, S, G, false><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (dense_merge_alone(c.B * c.Hkv)) quant_merge_kernel<T, D, G, 1><<<dim3(c.H, c.B), dim3(kWave), 0, st>>>(c, a, max_chunks);
+    else quant_merge_kernel<T, D, G, kMergeWaves><<<dim3(c.H, c.B), dim3(kMergeWaves * kWave), 0, st>>>(c, a, max_chunks);
+    return hipGetLastError();
+  }
   const dim3 grid = plan.rotate ? dim3(c.Hkv, c.B, plan.num_splits) : dim3(plan.num_splits, c.Hkv, c.B);
   if (stream_nt) quant_partial_kernel<T, D, S, G, true><<<grid, dim3(kDecWaves * kWave), 0, st>>>(c, a, plan);
   else quant_partial_kernel<T, D, S, G, false><<<grid, dim3(kDecWaves * kWave), 0, st>>>(c, a, plan);

@@ -19,12 +19,17 @@ struct WeighArgs {
 size_t weigh_floats(const CacheView& c);
 hipError_t launch_weigh(const CacheView& c, const WeighArgs& a, hipStream_t stream);
 
+// How the batch is cut: by the lengths on the device into at most max_chunks chunks (dense_plan.hpp), or, where that is 0, by a plan.
+struct WeighCut {
+  SplitPlan plan;
+  int max_chunks;
+};
 template <typename T, int D>
-hipError_t launch_weigh_partial(const CacheView& c, const WeighArgs& a, const SplitPlan& plan, float* part_ml, float* shares, hipStream_t stream);
-template <> hipError_t launch_weigh_partial<float, 64>(const CacheView&, const WeighArgs&, const SplitPlan&, float*, float*, hipStream_t);
-template <> hipError_t launch_weigh_partial<float, 128>(const CacheView&, const WeighArgs&, const SplitPlan&, float*, float*, hipStream_t);
-template <> hipError_t launch_weigh_partial<uint16_t, 64>(const CacheView&, const WeighArgs&, const SplitPlan&, float*, float*, hipStream_t);
-template <> hipError_t launch_weigh_partial<uint16_t, 128>(const CacheView&, const WeighArgs&, const SplitPlan&, float*, float*, hipStream_t);
+hipError_t launch_weigh_of(const CacheView& c, const WeighArgs& a, const WeighCut& cut, float* part_ml, float* shares, hipStream_t stream);
+#define UNIQUE_DECLARE(T, D) \
+  template <> hipError_t launch_weigh_of<T, D>(const CacheView&, const WeighArgs&, const WeighCut&, float*, float*, hipStream_t);
+UNIQUE_DECLARE(float, 64) UNIQUE_DECLARE(float, 128) UNIQUE_DECLARE(uint16_t, 64) UNIQUE_DECLARE(uint16_t, 128)
+#undef UNIQUE_DECLARE
 
 // Sequences of more than `budget` pages keep their first `sinks`, their last `recent` and the others with the largest accounts.
 struct EvictArgs {
