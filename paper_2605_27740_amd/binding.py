@@ -169,20 +169,20 @@ class Library:
     def quantise_pages(self, desc: CacheDesc, records, record_table=None, tok_begin=None, tok_end=None,
                        max_pages_touched_per_seq: int = 0):
         self.check(self.c.unique_quantise_pages(C.byref(desc), _p(tok_begin), _p(tok_end), max_pages_touched_per_seq,
-                                                _p(records), _p(record_table), int(records.shape[0]), _stream()))
+                                                _p(records), _p(record_table), records.shape[0], _stream()))
 
     def restore_pages(self, desc: CacheDesc, records, k_out, v_out, record_table=None, tok_begin=None, tok_end=None,
                       max_pages_touched_per_seq: int = 0):
         self.check(self.c.unique_restore_pages(C.byref(desc), _p(tok_begin), _p(tok_end), max_pages_touched_per_seq,
-                                               _p(records), _p(record_table), int(records.shape[0]), _p(k_out), _p(v_out),
+                                               _p(records), _p(record_table), records.shape[0], _p(k_out), _p(v_out),
                                                _stream()))
 
     def quantised_paged_decode(self, desc: CacheDesc, records, q, sel_pages, sel_count, sm_scale: float, out, lse_out,
                                workspace):
         self.check(self.c.unique_quantised_paged_decode(C.byref(desc), _p(records), _p(q), _p(sel_pages), _p(sel_count),
-                                                        0 if sel_pages is None else int(sel_pages.shape[-1]), sm_scale,
+                                                        0 if sel_pages is None else sel_pages.shape[-1], sm_scale,
                                                         _p(out), _p(lse_out), _p(workspace),
-                                                        workspace.numel() * workspace.element_size(), _stream()))
+                                                        workspace.nbytes, _stream()))
 
     def account_workspace_bytes(self, desc: CacheDesc) -> int:
         n = C.c_size_t(0)
@@ -192,15 +192,15 @@ class Library:
     def weighted_paged_decode(self, desc: CacheDesc, q, sm_scale: float, decay: float, weights_in, weights_out, out, lse_out,
                               workspace):
         self.check(self.c.unique_weighted_paged_decode(C.byref(desc), _p(q), sm_scale, decay, _p(weights_in),
-                                                       _p(weights_out), int(weights_out.shape[-1]), _p(out), _p(lse_out),
-                                                       _p(workspace), workspace.numel() * workspace.element_size(), _stream()))
+                                                       _p(weights_out), weights_out.shape[-1], _p(out), _p(lse_out),
+                                                       _p(workspace), workspace.nbytes, _stream()))
 
     def evict_pages(self, desc: CacheDesc, budget_pages: int, sink_pages: int, recent_pages: int, weights_in, weights_out,
                     page_table_out, seq_lens_out, freed_pages, freed_count, workspace):
         self.check(self.c.unique_evict_pages(C.byref(desc), budget_pages, sink_pages, recent_pages, _p(weights_in),
-                                             _p(weights_out), int(weights_in.shape[-1]), _p(page_table_out), _p(seq_lens_out),
-                                             _p(freed_pages), _p(freed_count), int(freed_pages.shape[-1]), _p(workspace),
-                                             workspace.numel() * workspace.element_size(), _stream()))
+                                             _p(weights_out), weights_in.shape[-1], _p(page_table_out), _p(seq_lens_out),
+                                             _p(freed_pages), _p(freed_count), freed_pages.shape[-1], _p(workspace),
+                                             workspace.nbytes, _stream()))
 
 
 _lib: Library | None = None

@@ -6,7 +6,8 @@
 // and take the scale's exponent bits alone, with 255 as NaN and 0 as 2^-127 (checked lane by lane), so that a byte shifted into
 // place is a scale.
 //
-// A wave takes a (page, KV head): a lane eight channels of a token, a load instruction 512 channels of consecutive tokens.
+// A wave takes a (page, KV head): a lane eight channels of a few consecutive tokens, whose V codes are consecutive bytes of the record
+// (16 of four tokens, D = 128), as are their scales; a load or store of full-precision channels covers whole rows.
 #include <type_traits>
 
 #include "device_utils.hpp"
@@ -17,55 +18,103 @@ namespace {
 
 constexpr int kQuantWaves = 4;
 
-__device__ __forceinline__ void load_eight(const bf16_t* p, float (&x)[8]) { load_vec(p, x); }
-__device__ __forceinline__ void load_eight(const float* p, float (&x)[8]) {
+// Eight channels as they are in memory.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<bf16_t> {
+  uint32_t w[4];
+};
+template <>
+struct Eight<float> {
+  float w[8];
+};
+__device__ __forceinline__ void load_eight(const bf16_t* p, Eight<bf16_t>& x) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  x.w[0] = v.x; x.w[1] = v.y; x.w[2] = v.z; x.w[3] = v.w;
+}
+__device__ __forceinline__ void load_eight(const float* p, Eight<float>& x) {
   float a[4], b[4];
   load_vec(p, a);
   load_vec(p + 4, b);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
-}
-__device__ __forceinline__ void store_eight(bf16_t* p, const float (&x)[8]) {  // every value is a bf16 number
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
-  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void store_eight(float* p, const float (&x)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
-}
-
-// The scale byte of a block whose lanes (four neighbours) hold eight channels each; the same in all four.
-__device__ __forceinline__ uint32_t block_scale(const float (&x)[8]) {
-  float top = 0.f;
-  uint32_t odd = 0;  // an infinity or NaN here
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    top = fmaxf(top, fabsf(x[i]));
-    odd |= (__float_as_uint(x[i]) & 0x7f800000u) == 0x7f800000u;
-  }
-  top = odd ? INFINITY : top;
-  top = group_allreduce<4>(top, OpMax());
-  const int exponent = (int)(__float_as_uint(top) >> 23);  // of 2^e times four
-  return exponent == 255 ? 255u : (uint32_t)max(exponent - 2, 1);
+  for (int i = 0; i < 4; ++i) { x.w[i] = a[i]; x.w[4 + i] = b[i]; }
 }
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-__device__ __forceinline__ uint32_t encode_eight(const float (&x)[8], float scale) {
+// The largest exponent field of eight channels. Magnitudes are compared as whole numbers, which puts infinity and NaN on top.
+__device__ __forceinline__ uint32_t top_exponent(const Eight<bf16_t>& x) {
+  typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+  u16x2_t m[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) m[i] = __builtin_bit_cast(u16x2_t, x.w[i] & 0x7fff7fffu);
+  const u16x2_t top = __builtin_elementwise_max(__builtin_elementwise_max(m[0], m[1]), __builtin_elementwise_max(m[2], m[3]));
+  return (uint32_t)max(top.x, top.y) >> 7;
+}
+__device__ __forceinline__ uint32_t top_exponent(const Eight<float>& x) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x.w[i]) & 0x7fffffffu);
+  return top >> 23;
+}
+// The scale byte of a block whose lanes (four neighbours) hold eight channels each; the same in all four.
+template <typename T>
+__device__ __forceinline__ uint32_t block_scale(const Eight<T>& x) {
+  int e = (int)top_exponent(x);  // of 2^e times four
+  e = max(e, __builtin_amdgcn_update_dpp(0, e, kDppXor1, 0xf, 0xf, true));
+  e = max(e, __builtin_amdgcn_update_dpp(0, e, kDppXor2, 0xf, 0xf, true));
+  return e == 255 ? 255u : (uint32_t)max(e - 2, 1);
+}
+
+__device__ __forceinline__ uint32_t encode_eight(const Eight<bf16_t>& x, float scale) {
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
   uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[0]), scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[1]), scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[2]), scale, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[3]), scale, 3);
   return w;
 }
-__device__ __forceinline__ void decode_eight(uint32_t w, float scale, float (&x)[8]) {
+__device__ __forceinline__ uint32_t encode_eight(const Eight<float>& x, float scale) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[0], x.w[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[2], x.w[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[4], x.w[5], scale, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[6], x.w[7], scale, 3);
+  return w;
+}
+__device__ __forceinline__ void decode_eight(uint32_t w, float scale, bf16_t* to) {
+  u32x4_t x;
+  x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  *reinterpret_cast<u32x4_t*>(to) = x;
+}
+__device__ __forceinline__ void decode_eight(uint32_t w, float scale, float* to) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
   const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
   const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-  x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
+  *reinterpret_cast<float4*>(to) = make_float4(a.x, a.y, b.x, b.y);
+  *reinterpret_cast<float4*>(to + 4) = make_float4(c.x, c.y, d.x, d.y);
 }
+
+// kBytes bytes as one access.
+template <int kBytes>
+struct Bytes;
+template <> struct Bytes<1> { using type = uint8_t; };
+template <> struct Bytes<2> { using type = uint16_t; };
+template <> struct Bytes<4> { using type = uint32_t; };
+template <> struct Bytes<8> { using type = uint64_t; };
+template <> struct Bytes<16> { using type = u32x4_t; };
+
+// How a wave goes over a page's tokens: kRun consecutive ones per lane, kStep at a time.
+template <int D, int S>
+struct QuantShape {
+  static constexpr int kLanes = D / 8, kRows = kWave / kLanes;  // lanes of a token
+  static constexpr int kRun = S / kRows < 4 ? S / kRows : 4, kStep = kRun * kRows;
+  static constexpr int kUnits = 128 / D, kUnitBytes = D / 32;   // V units of eight channels, their bytes
+};
 
 // The (page, head) of a wave and the tokens of it that count; false: nothing to do.
 struct QuantItem {
@@ -97,30 +146,69 @@ __device__ __forceinline__ bool quant_item(const CacheView& c, const QuantPool& 
 template <typename T, int D, int S>
 __global__ __launch_bounds__(kQuantWaves* kWave) void quantise_kernel(CacheView c, QuantPool pool, const int32_t* tok_begin,
                                                                       const int32_t* tok_end, int pages_per_seq) {
+  using Sh = QuantShape<D, S>;
   constexpr QuantTile kTile = {S, D};
-  constexpr int kLanes = D / 8, kTok = kWave / kLanes;  // lanes of a token, tokens of a load
+  constexpr int kRun = Sh::kRun;
   QuantItem it;
   if (!quant_item<D, S>(c, pool, tok_begin, tok_end, pages_per_seq, it)) return;
-  const int lane = threadIdx.x % kWave, oct = lane % kLanes;
-  const T* kc = reinterpret_cast<const T*>(c.k_cache) + it.full;
-  const T* vc = reinterpret_cast<const T*>(c.v_cache) + it.full;
-  for (int tok = it.t0 / kTok * kTok + lane / kLanes; tok < S; tok += kTok) {
-    if (tok >= it.t0 && tok < it.t1) {  // lanes of a block agree
-      float x[8], y[8];
-      load_eight(kc + tok * D + oct * 8, x);
-      load_eight(vc + tok * D + oct * 8, y);
-      const uint32_t ks = block_scale(x), vs = block_scale(y);
-      *reinterpret_cast<uint32_t*>(it.tile + kTile.k_codes() + tok * (D / 2) + oct * 4) = encode_eight(x, scale_of(ks));
-      const uint32_t v = encode_eight(y, scale_of(vs));
-      if constexpr (D == 128) {
-        *reinterpret_cast<uint32_t*>(it.tile + kTile.v_at(tok, oct)) = v;
-      } else {
-        *reinterpret_cast<uint16_t*>(it.tile + kTile.v_at(tok, 2 * oct)) = (uint16_t)v;
-        *reinterpret_cast<uint16_t*>(it.tile + kTile.v_at(tok, 2 * oct + 1)) = (uint16_t)(v >> 16);
+  const int lane = threadIdx.x % kWave, oct = lane % Sh::kLanes;
+  const T* kc = reinterpret_cast<const T*>(c.k_cache) + it.full + oct * 8;
+  const T* vc = reinterpret_cast<const T*>(c.v_cache) + it.full + oct * 8;
+  for (int first = it.t0 / Sh::kStep * Sh::kStep; first < it.t1; first += Sh::kStep) {
+    const int tok0 = first + lane / Sh::kLanes * kRun;
+    Eight<T> x[kRun], y[kRun];  // requested together; a slot that does not count reads one that does
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+      const int tok = max(it.t0, min(tok0 + j, it.t1 - 1));
+      load_eight(kc + tok * D, x[j]);
+      load_eight(vc + tok * D, y[j]);
+    }
+    typename Bytes<kRun>::type ks = 0, vs = 0;
+    uint32_t k[kRun], v[kRun];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+      const uint32_t a = block_scale(x[j]), b = block_scale(y[j]);
+      k[j] = encode_eight(x[j], scale_of(a));
+      v[j] = encode_eight(y[j], scale_of(b));
+      ks |= a << (8 * j);
+      vs |= b << (8 * j);
+    }
+    char* k_scale = it.tile + kTile.k_scales() + oct / 4 * S + tok0;
+    char* v_scale = it.tile + kTile.v_scales() + oct / 4 * S + tok0;
+    if (tok0 >= it.t0 && tok0 + kRun <= it.t1) {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) *reinterpret_cast<uint32_t*>(it.tile + kTile.k_codes() + (tok0 + j) * (D / 2) + oct * 4) = k[j];
+      using Unit = typename Bytes<Sh::kUnitBytes * kRun>::type;
+#pragma unroll
+      for (int u = 0; u < Sh::kUnits; ++u) {
+        Unit w;
+        if constexpr (sizeof(Unit) == 16) {
+          w = Unit{v[0], v[1], v[2], v[3]};
+        } else {
+          w = 0;
+#pragma unroll
+          for (int j = 0; j < kRun; ++j) w |= (Unit)(D == 128 ? v[j] : (v[j] >> (16 * u)) & 0xffffu) << (8 * Sh::kUnitBytes * j);
+        }
+        *reinterpret_cast<Unit*>(it.tile + kTile.v_at(tok0, Sh::kUnits * oct + u)) = w;
       }
       if (oct % 4 == 0) {
-        it.tile[kTile.k_scales() + oct / 4 * S + tok] = (char)ks;
-        it.tile[kTile.v_scales() + oct / 4 * S + tok] = (char)vs;
+        *reinterpret_cast<typename Bytes<kRun>::type*>(k_scale) = ks;
+        *reinterpret_cast<typename Bytes<kRun>::type*>(v_scale) = vs;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) {
+        const int tok = tok0 + j;
+        if (tok < it.t0 || tok >= it.t1) continue;
+        *reinterpret_cast<uint32_t*>(it.tile + kTile.k_codes() + tok * (D / 2) + oct * 4) = k[j];
+#pragma unroll
+        for (int u = 0; u < Sh::kUnits; ++u)
+          *reinterpret_cast<typename Bytes<Sh::kUnitBytes>::type*>(it.tile + kTile.v_at(tok, Sh::kUnits * oct + u)) =
+              (typename Bytes<Sh::kUnitBytes>::type)(v[j] >> (16 * u));
+        if (oct % 4 == 0) {
+          k_scale[j] = (char)(ks >> (8 * j));
+          v_scale[j] = (char)(vs >> (8 * j));
+        }
       }
     }
   }
@@ -129,27 +217,35 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantise_kernel(CacheView 
 template <typename T, int D, int S>
 __global__ __launch_bounds__(kQuantWaves* kWave) void restore_kernel(CacheView c, QuantPool pool, T* k_out, T* v_out, const int32_t* tok_begin,
                                                                      const int32_t* tok_end, int pages_per_seq) {
+  using Sh = QuantShape<D, S>;
   constexpr QuantTile kTile = {S, D};
-  constexpr int kLanes = D / 8, kTok = kWave / kLanes;
+  constexpr int kRun = Sh::kRun;
   QuantItem it;
   if (!quant_item<D, S>(c, pool, tok_begin, tok_end, pages_per_seq, it)) return;
-  const int lane = threadIdx.x % kWave, oct = lane % kLanes;
-  for (int tok = it.t0 / kTok * kTok + lane / kLanes; tok < S; tok += kTok) {
-    if (tok >= it.t0 && tok < it.t1) {
-      const uint32_t kw = *reinterpret_cast<const uint32_t*>(it.tile + kTile.k_codes() + tok * (D / 2) + oct * 4);
-      uint32_t vw;
-      if constexpr (D == 128) {
-        vw = *reinterpret_cast<const uint32_t*>(it.tile + kTile.v_at(tok, oct));
-      } else {
-        vw = *reinterpret_cast<const uint16_t*>(it.tile + kTile.v_at(tok, 2 * oct)) |
-             ((uint32_t)*reinterpret_cast<const uint16_t*>(it.tile + kTile.v_at(tok, 2 * oct + 1)) << 16);
-      }
-      const uint32_t ks = (uint8_t)it.tile[kTile.k_scales() + oct / 4 * S + tok], vs = (uint8_t)it.tile[kTile.v_scales() + oct / 4 * S + tok];
-      float x[8], y[8];
-      decode_eight(kw, scale_of(ks), x);
-      decode_eight(vw, scale_of(vs), y);
-      store_eight(k_out + it.full + tok * D + oct * 8, x);
-      store_eight(v_out + it.full + tok * D + oct * 8, y);
+  const int lane = threadIdx.x % kWave, oct = lane % Sh::kLanes;
+  for (int first = it.t0 / Sh::kStep * Sh::kStep; first < it.t1; first += Sh::kStep) {
+    const int tok0 = first + lane / Sh::kLanes * kRun;
+    uint32_t k[kRun], v[kRun];
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) k[j] = *reinterpret_cast<const uint32_t*>(it.tile + kTile.k_codes() + (tok0 + j) * (D / 2) + oct * 4);
+    using Unit = typename Bytes<Sh::kUnitBytes * kRun>::type;
+    Unit w[Sh::kUnits];
+#pragma unroll
+    for (int u = 0; u < Sh::kUnits; ++u) w[u] = *reinterpret_cast<const Unit*>(it.tile + kTile.v_at(tok0, Sh::kUnits * oct + u));
+    const uint32_t ks = *reinterpret_cast<const typename Bytes<kRun>::type*>(it.tile + kTile.k_scales() + oct / 4 * S + tok0);
+    const uint32_t vs = *reinterpret_cast<const typename Bytes<kRun>::type*>(it.tile + kTile.v_scales() + oct / 4 * S + tok0);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+      if constexpr (sizeof(Unit) == 16) v[j] = w[0][j];
+      else if constexpr (D == 128) v[j] = (uint32_t)(w[0] >> (32 * j));
+      else v[j] = ((uint32_t)(w[0] >> (16 * j)) & 0xffffu) | ((uint32_t)(w[Sh::kUnits - 1] >> (16 * j)) & 0xffffu) << 16;
+    }
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+      const int tok = tok0 + j;
+      if (tok < it.t0 || tok >= it.t1) continue;
+      decode_eight(k[j], scale_of(ks >> (8 * j) & 255u), k_out + it.full + tok * D + oct * 8);
+      decode_eight(v[j], scale_of(vs >> (8 * j) & 255u), v_out + it.full + tok * D + oct * 8);
     }
   }
 }
@@ -201,11 +297,13 @@ hipError_t launch_restore(const CacheView& c, const QuantPool& pool, void* k_out
 hipError_t launch_quant_decode(const CacheView& c, const void* records, const void* d_q, const int32_t* d_sel_pages, const int32_t* d_sel_count,
                                int sel_stride, int max_list_len, float sm_scale, void* d_out, float* d_lse_out, float* d_partials,
                                hipStream_t stream) {
+  // Lists are cut like those of bf16 pages, four times the bytes: latency and arithmetic are what bounds a short list. us with the
+  // records' own bytes / so: 12 x 8 rows of 200 pages of 16, eight heads 16.7 / 15.8, 16 x 8 x 256 18.3 / 18.8, 32 x 8 x 64 pages of 32 16.0 / 15.9.
   const int rows = c.B * c.Hkv, page_bytes = QuantTile{c.S, c.D}.bytes();
-  SplitPlan plan = d_sel_pages ? plan_splits(c.B, c.Hkv, max_list_len, c.max_pages_hint, page_bytes, false) : most_splits(rows, max_list_len);
+  SplitPlan plan = d_sel_pages ? plan_splits(c.B, c.Hkv, max_list_len, c.max_pages_hint, c.S * c.D * 4, false) : most_splits(rows, max_list_len);
   size_t slots = (size_t)rows * plan.num_splits;
   if (!d_sel_pages && dense_balances(c.B, c.Hkv, max_list_len, page_bytes, kQuantLeastBytes)) {
-    plan = SplitPlan{dense_max_chunks(rows, max_list_len, kQuantRound), 0, 0};
+    plan = SplitPlan{dense_max_chunks(rows, max_list_len, quant_round(rows, max_list_len)), 0, 0};
     slots = plan.pages_per_split;
   }
   const bool nt = (int64_t)rows * max_list_len * page_bytes > kStreamNtBytes;

@@ -41,8 +41,13 @@ hipError_t launch_quant_decode(const CacheView& c, const void* records, const vo
                                hipStream_t stream);
 
 // Every page of a batch whose sequences may differ in length is cut by the lengths on the device, as for full-precision pages
-// (dense_plan.hpp). Three workgroups run on a compute unit, and a page of records is a quarter of the bytes.
-constexpr DenseRound kQuantRound = {768, 512};
+// (dense_plan.hpp). Three workgroups run on a compute unit where there is a chunk for each; with fewer chunks than that
+// two have equal shares. us with 512 / 768 workgroups at a time (8 KV heads, G = 4, D = 128): 32 sequences of 4K to 131K tokens, pages
+// of 32 275 / 226, 16 x 131072 366 / 356; 12 of 2K to 50K, G = 8, which may be 672 chunks, 62.9 / 67.3. More rounds than one
+// cost more than they balance: from 256, 512 or 768 pages of a chunk on 372, 360 and 356 for 16 x 131072.
+inline DenseRound quant_round(int rows, int max_pages) {
+  return {rows * most_splits(rows, max_pages).num_splits >= 768 ? 768 : 512, 768};
+}
 constexpr int64_t kQuantLeastBytes = 24ll << 20;
 
 struct QuantDecodeArgs {

@@ -340,11 +340,12 @@ __global__ __launch_bounds__(kDecWaves* kWave, sizeof(T) == 4 ? 2 : 3) void quan
 
 // Every page of sequences that are cut by their lengths.
 template <typename T, int D, int S, int G, bool kNT>
-__global__ __launch_bounds__(kDecWaves* kWave, sizeof(T) == 4 ? 2 : 3) void quant_dense_kernel(CacheView c, QuantDecodeArgs a, int max_chunks) {
+__global__ __launch_bounds__(kDecWaves* kWave, sizeof(T) == 4 ? 2 : 3) void quant_dense_kernel(CacheView c, QuantDecodeArgs a, int max_chunks,
+                                                                                                  DenseRound round) {
   __shared__ QuantShared<T, D, G> sh;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, w = blockIdx.x;
   BatchChunks bc;
-  if (!cut_batch(c, S, max_chunks, w, bc, kQuantRound)) return;
+  if (!cut_batch(c, S, max_chunks, w, bc, round)) return;
   const unsigned long long here = sequence_of(c, bc, w);
   if (here == 0) return;
   const Chunk chunk = chunk_of(c, bc, here, w);
@@ -360,21 +361,22 @@ __global__ __launch_bounds__(kDecWaves* kWave, sizeof(T) == 4 ? 2 : 3) void quan
 }
 
 template <typename T, int D, int G, int kWaves>
-__global__ __launch_bounds__(kWaves* kWave) void quant_merge_kernel(CacheView c, QuantDecodeArgs a, int max_chunks) {
+__global__ __launch_bounds__(kWaves* kWave) void quant_merge_kernel(CacheView c, QuantDecodeArgs a, int max_chunks, DenseRound round) {
   __shared__ MergeShared<kWaves, D> sh;
-  merge_cut<T, D, G, kWaves>(c, blockIdx.y, blockIdx.x, max_chunks, kQuantRound, a.part_o, a.part_ml, reinterpret_cast<T*>(a.out), a.lse_out, sh);
+  merge_cut<T, D, G, kWaves>(c, blockIdx.y, blockIdx.x, max_chunks, round, a.part_o, a.part_ml, reinterpret_cast<T*>(a.out), a.lse_out, sh);
 }
 
 template <typename T, int D, int S, int G>
 hipError_t launch_t(const CacheView& c, const QuantDecodeArgs& a, const SplitPlan& plan, bool stream_nt, hipStream_t st) {
   if (plan.num_splits == 0) {
     const int max_chunks = plan.pages_per_split;
-    if (stream_nt) quant_dense_kernel<T, D, S, G, true><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks);
-    else quant_dense_kernel<T, D, S, G, false><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks);
+    const DenseRound round = quant_round(c.B * c.Hkv, c.max_pages_hint);
+    if (stream_nt) quant_dense_kernel<T, D, S, G, true><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks, round);
+    else quant_dense_kernel<T, D, S, G, false><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks, round);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (dense_merge_alone(c.B * c.Hkv)) quant_merge_kernel<T, D, G, 1><<<dim3(c.H, c.B), dim3(kWave), 0, st>>>(c, a, max_chunks);
-    else quant_merge_kernel<T, D, G, kMergeWaves><<<dim3(c.H, c.B), dim3(kMergeWaves * kWave), 0, st>>>(c, a, max_chunks);
+    if (dense_merge_alone(c.B * c.Hkv)) quant_merge_kernel<T, D, G, 1><<<dim3(c.H, c.B), dim3(kWave), 0, st>>>(c, a, max_chunks, round);
+    else quant_merge_kernel<T, D, G, kMergeWaves><<<dim3(c.H, c.B), dim3(kMergeWaves * kWave), 0, st>>>(c, a, max_chunks, round);
     return hipGetLastError();
   }
   const dim3 grid = plan.rotate ? dim3(c.Hkv, c.B, plan.num_splits) : dim3(plan.num_splits, c.Hkv, c.B);
