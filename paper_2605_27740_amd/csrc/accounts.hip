@@ -278,64 +278,85 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(CacheView c, Evict
 
 constexpr int kCloseThreads = 512, kCloseBatch = 8;
 
-// Closes rows of accounts up to the kept pages, in place or not: kept[] ascends, so that entry i comes from kept[i] >= i and a round
-// of the workgroup, which reads before it writes, leaves what later rounds read.
+// Closes rows up to the kept pages, in place or not: kept[] ascends, so that entry i comes from kept[i] >= i and a round of the
+// workgroup, which reads before it writes, leaves what later rounds read. blockIdx.x < Hkv: the accounts of a KV head; else the table.
 __global__ __launch_bounds__(kCloseThreads) void close_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept,
                                                               const int32_t* __restrict__ pages, const int32_t* __restrict__ kept_count) {
   const int b = blockIdx.y, t = threadIdx.x;
   const int P = pages[b], n = kept_count[b];
-  const int32_t* from = kept + (int64_t)b * a.budget;
-  const int64_t row = ((int64_t)b * c.Hkv + blockIdx.x) * a.weight_stride;
-  const float* in = a.weights_in + row;
-  float* out = a.weights_out + row;
+  const Row from(kept + (int64_t)b * a.budget, n);
+  const bool accounts = (int)blockIdx.x < c.Hkv;
+  const int64_t row = accounts ? ((int64_t)b * c.Hkv + blockIdx.x) * a.weight_stride : (int64_t)b * c.max_pages;
+  const Row in(accounts ? (const void*)(a.weights_in + row) : c.page_table + row, P);
+  const Row out(accounts ? (void*)(a.weights_out + row) : a.page_table_out + row, P);
   for (int i0 = 0; i0 < n; i0 += kCloseThreads * kCloseBatch) {
-    int at[kCloseBatch];
-    float v[kCloseBatch];
+    uint32_t v[kCloseBatch];
 #pragma unroll
-    for (int u = 0; u < kCloseBatch; ++u) at[u] = from[min(i0 + u * kCloseThreads + t, n - 1)];
+    for (int u = 0; u < kCloseBatch; ++u) v[u] = from.word((uint32_t)(i0 + u * kCloseThreads + t) * 4);  // 0 behind the last
 #pragma unroll
-    for (int u = 0; u < kCloseBatch; ++u) v[u] = in[at[u]];
+    for (int u = 0; u < kCloseBatch; ++u) v[u] = in.word(v[u] * 4);
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kCloseBatch; ++u)
-      if (i0 + u * kCloseThreads + t < n) out[i0 + u * kCloseThreads + t] = v[u];
+    for (int u = 0; u < kCloseBatch; ++u) {
+      const int i = i0 + u * kCloseThreads + t;
+      out.put(i < n ? (uint32_t)i * 4 : kNowhere, v[u]);
+    }
   }
   __syncthreads();
-  for (int i = n + t; i < P; i += kCloseThreads) out[i] = 0.f;
+  const uint32_t vacant = accounts ? 0u : ~0u;
+  for (int i = n + t; i < P; i += kCloseThreads) out.put((uint32_t)i * 4, vacant);
 }
 
-// The table of a sequence whose pages launch_select has chosen (evict_kernel's end, for rows that no workgroup holds).
-__global__ __launch_bounds__(kEvictThreads) void close_table_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept,
-                                                                    const int32_t* __restrict__ kept_count, int32_t* __restrict__ pages) {
-  const int b = blockIdx.x, t = threadIdx.x;
+// The freed pages of a part of a sequence whose kept pages launch_select has chosen, for rows that no workgroup holds; the first part also writes
+// what else there is of the sequence. Before close_kernel, which may overwrite the table.
+constexpr int kFreedEach = 4, kFreedPages = kFreedEach * kEvictThreads;
+__global__ __launch_bounds__(kEvictThreads) void freed_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept,
+                                                              const int32_t* __restrict__ kept_count, int32_t* __restrict__ pages) {
+  __shared__ uint32_t s_stays[kFreedPages];
+  __shared__ int s_counts[kEvictWaves];
+  const int b = blockIdx.y, t = threadIdx.x, lane = t % kWave, wave = t / kWave;
   const int N = c.seq_lens[b];
-  const int P = max(min((N + c.S - 1) / c.S, c.max_pages_hint), 0), n = kept_count[b];
+  const int P = max(min((N + c.S - 1) / c.S, c.max_pages_hint), 0), n = kept_count[b], first = blockIdx.x * kFreedPages;
   const int32_t* from = kept + (int64_t)b * a.budget;
-  const int32_t* table = c.page_table + (int64_t)b * c.max_pages;
-  int32_t* table_out = a.page_table_out + (int64_t)b * c.max_pages;
   int32_t* freed = a.freed_pages + (int64_t)b * a.freed_stride;
-  for (int p = t; p < P; p += kEvictThreads) {  // kept pages below p
-    int lo = 0, hi = n;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (from[mid] < p) lo = mid + 1;
-      else hi = mid;
+  if (first == 0) {
+    for (int i = P - n + t; i < a.freed_stride; i += kEvictThreads) freed[i] = -1;
+    if (t == 0) {
+      a.freed_count[b] = P - n;
+      a.seq_lens_out[b] = N - (P - n) * c.S;
+      pages[b] = P;
     }
-    if (lo == n || from[lo] != p) freed[p - lo] = table[p];
   }
-  for (int i = P - n + t; i < a.freed_stride; i += kEvictThreads) freed[i] = -1;
+  if (first >= P) return;
+  int lo = 0, hi = n;  // kept pages before `first`
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (from[mid] < first) lo = mid + 1;
+    else hi = mid;
+  }
+#pragma unroll
+  for (int u = 0; u < kFreedEach; ++u) s_stays[u * kEvictThreads + t] = 0;
   __syncthreads();
-  for (int i0 = 0; i0 < P; i0 += kEvictThreads) {
-    const int i = i0 + t;
-    int32_t v = -1;
-    if (i < n) v = table[from[i]];
-    __syncthreads();
-    if (i < P) table_out[i] = v;
+  for (int i = lo + t; i < n; i += kEvictThreads) {
+    const int p = from[i] - first;
+    if (p >= kFreedPages) break;
+    s_stays[p] = 1;
   }
-  if (t == 0) {
-    a.freed_count[b] = P - n;
-    a.seq_lens_out[b] = N - (P - n) * c.S;
-    pages[b] = P;
+  __syncthreads();
+  uint32_t stays[kFreedEach];
+  int mine = 0;
+#pragma unroll
+  for (int u = 0; u < kFreedEach; ++u) mine += stays[u] = s_stays[t * kFreedEach + u];
+  const int upto = wave_inclusive_scan(mine);
+  if (lane == kWave - 1) s_counts[wave] = upto;
+  __syncthreads();
+  int before = lo + upto - mine;
+  for (int w = 0; w < wave; ++w) before += s_counts[w];
+#pragma unroll
+  for (int u = 0; u < kFreedEach; ++u) {
+    const int p = first + t * kFreedEach + u;
+    if (p < P && !stays[u]) freed[p - before] = c.page_table[(int64_t)b * c.max_pages + p];
+    before += stays[u];
   }
 }
 
@@ -377,7 +398,7 @@ hipError_t launch_evict(const CacheView& c, const EvictArgs& args, hipStream_t s
   int32_t* pages = reinterpret_cast<int32_t*>(ws);
   int32_t* kept_count = reinterpret_cast<int32_t*>(ws + aligned((size_t)c.B * sizeof(int32_t)));
   hipError_t e = hipSuccess;
-  const bool sums = (int64_t)c.Hkv * c.max_pages_hint <= kSumsHere && c.max_pages_hint <= kEvictMost;
+  const bool sums = (int64_t)c.Hkv * c.max_pages_hint <= kSumsHere && c.max_pages_hint <= 8192;  // (16 keys and accounts a thread spill)
   if (!sums) {
     const dim3 grid((c.max_pages_hint + kAccountThreads - 1) / kAccountThreads, c.B);
     rank_kernel<<<grid, dim3(kAccountThreads), 0, stream>>>(c, a.weights_in, a.weight_stride, a.sinks, rank, rank_stride);
@@ -395,18 +416,19 @@ hipError_t launch_evict(const CacheView& c, const EvictArgs& args, hipStream_t s
   if (c.max_pages_hint <= 1024) e = held(std::integral_constant<int, 1>());
   else if (c.max_pages_hint <= 4096) e = held(std::integral_constant<int, 4>());
   else if (c.max_pages_hint <= 8192) e = held(std::integral_constant<int, 8>());
-  else if (c.max_pages_hint <= kEvictMost) e = held(std::integral_constant<int, 16>());
+  else if (c.max_pages_hint <= kEvictMost) e = go(evict_kernel<16, false>);
   else {
     CacheView one = c;  // a row per sequence
     one.Hkv = one.H = 1;
     one.force_recent = a.recent;
     e = launch_select(one, rank, nullptr, rank_stride, a.budget, kept, kept_count, stream);
     if (e != hipSuccess) return e;
-    close_table_kernel<<<dim3(c.B), dim3(kEvictThreads), 0, stream>>>(c, a, kept, kept_count, pages);
+    freed_kernel<<<dim3((c.max_pages_hint + kFreedPages - 1) / kFreedPages, c.B), dim3(kEvictThreads), 0, stream>>>(c, a, kept, kept_count, pages);
     e = hipGetLastError();
   }
   if (e != hipSuccess || sums) return e;
-  close_kernel<<<dim3(c.Hkv, c.B), dim3(kCloseThreads), 0, stream>>>(c, a, kept, pages, kept_count);
+  const bool held_here = c.max_pages_hint <= kEvictMost;  // then the table is closed already
+  close_kernel<<<dim3(held_here ? c.Hkv : c.Hkv + 1, c.B), dim3(kCloseThreads), 0, stream>>>(c, a, kept, pages, kept_count);
   return hipGetLastError();
 }
 

@@ -6,7 +6,7 @@
 // and take the scale's exponent bits alone, with 255 as NaN and 0 as 2^-127 (checked lane by lane), so that a byte shifted into
 // place is a scale.
 //
-// A wave takes a (page, KV head): a lane eight channels of a few consecutive tokens, whose V codes are consecutive bytes of the record
+// A wave takes a (page, KV head): a lane 16 bytes of channels of a few consecutive tokens, whose V codes are consecutive bytes of the record
 // (16 of four tokens, D = 128), as are their scales; a load or store of full-precision channels covers whole rows.
 #include <type_traits>
 
@@ -19,19 +19,8 @@ namespace {
 constexpr int kQuantWaves = 4;
 
 // kNT: what is read or written in full precision bypasses the caches, of a launch that moves more than they keep (bf16, 8 KV heads, D = 128: 32768 tokens
-// restored in 37.2 / 28.3 us, 80000 quantised and restored in 180 / 139). fp32 takes two accesses of 16 bytes for eight channels, each to half of
-// a line, and must not (16 heads' worth, 32000 tokens: 79 / 126).
-// Eight channels as they are in memory.
-template <typename T>
-struct Eight;
-template <>
-struct Eight<bf16_t> {
-  uint32_t w[4];
-};
-template <>
-struct Eight<float> {
-  float w[8];
-};
+// restored in 37.2 / 28.3 us, 80000 quantised and restored in 180 / 139). It needs accesses that cover whole lines: with two of 16 bytes for eight fp32
+// channels of a lane it took 126 us where plain ones took 79.
 template <bool kNT, typename V>
 __device__ __forceinline__ V load_as(const void* p) {
   if constexpr (kNT) return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
@@ -42,78 +31,49 @@ __device__ __forceinline__ void store_as(void* p, V v) {
   if constexpr (kNT) __builtin_nontemporal_store(v, reinterpret_cast<V*>(p));
   else *reinterpret_cast<V*>(p) = v;
 }
-template <bool kNT>
-__device__ __forceinline__ void load_eight(const bf16_t* p, Eight<bf16_t>& x) {
-  const u32x4_t v = load_as<kNT, u32x4_t>(p);
-  x.w[0] = v.x; x.w[1] = v.y; x.w[2] = v.z; x.w[3] = v.w;
-}
-template <bool kNT>
-__device__ __forceinline__ void load_eight(const float* p, Eight<float>& x) {
-  float a[4], b[4];
-  load_vec(p, a);
-  load_vec(p + 4, b);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { x.w[i] = a[i]; x.w[4 + i] = b[i]; }
-}
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// The largest exponent field of eight channels. Magnitudes are compared as whole numbers, which puts infinity and NaN on top.
-__device__ __forceinline__ uint32_t top_exponent(const Eight<bf16_t>& x) {
+// 16 bytes of channels, eight of bf16 or four of fp32: their largest exponent field, their codes, and the way back. Magnitudes are
+// compared as whole numbers, which puts infinity and NaN on top.
+__device__ __forceinline__ int top_exponent(u32x4_t x, const bf16_t*) {
   typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
   u16x2_t m[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m[i] = __builtin_bit_cast(u16x2_t, x.w[i] & 0x7fff7fffu);
+  for (int i = 0; i < 4; ++i) m[i] = __builtin_bit_cast(u16x2_t, x[i] & 0x7fff7fffu);
   const u16x2_t top = __builtin_elementwise_max(__builtin_elementwise_max(m[0], m[1]), __builtin_elementwise_max(m[2], m[3]));
-  return (uint32_t)max(top.x, top.y) >> 7;
+  return max(top.x, top.y) >> 7;
 }
-__device__ __forceinline__ uint32_t top_exponent(const Eight<float>& x) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x.w[i]) & 0x7fffffffu);
-  return top >> 23;
+__device__ __forceinline__ int top_exponent(u32x4_t x, const float*) {
+  const u32x4_t m = x & 0x7fffffffu;
+  return (int)(max(max(m.x, m.y), max(m.z, m.w)) >> 23);
 }
-// The scale byte of a block whose lanes (four neighbours) hold eight channels each; the same in all four.
-template <typename T>
-__device__ __forceinline__ uint32_t block_scale(const Eight<T>& x) {
-  int e = (int)top_exponent(x);  // of 2^e times four
-  e = max(e, __builtin_amdgcn_update_dpp(0, e, kDppXor1, 0xf, 0xf, true));
-  e = max(e, __builtin_amdgcn_update_dpp(0, e, kDppXor2, 0xf, 0xf, true));
-  return e == 255 ? 255u : (uint32_t)max(e - 2, 1);
-}
-
-__device__ __forceinline__ uint32_t encode_eight(const Eight<bf16_t>& x, float scale) {
+__device__ __forceinline__ uint32_t encode(u32x4_t x, float scale, const bf16_t*) {
   typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
   uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[0]), scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[1]), scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[2]), scale, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, x.w[3]), scale, 3);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, (uint32_t)x.x), scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, (uint32_t)x.y), scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, (uint32_t)x.z), scale, 2);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2_t, (uint32_t)x.w), scale, 3);
   return w;
 }
-__device__ __forceinline__ uint32_t encode_eight(const Eight<float>& x, float scale) {
+__device__ __forceinline__ uint32_t encode(u32x4_t x, float scale, const float*) {
   uint32_t w = 0;
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[0], x.w[1], scale, 0);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[2], x.w[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[4], x.w[5], scale, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x.w[6], x.w[7], scale, 3);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x.x), __uint_as_float(x.y), scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, __uint_as_float(x.z), __uint_as_float(x.w), scale, 1);
   return w;
 }
-template <bool kNT>
-__device__ __forceinline__ void decode_eight(uint32_t w, float scale, bf16_t* to) {
+__device__ __forceinline__ u32x4_t decode(uint32_t w, float scale, const bf16_t*) {
   u32x4_t x;
   x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
   x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
   x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
   x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
-  store_as<kNT>(to, x);
+  return x;
 }
-template <bool kNT>
-__device__ __forceinline__ void decode_eight(uint32_t w, float scale, float* to) {
+__device__ __forceinline__ u32x4_t decode(uint32_t w, float scale, const float*) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
   const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
-  const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-  *reinterpret_cast<float4*>(to) = make_float4(a.x, a.y, b.x, b.y);
-  *reinterpret_cast<float4*>(to + 4) = make_float4(c.x, c.y, d.x, d.y);
+  return u32x4_t{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
 }
 
 // kBytes bytes as one access.
@@ -126,12 +86,29 @@ template <> struct Bytes<8> { using type = uint64_t; };
 template <> struct Bytes<16> { using type = u32x4_t; };
 
 // How a wave goes over a page's tokens: kRun consecutive ones per lane, kStep at a time.
-template <int D, int S>
+template <typename T, int D, int S>
 struct QuantShape {
-  static constexpr int kLanes = D / 8, kRows = kWave / kLanes;  // lanes of a token
+  static constexpr int kVec = Elem<T>::kVec, kLanes = D / kVec, kRows = kWave / kLanes;  // channels of a lane, lanes of a token
   static constexpr int kRun = S / kRows < 4 ? S / kRows : 4, kStep = kRun * kRows;
-  static constexpr int kUnits = 128 / D, kUnitBytes = D / 32;   // V units of eight channels, their bytes
+  static constexpr int kBlock = kQuantBlock / kVec;     // lanes of a scale
+  static constexpr int kUnit = D / 16;                  // channels of a V unit: half of a lane's, all, or twice as many
+  static constexpr int kUnits = kVec > kUnit ? kVec / kUnit : 1;
+  static constexpr bool kShared = kVec < kUnit;         // two lanes to a unit
+  using Code = typename Bytes<kVec / 2>::type;          // of a lane and token
+  using Scales = typename Bytes<kRun>::type;            // of a lane's tokens
+  using Unit = typename Bytes<kUnit / 2>::type;         // of a token
+  using Units = typename Bytes<kUnit / 2 * kRun>::type; // of a lane's tokens
 };
+
+// The scale byte of a block whose kBlock neighbouring lanes hold 16 bytes of channels each; the same in all of them.
+template <int kBlock, typename T>
+__device__ __forceinline__ uint32_t block_scale(u32x4_t x) {
+  int e = top_exponent(x, (const T*)nullptr);  // of 2^e times four
+  e = max(e, __builtin_amdgcn_update_dpp(0, e, kDppXor1, 0xf, 0xf, true));
+  e = max(e, __builtin_amdgcn_update_dpp(0, e, kDppXor2, 0xf, 0xf, true));
+  if constexpr (kBlock == 8) e = max(e, __builtin_amdgcn_update_dpp(0, e, kDppHalfMirror, 0xf, 0xf, true));
+  return e == 255 ? 255u : (uint32_t)max(e - 2, 1);
+}
 
 // The (page, head) of a wave and the tokens of it that count; false: nothing to do.
 struct QuantItem {
@@ -163,66 +140,73 @@ __device__ __forceinline__ bool quant_item(const CacheView& c, const QuantPool& 
 template <typename T, int D, int S, bool kNT>
 __global__ __launch_bounds__(kQuantWaves* kWave) void quantise_kernel(CacheView c, QuantPool pool, const int32_t* tok_begin,
                                                                       const int32_t* tok_end, int pages_per_seq) {
-  using Sh = QuantShape<D, S>;
+  using Sh = QuantShape<T, D, S>;
   constexpr QuantTile kTile = {S, D};
-  constexpr int kRun = Sh::kRun;
+  constexpr int kRun = Sh::kRun, kVec = Sh::kVec;
   QuantItem it;
   if (!quant_item<D, S>(c, pool, tok_begin, tok_end, pages_per_seq, it)) return;
-  const int lane = threadIdx.x % kWave, oct = lane % Sh::kLanes;
-  const T* kc = reinterpret_cast<const T*>(c.k_cache) + it.full + oct * 8;
-  const T* vc = reinterpret_cast<const T*>(c.v_cache) + it.full + oct * 8;
+  const int lane = threadIdx.x % kWave, ch = lane % Sh::kLanes;
+  const T* kc = reinterpret_cast<const T*>(c.k_cache) + it.full + ch * kVec;
+  const T* vc = reinterpret_cast<const T*>(c.v_cache) + it.full + ch * kVec;
+  char* codes = it.tile + kTile.k_codes() + ch * (kVec / 2);
+  const bool first_of_block = ch % Sh::kBlock == 0, writes_unit = !Sh::kShared || ch % 2 == 0;
+  const int unit = ch * kVec / Sh::kUnit;
   for (int first = it.t0 / Sh::kStep * Sh::kStep; first < it.t1; first += Sh::kStep) {
     const int tok0 = first + lane / Sh::kLanes * kRun;
-    Eight<T> x[kRun], y[kRun];  // requested together; a slot that does not count reads one that does
+    u32x4_t x[kRun], y[kRun];  // requested together; a slot that does not count reads one that does
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
       const int tok = max(it.t0, min(tok0 + j, it.t1 - 1));
-      load_eight<kNT>(kc + tok * D, x[j]);
-      load_eight<kNT>(vc + tok * D, y[j]);
+      x[j] = load_as<kNT, u32x4_t>(kc + tok * D);
+      y[j] = load_as<kNT, u32x4_t>(vc + tok * D);
     }
-    typename Bytes<kRun>::type ks = 0, vs = 0;
+    typename Sh::Scales ks = 0, vs = 0;
     uint32_t k[kRun], v[kRun];
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-      const uint32_t a = block_scale(x[j]), b = block_scale(y[j]);
-      k[j] = encode_eight(x[j], scale_of(a));
-      v[j] = encode_eight(y[j], scale_of(b));
+      const uint32_t a = block_scale<Sh::kBlock, T>(x[j]), b = block_scale<Sh::kBlock, T>(y[j]);
+      k[j] = encode(x[j], scale_of(a), (const T*)nullptr);
+      v[j] = encode(y[j], scale_of(b), (const T*)nullptr);
+      if constexpr (Sh::kShared) v[j] |= (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v[j], kDppXor1, 0xf, 0xf, true) << 16;
       ks |= a << (8 * j);
       vs |= b << (8 * j);
     }
-    char* k_scale = it.tile + kTile.k_scales() + oct / 4 * S + tok0;
-    char* v_scale = it.tile + kTile.v_scales() + oct / 4 * S + tok0;
+    char* k_scale = it.tile + kTile.k_scales() + ch / Sh::kBlock * S + tok0;
+    char* v_scale = it.tile + kTile.v_scales() + ch / Sh::kBlock * S + tok0;
     if (tok0 >= it.t0 && tok0 + kRun <= it.t1) {
 #pragma unroll
-      for (int j = 0; j < kRun; ++j) *reinterpret_cast<uint32_t*>(it.tile + kTile.k_codes() + (tok0 + j) * (D / 2) + oct * 4) = k[j];
-      using Unit = typename Bytes<Sh::kUnitBytes * kRun>::type;
+      for (int j = 0; j < kRun; ++j) *reinterpret_cast<typename Sh::Code*>(codes + (tok0 + j) * (D / 2)) = (typename Sh::Code)k[j];
+      if (writes_unit) {
 #pragma unroll
-      for (int u = 0; u < Sh::kUnits; ++u) {
-        Unit w;
-        if constexpr (sizeof(Unit) == 16) {
-          w = Unit{v[0], v[1], v[2], v[3]};
-        } else {
-          w = 0;
+        for (int u = 0; u < Sh::kUnits; ++u) {
+          typename Sh::Units w;
+          if constexpr (sizeof(w) == 16) {
+            w = u32x4_t{v[0], v[1], v[2], v[3]};
+          } else {
+            w = 0;
 #pragma unroll
-          for (int j = 0; j < kRun; ++j) w |= (Unit)(D == 128 ? v[j] : (v[j] >> (16 * u)) & 0xffffu) << (8 * Sh::kUnitBytes * j);
+            for (int j = 0; j < kRun; ++j)
+              w |= (typename Sh::Units)(typename Sh::Unit)(v[j] >> (16 * u)) << (8 * (int)sizeof(typename Sh::Unit) * j);
+          }
+          *reinterpret_cast<typename Sh::Units*>(it.tile + kTile.v_at(tok0, unit + u)) = w;
         }
-        *reinterpret_cast<Unit*>(it.tile + kTile.v_at(tok0, Sh::kUnits * oct + u)) = w;
       }
-      if (oct % 4 == 0) {
-        *reinterpret_cast<typename Bytes<kRun>::type*>(k_scale) = ks;
-        *reinterpret_cast<typename Bytes<kRun>::type*>(v_scale) = vs;
+      if (first_of_block) {
+        *reinterpret_cast<typename Sh::Scales*>(k_scale) = ks;
+        *reinterpret_cast<typename Sh::Scales*>(v_scale) = vs;
       }
     } else {
 #pragma unroll
       for (int j = 0; j < kRun; ++j) {
         const int tok = tok0 + j;
         if (tok < it.t0 || tok >= it.t1) continue;
-        *reinterpret_cast<uint32_t*>(it.tile + kTile.k_codes() + tok * (D / 2) + oct * 4) = k[j];
+        *reinterpret_cast<typename Sh::Code*>(codes + tok * (D / 2)) = (typename Sh::Code)k[j];
+        if (writes_unit) {
 #pragma unroll
-        for (int u = 0; u < Sh::kUnits; ++u)
-          *reinterpret_cast<typename Bytes<Sh::kUnitBytes>::type*>(it.tile + kTile.v_at(tok, Sh::kUnits * oct + u)) =
-              (typename Bytes<Sh::kUnitBytes>::type)(v[j] >> (16 * u));
-        if (oct % 4 == 0) {
+          for (int u = 0; u < Sh::kUnits; ++u)
+            *reinterpret_cast<typename Sh::Unit*>(it.tile + kTile.v_at(tok, unit + u)) = (typename Sh::Unit)(v[j] >> (16 * u));
+        }
+        if (first_of_block) {
           k_scale[j] = (char)(ks >> (8 * j));
           v_scale[j] = (char)(vs >> (8 * j));
         }
@@ -234,35 +218,41 @@ __global__ __launch_bounds__(kQuantWaves* kWave) void quantise_kernel(CacheView 
 template <typename T, int D, int S, bool kNT>
 __global__ __launch_bounds__(kQuantWaves* kWave) void restore_kernel(CacheView c, QuantPool pool, T* k_out, T* v_out, const int32_t* tok_begin,
                                                                      const int32_t* tok_end, int pages_per_seq) {
-  using Sh = QuantShape<D, S>;
+  using Sh = QuantShape<T, D, S>;
   constexpr QuantTile kTile = {S, D};
-  constexpr int kRun = Sh::kRun;
+  constexpr int kRun = Sh::kRun, kVec = Sh::kVec;
   QuantItem it;
   if (!quant_item<D, S>(c, pool, tok_begin, tok_end, pages_per_seq, it)) return;
-  const int lane = threadIdx.x % kWave, oct = lane % Sh::kLanes;
+  const int lane = threadIdx.x % kWave, ch = lane % Sh::kLanes, unit = ch * kVec / Sh::kUnit;
   for (int first = it.t0 / Sh::kStep * Sh::kStep; first < it.t1; first += Sh::kStep) {
     const int tok0 = first + lane / Sh::kLanes * kRun;
     uint32_t k[kRun], v[kRun];
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) k[j] = *reinterpret_cast<const uint32_t*>(it.tile + kTile.k_codes() + (tok0 + j) * (D / 2) + oct * 4);
-    using Unit = typename Bytes<Sh::kUnitBytes * kRun>::type;
-    Unit w[Sh::kUnits];
+    for (int j = 0; j < kRun; ++j)
+      k[j] = *reinterpret_cast<const typename Sh::Code*>(it.tile + kTile.k_codes() + (tok0 + j) * (D / 2) + ch * (kVec / 2));
+    typename Sh::Units w[Sh::kUnits];
 #pragma unroll
-    for (int u = 0; u < Sh::kUnits; ++u) w[u] = *reinterpret_cast<const Unit*>(it.tile + kTile.v_at(tok0, Sh::kUnits * oct + u));
-    const uint32_t ks = *reinterpret_cast<const typename Bytes<kRun>::type*>(it.tile + kTile.k_scales() + oct / 4 * S + tok0);
-    const uint32_t vs = *reinterpret_cast<const typename Bytes<kRun>::type*>(it.tile + kTile.v_scales() + oct / 4 * S + tok0);
+    for (int u = 0; u < Sh::kUnits; ++u) w[u] = *reinterpret_cast<const typename Sh::Units*>(it.tile + kTile.v_at(tok0, unit + u));
+    const uint32_t ks = *reinterpret_cast<const typename Sh::Scales*>(it.tile + kTile.k_scales() + ch / Sh::kBlock * S + tok0);
+    const uint32_t vs = *reinterpret_cast<const typename Sh::Scales*>(it.tile + kTile.v_scales() + ch / Sh::kBlock * S + tok0);
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-      if constexpr (sizeof(Unit) == 16) v[j] = w[0][j];
-      else if constexpr (D == 128) v[j] = (uint32_t)(w[0] >> (32 * j));
-      else v[j] = ((uint32_t)(w[0] >> (16 * j)) & 0xffffu) | ((uint32_t)(w[Sh::kUnits - 1] >> (16 * j)) & 0xffffu) << 16;
+      v[j] = 0;
+#pragma unroll
+      for (int u = 0; u < Sh::kUnits; ++u) {
+        uint32_t of_unit;
+        if constexpr (sizeof(typename Sh::Units) == 16) of_unit = w[u][j];
+        else of_unit = (typename Sh::Unit)(w[u] >> (8 * (int)sizeof(typename Sh::Unit) * j));
+        v[j] |= of_unit << (16 * u);
+      }
+      if constexpr (Sh::kShared) v[j] >>= 16 * (ch % 2);
     }
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
       const int tok = tok0 + j;
       if (tok < it.t0 || tok >= it.t1) continue;
-      decode_eight<kNT>(k[j], scale_of(ks >> (8 * j) & 255u), k_out + it.full + tok * D + oct * 8);
-      decode_eight<kNT>(v[j], scale_of(vs >> (8 * j) & 255u), v_out + it.full + tok * D + oct * 8);
+      store_as<kNT>(k_out + it.full + tok * D + ch * kVec, decode(k[j], scale_of(ks >> (8 * j) & 255u), (const T*)nullptr));
+      store_as<kNT>(v_out + it.full + tok * D + ch * kVec, decode(v[j], scale_of(vs >> (8 * j) & 255u), (const T*)nullptr));
     }
   }
 }
@@ -271,13 +261,8 @@ template <typename Launch>
 hipError_t with_shape(const CacheView& c, int pages_per_seq, Launch launch) {
   const bool nt = (int64_t)c.B * pages_per_seq * c.Hkv * c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2) > kStreamNtBytes;
   auto streamed = [&](auto elem, auto dim, auto page) {
-    if constexpr (sizeof(elem) == 2) {
-      if (nt) {
-        launch(elem, dim, page, std::true_type());
-        return;
-      }
-    }
-    launch(elem, dim, page, std::false_type());
+    if (nt) launch(elem, dim, page, std::true_type());
+    else launch(elem, dim, page, std::false_type());
   };
   auto page = [&](auto elem, auto dim) {
     switch (c.S) {
