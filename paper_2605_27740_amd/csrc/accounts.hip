@@ -371,7 +371,8 @@ size_t weigh_floats(const CacheView& c) {
 
 hipError_t launch_weigh(const CacheView& c, const WeighArgs& a, hipStream_t stream) {
   const int rows = c.B * c.Hkv;
-  WeighCut cut = {most_splits(rows, c.max_pages_hint), 0};
+  WeighCut cut = {selection_plan(c, c.max_pages_hint), 0};  // uncut, or as unique_dense_paged_decode
+  if (cut.plan.num_splits > 1) cut.plan = most_splits(rows, c.max_pages_hint);
   if (dense_balances(c.B, c.Hkv, c.max_pages_hint, c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2))) cut.max_chunks = dense_max_chunks(rows, c.max_pages_hint);
   const size_t slots = cut.max_chunks > 0 ? cut.max_chunks : (size_t)rows * cut.plan.num_splits;
   float* part_ml = a.partials + slots * (c.H / c.Hkv) * c.D;

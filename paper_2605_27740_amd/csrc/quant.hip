@@ -309,10 +309,12 @@ hipError_t launch_restore(const CacheView& c, const QuantPool& pool, void* k_out
 hipError_t launch_quant_decode(const CacheView& c, const void* records, const void* d_q, const int32_t* d_sel_pages, const int32_t* d_sel_count,
                                int sel_stride, int max_list_len, float sm_scale, void* d_out, float* d_lse_out, float* d_partials,
                                hipStream_t stream) {
-  // Lists are cut like those of bf16 pages, four times the bytes: latency and arithmetic are what bounds a short list. us with the
-  // records' own bytes / so: 12 x 8 rows of 200 pages of 16, eight heads 16.7 / 15.8, 16 x 8 x 256 18.3 / 18.8, 32 x 8 x 64 pages of 32 16.0 / 15.9.
+  // Lists, and every page of sequences that are not cut by their lengths, by the rule for lists as if a page had 2 S D bytes, twice its own: latency and
+  // arithmetic are what bounds a short list. us as if it had those of a bf16 page / so / with its own: every page of 1 x 500 tokens 8.3 / 6.2 /
+  // 6.3, 2 x 600, eight heads 9.4 / 8.0 / 7.6, the toy model of 2048 tokens 9.0 / 8.9 / 11.5, 4 x 1500 9.6 / 10.0 / 11.2; lists of 16 x 8 rows x 256 18.8 /
+  // 18.4 / 18.1, 12 x 8 x 200, eight heads 16.1 / 16.2 / 16.9. (Every page as for full-precision caches, most_splits: 1 x 113 tokens 9.9 / 7.2 so.)
   const int rows = c.B * c.Hkv, page_bytes = QuantTile{c.S, c.D}.bytes();
-  SplitPlan plan = d_sel_pages ? plan_splits(c.B, c.Hkv, max_list_len, c.max_pages_hint, c.S * c.D * 4, false) : most_splits(rows, max_list_len);
+  SplitPlan plan = plan_splits(c.B, c.Hkv, max_list_len, c.max_pages_hint, c.S * c.D * 2, false);
   size_t slots = (size_t)rows * plan.num_splits;
   if (!d_sel_pages && dense_balances(c.B, c.Hkv, max_list_len, page_bytes, kQuantLeastBytes)) {
     plan = SplitPlan{dense_max_chunks(rows, max_list_len, quant_round(rows, max_list_len)), 0, 0};

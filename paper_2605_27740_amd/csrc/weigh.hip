@@ -10,11 +10,16 @@
 namespace unique {
 namespace {
 
+// A page's part of the attention weights of a head: its share, the log2 of a sum, over the head's whole sum 2^M L; inverse: 1 / L.
+__device__ __forceinline__ float add_weight(float w, float share, float M, float inverse) { return fmaf(fast_exp2(share - M), inverse, w); }
+
+// With one chunk to a row there is nothing to merge: the workgroup writes the output and the row's accounts itself.
 template <typename T, int D, int S, int G, bool kNT>
-__global__ __launch_bounds__(kDecWaves* kWave) void weigh_partial_kernel(CacheView c, const T* __restrict__ q, WeighCut cut, float scale_log2,
-                                                                         float* __restrict__ part_o, float* __restrict__ part_ml,
-                                                                         float* __restrict__ shares) {
+__global__ __launch_bounds__(kDecWaves* kWave) void weigh_partial_kernel(CacheView c, WeighArgs a, WeighCut cut, float* __restrict__ part_ml,
+                                                                         float* shares) {
   __shared__ DecodeShared<T, D, G> sh;
+  const bool alone = cut.max_chunks == 0 && cut.plan.num_splits == 1;
+  const ChunkOut<T> to = {a.partials, part_ml, reinterpret_cast<T*>(a.out), a.lse_out, alone ? 1 : 2};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   Chunk chunk;
   if (cut.max_chunks > 0) {
@@ -29,11 +34,13 @@ __global__ __launch_bounds__(kDecWaves* kWave) void weigh_partial_kernel(CacheVi
     locate_chunk(c, cut.plan, split, hkv, b);
     const int N = c.seq_lens[b], begin = split * cut.plan.pages_per_split;
     const int P = min((N + S - 1) / S, c.max_pages_hint);
-    if (begin >= P) return;
+    if (begin >= P) {
+      write_empty<T, D, G>(c, to, b, hkv);
+      return;
+    }
     chunk = {hkv, b, begin, min(begin + cut.plan.pages_per_split, P), N, (int64_t)(b * c.Hkv + hkv) * cut.plan.num_splits + split};
   }
   const int b = chunk.b, N = chunk.N;
-  const ChunkOut<T> to = {part_o, part_ml, nullptr, nullptr, 2};
   auto lookup = [&](int e, bool, int& phys, int& ntok) {
     const int ph = c.page_table[(int64_t)b * c.max_pages + e];
     if (ph >= 0 && (int64_t)ph < c.num_phys) {
@@ -41,15 +48,34 @@ __global__ __launch_bounds__(kDecWaves* kWave) void weigh_partial_kernel(CacheVi
       ntok = min(S, N - e * S);
     }
   };
-  const PageShares<G> tell = {shares + (int64_t)(b * c.Hkv + chunk.hkv) * c.max_pages_hint * G};
-  decode_chunk<D, S, G, kNT>(c, q, chunk, wave, lane, lookup, scale_log2, to, sh, tell);
+  const int64_t row = b * c.Hkv + chunk.hkv;
+  const PageShares<G> tell = {shares + row * c.max_pages_hint * G};
+  decode_chunk<D, S, G, kNT>(c, reinterpret_cast<const T*>(a.q), chunk, wave, lane, lookup, a.scale_log2, to, sh, tell);
+  if (!alone) return;
+  float M[G], inverse[G];
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    M[g] = fmaxf(fmaxf(sh.m[0][g], sh.m[1][g]), fmaxf(sh.m[2][g], sh.m[3][g]));
+    float L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kDecWaves; ++w) L = fmaf(sh.l[w][g], fast_exp2(sh.m[w][g] - M[g]), L);
+    inverse[g] = L > 0.f ? 1.f / L : 0.f;
+  }
+  __syncthreads();  // the shares of all waves are written
+  for (int p = threadIdx.x; p < chunk.end; p += kDecWaves * kWave) {
+    float w = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) w = add_weight(w, tell.at[(int64_t)p * G + g], M[g], inverse[g]);
+    const int64_t at = row * a.weight_stride + p;
+    a.weights_out[at] = a.weights_in ? fmaf(a.decay, a.weights_in[at], w) : w;
+  }
 }
 
 constexpr int kFinishThreads = kMergeWaves * kWave;
 constexpr int kPagesEach = 2;  // of a thread
 
 // The first H workgroups of a sequence merge a head's chunks, the others add up accounts: of a KV head, kPagesEach pages a thread,
-// the sum over its heads of 2^(share - M) / L with the maximum M and the sum L of the chunks' (m, l), which every workgroup forms for itself.
+// the sum over its heads of 2^(share - M) / L (add_weight) with the maximum M and the sum L of the chunks' (m, l), which every workgroup forms for itself.
 template <typename T, int D, int G>
 __global__ __launch_bounds__(kFinishThreads) void weigh_finish_kernel(CacheView c, WeighArgs a, WeighCut cut, const float* __restrict__ part_ml,
                                                                       const float* __restrict__ shares, int parts /*workgroups of a KV head*/) {
@@ -108,7 +134,7 @@ __global__ __launch_bounds__(kFinishThreads) void weigh_finish_kernel(CacheView 
     const int p = first + u * kFinishThreads + threadIdx.x;
     float w = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) w = fmaf(fast_exp2(share[u][g] - s_m[g]), s_r[g], w);
+    for (int g = 0; g < G; ++g) w = add_weight(w, share[u][g], s_m[g], s_r[g]);
     if (p < P) a.weights_out[(int64_t)row * a.weight_stride + p] = a.weights_in ? fmaf(a.decay, old[u], w) : w;
   }
 }
@@ -117,12 +143,12 @@ template <typename T, int D, int S, int G>
 hipError_t launch_t(const CacheView& c, const WeighArgs& a, const WeighCut& cut, float* part_ml, float* shares, hipStream_t st) {
   auto go = [&](auto kernel) {
     const dim3 grid = cut.max_chunks > 0 ? dim3(cut.max_chunks) : dim3(cut.plan.num_splits, c.Hkv, c.B);
-    kernel<<<grid, dim3(kDecWaves * kWave), 0, st>>>(c, reinterpret_cast<const T*>(a.q), cut, a.scale_log2, a.partials, part_ml, shares);
+    kernel<<<grid, dim3(kDecWaves * kWave), 0, st>>>(c, a, cut, part_ml, shares);
   };
   if (decode_streams(c, c.max_pages_hint)) go(weigh_partial_kernel<T, D, S, G, true>);
   else go(weigh_partial_kernel<T, D, S, G, false>);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || (cut.max_chunks == 0 && cut.plan.num_splits == 1)) return e;
   const int parts = (c.max_pages_hint + kFinishThreads * kPagesEach - 1) / (kFinishThreads * kPagesEach);
   weigh_finish_kernel<T, D, G><<<dim3(c.H + c.Hkv * parts, c.B), dim3(kFinishThreads), 0, st>>>(c, a, cut, part_ml, shares, parts);
   return hipGetLastError();
