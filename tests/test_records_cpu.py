@@ -1,5 +1,8 @@
 """The calls on 4-bit records, page accounts and eviction without a GPU: refusals, sizes, and the plain 64-bit counterparts themselves."""
 import ctypes as C
+import os
+import random
+import subprocess
 
 import pytest
 import torch
@@ -155,3 +158,58 @@ def test_evict_counterpart():
     (keep, freed, n), = R.evict(table, torch.tensor([73]), w, 8, 5, 1, 2)   # ten pages, the last of one token
     assert keep == [0, 1, 4, 8, 9] and freed == [2, 3, 5, 6, 7] and n == 73 - 40
     assert R.evict(table, torch.tensor([40]), w, 8, 5, 1, 2) == [(list(range(5)), [], 40)]
+
+
+# ------------------------------------------------------------------ the layout and the cuts that the library compiles
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    here = os.path.dirname(os.path.abspath(__file__))
+    so = str(tmp_path_factory.mktemp("rules") / "record_rules.so")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-ftrapv", "-shared", "-fPIC", "-o", so, os.path.join(here, "c_abi", "record_rules.cpp")], check=True)
+    return C.CDLL(so)
+
+
+@pytest.mark.parametrize("S", [8, 16, 32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_layout_of_the_library(rules, S, D):
+    assert rules.tile_bytes(S, D) == R.tile_bytes(S, D) and rules.tile_bytes(S, D) % 16 == 0
+    assert [rules.tile_part(S, D, i) for i in range(4)] == [0, S * D // 2, S * D, S * D + S * (D // 32)]
+    for t in range(S):
+        for u in range(16):
+            assert rules.v_at(S, D, t, u) == R.v_byte(S, D, t, u * (D // 16))
+    # what a lane of the attention takes at once: D/16 channels of four tokens, consecutive and aligned
+    for t in range(0, S, 4):
+        for u in range(16):
+            at = rules.v_at(S, D, t, u)
+            assert at % (D // 8) == 0 and [rules.v_at(S, D, t + i, u) for i in range(4)] == [at + i * (D // 32) for i in range(4)]
+
+
+def test_cuts_of_batches_of_records(rules):
+    """Whatever the lengths: the chunks fit the launch and the launch's partial results, and no sequence with pages is without one."""
+    rng = random.Random(5)
+    seen = 0
+    for _ in range(3000):
+        heads, batch, most = rng.choice([1, 2, 4, 8, 16, 32]), rng.randint(1, 64), int(2 ** rng.uniform(1, 17))
+        if not rules.balances(batch, heads, most, rng.choice([544, 1088, 2176, 4352])):
+            continue
+        seen += 1
+        lens = [rng.choice([0, 1, most, rng.randint(0, most), int(most ** rng.random())]) for _ in range(batch)]
+        if rng.random() < 0.2:
+            lens = [most] * batch
+        out, chunks = (C.c_longlong * 3)(), (C.c_int * batch)()
+        rules.cut(batch, heads, most, (C.c_int * batch)(*lens), out, chunks)
+        assert out[1] <= out[0] and out[2] <= out[1] and out[2] > batch * heads
+        assert sum(chunks) * heads <= out[1]
+        assert all((n > 0) == (k > 0) and k <= max(n, 1) for n, k in zip(lens, chunks))
+    assert seen > 500
+
+
+def test_plans_of_lists_of_records(rules):
+    """A plan never needs more partial results than a workspace of unique_workspace_bytes holds, and covers the list."""
+    rng = random.Random(6)
+    for _ in range(3000):
+        batch, heads, length, pages = rng.randint(1, 600), rng.choice([1, 2, 4, 8, 16, 32]), int(2 ** rng.uniform(0, 14)), int(2 ** rng.uniform(0, 15))
+        out = (C.c_int * 4)()
+        rules.list_plan(batch, heads, length, pages, rng.choice([8, 16, 32]), rng.choice([64, 128]), out)
+        assert out[0] * out[1] >= length > out[0] * (out[1] - 1) and out[1] <= out[3] and out[2] <= batch

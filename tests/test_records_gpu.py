@@ -534,3 +534,105 @@ def test_calls_run_on_the_current_stream(gpu_lib):
     torch.cuda.synchronize()
     for c in caches[:2]:
         assert torch.equal(c.out, want[0]) and torch.equal(c.lse, want[1])
+
+
+def test_all_calls_in_one_graph_replayed(gpu_lib):
+    """Quantise, restore, both forms of attention over records, weighted attention and an eviction in place in one HIP graph; every replay, on other
+    inputs and with eager work between, equals the eager calls bit for bit."""
+    H, Hkv, D, S, lens, budget = 16, 4, 128, 16, [1000, 37, 700], 40
+    wl = paged(lens, H, Hkv, D, S, torch.bfloat16, 12).to(DEV)
+    wl.k_cache.nan_to_num_(0.0), wl.v_cache.nan_to_num_(0.0)
+    geo = dict(q_heads=H, kv_heads=Hkv, head_dim=D, page_size=S, dtype=wl.dtype, num_pages=wl.num_phys_pages, page_table=wl.page_table, seq_lens=wl.seq_lens)
+    sess, cache = DecodeSession(wl, track_weights=True), QuantisedCache(top_k=8, **geo)
+    acc = PageAccounts(budget_pages=budget, sink_pages=1, recent_pages=2, weights=sess.page_weights, **geo)
+    k_out, v_out = torch.zeros_like(wl.k_cache), torch.zeros_like(wl.v_cache)
+    listed = torch.zeros_like(cache.out)
+    sel = torch.arange(8, dtype=torch.int32, device=DEV).expand(3, Hkv, 8).contiguous()
+    count = torch.full((3, Hkv), 8, dtype=torch.int32, device=DEV)
+    start = [wl.page_table.clone(), wl.seq_lens.clone()]
+
+    def calls():
+        cache.quantise_pages(wl.k_cache, wl.v_cache)
+        cache.restore_pages(k_out, v_out)
+        listed.copy_(cache.paged_decode(wl.q, sel, count)[0])
+        cache.paged_decode(wl.q)
+        sess.weighted_paged_decode(decay=0.5, weights_in=sess.page_weights, weights_out=sess.page_weights)
+        acc.evict_pages()
+
+    def begin(seed):
+        torch.manual_seed(seed)
+        wl.page_table.copy_(start[0]), wl.seq_lens.copy_(start[1])
+        wl.q.copy_(torch.randn(wl.q.shape))
+        wl.k_cache.copy_(torch.randn(wl.k_cache.shape))
+        wl.v_cache.copy_(torch.randn(wl.v_cache.shape))
+        sess.page_weights.copy_(torch.rand(sess.page_weights.shape))
+        for x in (cache.records, k_out, v_out, listed, cache.out, sess.out_dense, acc.freed_pages):
+            x.zero_()
+
+    def results():
+        torch.cuda.synchronize()
+        return [x.clone() for x in (cache.records, k_out, v_out, listed, cache.out, cache.lse, sess.out_dense, sess.lse_dense, sess.page_weights, wl.page_table,
+                                    wl.seq_lens, acc.freed_pages, acc.freed_count)]
+
+    begin(0)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        calls()
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for seed in range(1, 5):
+        begin(seed)
+        calls()
+        want = results()
+        assert int(acc.freed_count.max()) > 0
+        begin(seed)
+        graph.replay()
+        for x, y in zip(results(), want):
+            assert torch.equal(x, y), seed
+
+
+def test_bounds_below_the_table(gpu_lib):
+    """A length bound far below the table's width, and accounts wider than the bound: the calls read and write the sequences' part only."""
+    H, Hkv, D, S, lens, budget = 8, 2, 64, 8, [100, 61], 6
+    wl = paged(lens, H, Hkv, D, S, torch.float32, 31, spare_tokens=400)
+    wl = wl.to(DEV)
+    geo = dict(q_heads=H, kv_heads=Hkv, head_dim=D, page_size=S, dtype=wl.dtype, num_pages=wl.num_phys_pages, page_table=wl.page_table, seq_lens=wl.seq_lens,
+               max_seq_len=104)
+    sess = DecodeSession(wl, track_weights=True, max_seq_len_hint=104)
+    sess.page_weights.fill_(3.0)
+    sess.weighted_paged_decode(decay=0.0)
+    torch.cuda.synchronize()
+    check_weighted(wl, sess, None, sess.page_weights, 0.0)
+    assert (sess.page_weights[0, :, 13:] == 3).all() and (sess.page_weights[1, :, 8:] == 3).all()
+    cache = QuantisedCache(**geo)
+    cache.quantise_pages(wl.k_cache, wl.v_cache)
+    q = wl.q.cpu()
+    cache.paged_decode(wl.q)
+    torch.cuda.synchronize()
+    rec = R.tiles_of(wl.k_cache.cpu().nan_to_num(0.0).flatten(0, 1), wl.v_cache.cpu().nan_to_num(0.0).flatten(0, 1)).view(wl.num_phys_pages, Hkv, -1)
+    check_decode(cache, rec, q, wl.page_table.cpu(), lens, Hkv, S, D)
+    before = wl.page_table.cpu().clone(), wl.seq_lens.cpu().clone(), sess.page_weights.cpu().clone()
+    acc = PageAccounts(budget_pages=budget, sink_pages=0, recent_pages=1, weights=sess.page_weights, **geo)
+    acc.evict_pages()
+    torch.cuda.synchronize()
+    check_evict(acc, *before, S, (budget, 0, 1), wl.page_table.cpu(), wl.seq_lens.cpu(), sess.page_weights.cpu())
+    assert torch.equal(wl.page_table.cpu()[:, 13:], before[0][:, 13:]) and (sess.page_weights[0, :, 13:] == 3).all()
+
+
+@pytest.mark.parametrize("batch,tokens", [(300, 90), (33, 700)])
+def test_many_sequences(gpu_lib, batch, tokens):
+    """More rows than compute units, short sequences among them, fp32 records with eight heads; every row of some sequences."""
+    Hkv, G, D, S = 8, 8, 128, 16
+    lens = [(tokens * (b % 7 + 1)) // 7 for b in range(batch)]
+    g = torch.Generator().manual_seed(batch)
+    table, pool = tables(lens, S, g)
+    rec = random_records(pool, Hkv, S, D, g)
+    q = torch.randn((batch, Hkv * G, D), generator=g)
+    cache = QuantisedCache(records=rec.to(DEV).view(pool, -1), **geometry(Hkv * G, Hkv, D, S, torch.float32, pool, table, lens))
+    cache.paged_decode(q.to(DEV))
+    torch.cuda.synchronize()
+    check_decode(cache, rec, q, table, lens, Hkv, S, D, rows=[(b, h) for b in (0, 6, batch - 1) for h in range(Hkv)])
