@@ -166,41 +166,58 @@ class Library:
     def page_record_bytes(self, desc: CacheDesc) -> int:
         return int(self.c.unique_page_record_bytes(C.byref(desc)))
 
-    def quantise_pages(self, desc: CacheDesc, records, record_table=None, tok_begin=None, tok_end=None,
-                       max_pages_touched_per_seq: int = 0):
-        self.check(self.c.unique_quantise_pages(C.byref(desc), _p(tok_begin), _p(tok_end), max_pages_touched_per_seq,
-                                                _p(records), _p(record_table), records.shape[0], _stream()))
-
-    def restore_pages(self, desc: CacheDesc, records, k_out, v_out, record_table=None, tok_begin=None, tok_end=None,
-                      max_pages_touched_per_seq: int = 0):
-        self.check(self.c.unique_restore_pages(C.byref(desc), _p(tok_begin), _p(tok_end), max_pages_touched_per_seq,
-                                               _p(records), _p(record_table), records.shape[0], _p(k_out), _p(v_out),
-                                               _stream()))
-
-    def quantised_paged_decode(self, desc: CacheDesc, records, q, sel_pages, sel_count, sm_scale: float, out, lse_out,
-                               workspace):
-        self.check(self.c.unique_quantised_paged_decode(C.byref(desc), _p(records), _p(q), _p(sel_pages), _p(sel_count),
-                                                        0 if sel_pages is None else sel_pages.shape[-1], sm_scale,
-                                                        _p(out), _p(lse_out), _p(workspace),
-                                                        workspace.nbytes, _stream()))
-
     def account_workspace_bytes(self, desc: CacheDesc) -> int:
         n = C.c_size_t(0)
         self.check(self.c.unique_account_workspace_bytes(C.byref(desc), C.byref(n)))
         return int(n.value)
 
+    # (written out: a helper per argument costs a microsecond in a call of six)
+    def quantise_pages(self, desc: CacheDesc, records, record_table=None, tok_begin=None, tok_end=None,
+                       max_pages_touched_per_seq: int = 0):
+        rc = self.c.unique_quantise_pages(desc, None if tok_begin is None else tok_begin.data_ptr(),
+                                          None if tok_end is None else tok_end.data_ptr(), max_pages_touched_per_seq,
+                                          records.data_ptr(), None if record_table is None else record_table.data_ptr(),
+                                          records.shape[0], _stream())
+        if rc:
+            self.check(rc)
+
+    def restore_pages(self, desc: CacheDesc, records, k_out, v_out, record_table=None, tok_begin=None, tok_end=None,
+                      max_pages_touched_per_seq: int = 0):
+        rc = self.c.unique_restore_pages(desc, None if tok_begin is None else tok_begin.data_ptr(),
+                                         None if tok_end is None else tok_end.data_ptr(), max_pages_touched_per_seq,
+                                         records.data_ptr(), None if record_table is None else record_table.data_ptr(),
+                                         records.shape[0], k_out.data_ptr(), v_out.data_ptr(), _stream())
+        if rc:
+            self.check(rc)
+
+    def quantised_paged_decode(self, desc: CacheDesc, records, q, sel_pages, sel_count, sm_scale: float, out, lse_out,
+                               workspace):
+        if sel_pages is None:
+            rc = self.c.unique_quantised_paged_decode(desc, records.data_ptr(), q.data_ptr(), None, None, 0, sm_scale, out.data_ptr(),
+                                                      _p(lse_out), workspace.data_ptr(), workspace.nbytes, _stream())
+        else:
+            rc = self.c.unique_quantised_paged_decode(desc, records.data_ptr(), q.data_ptr(), sel_pages.data_ptr(), _p(sel_count),
+                                                      sel_pages.shape[-1], sm_scale, out.data_ptr(), _p(lse_out),
+                                                      workspace.data_ptr(), workspace.nbytes, _stream())
+        if rc:
+            self.check(rc)
+
     def weighted_paged_decode(self, desc: CacheDesc, q, sm_scale: float, decay: float, weights_in, weights_out, out, lse_out,
                               workspace):
-        self.check(self.c.unique_weighted_paged_decode(C.byref(desc), _p(q), sm_scale, decay, _p(weights_in),
-                                                       _p(weights_out), weights_out.shape[-1], _p(out), _p(lse_out),
-                                                       _p(workspace), workspace.nbytes, _stream()))
+        rc = self.c.unique_weighted_paged_decode(desc, q.data_ptr(), sm_scale, decay, _p(weights_in), weights_out.data_ptr(),
+                                                 weights_out.shape[-1], out.data_ptr(), _p(lse_out), workspace.data_ptr(),
+                                                 workspace.nbytes, _stream())
+        if rc:
+            self.check(rc)
 
     def evict_pages(self, desc: CacheDesc, budget_pages: int, sink_pages: int, recent_pages: int, weights_in, weights_out,
                     page_table_out, seq_lens_out, freed_pages, freed_count, workspace):
-        self.check(self.c.unique_evict_pages(C.byref(desc), budget_pages, sink_pages, recent_pages, _p(weights_in),
-                                             _p(weights_out), weights_in.shape[-1], _p(page_table_out), _p(seq_lens_out),
-                                             _p(freed_pages), _p(freed_count), freed_pages.shape[-1], _p(workspace),
-                                             workspace.nbytes, _stream()))
+        rc = self.c.unique_evict_pages(desc, budget_pages, sink_pages, recent_pages, weights_in.data_ptr(), weights_out.data_ptr(),
+                                       weights_in.shape[-1], page_table_out.data_ptr(), seq_lens_out.data_ptr(),
+                                       freed_pages.data_ptr(), freed_count.data_ptr(), freed_pages.shape[-1], workspace.data_ptr(),
+                                       workspace.nbytes, _stream())
+        if rc:
+            self.check(rc)
 
 
 _lib: Library | None = None

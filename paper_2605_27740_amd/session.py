@@ -122,7 +122,7 @@ class QuantisedCache:
         assert records.dtype == torch.uint8 and records.is_contiguous() and records.shape[0] == num_pages
         assert records.numel() == num_pages * record
         self.records = records
-        self._tile, self._tile_stride, self._table_shape = (kv_heads, page_size, head_dim), (head_dim, 1), tuple(page_table.shape)
+        self._tile, self._table_shape = (kv_heads, page_size, head_dim), tuple(page_table.shape)
         self._out_shape = (page_table.shape[0], q_heads, head_dim)
         B = page_table.shape[0]
         self.out = torch.zeros(self._out_shape, device=dev, dtype=dtype)
@@ -130,12 +130,15 @@ class QuantisedCache:
         self.workspace = torch.empty((max(self.lib.workspace_bytes(self.desc, max(top_k, 1)), 256),), device=dev, dtype=torch.uint8)
 
     def _full_desc(self, k, v, table):
-        """The descriptor with full-precision pages instead of the pool (a copy: half the time of ``binding.make_desc``)."""
-        shape, stride = k.shape, k.stride()
-        assert k.dtype is v.dtype is self.dtype and shape[1:] == self._tile and stride[2:] == self._tile_stride
-        assert v.shape == shape and v.stride() == stride
+        """The descriptor with full-precision pages instead of the pool (a copy: a third of the time of ``binding.make_desc``)."""
+        shape = k.shape
+        assert k.dtype is v.dtype is self.dtype and shape[1:] == self._tile and v.shape == shape
         d = binding.CacheDesc.from_buffer_copy(self.desc)
-        d.num_phys_pages, d.k_cache, d.v_cache, d.kv_page_stride, d.kv_head_stride = shape[0], k.data_ptr(), v.data_ptr(), stride[0], stride[1]
+        d.num_phys_pages, d.k_cache, d.v_cache = shape[0], k.data_ptr(), v.data_ptr()
+        if not (k.is_contiguous() and v.is_contiguous()):
+            stride = k.stride()
+            assert v.stride() == stride and stride[2:] == (self._tile[2], 1)
+            d.kv_page_stride, d.kv_head_stride = stride[:2]
         if table is not None:
             assert table.dtype is torch.int32 and table.is_contiguous() and table.shape == self._table_shape
             d.page_table = table.data_ptr()
