@@ -116,7 +116,7 @@ def evict(table, lens, weights, S, budget, sinks, recent):
         rank = weights[b, :, :P].double().sum(0).float().tolist()
         fixed = set(range(sinks)) | set(range(P - recent, P))
         rest = sorted((p for p in range(P) if p not in fixed), key=lambda p: (math.isnan(rank[p]), -rank[p] if not math.isnan(rank[p]) else 0, p))
-        keep = sorted(fixed | set(rest[:budget - len(fixed)]))
-        gone = [p for p in range(P) if p not in set(keep)]
+        stay = fixed | set(rest[:budget - len(fixed)])
+        keep, gone = sorted(stay), [p for p in range(P) if p not in stay]
         got.append((keep, table[b, gone].tolist(), n - len(gone) * S))
     return got

@@ -636,3 +636,36 @@ def test_many_sequences(gpu_lib, batch, tokens):
     cache.paged_decode(q.to(DEV))
     torch.cuda.synchronize()
     check_decode(cache, rec, q, table, lens, Hkv, S, D, rows=[(b, h) for b in (0, 6, batch - 1) for h in range(Hkv)])
+
+
+@pytest.mark.parametrize("pages", [600, 3000, 7000, 12_000])
+@pytest.mark.parametrize("kind", ["equal", "zero", "two values", "wide", "infinite", "nan", "signs", "rising"])
+def test_evict_whatever_the_accounts(gpu_lib, kind, pages):
+    """Accounts that a search for the separating one could stumble over; budgets that only the pages kept in any case fill, and ones page more or less."""
+    S, Hkv = 8, 2
+    g = torch.Generator().manual_seed(pages)
+    lens = [pages * S - 1] * 2
+    table, pool = tables(lens, S, g)
+    w = torch.rand((2, Hkv, pages), generator=g)
+    if kind == "equal":
+        w[:] = 0.125
+    elif kind == "zero":
+        w[:] = 0.0
+    elif kind == "two values":
+        w = (w > 0.5).float()
+    elif kind == "wide":
+        w = torch.pow(2.0, 250 * w - 125)
+    elif kind == "infinite":
+        w[:, :, ::3] = float("inf")
+    elif kind == "nan":
+        w[:, 0, 1::2] = float("nan")
+    elif kind == "signs":
+        w -= 0.5
+    else:
+        w[:] = torch.arange(pages) / 7.0
+    for budget, sinks, recent in ((pages // 3, 2, 5), (40, 30, 10), (pages - 1, 0, 1), (pages - 5, 1, 1), (1, 0, 1)):
+        geo = geometry(Hkv, Hkv, 64, S, torch.bfloat16, pool, table, lens)
+        acc = PageAccounts(budget_pages=budget, sink_pages=sinks, recent_pages=recent, weights=w.to(DEV), **geo)
+        acc.evict_pages()
+        torch.cuda.synchronize()
+        check_evict(acc, table, torch.tensor(lens), w, S, (budget, sinks, recent), geo["page_table"].cpu(), geo["seq_lens"].cpu(), acc.weights.cpu())
