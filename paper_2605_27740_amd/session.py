@@ -89,7 +89,7 @@ class DecodeSession:
         """``dense_paged_decode`` that adds each page's share to its account: ``page_weights``, or from one array to another."""
         if weights_out is None:
             weights_in = weights_out = self.page_weights
-        _check_accounts(self.page_weights.shape, weights_in, weights_out)
+        _check_accounts(self.page_weights.shape, self.page_weights.get_device(), weights_in, weights_out)
         self.lib.weighted_paged_decode(self.desc, self.wl.q, sm_scale, decay, weights_in, weights_out, self.out_dense,
                                        self.lse_dense, self.workspace)
 
@@ -99,9 +99,14 @@ class DecodeSession:
         self.sparse_paged_decode()
 
 
-def _check_accounts(shape, *weights):
+def _check_accounts(shape, device: int, *weights):
     for w in weights:
-        assert w is None or (w.dtype is torch.float32 and w.is_contiguous() and w.shape == shape)
+        assert w is None or (w.dtype is torch.float32 and w.is_contiguous() and w.shape == shape and w.get_device() == device)
+
+
+# Device tensors of the current device are asked for throughout: a host address would fault the GPU, another device's stream fail the
+# launch. (Written out in the calls below, where a helper costs as much as what it checks.)
+_current_device = torch._C._cuda_getDevice
 
 
 class QuantisedCache:
@@ -111,8 +116,10 @@ class QuantisedCache:
 
     def __init__(self, *, q_heads: int, kv_heads: int, head_dim: int, page_size: int, dtype, num_pages: int, page_table, seq_lens,
                  max_seq_len: int = 0, top_k: int = 0, records=None, lib: binding.Library | None = None):
+        assert page_table.is_cuda, "the page table must live on the GPU"
         self.lib = lib or binding.load()
-        dev = page_table.device
+        dev, self._device = page_table.device, page_table.get_device()
+        assert _current_device() == self._device == seq_lens.get_device() and (records is None or records.get_device() == self._device)
         self.page_table, self.seq_lens, self.dtype = page_table, seq_lens, dtype
         self.desc = binding.make_shape_desc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page_size=page_size, dtype=dtype,
                                             num_pages=num_pages, page_table=page_table, seq_lens=seq_lens, max_seq_len_hint=max_seq_len)
@@ -132,6 +139,7 @@ class QuantisedCache:
     def _full_desc(self, k, v, table):
         """The descriptor with full-precision pages instead of the pool (a copy: a third of the time of ``binding.make_desc``)."""
         shape = k.shape
+        assert _current_device() == self._device == k.get_device() == v.get_device()
         assert k.dtype is v.dtype is self.dtype and shape[1:] == self._tile and v.shape == shape
         d = binding.CacheDesc.from_buffer_copy(self.desc)
         d.num_phys_pages, d.k_cache, d.v_cache = shape[0], k.data_ptr(), v.data_ptr()
@@ -140,24 +148,33 @@ class QuantisedCache:
             assert v.stride() == stride and stride[2:] == (self._tile[2], 1)
             d.kv_page_stride, d.kv_head_stride = stride[:2]
         if table is not None:
-            assert table.dtype is torch.int32 and table.is_contiguous() and table.shape == self._table_shape
+            assert table.get_device() == self._device and table.dtype is torch.int32
+            assert table.is_contiguous() and table.shape == self._table_shape
             d.page_table = table.data_ptr()
         return d
 
     def quantise_pages(self, k_cache, v_cache, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int = 0):
         """Tokens of full-precision pages, found by ``page_table`` (default: the pool's own), into records."""
+        if tok_begin is not None:
+            assert tok_begin.get_device() == tok_end.get_device() == self._device and tok_begin.dtype is tok_end.dtype is torch.int32
+            assert tok_begin.is_contiguous() and tok_end.is_contiguous() and tok_begin.numel() == tok_end.numel() == self._table_shape[0]
         self.lib.quantise_pages(self._full_desc(k_cache, v_cache, page_table), self.records, self.page_table, tok_begin, tok_end,
                                 max_pages_touched_per_seq)
 
     def restore_pages(self, k_out, v_out, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int = 0):
         """The values of the records' tokens into full-precision pages."""
+        if tok_begin is not None:
+            assert tok_begin.get_device() == tok_end.get_device() == self._device and tok_begin.dtype is tok_end.dtype is torch.int32
+            assert tok_begin.is_contiguous() and tok_end.is_contiguous() and tok_begin.numel() == tok_end.numel() == self._table_shape[0]
         self.lib.restore_pages(self._full_desc(k_out, v_out, page_table), self.records, k_out, v_out, self.page_table, tok_begin,
                                tok_end, max_pages_touched_per_seq)
 
     def paged_decode(self, q, sel_pages=None, sel_count=None, sm_scale: float = 0.0):
         """Attention over every page, or over the pages of a selection. -> ``out``, ``lse`` (the same tensors every time)."""
+        assert _current_device() == self._device == q.get_device()
         assert q.dtype is self.dtype and q.is_contiguous() and q.shape == self._out_shape
         if sel_pages is not None:
+            assert sel_pages.get_device() == sel_count.get_device() == self._device
             assert sel_pages.dtype is sel_count.dtype is torch.int32 and sel_pages.is_contiguous() and sel_count.is_contiguous()
             assert sel_pages.shape[:2] == sel_count.shape == (self._out_shape[0], self._tile[0])
         self.lib.quantised_paged_decode(self.desc, self.records, q, sel_pages, sel_count, sm_scale, self.out, self.lse, self.workspace)
@@ -173,14 +190,17 @@ class PageAccounts:
     def __init__(self, *, budget_pages: int, sink_pages: int = 0, recent_pages: int = 1, q_heads: int, kv_heads: int, head_dim: int,
                  page_size: int, dtype, num_pages: int, page_table, seq_lens, max_seq_len: int = 0, weights=None,
                  lib: binding.Library | None = None):
+        assert page_table.is_cuda, "the page table must live on the GPU"
         self.lib = lib or binding.load()
-        dev, (B, max_pages) = page_table.device, page_table.shape
+        dev, (B, max_pages), self._device = page_table.device, page_table.shape, page_table.get_device()
+        assert _current_device() == self._device == seq_lens.get_device()
         self.page_table, self.seq_lens = page_table, seq_lens
         self.policy = (int(budget_pages), int(sink_pages), int(recent_pages))
         self.desc = binding.make_shape_desc(q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page_size=page_size, dtype=dtype,
                                             num_pages=num_pages, page_table=page_table, seq_lens=seq_lens, max_seq_len_hint=max_seq_len)
         self.weights = torch.zeros((B, kv_heads, max_pages), device=dev, dtype=torch.float32) if weights is None else weights
-        _check_accounts((B, kv_heads, max_pages), self.weights)
+        self._shape = (B, kv_heads, max_pages)
+        _check_accounts(self._shape, self._device, self.weights)
         self.freed_pages = torch.full((B, max(max_pages - self.policy[0], 1)), -1, device=dev, dtype=torch.int32)
         self.freed_count = torch.zeros((B,), device=dev, dtype=torch.int32)
         self.workspace = torch.empty((self.lib.account_workspace_bytes(self.desc),), device=dev, dtype=torch.uint8)
@@ -190,8 +210,10 @@ class PageAccounts:
         weights_in = self.weights if weights_in is None else weights_in
         if weights_out is None:
             weights_out = weights_in
-        _check_accounts(self.weights.shape, weights_in, weights_out)
+        assert _current_device() == self._device
+        _check_accounts(self._shape, self._device, weights_in, weights_out)
         for given, mine in ((page_table_out, self.page_table), (seq_lens_out, self.seq_lens)):
-            assert given is None or (given.dtype is torch.int32 and given.is_contiguous() and given.shape == mine.shape)
+            assert given is None or (given.get_device() == self._device and given.dtype is torch.int32 and given.is_contiguous()
+                                     and given.shape == mine.shape)
         self.lib.evict_pages(self.desc, *self.policy, weights_in, weights_out, self.page_table if page_table_out is None else page_table_out,
                              self.seq_lens if seq_lens_out is None else seq_lens_out, self.freed_pages, self.freed_count, self.workspace)

@@ -125,6 +125,17 @@ def test_evict_refuses(c):
     assert f(d, *good[:12], 256, None) == WORKSPACE
 
 
+def test_host_tensors_are_refused():
+    """The Python layer takes device tensors only: nothing reaches the library with a host address."""
+    from paper_2605_27740_amd.session import PageAccounts, QuantisedCache
+    geo = dict(q_heads=8, kv_heads=2, head_dim=64, page_size=8, dtype=torch.float32, num_pages=4, page_table=torch.zeros((1, 4), dtype=torch.int32),
+               seq_lens=torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(AssertionError, match="on the GPU"):
+        QuantisedCache(**geo)
+    with pytest.raises(AssertionError, match="on the GPU"):
+        PageAccounts(budget_pages=2, **geo)
+
+
 def test_the_number_format():
     x = torch.zeros(64)
     x[:16] = torch.tensor([6.0, 5.0, 5.01, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25, 0.26, -0.75, -5.0, -3.5, 0.0, -0.2, 7.9])

@@ -669,3 +669,65 @@ def test_evict_whatever_the_accounts(gpu_lib, kind, pages):
         acc.evict_pages()
         torch.cuda.synchronize()
         check_evict(acc, table, torch.tensor(lens), w, S, (budget, sinks, recent), geo["page_table"].cpu(), geo["seq_lens"].cpu(), acc.weights.cpu())
+
+
+def test_the_python_layer_refuses(gpu_lib):
+    """Host tensors, other types, shapes and layouts: refused before the library is called."""
+    D, S, Hkv, H, lens = 64, 8, 2, 8, [20, 9]
+    g = torch.Generator().manual_seed(0)
+    table, pool = tables(lens, S, g)
+    geo = geometry(H, Hkv, D, S, torch.float32, pool, table, lens)
+    cache, acc = QuantisedCache(top_k=4, **geo), PageAccounts(budget_pages=2, **geo)
+    k = torch.zeros((pool, Hkv, S, D), device=DEV)
+    q = torch.zeros((2, H, D), device=DEV)
+    ints = torch.zeros(2, dtype=torch.int32, device=DEV)
+    sel = torch.zeros((2, Hkv, 4), dtype=torch.int32, device=DEV)
+    count = torch.zeros((2, Hkv), dtype=torch.int32, device=DEV)
+    w = torch.zeros_like(acc.weights)
+    bad = [lambda: cache.quantise_pages(k.cpu(), k), lambda: cache.quantise_pages(k, k.bfloat16()), lambda: cache.quantise_pages(k[:, :1], k[:, :1]),
+           lambda: cache.quantise_pages(k, k[:-1]), lambda: cache.quantise_pages(k.transpose(2, 3).contiguous().transpose(2, 3), k),
+           lambda: cache.quantise_pages(k, k, geo["page_table"][:, :1].contiguous()), lambda: cache.quantise_pages(k, k, None, ints.long(), ints, 1),
+           lambda: cache.quantise_pages(k, k, None, ints.cpu(), ints, 1), lambda: cache.quantise_pages(k, k, None, ints[:1], ints, 1),
+           lambda: cache.restore_pages(k, k.cpu()), lambda: cache.restore_pages(k, k, geo["page_table"].cpu()),
+           lambda: cache.paged_decode(q.cpu()), lambda: cache.paged_decode(q.bfloat16()), lambda: cache.paged_decode(q[:1]),
+           lambda: cache.paged_decode(q, sel.long(), count), lambda: cache.paged_decode(q, sel, count[:1]), lambda: cache.paged_decode(q, sel.cpu(), count),
+           lambda: acc.evict_pages(weights_in=w.cpu()), lambda: acc.evict_pages(weights_in=w.double()), lambda: acc.evict_pages(weights_out=w[:, :1]),
+           lambda: acc.evict_pages(page_table_out=geo["page_table"].long()), lambda: acc.evict_pages(seq_lens_out=ints.cpu()),
+           lambda: QuantisedCache(records=torch.zeros((pool, 7), dtype=torch.uint8, device=DEV), **geo),
+           lambda: PageAccounts(budget_pages=2, weights=w[:, :, 1:], **geo)]
+    for i, call in enumerate(bad):
+        with pytest.raises(AssertionError):
+            call()
+            raise RuntimeError(f"call {i} was taken")
+    longer = torch.zeros((2, Hkv, 4000), dtype=torch.int32, device=DEV)  # a list that the workspace was not made for
+    with pytest.raises(binding.UniqueError) as e:
+        cache.paged_decode(q, longer, count)
+    assert e.value.code == binding.ERR_WORKSPACE
+    with pytest.raises(binding.UniqueError):
+        PageAccounts(budget_pages=2, sink_pages=2, recent_pages=1, **geo).evict_pages()
+
+
+def test_a_step_after_an_eviction_far_below_the_session_s_lower_bound(gpu_lib):
+    """The session's bounds on the lengths are those of its start; sequences that eviction has made much shorter are selected and attended to as in a new session."""
+    H, Hkv, D, S, lens, budget = 16, 4, 128, 16, [9000, 6400, 8011], 24
+    wl = paged(lens, H, Hkv, D, S, torch.bfloat16, 99).to(DEV)
+    sess = DecodeSession(wl, track_weights=True, top_k=8)
+    sess.update_page_stats()
+    sess.weighted_paged_decode()
+    acc = PageAccounts(budget_pages=budget, sink_pages=1, recent_pages=3, q_heads=H, kv_heads=Hkv, head_dim=D, page_size=S, dtype=wl.dtype,
+                       num_pages=wl.num_phys_pages, page_table=wl.page_table, seq_lens=wl.seq_lens, weights=sess.page_weights)
+    acc.evict_pages()
+    assert int(wl.seq_lens.max()) <= budget * S
+    sess.decode_step(refresh_tail=True)
+    sess.dense_paged_decode()
+    fresh = DecodeSession(wl, top_k=8)
+    fresh.update_page_stats()
+    fresh.decode_step(refresh_tail=True)
+    fresh.dense_paged_decode()
+    torch.cuda.synchronize()
+    assert torch.equal(sess.sel_pages, fresh.sel_pages) and torch.equal(sess.sel_count, fresh.sel_count)
+    for x, y in ((sess.out, fresh.out), (sess.out_dense, fresh.out_dense)):
+        assert (x.float() - y.float()).abs().max() <= 2.0 ** -7 * y.float().abs().max()
+    sess.weighted_paged_decode(weights_in=None, weights_out=sess.page_weights)
+    torch.cuda.synchronize()
+    check_weighted(wl, sess, None, sess.page_weights, 0.0)
