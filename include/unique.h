@@ -248,10 +248,14 @@ int unique_restore_pages(const unique_cache_desc* desc, const int32_t* d_tok_beg
                          int32_t max_pages_touched_per_seq, const void* d_records, const int32_t* d_record_table, int64_t num_records,
                          void* d_k_out, void* d_v_out, void* stream);
 
+/* Bytes of device workspace that the call below may need for this descriptor and lists of at most top_k pages (0 = without lists). */
+int unique_quantised_workspace_bytes(const unique_cache_desc* desc, int32_t top_k, size_t* out_bytes);
+
 /* unique_sparse_paged_decode, or with d_sel_pages and d_sel_count NULL unique_dense_paged_decode, over a pool of records. desc->page_table
  * and desc->num_phys_pages are the pool's; k_cache and v_cache are not used and may be NULL. d_q and d_out have desc->dtype. Slots of a page behind
- * seq_lens[b] may be read but never count. The workspace needs unique_workspace_bytes(desc, sel_stride), any top_k without lists.
- * The result of a head that attends a NaN scale is unspecified. */
+ * seq_lens[b] may be read but never count. The result of a head that attends a NaN scale is unspecified.
+ * The workspace needs unique_quantised_workspace_bytes(desc, sel_stride) bytes. What unique_workspace_bytes returns is taken as well; without
+ * lists a batch of unlike lengths may then take longer, and its results differ in rounding. */
 int unique_quantised_paged_decode(const unique_cache_desc* desc, const void* d_records, const void* d_q, const int32_t* d_sel_pages,
                                   const int32_t* d_sel_count, int32_t sel_stride, float sm_scale, void* d_out, float* d_lse_out,
                                   void* d_workspace, size_t workspace_bytes, void* stream);

@@ -19,7 +19,7 @@ DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1}
 
 EXPORTS = ("unique_workspace_bytes", "unique_page_stats_record_bytes", "unique_update_page_stats", "unique_score_select_topk",
            "unique_page_scores", "unique_select_topk", "unique_decode_step", "unique_decode_step_static", "unique_sparse_paged_decode", "unique_dense_paged_decode",
-           "unique_page_record_bytes", "unique_quantise_pages", "unique_restore_pages", "unique_quantised_paged_decode",
+           "unique_page_record_bytes", "unique_quantise_pages", "unique_restore_pages", "unique_quantised_workspace_bytes", "unique_quantised_paged_decode",
            "unique_account_workspace_bytes", "unique_weighted_paged_decode", "unique_evict_pages", "unique_status_string",
            "unique_last_error", "unique_version")
 
@@ -96,6 +96,7 @@ class Library:
         self.c.unique_page_record_bytes.restype = C.c_int64
         self.c.unique_quantise_pages.argtypes = [desc, ptr, ptr, i32, ptr, ptr, C.c_int64, ptr]
         self.c.unique_restore_pages.argtypes = [desc, ptr, ptr, i32, ptr, ptr, C.c_int64, ptr, ptr, ptr]
+        self.c.unique_quantised_workspace_bytes.argtypes = [desc, i32, C.POINTER(C.c_size_t)]
         self.c.unique_quantised_paged_decode.argtypes = [desc, ptr, ptr, ptr, ptr, i32, C.c_float, ptr, ptr, ptr, C.c_size_t, ptr]
         self.c.unique_account_workspace_bytes.argtypes = [desc, C.POINTER(C.c_size_t)]
         self.c.unique_weighted_paged_decode.argtypes = [desc, ptr, C.c_float, C.c_float, ptr, ptr, i32, ptr, ptr, ptr, C.c_size_t, ptr]
@@ -165,6 +166,11 @@ class Library:
 
     def page_record_bytes(self, desc: CacheDesc) -> int:
         return int(self.c.unique_page_record_bytes(C.byref(desc)))
+
+    def quantised_workspace_bytes(self, desc: CacheDesc, top_k: int) -> int:
+        n = C.c_size_t(0)
+        self.check(self.c.unique_quantised_workspace_bytes(C.byref(desc), top_k, C.byref(n)))
+        return int(n.value)
 
     def account_workspace_bytes(self, desc: CacheDesc) -> int:
         n = C.c_size_t(0)

@@ -253,6 +253,16 @@ int make_shape_view(const unique_cache_desc* desc, unique::CacheView* v) {
   return make_view(&d, v, false, false);
 }
 
+// The same for a size, which depends on dimensions only.
+int make_size_view(const unique_cache_desc* desc, unique::CacheView* v) {
+  if (!desc) return fail(UNIQUE_ERR_INVALID_ARG, "desc is NULL");
+  static const int32_t dummy = 0;
+  unique_cache_desc d = *desc;
+  if (!d.page_table) d.page_table = &dummy;
+  if (!d.seq_lens) d.seq_lens = &dummy;
+  return make_shape_view(&d, v);
+}
+
 // What the two calls between pages and records share.
 int record_call(const unique::CacheView& v, const void* d_records, const int32_t* d_record_table, int64_t num_records,
                 const int32_t* d_tok_begin, const int32_t* d_tok_end, int32_t max_pages_touched_per_seq, unique::QuantPool* pool, int* touched) {
@@ -485,6 +495,17 @@ int unique_restore_pages(const unique_cache_desc* desc, const int32_t* d_tok_beg
   return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "restore launch");
 }
 
+int unique_quantised_workspace_bytes(const unique_cache_desc* desc, int32_t top_k, size_t* out_bytes) {
+  if (!out_bytes) return fail(UNIQUE_ERR_INVALID_ARG, "out_bytes is NULL");
+  if (top_k < 0) return fail(UNIQUE_ERR_INVALID_ARG, "top_k must be >= 0 (got %d)", top_k);
+  unique::CacheView v;
+  const int rc = make_size_view(desc, &v);
+  if (rc != UNIQUE_OK) return rc;
+  const size_t lists = top_k > 0 ? decode_bytes(v, top_k) : 0;
+  *out_bytes = round_up(std::max({lists, decode_bytes(v, v.max_pages_hint), unique::quant_cut_floats(v) * sizeof(float)}), kAlign);
+  return UNIQUE_OK;
+}
+
 int unique_quantised_paged_decode(const unique_cache_desc* desc, const void* d_records, const void* d_q, const int32_t* d_sel_pages,
                                   const int32_t* d_sel_count, int32_t sel_stride, float sm_scale, void* d_out, float* d_lse_out,
                                   void* d_workspace, size_t workspace_bytes, void* stream) {
@@ -502,19 +523,14 @@ int unique_quantised_paged_decode(const unique_cache_desc* desc, const void* d_r
   rc = check_workspace(d_workspace, workspace_bytes, decode_bytes(v, list_len));
   if (rc != UNIQUE_OK) return rc;
   const hipError_t e = unique::launch_quant_decode(v, d_records, d_q, d_sel_pages, d_sel_count, list_len, list_len, sm_scale, d_out, d_lse_out,
-                                                   reinterpret_cast<float*>(d_workspace), (hipStream_t)stream);
+                                                   reinterpret_cast<float*>(d_workspace), workspace_bytes / sizeof(float), (hipStream_t)stream);
   return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "quantised decode launch");
 }
 
 int unique_account_workspace_bytes(const unique_cache_desc* desc, size_t* out_bytes) {
   if (!out_bytes) return fail(UNIQUE_ERR_INVALID_ARG, "out_bytes is NULL");
-  if (!desc) return fail(UNIQUE_ERR_INVALID_ARG, "desc is NULL");
-  static const int32_t dummy = 0;
-  unique_cache_desc d = *desc;  // the size depends on dimensions only
-  if (!d.page_table) d.page_table = &dummy;
-  if (!d.seq_lens) d.seq_lens = &dummy;
   unique::CacheView v;
-  const int rc = make_shape_view(&d, &v);
+  const int rc = make_size_view(desc, &v);
   if (rc != UNIQUE_OK) return rc;
   *out_bytes = round_up(std::max(unique::weigh_floats(v) * sizeof(float), unique::evict_bytes(v)), kAlign);
   return UNIQUE_OK;

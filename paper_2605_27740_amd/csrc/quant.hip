@@ -306,9 +306,14 @@ hipError_t launch_restore(const CacheView& c, const QuantPool& pool, void* k_out
   });
 }
 
+size_t quant_cut_floats(const CacheView& c) {
+  const QuantBatch batch = quant_batch(c);
+  return batch.balances() ? (size_t)batch.max_chunks() * (c.H / c.Hkv) * (c.D + 2) : 0;
+}
+
 hipError_t launch_quant_decode(const CacheView& c, const void* records, const void* d_q, const int32_t* d_sel_pages, const int32_t* d_sel_count,
                                int sel_stride, int max_list_len, float sm_scale, void* d_out, float* d_lse_out, float* d_partials,
-                               hipStream_t stream) {
+                               size_t partial_floats, hipStream_t stream) {
   // Lists, and every page of sequences that are not cut by their lengths, by the rule for lists as if a page had 2 S D bytes, twice its own: latency and
   // arithmetic are what bounds a short list. us as if it had those of a bf16 page / so / with its own: every page of 1 x 500 tokens 8.3 / 6.2 /
   // 6.3, 2 x 600, eight heads 9.4 / 8.0 / 7.6, the toy model of 2048 tokens 9.0 / 8.9 / 11.5, 4 x 1500 9.6 / 10.0 / 11.2; lists of 16 x 8 rows x 256 18.8 /
@@ -316,8 +321,9 @@ hipError_t launch_quant_decode(const CacheView& c, const void* records, const vo
   const int rows = c.B * c.Hkv, page_bytes = QuantTile{c.S, c.D}.bytes();
   SplitPlan plan = plan_splits(c.B, c.Hkv, max_list_len, c.max_pages_hint, c.S * c.D * 2, false);
   size_t slots = (size_t)rows * plan.num_splits;
-  if (!d_sel_pages && dense_balances(c.B, c.Hkv, max_list_len, page_bytes, kQuantLeastBytes)) {
-    plan = SplitPlan{dense_max_chunks(rows, max_list_len, quant_round(rows, max_list_len)), 0, 0};
+  const size_t cut_floats = d_sel_pages ? 0 : quant_cut_floats(c);
+  if (cut_floats > 0 && partial_floats >= cut_floats) {
+    plan = SplitPlan{quant_batch(c).max_chunks(), 0, 0};
     slots = plan.pages_per_split;
   }
   const bool nt = (int64_t)rows * max_list_len * page_bytes > kStreamNtBytes;

@@ -17,10 +17,15 @@ hipError_t launch_quantise(const CacheView& c, const QuantPool& pool, const int3
 hipError_t launch_restore(const CacheView& c, const QuantPool& pool, void* k_out, void* v_out, const int32_t* d_tok_begin,
                           const int32_t* d_tok_end, int max_pages_touched, hipStream_t stream);
 
-// Attention over records, which c.page_table and c.num_phys describe. d_sel_pages == nullptr: every page.
+// Attention over records, which c.page_table and c.num_phys describe. d_sel_pages == nullptr: every page, cut by the lengths (quant_plan.hpp)
+// where that is worth while and the partial results that it may have, quant_cut_floats(c), find room.
+size_t quant_cut_floats(const CacheView& c);
+inline QuantBatch quant_batch(const CacheView& c) {
+  return {c.B, c.Hkv, c.max_pages_hint, QuantTile{c.S, c.D}.bytes(), c.dtype == 1 || c.D == 64};
+}
 hipError_t launch_quant_decode(const CacheView& c, const void* records, const void* d_q, const int32_t* d_sel_pages, const int32_t* d_sel_count,
                                int sel_stride, int max_list_len, float sm_scale, void* d_out, float* d_lse_out, float* d_partials,
-                               hipStream_t stream);
+                               size_t partial_floats, hipStream_t stream);
 
 struct QuantDecodeArgs {
   const char* records;

@@ -370,7 +370,7 @@ template <typename T, int D, int S, int G>
 hipError_t launch_t(const CacheView& c, const QuantDecodeArgs& a, const SplitPlan& plan, bool stream_nt, hipStream_t st) {
   if (plan.num_splits == 0) {
     const int max_chunks = plan.pages_per_split;
-    const DenseRound round = quant_round(c.B * c.Hkv, c.max_pages_hint);
+    const DenseRound round = quant_batch(c).round();
     if (stream_nt) quant_dense_kernel<T, D, S, G, true><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks, round);
     else quant_dense_kernel<T, D, S, G, false><<<dim3(max_chunks), dim3(kDecWaves * kWave), 0, st>>>(c, a, max_chunks, round);
     const hipError_t e = hipGetLastError();

@@ -25,15 +25,32 @@ struct QuantTile {
   constexpr int v_at(int tok, int unit) const { return v_codes() + ((tok / 8 * 16 + unit) * 8 + tok % 8) * v_unit_bytes(); }
 };
 
-// Every page of a batch whose sequences may differ in length is cut by the lengths on the device, as for full-precision pages
-// (dense_plan.hpp). Three workgroups run on a compute unit where there is a chunk for each; with fewer chunks than that
-// two have equal shares. us with 512 / 768 workgroups at a time (8 KV heads, G = 4, D = 128): 32 sequences of 4K to 131K tokens, pages
-// of 32 275 / 226, 16 x 131072 366 / 356; 12 of 2K to 50K, G = 8, which may be 672 chunks, 62.9 / 67.3. More rounds than one
-// cost more than they balance: from 256, 512 or 768 pages of a chunk on 372, 360 and 356 for 16 x 131072.
-inline DenseRound quant_round(int rows, int max_pages) {
-  return {rows * most_splits(rows, max_pages).num_splits >= 768 ? 768 : 512, 768};
-}
-// (Batches that can read less than this are cut as if all were as long as the longest: 8 x 4000 tokens, 22 MB, 14.9 us either way.)
-constexpr int64_t kQuantLeastBytes = 24ll << 20;
+// Every page of a batch whose sequences may differ in length is cut by the lengths on the device, as for full-precision pages (dense_plan.hpp),
+// into as many chunks as workgroups run at the same time, or a multiple that is two to a row. us without / with a cut (8 KV heads, G = 4, D = 128,
+// pages of 16): 40 sequences of 1K to 4K tokens 32.5 / 27.2, even 38.2 / 39.3; 60 of 500 to 20K 80.4 / 75.7; 40 of 500 to 6K, D = 64, 27.3 / 21.5. With
+// more than 256 rows a row that is short is soon done, and the merge is another launch: 64 x 2000 27.1 / 37.2, 64 of 100 to 700 11.1 / 19.6.
+// Three workgroups run on a compute unit, two of fp32 outputs with D = 128, and two have enough to do where there is little (and no more rows than 256): with
+// 512 / 768 at a time 32 sequences of 4K to 131K tokens, pages of 32, 275 / 226, 16 x 131072 366 / 356; 16 of 400 to 1500 14.2 / 15.1, 4 of 6K to 30K 21.4 / 21.9; fp32,
+// 8 of 1K to 30K 33.4 / 36.4. More rounds than one cost more than they balance: from 256, 512 or 768 pages of a chunk on 372, 360 and 356 for 16 x 131072.
+constexpr int kQuantMostRows = 1024;
+constexpr int64_t kQuantLeastBytes = 24ll << 20, kQuantLeastRow = 384ll << 10, kQuantThreeBytes = 256ll << 20;
+struct QuantBatch {
+  int batch, kv_heads, max_pages, page_bytes;  // of the part of a KV head
+  bool three_fit;
+  constexpr int rows() const { return batch * kv_heads; }
+  constexpr int64_t row_bytes() const { return (int64_t)max_pages * page_bytes; }
+  DenseRound round() const {
+    const int slots = three_fit && (rows() > 256 || rows() * row_bytes() >= kQuantThreeBytes) ? 768 : 512;
+    return {(2 * rows() + slots - 1) / slots * slots, 768};
+  }
+  int max_chunks() const {
+    const DenseRound r = round();
+    return (int)std::max<int64_t>((int64_t)rows() * max_pages / ((int64_t)r.slots * r.pages), 1) * r.slots;
+  }
+  bool balances() const {
+    if (batch < 2 || batch > kDenseMaxBatch || rows() > kQuantMostRows || (int64_t)rows() * max_pages > INT32_MAX) return false;
+    return rows() * row_bytes() >= kQuantLeastBytes && (rows() <= 256 || row_bytes() >= kQuantLeastRow);
+  }
+};
 
 }  // namespace unique

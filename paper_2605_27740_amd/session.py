@@ -134,7 +134,7 @@ class QuantisedCache:
         B = page_table.shape[0]
         self.out = torch.zeros(self._out_shape, device=dev, dtype=dtype)
         self.lse = torch.zeros((B, q_heads), device=dev, dtype=torch.float32)
-        self.workspace = torch.empty((max(self.lib.workspace_bytes(self.desc, max(top_k, 1)), 256),), device=dev, dtype=torch.uint8)
+        self.workspace = torch.empty((self.lib.quantised_workspace_bytes(self.desc, top_k),), device=dev, dtype=torch.uint8)
 
     def _full_desc(self, k, v, table):
         """The descriptor with full-precision pages instead of the pool (a copy: a third of the time of ``binding.make_desc``)."""

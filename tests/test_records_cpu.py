@@ -88,6 +88,19 @@ def test_decode_over_records_refuses(c):
     assert f(d, A, A, A, A, 4, 0.0, A, None, A, 16, None) == WORKSPACE
 
 
+def test_workspace_of_the_decode_over_records(c):
+    n, old = C.c_size_t(), C.c_size_t()
+    f = c.unique_quantised_workspace_bytes
+    for over in (dict(), dict(batch=40, max_pages_per_seq=250), dict(batch=1, max_pages_per_seq=9000), dict(dtype=0, batch=64, max_pages_per_seq=300)):
+        d = C.byref(good_desc(k_cache=0, v_cache=0, page_table=0, seq_lens=0, **over))
+        for k in (0, 1, 64, 700):
+            assert f(d, k, C.byref(n)) == 0 and n.value % 256 == 0 and n.value > 0
+            few = n.value
+        assert f(d, 0, C.byref(old)) == 0 and old.value <= few
+    assert f(None, 0, C.byref(n)) == BAD and f(d, -1, C.byref(n)) == BAD and f(d, 0, None) == BAD
+    assert f(C.byref(good_desc(head_dim=96)), 0, C.byref(n)) == UNSUPPORTED
+
+
 def test_weighted_decode_refuses(c):
     d = C.byref(good_desc())
     f = c.unique_weighted_paged_decode
@@ -201,17 +214,17 @@ def test_cuts_of_batches_of_records(rules):
     rng = random.Random(5)
     seen = 0
     for _ in range(3000):
-        heads, batch, most = rng.choice([1, 2, 4, 8, 16, 32]), rng.randint(1, 64), int(2 ** rng.uniform(1, 17))
-        if not rules.balances(batch, heads, most, rng.choice([544, 1088, 2176, 4352])):
+        heads, batch, most, page = rng.choice([1, 2, 4, 8, 16, 32]), rng.randint(1, 64), int(2 ** rng.uniform(1, 17)), rng.choice([544, 1088, 2176, 4352])
+        if not rules.balances(batch, heads, most, page):
             continue
         seen += 1
         lens = [rng.choice([0, 1, most, rng.randint(0, most), int(most ** rng.random())]) for _ in range(batch)]
         if rng.random() < 0.2:
             lens = [most] * batch
-        out, chunks = (C.c_longlong * 3)(), (C.c_int * batch)()
-        rules.cut(batch, heads, most, (C.c_int * batch)(*lens), out, chunks)
-        assert out[1] <= out[0] and out[2] <= out[1] and out[2] > batch * heads
-        assert sum(chunks) * heads <= out[1]
+        out, chunks = (C.c_int * 2)(), (C.c_int * batch)()
+        rules.cut(batch, heads, most, page, rng.randint(0, 1), (C.c_int * batch)(*lens), out, chunks)
+        assert out[1] <= out[0] and out[1] >= 2 * batch * heads
+        assert sum(chunks) * heads <= out[0]
         assert all((n > 0) == (k > 0) and k <= max(n, 1) for n, k in zip(lens, chunks))
     assert seen > 500
 

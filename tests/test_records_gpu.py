@@ -731,3 +731,26 @@ def test_a_step_after_an_eviction_far_below_the_session_s_lower_bound(gpu_lib):
     sess.weighted_paged_decode(weights_in=None, weights_out=sess.page_weights)
     torch.cuda.synchronize()
     check_weighted(wl, sess, None, sess.page_weights, 0.0)
+
+
+@pytest.mark.parametrize("dtype,D,S,Hkv,batch,tokens", [(torch.bfloat16, 128, 16, 8, 40, 4000), (torch.float32, 128, 16, 8, 33, 5000), (torch.bfloat16, 64, 32, 16, 50, 7000)])
+def test_batches_of_many_rows_cut_by_their_lengths(gpu_lib, dtype, D, S, Hkv, batch, tokens):
+    """With the workspace that is asked for, and with the smaller one of unique_workspace_bytes, which is cut otherwise: the same within rounding, and what a cut
+    writes stays in the workspace."""
+    G = 2
+    lens = [max(0, tokens - 97 * b) for b in range(batch)]
+    g = torch.Generator().manual_seed(batch)
+    table, pool = tables(lens, S, g)
+    rec = random_records(pool, Hkv, S, D, g)
+    q = torch.randn((batch, Hkv * G, D), generator=g).to(dtype)
+    cache = QuantisedCache(records=rec.to(DEV).view(pool, -1), **geometry(Hkv * G, Hkv, D, S, dtype, pool, table, lens))
+    small = gpu_lib.workspace_bytes(cache.desc, 1)
+    assert small < cache.workspace.numel()
+    guard = torch.full((cache.workspace.numel() + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    for size in (cache.workspace.numel(), small):
+        guard.fill_(0xA5)
+        cache.workspace = guard[:size]
+        cache.paged_decode(q.to(DEV))
+        torch.cuda.synchronize()
+        assert (guard[size:] == 0xA5).all()
+        check_decode(cache, rec, q, table, lens, Hkv, S, D, rows=[(0, 0), (1, Hkv - 1), (batch // 2, 3), (batch - 1, 1)])
