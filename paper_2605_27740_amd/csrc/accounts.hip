@@ -394,18 +394,37 @@ int rank_stride_of(const CacheView& c) { return (c.max_pages_hint + kScoreStride
 
 }  // namespace
 
+// Cut as unique_dense_paged_decode cuts, or not at all where lists would not be; and batches of more rows than it cuts by their lengths are, where
+// a row is long, into two chunks to a row or more: with one workgroup to a row the longest row bounds them, and so do rows that are not a multiple of
+// the workgroups at a time. us one to a row / so (8 KV heads, G = 4, D = 128, pages of 16): 40 sequences of 1K to 4K tokens 107 / 75, even 138 / 111, 64 of 300 to
+// 3100 87 / 68, 40 of 500 to 5000 with eight heads 131 / 66, 33 of 300 to 3000, fp32, 108 / 60, 33 x 2000 69 / 57. About 512 rows that are even and not
+// so long fill two workgroups to a compute unit as they are: 64 x 2000 83 / 91, which is why these have to be longer (64 of 200 to 2000 would gain, 55 / 48).
+static WeighCut weigh_cut(const CacheView& c) {
+  const int rows = c.B * c.Hkv, page_bytes = c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2);
+  WeighCut cut = {selection_plan(c, c.max_pages_hint), 0, {}};
+  if (cut.plan.num_splits > 1) cut.plan = most_splits(rows, c.max_pages_hint);
+  if (dense_balances(c.B, c.Hkv, c.max_pages_hint, page_bytes)) {
+    cut.max_chunks = dense_max_chunks(rows, c.max_pages_hint);
+  } else if (rows > kDenseSlots / 2 && rows <= 2 * kDenseSlots && c.B <= kDenseMaxBatch && (int64_t)rows * c.max_pages_hint <= INT32_MAX &&
+             (int64_t)c.max_pages_hint * page_bytes >= (rows <= 384 ? 512 << 10 : 1024 << 10)) {
+    cut.round.slots = (2 * rows + kDenseSlots - 1) / kDenseSlots * kDenseSlots;
+    cut.max_chunks = (int)std::max<int64_t>((int64_t)rows * c.max_pages_hint / (cut.round.slots * cut.round.pages), 1) * cut.round.slots;
+  }
+  return cut;
+}
+static size_t weigh_slots(const CacheView& c, const WeighCut& cut) {
+  return cut.max_chunks > 0 ? cut.max_chunks : (size_t)c.B * c.Hkv * cut.plan.num_splits;
+}
+
 size_t weigh_floats(const CacheView& c) {
-  return decode_partial_floats(c, c.max_pages_hint) + (size_t)c.B * c.H * c.max_pages_hint;
+  return weigh_slots(c, weigh_cut(c)) * (c.H / c.Hkv) * (c.D + 2) + (size_t)c.B * c.H * c.max_pages_hint;
 }
 
 hipError_t launch_weigh(const CacheView& c, const WeighArgs& a, hipStream_t stream) {
-  const int rows = c.B * c.Hkv;
-  WeighCut cut = {selection_plan(c, c.max_pages_hint), 0};  // uncut, or as unique_dense_paged_decode
-  if (cut.plan.num_splits > 1) cut.plan = most_splits(rows, c.max_pages_hint);
-  if (dense_balances(c.B, c.Hkv, c.max_pages_hint, c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2))) cut.max_chunks = dense_max_chunks(rows, c.max_pages_hint);
-  const size_t slots = cut.max_chunks > 0 ? cut.max_chunks : (size_t)rows * cut.plan.num_splits;
-  float* part_ml = a.partials + slots * (c.H / c.Hkv) * c.D;
-  float* shares = a.partials + decode_partial_floats(c, c.max_pages_hint);
+  const WeighCut cut = weigh_cut(c);
+  const size_t heads = weigh_slots(c, cut) * (c.H / c.Hkv);
+  float* part_ml = a.partials + heads * c.D;
+  float* shares = part_ml + heads * 2;
   auto run = [&](auto launch) { return launch(c, a, cut, part_ml, shares, stream); };
   return c.dtype == 0 ? (c.D == 64 ? run(launch_weigh_of<float, 64>) : run(launch_weigh_of<float, 128>))
                       : (c.D == 64 ? run(launch_weigh_of<bf16_t, 64>) : run(launch_weigh_of<bf16_t, 128>));

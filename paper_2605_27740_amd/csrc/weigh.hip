@@ -25,7 +25,7 @@ __global__ __launch_bounds__(kDecWaves* kWave) void weigh_partial_kernel(CacheVi
   if (cut.max_chunks > 0) {
     const int w = blockIdx.x;
     BatchChunks bc;
-    if (!cut_batch(c, S, cut.max_chunks, w, bc)) return;
+    if (!cut_batch(c, S, cut.max_chunks, w, bc, cut.round)) return;
     const unsigned long long here = sequence_of(c, bc, w);
     if (here == 0) return;
     chunk = chunk_of(c, bc, here, w);
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(kFinishThreads) void weigh_finish_kernel(CacheView 
   int n, have;
   if (cut.max_chunks > 0) {
     BatchChunks bc;
-    cut_batch(c, c.S, cut.max_chunks, 0, bc);
+    cut_batch(c, c.S, cut.max_chunks, 0, bc, cut.round);
     n = have = __builtin_amdgcn_readlane(bc.chunks, b);
     base = (int64_t)__builtin_amdgcn_readlane(bc.before, b) * c.Hkv + (int64_t)hkv * n;
   } else {

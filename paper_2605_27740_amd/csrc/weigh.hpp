@@ -1,5 +1,6 @@
 // Accounts of pages: attention that tells each page's share, and the eviction of the pages with the smallest accounts.
 #pragma once
+#include "dense_plan.hpp"
 #include "kernels.hpp"
 
 namespace unique {
@@ -23,6 +24,7 @@ hipError_t launch_weigh(const CacheView& c, const WeighArgs& a, hipStream_t stre
 struct WeighCut {
   SplitPlan plan;
   int max_chunks;
+  DenseRound round;
 };
 template <typename T, int D>
 hipError_t launch_weigh_of(const CacheView& c, const WeighArgs& a, const WeighCut& cut, float* part_ml, float* shares, hipStream_t stream);

@@ -754,3 +754,28 @@ def test_batches_of_many_rows_cut_by_their_lengths(gpu_lib, dtype, D, S, Hkv, ba
         torch.cuda.synchronize()
         assert (guard[size:] == 0xA5).all()
         check_decode(cache, rec, q, table, lens, Hkv, S, D, rows=[(0, 0), (1, Hkv - 1), (batch // 2, 3), (batch - 1, 1)])
+
+
+@pytest.mark.parametrize("dtype,G,D,batch,tokens", [(torch.bfloat16, 4, 128, 40, 2500), (torch.float32, 2, 64, 50, 4200)])
+def test_weighted_batches_of_many_rows(gpu_lib, dtype, G, D, batch, tokens):
+    """More rows than compute units, long ones among them: cut by their lengths into a workspace that a guard follows."""
+    Hkv = 8
+    lens = [max(0, tokens - (tokens // batch + 1) * b) for b in range(batch)]
+    wl = paged(lens, Hkv * G, Hkv, D, 16, dtype, 70).to(DEV)
+    sess = DecodeSession(wl, track_weights=True, max_seq_len_hint=tokens)
+    need = gpu_lib.account_workspace_bytes(sess.desc)
+    guard = torch.full((need + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    sess.workspace = guard[:need]
+    w = torch.rand_like(sess.page_weights)
+    before = w.clone()
+    sess.weighted_paged_decode(decay=0.5, weights_in=w, weights_out=w)
+    torch.cuda.synchronize()
+    assert (guard[need:] == 0xA5).all()
+    check_weighted(wl, sess, before, w, 0.5, rows=[(0, 0), (1, 7), (batch // 2, 3), (batch - 1, 1)])
+    pages = (wl.seq_lens + 15) // 16
+    for b in (1, batch - 1):
+        assert torch.equal(w[b, :, int(pages[b]):], before[b, :, int(pages[b]):])
+    sess.workspace = guard[:need - 256]
+    with pytest.raises(binding.UniqueError) as e:
+        sess.weighted_paged_decode(decay=0.5, weights_in=w, weights_out=w)
+    assert e.value.code == binding.ERR_WORKSPACE
