@@ -264,7 +264,7 @@ int unique_quantised_paged_decode(const unique_cache_desc* desc, const void* d_r
  * calls, one for each stream that may overlap another). */
 int unique_account_workspace_bytes(const unique_cache_desc* desc, size_t* out_bytes);
 
-/* unique_dense_paged_decode that also keeps an account of what each page is worth: for every sequence, KV head and page
+/* unique_dense_paged_decode (but for the order of its sums) that also keeps an account of what each page is worth: for every sequence, KV head and page
  *   d_weights_out[p] = decay * d_weights_in[p] + sum over the group's query heads and the page's tokens of the attention weights,
  * float, row (b, h_kv) at (b*H_kv + h_kv)*weight_stride, weight_stride >= max_pages_per_seq (or the page bound implied by
  * max_seq_len_hint). Entries at and beyond the pages of a sequence are left as they are (0 is what they should hold
