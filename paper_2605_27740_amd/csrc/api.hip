@@ -459,8 +459,8 @@ int unique_dense_paged_decode(const unique_cache_desc* desc, const void* d_q, fl
 }
 
 int64_t unique_page_record_bytes(const unique_cache_desc* desc) {
-  if (!desc || desc->num_kv_heads < 1 || (desc->head_dim != 64 && desc->head_dim != 128) ||
-      (desc->page_size != 8 && desc->page_size != 16 && desc->page_size != 32))
+  if (!desc || desc->num_kv_heads < 1 || desc->num_kv_heads > 32 || (desc->num_kv_heads & (desc->num_kv_heads - 1)) != 0 ||
+      (desc->head_dim != 64 && desc->head_dim != 128) || (desc->page_size != 8 && desc->page_size != 16 && desc->page_size != 32))
     return 0;
   return (int64_t)desc->num_kv_heads * unique::QuantTile{desc->page_size, desc->head_dim}.bytes();
 }

@@ -48,6 +48,7 @@ class DecodeSession:
         self.lse_dense = torch.zeros_like(self.lse)
         assert self.lib.page_stats_record_bytes(self.desc) == self.page_stats.shape[1]
         self.workspace_bytes = self.lib.workspace_bytes(self.desc, self.top_k)
+        self.page_weights = None
         if track_weights:  # accounts of the pages for weighted_paged_decode
             self.page_weights = torch.zeros((wl.B, wl.Hkv, wl.max_pages), device=dev, dtype=torch.float32)
             self.workspace_bytes = max(self.workspace_bytes, self.lib.account_workspace_bytes(self.desc))
@@ -86,9 +87,12 @@ class DecodeSession:
         self.lib.dense_paged_decode(self.desc, self.wl.q, sm_scale, self.out_dense, self.lse_dense, self.workspace)
 
     def weighted_paged_decode(self, sm_scale: float = 0.0, decay: float = 1.0, weights_in=None, weights_out=None):
-        """``dense_paged_decode`` that adds each page's share to its account: ``page_weights``, or from one array to another."""
+        """``dense_paged_decode`` that adds each page's share to its account: ``page_weights``, or from one array to another (an
+        output without an input: nothing so far)."""
+        assert self.page_weights is not None, "a session made with track_weights=True has the accounts and the workspace"
+        assert _current_device() == self.page_weights.get_device()
         if weights_out is None:
-            weights_in = weights_out = self.page_weights
+            weights_in, weights_out = self.page_weights if weights_in is None else weights_in, self.page_weights
         _check_accounts(self.page_weights.shape, self.page_weights.get_device(), weights_in, weights_out)
         self.lib.weighted_paged_decode(self.desc, self.wl.q, sm_scale, decay, weights_in, weights_out, self.out_dense,
                                        self.lse_dense, self.workspace)
@@ -145,7 +149,7 @@ class QuantisedCache:
         d.num_phys_pages, d.k_cache, d.v_cache = shape[0], k.data_ptr(), v.data_ptr()
         if not (k.is_contiguous() and v.is_contiguous()):
             stride = k.stride()
-            assert v.stride() == stride and stride[2:] == (self._tile[2], 1)
+            assert v.stride() == stride and stride[2:] == (self._tile[2], 1) and stride[0] and stride[1]  # (0 would stand for the default)
             d.kv_page_stride, d.kv_head_stride = stride[:2]
         if table is not None:
             assert table.get_device() == self._device and table.dtype is torch.int32
@@ -176,7 +180,7 @@ class QuantisedCache:
         if sel_pages is not None:
             assert sel_pages.get_device() == sel_count.get_device() == self._device
             assert sel_pages.dtype is sel_count.dtype is torch.int32 and sel_pages.is_contiguous() and sel_count.is_contiguous()
-            assert sel_pages.shape[:2] == sel_count.shape == (self._out_shape[0], self._tile[0])
+            assert sel_pages.dim() == 3 and sel_pages.shape[:2] == sel_count.shape == (self._out_shape[0], self._tile[0])
         self.lib.quantised_paged_decode(self.desc, self.records, q, sel_pages, sel_count, sm_scale, self.out, self.lse, self.workspace)
         return self.out, self.lse
 

@@ -138,6 +138,11 @@ def test_evict_refuses(c):
     assert f(d, *good[:12], 256, None) == WORKSPACE
 
 
+@pytest.mark.parametrize("heads,size", [(1, 1), (16, 16), (32, 32), (3, 0), (12, 0), (64, 0)])
+def test_record_bytes_of_the_supported_numbers_of_heads(c, heads, size):
+    assert c.unique_page_record_bytes(C.byref(good_desc(num_kv_heads=heads, num_q_heads=heads))) == size * (16 * 128 + 2 * 16 * 4)
+
+
 def test_host_tensors_are_refused():
     """The Python layer takes device tensors only: nothing reaches the library with a host address."""
     from paper_2605_27740_amd.session import PageAccounts, QuantisedCache

@@ -779,3 +779,38 @@ def test_weighted_batches_of_many_rows(gpu_lib, dtype, G, D, batch, tokens):
     with pytest.raises(binding.UniqueError) as e:
         sess.weighted_paged_decode(decay=0.5, weights_in=w, weights_out=w)
     assert e.value.code == binding.ERR_WORKSPACE
+
+
+def test_the_python_layer_refuses_repeated_pages_and_flat_lists(gpu_lib):
+    """A stride of 0 is the descriptor's word for the default, and a list of pages has a row per KV head: both would have the kernels read elsewhere."""
+    D, S, Hkv, H, lens = 64, 8, 2, 8, [20, 9]
+    table, pool = tables(lens, S, torch.Generator().manual_seed(0))
+    cache = QuantisedCache(top_k=4, **geometry(H, Hkv, D, S, torch.float32, pool, table, lens))
+    page = torch.zeros((1, Hkv, S, D), device=DEV).expand(pool, Hkv, S, D)
+    head = torch.zeros((pool, 1, S, D), device=DEV).expand(pool, Hkv, S, D)
+    q, count = torch.zeros((2, H, D), device=DEV), torch.zeros((2, Hkv), dtype=torch.int32, device=DEV)
+    for call in (lambda: cache.quantise_pages(page, page), lambda: cache.quantise_pages(head, head), lambda: cache.restore_pages(page, page),
+                 lambda: cache.paged_decode(q, count, count), lambda: cache.paged_decode(q, count.reshape(2, Hkv, 1, 1), count)):
+        with pytest.raises(AssertionError):
+            call()
+
+
+def test_accounts_of_a_session_from_one_array_to_another(gpu_lib):
+    """The account arrays of a session: its own, one given as the input alone, a pair, and an output alone; none without ``track_weights``."""
+    wl = paged([70, 33], 16, 4, 64, 8, torch.bfloat16, 9).to(DEV)
+    sess = DecodeSession(wl, top_k=2, track_weights=True)
+    given, out = torch.rand_like(sess.page_weights), torch.zeros_like(sess.page_weights)
+    sess.weighted_paged_decode()
+    share = sess.page_weights.clone()
+    sess.weighted_paged_decode(decay=0.5, weights_in=given)
+    other = given.clone()
+    sess.weighted_paged_decode(decay=0.5, weights_in=other, weights_out=other)
+    sess.weighted_paged_decode(decay=0.5, weights_out=out)
+    pages = [-(-n // 8) for n in (70, 33)]
+    for b, n in enumerate(pages):
+        assert torch.equal(sess.page_weights[b, :, :n], other[b, :, :n]) and torch.equal(out[b, :, :n], share[b, :, :n])
+        # decay * in + share, rounded once, below 8 (G = 4 and a half)
+        assert (other[b, :, :n].double() - given[b, :, :n].double() / 2 - share[b, :, :n].double()).abs().max() <= 8 * 2.0 ** -24
+        assert torch.equal(other[b, :, n:], given[b, :, n:])
+    with pytest.raises(AssertionError, match="track_weights"):
+        DecodeSession(wl, top_k=2).weighted_paged_decode()
