@@ -10,8 +10,9 @@
 // p.V, one v_mfma_f32_16x16x32_bf16 per 16 channels and tile: A = the probabilities, which stay in their lanes -- its eight
 // k are the two halves' four slots --, as parts of 8 bits in rows parts times heads; B = the values of those slots, channels
 // D/16 * (L % 16) + e: 16 bytes of a half at D = 128, with a scale for each slot.
-// fp32 queries are taken as three bf16 numbers (24 bits, exactly), three products instead of one. The probabilities are three parts
-// (24 bits) for fp32 outputs, two for bf16: what is left out is below 2^-16 of a probability, the output's own rounding 2^-9.
+// fp32 queries are taken as three bf16 numbers (24 bits, exactly), three products instead of one. The probabilities are three parts as well
+// (24 bits, exactly): with two an output whose terms cancel was off by 2^-16 of the terms. us with two / three for bf16 (8 KV heads, D = 128):
+// 16 x 131072 tokens 353 / 356, eight heads, 12 of 2K to 50K, pages of 32 63.1 / 64.5, the latter's lists of 200 pages 15.7 / 16.8.
 #include <type_traits>
 
 #include "dense_cut.hpp"
@@ -22,8 +23,7 @@ namespace {
 
 template <typename T, int D, int G>
 struct QuantShared {  // the waves' results; output rows are parts times heads
-  static constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
-  static constexpr int kSlots = kParts * G > 16 ? 16 : kParts * G;
+  static constexpr int kSlots = G == 8 ? 16 : 3 * G;
   __attribute__((aligned(16))) float acc[kDecWaves][kSlots][D];
   float m[kDecWaves][G], l[kDecWaves][G];
 };
@@ -79,7 +79,7 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
   constexpr int kVB = D / 16;                        // channels of a value row per lane
   constexpr int kQ = sizeof(T) == 4 ? 3 : 1;         // bf16 numbers of a query element
   constexpr int kSlots = QuantShared<T, D, G>::kSlots;
-  constexpr bool kThird = G == 8 && sizeof(T) == 4;  // the third part of a probability is a product of its own
+  constexpr bool kThird = G == 8;                    // the third part of a probability is a product of its own
   constexpr float kRoom = 6.f;                       // log2: how far above the largest logit the reference is put
 
   const int hkv = k.hkv, b = k.b, begin = k.begin, end = k.end;
@@ -238,7 +238,7 @@ __device__ __forceinline__ void quant_chunk(const CacheView& c, const char* __re
         if constexpr (kThird) {
           const float r1 = p - bf16_part(p);
           pb[i] = __float_as_uint(r1 - bf16_part(r1)) & ~not_first;
-        } else if constexpr (sizeof(T) == 4) {
+        } else {
           r -= __uint_as_float(__float_as_uint(r) & not_second);
         }
         pa[i] = __float_as_uint(r);

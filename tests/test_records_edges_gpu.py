@@ -1,0 +1,51 @@
+"""Edges of the calls on 4-bit records, page accounts and eviction on the GPU against plain 64-bit counterparts (records_ref.py)."""
+import math
+
+import pytest
+import torch
+
+from paper_2605_27740_amd.session import QuantisedCache
+from tests import records_ref as R
+from tests.test_records_gpu import DEV, DTYPES, geometry, say, tables
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("G,D,S", [(1, 128, 16), (2, 64, 8), (4, 128, 16), (4, 64, 32), (8, 128, 32), (8, 64, 8)])
+def test_probabilities_of_records_are_32_bit_numbers(gpu_lib, dtype, G, D, S):
+    """Two tokens with opposite values and nearly equal weights: what is left of the output is as small as 2^-10 of what it is the
+    difference of, so that its own rounding does not hide a probability of few bits.
+
+    Only channel 0 of a query is not zero, so a logit is one product, exact in 32 bits. Relative to the reference, which is 6 above the larger
+    one, a logit lies in (-8, 0]: one rounding of 2^-22, ln 2 times that in the exponential, and 2^-23 for the exponential's last bit: 2^-21.7 of
+    a probability. The reference is common to probabilities and normaliser; their sums add at most four roundings of the small difference. 2^-21
+    of the sum of |p v| covers these; 16 bits of a probability would be off by up to 2^-16 of it."""
+    say(f"two tokens {dtype} G={G} D={D} S={S}")
+    B, Hkv = 16, 4
+    lens = [2] * B
+    g = torch.Generator().manual_seed(G + D + S)
+    table, pool = tables(lens, S, g)
+    code = torch.randint(1, 8, (pool, Hkv, D), generator=g)
+    k = torch.zeros((pool, Hkv, S, D), dtype=torch.float64)
+    v = torch.zeros_like(k)
+    k[:, :, 0, 0], k[:, :, 1, 0] = 6.0, R.LEVELS[torch.randint(0, 7, (pool, Hkv), generator=g)]
+    v[:, :, 0] = R.LEVELS[code]
+    v[:, :, 0, ::32] = 6.0           # the largest of every block: all scales are 1
+    v[:, :, 1] = -v[:, :, 0]
+    rec = R.tiles_of(k.flatten(0, 1), v.flatten(0, 1)).view(pool, Hkv, -1)
+    q = torch.zeros((B, Hkv * G, D))
+    q[:, :, 0] = (1 + torch.rand((B, Hkv * G), generator=g)) * 2.0 ** -10
+    q = q.to(dtype)
+    cache = QuantisedCache(records=rec.to(DEV).view(pool, -1), **geometry(Hkv * G, Hkv, D, S, dtype, pool, table, lens))
+    cache.paged_decode(q.to(DEV))
+    torch.cuda.synchronize()
+    out = cache.out.cpu().double().view(B, Hkv, G, D)
+    page = table[:, 0].long()
+    x = q.double().view(B, Hkv, G, D)[..., :1] * k[page][:, :, None, :2, 0] / math.sqrt(D)  # [B, Hkv, G, 2]
+    p = torch.softmax(x, -1)
+    want = (p[..., :1] - p[..., 1:]) * v[page][:, :, None, 0]
+    mass = v[page][:, :, None, 0].abs().expand_as(want)
+    tol = 1.01 * torch.finfo(dtype).eps / 2 * want.abs() + 2.0 ** -21 * mass
+    worst = float(((out - want).abs() / tol).max())
+    assert worst <= 1
