@@ -308,7 +308,8 @@ __global__ __launch_bounds__(kEvictThreads) void evict_kernel(CacheView c, Evict
 constexpr int kCloseThreads = 512, kCloseBatch = 8;
 
 // Closes rows up to the kept pages, in place or not: kept[] ascends, so that entry i comes from kept[i] >= i and a round of the
-// workgroup, which reads before it writes, leaves what later rounds read. blockIdx.x < Hkv: the accounts of a KV head; else the table.
+// workgroup, which reads before it writes, leaves what later rounds read. blockIdx.x < Hkv: the accounts of a KV head; else the table, and
+// the length, which nothing else of this launch reads: it may be written in place.
 __global__ __launch_bounds__(kCloseThreads) void close_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept,
                                                               const int32_t* __restrict__ pages, const int32_t* __restrict__ kept_count) {
   const int b = blockIdx.y, t = threadIdx.x;
@@ -332,27 +333,26 @@ __global__ __launch_bounds__(kCloseThreads) void close_kernel(CacheView c, Evict
     }
   }
   __syncthreads();
+  if (!accounts && t == 0) a.seq_lens_out[b] = c.seq_lens[b] - (P - n) * c.S;
   const uint32_t vacant = accounts ? 0u : ~0u;
   for (int i = n + t; i < P; i += kCloseThreads) out.put((uint32_t)i * 4, vacant);
 }
 
 // The freed pages of a part of a sequence whose kept pages launch_select has chosen, for rows that no workgroup holds; the first part also writes
-// what else there is of the sequence. Before close_kernel, which may overwrite the table.
+// their number and what lies behind them. Before close_kernel, which may overwrite the table and the lengths: every part reads both.
 constexpr int kFreedEach = 4, kFreedPages = kFreedEach * kEvictThreads;
 __global__ __launch_bounds__(kEvictThreads) void freed_kernel(CacheView c, EvictArgs a, const int32_t* __restrict__ kept,
                                                               const int32_t* __restrict__ kept_count, int32_t* __restrict__ pages) {
   __shared__ uint32_t s_stays[kFreedPages];
   __shared__ int s_counts[kEvictWaves];
   const int b = blockIdx.y, t = threadIdx.x, lane = t % kWave, wave = t / kWave;
-  const int N = c.seq_lens[b];
-  const int P = max(min((N + c.S - 1) / c.S, c.max_pages_hint), 0), n = kept_count[b], first = blockIdx.x * kFreedPages;
+  const int P = max(min((c.seq_lens[b] + c.S - 1) / c.S, c.max_pages_hint), 0), n = kept_count[b], first = blockIdx.x * kFreedPages;
   const int32_t* from = kept + (int64_t)b * a.budget;
   int32_t* freed = a.freed_pages + (int64_t)b * a.freed_stride;
   if (first == 0) {
     for (int i = P - n + t; i < a.freed_stride; i += kEvictThreads) freed[i] = -1;
     if (t == 0) {
       a.freed_count[b] = P - n;
-      a.seq_lens_out[b] = N - (P - n) * c.S;
       pages[b] = P;
     }
   }

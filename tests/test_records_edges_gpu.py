@@ -4,9 +4,9 @@ import math
 import pytest
 import torch
 
-from paper_2605_27740_amd.session import QuantisedCache
+from paper_2605_27740_amd.session import PageAccounts, QuantisedCache
 from tests import records_ref as R
-from tests.test_records_gpu import DEV, DTYPES, geometry, say, tables
+from tests.test_records_gpu import DEV, DTYPES, check_evict, geometry, say, tables
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,23 @@ def test_probabilities_of_records_are_32_bit_numbers(gpu_lib, dtype, G, D, S):
     tol = 1.01 * torch.finfo(dtype).eps / 2 * want.abs() + 2.0 ** -21 * mass
     worst = float(((out - want).abs() / tol).max())
     assert worst <= 1
+
+
+def test_evict_in_place_from_many_long_sequences(gpu_lib):
+    """More workgroups than the GPU holds at a time share the sequences, nine to the longest: the lengths that a call shortens in place are those
+    that all of them work from. Twice, the second time with ids of the first in the list of freed pages."""
+    S, Hkv, B, budget, policy = 8, 1, 70, 9000, (4, 16)
+    say(f"evict {B} long sequences")
+    g = torch.Generator().manual_seed(5)
+    for longest in (33_500, 36_000):
+        lens = [longest * S - 7 - 64 * b if b % 10 else budget * S - 8 * (b - 1) for b in range(B)]
+        table, pool = tables(lens, S, g)
+        weights = torch.rand((B, Hkv, table.shape[1]), generator=g)
+        geo = geometry(Hkv, Hkv, 64, S, torch.bfloat16, pool, table, lens)
+        acc = PageAccounts(budget_pages=budget, sink_pages=policy[0], recent_pages=policy[1], weights=weights.to(DEV), **geo)
+        acc.freed_pages.copy_(torch.arange(acc.freed_pages.numel()).view(acc.freed_pages.shape))  # what an earlier call may have left
+        acc.freed_count.fill_(-3)
+        acc.evict_pages()
+        torch.cuda.synchronize()
+        acc.freed_pages, acc.freed_count = acc.freed_pages.cpu(), acc.freed_count.cpu()
+        check_evict(acc, table, torch.tensor(lens), weights, S, (budget, *policy), geo["page_table"].cpu(), geo["seq_lens"].cpu(), acc.weights.cpu())
