@@ -69,3 +69,40 @@ def test_evict_in_place_from_many_long_sequences(gpu_lib):
         torch.cuda.synchronize()
         acc.freed_pages, acc.freed_count = acc.freed_pages.cpu(), acc.freed_count.cpu()
         check_evict(acc, table, torch.tensor(lens), weights, S, (budget, *policy), geo["page_table"].cpu(), geo["seq_lens"].cpu(), acc.weights.cpu())
+
+
+@pytest.mark.parametrize("kind", ["equal", "two values", "wide", "infinite", "nan", "signs"])
+@pytest.mark.parametrize("pages,Hkv", [(1000, 32), (3900, 8), (8188, 8), (20_000, 2)])
+def test_evict_whatever_the_accounts_and_the_heads(gpu_lib, kind, pages, Hkv):
+    """Rows whose sums other workgroups have formed, and rows that no workgroup holds; in place and into other arrays."""
+    S, B = 8, 2
+    say(f"evict {pages} pages, {Hkv} heads, {kind}")
+    g = torch.Generator().manual_seed(pages)
+    lens = [pages * S - 1, (pages - 77) * S]
+    table, pool = tables(lens, S, g)
+    w = torch.rand((B, Hkv, pages), generator=g)
+    if kind == "equal":
+        w[:] = 0.125
+    elif kind == "two values":
+        w = (w > 0.5).float()
+    elif kind == "wide":
+        w = torch.pow(2.0, 250 * w - 125)
+    elif kind == "infinite":
+        w[:, :, 1::3] = float("inf")
+    elif kind == "nan":
+        w[:, 0, 1::2] = float("nan")
+    else:
+        w -= 0.5
+    for budget, sinks, recent in ((pages // 3, 2, 5), (pages - 3, 1, 1), (pages - 100, 0, 40)):
+        geo = geometry(Hkv, Hkv, 64, S, torch.bfloat16, pool, table, lens)
+        acc = PageAccounts(budget_pages=budget, sink_pages=sinks, recent_pages=recent, weights=w.to(DEV), **geo)
+        args = table, torch.tensor(lens), w, S, (budget, sinks, recent)
+        t_out, l_out, w_out = torch.full_like(geo["page_table"], 77), torch.full_like(geo["seq_lens"], 77), torch.full_like(acc.weights, 77.0)
+        acc.evict_pages(weights_out=w_out, page_table_out=t_out, seq_lens_out=l_out)
+        torch.cuda.synchronize()
+        check_evict(acc, *args, t_out.cpu(), l_out.cpu(), w_out.cpu())
+        assert torch.equal(geo["page_table"].cpu(), table) and geo["seq_lens"].tolist() == lens
+        acc.freed_pages.fill_(5)
+        acc.evict_pages()
+        torch.cuda.synchronize()
+        check_evict(acc, *args, geo["page_table"].cpu(), geo["seq_lens"].cpu(), acc.weights.cpu())
