@@ -106,3 +106,28 @@ def test_evict_whatever_the_accounts_and_the_heads(gpu_lib, kind, pages, Hkv):
         acc.evict_pages()
         torch.cuda.synchronize()
         check_evict(acc, *args, geo["page_table"].cpu(), geo["seq_lens"].cpu(), acc.weights.cpu())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D", [64, 128])
+def test_records_of_values_that_are_denormal_in_the_cache(gpu_lib, dtype, D):
+    """Multiples of 2^-130 on either side of the smallest level, 2^-127, whose restored value is a denormal of both types, and of its ties; bytes and values exactly."""
+    S, Hkv = 8, 1
+    step = torch.arange(S * D, dtype=torch.float64).view(1, Hkv, S, D) % 97
+    k = step * 2.0 ** -130 * (1 - 2 * (torch.arange(D) % 2)) + 0.0
+    v = (96 - step) * 2.0 ** -130
+    v[..., -1, 32:] *= 2.0 ** 8  # blocks of an ordinary exponent beside them
+    assert torch.equal(k.to(dtype).double(), k) and torch.equal(v.to(dtype).double(), v)
+    want = [R.values(*R.encode(x)) for x in (k, v)]
+    assert all((x.abs() == 2.0 ** -127).any() and (x == 0).any() for x in want)
+    table = torch.zeros((1, 1), dtype=torch.int32)
+    cache = QuantisedCache(**geometry(1, 1, D, S, dtype, 1, table, [S]))
+    cache.quantise_pages(k.to(dtype).to(DEV), v.to(dtype).to(DEV))
+    ko, vo = (torch.full((1, 1, S, D), -77.0, dtype=dtype, device=DEV) for _ in range(2))
+    cache.restore_pages(ko, vo)
+    torch.cuda.synchronize()
+    for got, x in zip((ko, vo), want):
+        wrong = got.cpu().double() != x
+        assert not wrong.any(), (int(wrong.sum()), got.cpu().double()[wrong][:4].tolist(), x[wrong][:4].tolist())
+    wrong = (cache.records.cpu().view(-1) != R.tiles_of(k.flatten(0, 1), v.flatten(0, 1)).view(-1)).nonzero().flatten().tolist()
+    assert wrong == []
