@@ -210,10 +210,10 @@ class PageAccounts:
         self.workspace = torch.empty((self.lib.account_workspace_bytes(self.desc),), device=dev, dtype=torch.uint8)
 
     def evict_pages(self, weights_in=None, weights_out=None, page_table_out=None, seq_lens_out=None):
-        """In place by default; outputs that are given are written instead of the cache's own arrays."""
+        """In place by default; inputs that are given are read and outputs that are given are written instead of the own arrays (accounts
+        given as the input alone stay as they are: what becomes of them goes to ``weights``)."""
         weights_in = self.weights if weights_in is None else weights_in
-        if weights_out is None:
-            weights_out = weights_in
+        weights_out = self.weights if weights_out is None else weights_out
         assert _current_device() == self._device
         _check_accounts(self._shape, self._device, weights_in, weights_out)
         for given, mine in ((page_table_out, self.page_table), (seq_lens_out, self.seq_lens)):

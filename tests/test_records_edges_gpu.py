@@ -131,3 +131,28 @@ def test_records_of_values_that_are_denormal_in_the_cache(gpu_lib, dtype, D):
         assert not wrong.any(), (int(wrong.sum()), got.cpu().double()[wrong][:4].tolist(), x[wrong][:4].tolist())
     wrong = (cache.records.cpu().view(-1) != R.tiles_of(k.flatten(0, 1), v.flatten(0, 1)).view(-1)).nonzero().flatten().tolist()
     assert wrong == []
+
+
+def test_evict_reads_given_accounts_and_writes_its_own(gpu_lib):
+    """Accounts given as the input alone are read and stay as they are, as in ``DecodeSession.weighted_paged_decode``; given as the output alone they
+    take what becomes of the own ones."""
+    S, Hkv, budget, lens = 8, 2, 6, [77, 30, 160]
+    g = torch.Generator().manual_seed(3)
+    table, pool = tables(lens, S, g)
+    own, given = (torch.rand((3, Hkv, table.shape[1]), generator=g) for _ in range(2))
+    for which in ("in", "out", "both"):
+        geo = geometry(Hkv, Hkv, 64, S, torch.bfloat16, pool, table, lens)
+        acc = PageAccounts(budget_pages=budget, weights=own.to(DEV), **geo)
+        w, other = given.to(DEV), torch.full_like(own, 9.0).to(DEV)
+        if which == "in":
+            acc.evict_pages(weights_in=w)
+            source, result, untouched = given, acc.weights, (w, given)
+        elif which == "out":
+            acc.evict_pages(weights_out=w)
+            source, result, untouched = own, w, (acc.weights, own)
+        else:
+            acc.evict_pages(weights_in=w, weights_out=other)
+            source, result, untouched = given, other, (acc.weights, own)
+        torch.cuda.synchronize()
+        assert torch.equal(untouched[0].cpu(), untouched[1]), which
+        check_evict(acc, table, torch.tensor(lens), source, S, (budget, 0, 1), geo["page_table"].cpu(), geo["seq_lens"].cpu(), result.cpu())
