@@ -199,8 +199,8 @@ class Library:
     def quantised_paged_decode(self, desc: CacheDesc, records, q, sel_pages, sel_count, sm_scale: float, out, lse_out,
                                workspace):
         if sel_pages is None:
-            rc = self.c.unique_quantised_paged_decode(desc, records.data_ptr(), q.data_ptr(), None, None, 0, sm_scale, out.data_ptr(),
-                                                      _p(lse_out), workspace.data_ptr(), workspace.nbytes, _stream())
+            rc = self.c.unique_quantised_paged_decode(desc, records.data_ptr(), q.data_ptr(), None, _p(sel_count), 0, sm_scale,
+                                                      out.data_ptr(), _p(lse_out), workspace.data_ptr(), workspace.nbytes, _stream())
         else:
             rc = self.c.unique_quantised_paged_decode(desc, records.data_ptr(), q.data_ptr(), sel_pages.data_ptr(), _p(sel_count),
                                                       sel_pages.shape[-1], sm_scale, out.data_ptr(), _p(lse_out),

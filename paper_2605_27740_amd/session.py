@@ -181,6 +181,8 @@ class QuantisedCache:
             assert sel_pages.get_device() == sel_count.get_device() == self._device
             assert sel_pages.dtype is sel_count.dtype is torch.int32 and sel_pages.is_contiguous() and sel_count.is_contiguous()
             assert sel_pages.dim() == 3 and sel_pages.shape[:2] == sel_count.shape == (self._out_shape[0], self._tile[0])
+        else:
+            assert sel_count is None, "counts without lists"
         self.lib.quantised_paged_decode(self.desc, self.records, q, sel_pages, sel_count, sm_scale, self.out, self.lse, self.workspace)
         return self.out, self.lse
 

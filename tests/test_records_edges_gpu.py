@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from paper_2605_27740_amd import binding
 from paper_2605_27740_amd.session import PageAccounts, QuantisedCache
 from tests import records_ref as R
 from tests.test_records_gpu import DEV, DTYPES, check_evict, geometry, say, tables
@@ -156,3 +157,18 @@ def test_evict_reads_given_accounts_and_writes_its_own(gpu_lib):
         torch.cuda.synchronize()
         assert torch.equal(untouched[0].cpu(), untouched[1]), which
         check_evict(acc, table, torch.tensor(lens), source, S, (budget, 0, 1), geo["page_table"].cpu(), geo["seq_lens"].cpu(), result.cpu())
+
+
+def test_counts_without_lists_are_refused(gpu_lib):
+    """In the handle and in the binding; lists without counts, too."""
+    D, S, Hkv, H, lens = 64, 8, 2, 8, [20, 9]
+    table, pool = tables(lens, S, torch.Generator().manual_seed(0))
+    cache = QuantisedCache(top_k=4, **geometry(H, Hkv, D, S, torch.float32, pool, table, lens))
+    q, count = torch.zeros((2, H, D), device=DEV), torch.ones((2, Hkv), dtype=torch.int32, device=DEV)
+    sel = torch.zeros((2, Hkv, 4), dtype=torch.int32, device=DEV)
+    with pytest.raises(AssertionError, match="counts"):
+        cache.paged_decode(q, None, count)
+    for pages, n in ((None, count), (sel, None)):
+        with pytest.raises(binding.UniqueError) as e:
+            gpu_lib.quantised_paged_decode(cache.desc, cache.records, q, pages, n, 0.0, cache.out, cache.lse, cache.workspace)
+        assert e.value.code == binding.ERR_INVALID_ARG
