@@ -157,19 +157,25 @@ class QuantisedCache:
             d.page_table = table.data_ptr()
         return d
 
-    def quantise_pages(self, k_cache, v_cache, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int = 0):
-        """Tokens of full-precision pages, found by ``page_table`` (default: the pool's own), into records."""
+    def quantise_pages(self, k_cache, v_cache, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int | None = None):
+        """Tokens of full-precision pages, found by ``page_table`` (default: the pool's own), into records: all, or those of a range of
+        each sequence. ``max_pages_touched_per_seq`` bounds the pages that a range overlaps (those beyond it are left as they are) and so the
+        launch; without it a launch is as large as for all tokens."""
         if tok_begin is not None:
             assert tok_begin.get_device() == tok_end.get_device() == self._device and tok_begin.dtype is tok_end.dtype is torch.int32
             assert tok_begin.is_contiguous() and tok_end.is_contiguous() and tok_begin.numel() == tok_end.numel() == self._table_shape[0]
+        if max_pages_touched_per_seq is None:
+            max_pages_touched_per_seq = self._table_shape[1]
         self.lib.quantise_pages(self._full_desc(k_cache, v_cache, page_table), self.records, self.page_table, tok_begin, tok_end,
                                 max_pages_touched_per_seq)
 
-    def restore_pages(self, k_out, v_out, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int = 0):
+    def restore_pages(self, k_out, v_out, page_table=None, tok_begin=None, tok_end=None, max_pages_touched_per_seq: int | None = None):
         """The values of the records' tokens into full-precision pages."""
         if tok_begin is not None:
             assert tok_begin.get_device() == tok_end.get_device() == self._device and tok_begin.dtype is tok_end.dtype is torch.int32
             assert tok_begin.is_contiguous() and tok_end.is_contiguous() and tok_begin.numel() == tok_end.numel() == self._table_shape[0]
+        if max_pages_touched_per_seq is None:
+            max_pages_touched_per_seq = self._table_shape[1]
         self.lib.restore_pages(self._full_desc(k_out, v_out, page_table), self.records, k_out, v_out, self.page_table, tok_begin,
                                tok_end, max_pages_touched_per_seq)
 

@@ -172,3 +172,25 @@ def test_counts_without_lists_are_refused(gpu_lib):
         with pytest.raises(binding.UniqueError) as e:
             gpu_lib.quantised_paged_decode(cache.desc, cache.records, q, pages, n, 0.0, cache.out, cache.lse, cache.workspace)
         assert e.value.code == binding.ERR_INVALID_ARG
+
+
+def test_ranges_without_a_bound_on_their_pages(gpu_lib):
+    """All pages of a range are written and read back; with a bound, those that it covers."""
+    D, S, Hkv, lens = 64, 8, 2, [100, 3, 61]
+    g = torch.Generator().manual_seed(8)
+    table, pool = tables(lens, S, g)
+    k, v = (torch.randn((pool, Hkv, S, D), generator=g).to(DEV) for _ in range(2))
+    begin, end = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([5, 0, 60], [99, 3, 61]))
+    want = [R.values(*R.encode(x.cpu())) for x in (k, v)]
+    for bound, pages in ((None, [13, 1, 8]), (2, [2, 1, 8]), (0, [0, 0, 0])):
+        cache = QuantisedCache(**geometry(Hkv, Hkv, D, S, torch.float32, pool, table, lens))
+        cache.quantise_pages(k, v, tok_begin=begin, tok_end=end, **({} if bound is None else dict(max_pages_touched_per_seq=bound)))
+        got = [torch.full_like(k, -77.0) for _ in range(2)]
+        cache.restore_pages(*got, tok_begin=begin, tok_end=end, **({} if bound is None else dict(max_pages_touched_per_seq=bound)))
+        torch.cuda.synchronize()
+        mine = torch.zeros((pool, 1, S, 1), dtype=torch.bool)
+        for b in range(3):
+            for t in range(int(begin[b]), int(end[b])):
+                mine[int(table[b, t // S]), 0, t % S] = t // S < pages[b]
+        for x, y in zip(got, want):
+            assert torch.equal(x.cpu().double(), torch.where(mine, y, torch.full((), -77.0, dtype=torch.float64))), bound
