@@ -30,8 +30,10 @@ class DecodeSession:
         self.page_pad = self.page_stats[:, mean_bytes + 4 * wl.Hkv:]
         if max_seq_len_hint is None:
             max_seq_len_hint = int(wl.seq_lens.max().item()) + int(wl.meta.get("spare_tokens", 0))
-        if min_seq_len_hint is None:  # sequences only grow while a session lives, so today's shortest is a lower bound
-            min_seq_len_hint = min(int(wl.seq_lens.min().item()), max_seq_len_hint)
+        if min_seq_len_hint is None:
+            # Today's shortest is a lower bound as long as sequences only grow. Where pages have accounts they may be evicted: no bound is known
+            # then (a caller whose budget gives one can say so).
+            min_seq_len_hint = 0 if track_weights else min(int(wl.seq_lens.min().item()), max_seq_len_hint)
         self.desc = binding.make_desc(q_heads=wl.H, k_cache=wl.k_cache, v_cache=wl.v_cache,
                                       page_stats=self.page_stats, stats_dtype=stats_dtype,
                                       page_table=wl.page_table, seq_lens=wl.seq_lens,

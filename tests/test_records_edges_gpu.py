@@ -5,9 +5,9 @@ import pytest
 import torch
 
 from paper_2605_27740_amd import binding
-from paper_2605_27740_amd.session import PageAccounts, QuantisedCache
+from paper_2605_27740_amd.session import DecodeSession, PageAccounts, QuantisedCache
 from tests import records_ref as R
-from tests.test_records_gpu import DEV, DTYPES, check_evict, geometry, say, tables
+from tests.test_records_gpu import DEV, DTYPES, check_evict, geometry, paged, say, tables
 
 pytestmark = pytest.mark.gpu
 
@@ -194,3 +194,11 @@ def test_ranges_without_a_bound_on_their_pages(gpu_lib):
                 mine[int(table[b, t // S]), 0, t % S] = t // S < pages[b]
         for x, y in zip(got, want):
             assert torch.equal(x.cpu().double(), torch.where(mine, y, torch.full((), -77.0, dtype=torch.float64))), bound
+
+
+def test_a_session_with_accounts_claims_no_lower_bound_on_its_lengths(gpu_lib):
+    """The descriptor's hint has to hold for every later call, also behind an eviction; one that is given is kept."""
+    wl = paged([700, 900], 8, 2, 64, 8, torch.bfloat16, 2).to(DEV)
+    assert DecodeSession(wl, track_weights=True).desc.min_seq_len_hint == 0
+    assert DecodeSession(wl, track_weights=True, min_seq_len_hint=40).desc.min_seq_len_hint == 40
+    assert DecodeSession(wl).desc.min_seq_len_hint == 700
