@@ -408,7 +408,7 @@ static WeighCut weigh_cut(const CacheView& c) {
   } else if (rows > kDenseSlots / 2 && rows <= 2 * kDenseSlots && c.B <= kDenseMaxBatch && (int64_t)rows * c.max_pages_hint <= INT32_MAX &&
              (int64_t)c.max_pages_hint * page_bytes >= (rows <= 384 ? 512 << 10 : 1024 << 10)) {
     cut.round.slots = (2 * rows + kDenseSlots - 1) / kDenseSlots * kDenseSlots;
-    cut.max_chunks = (int)std::max<int64_t>((int64_t)rows * c.max_pages_hint / (cut.round.slots * cut.round.pages), 1) * cut.round.slots;
+    cut.max_chunks = (int)dense_wanted_chunks(rows, c.max_pages_hint, cut.round);
   }
   return cut;
 }

@@ -16,11 +16,14 @@ struct DenseRound {  // workgroups at a time, and the pages of a chunk from whic
 constexpr int64_t kDenseLeastBytes = 96ll << 20;
 constexpr int kDenseMaxBatch = 64;  // a lane per sequence
 
-// Chunks of the whole batch, at most as many as the partial results of most_splits hold.
-inline int dense_max_chunks(int rows, int max_pages, DenseRound round = {}) {
+// Chunks of the whole batch: of all rows as long as the longest may be, in whole rounds.
+inline int64_t dense_wanted_chunks(int rows, int max_pages, DenseRound round = {}) {
+  return std::max<int64_t>((int64_t)rows * max_pages / (round.slots * round.pages), 1) * round.slots;
+}
+// At most as many as the partial results of most_splits hold.
+inline int dense_max_chunks(int rows, int max_pages) {
   const int64_t all = (int64_t)rows * most_splits(rows, max_pages).num_splits;
-  const int64_t wanted = std::max<int64_t>((int64_t)rows * max_pages / (round.slots * round.pages), 1) * round.slots;
-  return (int)std::min(all, wanted);
+  return (int)std::min(all, dense_wanted_chunks(rows, max_pages));
 }
 
 // Finding the cut costs 0.5 us or more in both kernels, which launches that cannot read 96 MB do not get back (2 sequences of up to 4000
@@ -28,10 +31,10 @@ inline int dense_max_chunks(int rows, int max_pages, DenseRound round = {}) {
 // 8 KV heads, G = 4, D = 128, pages of 16): 4 sequences of 6K to 30K tokens 66.4 / 43.2; 8 of 2K to 60K, 1012 MB 205 / 163; 16 of 1K
 // to 16K 128 / 70; even ones 8 x 16384 86.6 / 86.5, 16 x 30000 312 / 299, 5 x 7000 31.3 / 30.1. More rows than half the slots, and a
 // single sequence, have nothing to gain.
-inline bool dense_balances(int batch, int kv_heads, int max_pages, int page_bytes, int64_t least_bytes = kDenseLeastBytes) {
+inline bool dense_balances(int batch, int kv_heads, int max_pages, int page_bytes) {
   const int64_t rows = (int64_t)batch * kv_heads;
   if (batch < 2 || batch > kDenseMaxBatch || rows > kDenseSlots / 2 || rows * max_pages > INT32_MAX) return false;
-  return most_splits((int)rows, max_pages).num_splits > 1 && rows * max_pages * page_bytes >= least_bytes;
+  return most_splits((int)rows, max_pages).num_splits > 1 && rows * max_pages * page_bytes >= kDenseLeastBytes;
 }
 
 // One wave merges a head's chunks where the slots are four or fewer to a row, on average: every wave finds the cut for itself, which costs more

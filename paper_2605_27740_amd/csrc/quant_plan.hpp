@@ -43,10 +43,7 @@ struct QuantBatch {
     const int slots = three_fit && (rows() > 256 || rows() * row_bytes() >= kQuantThreeBytes) ? 768 : 512;
     return {(2 * rows() + slots - 1) / slots * slots, 768};
   }
-  int max_chunks() const {
-    const DenseRound r = round();
-    return (int)std::max<int64_t>((int64_t)rows() * max_pages / ((int64_t)r.slots * r.pages), 1) * r.slots;
-  }
+  int max_chunks() const { return (int)dense_wanted_chunks(rows(), max_pages, round()); }
   bool balances() const {
     if (batch < 2 || batch > kDenseMaxBatch || rows() > kQuantMostRows || (int64_t)rows() * max_pages > INT32_MAX) return false;
     return rows() * row_bytes() >= kQuantLeastBytes && (rows() <= 256 || row_bytes() >= kQuantLeastRow);
