@@ -227,8 +227,10 @@ int unique_dense_paged_decode(const unique_cache_desc* desc, const void* d_q, fl
  *              D/32 * S bytes  K scales [D/32][S]
  *              D/32 * S bytes  V scales [D/32][S]
  *            unique_page_record_bytes in all; a pool of them is [num_records][record], 16-byte aligned.
- * The pool has a page table of its own (d_record_table, shaped like the descriptor's), so that full-precision pages need exist only where
- * tokens are being written: entries outside a pool (-1) are skipped. One table for both is allowed. */
+ * The pool has a page table of its own (d_record_table, shaped like the descriptor's), so that for attention over every page full-precision
+ * pages need exist only where tokens are being written: entries outside a pool (-1) are skipped. One table for both is allowed, and
+ * needed by what reads more than records: page statistics are made from full-precision keys and kept at their PHYSICAL page, so a selection of records by
+ * unique_score_select_topk takes keys and records at the same ids, and unique_weighted_paged_decode reads full-precision pages, all of them. */
 
 /* Bytes of a page's record for this descriptor's num_kv_heads, head_dim and page_size; 0 if desc is NULL or they are not supported. */
 int64_t unique_page_record_bytes(const unique_cache_desc* desc);
@@ -269,6 +271,7 @@ int unique_account_workspace_bytes(const unique_cache_desc* desc, size_t* out_by
  * float, row (b, h_kv) at (b*H_kv + h_kv)*weight_stride, weight_stride >= max_pages_per_seq (or the page bound implied by
  * max_seq_len_hint). Entries at and beyond the pages of a sequence are left as they are (0 is what they should hold
  * when the sequence grows into them).
+ * An account that has become infinite or NaN stays so, also with a decay of 0: start again from NULL.
  *   decay        : in [0, 1]; 1 = the plain sum of the steps.
  *   d_weights_in : NULL = nothing so far (and decay does not count); may be d_weights_out. */
 int unique_weighted_paged_decode(const unique_cache_desc* desc, const void* d_q, float sm_scale, float decay, const float* d_weights_in,
@@ -280,7 +283,8 @@ int unique_weighted_paged_decode(const unique_cache_desc* desc, const void* d_q,
  * KV heads in 64 bits and ranked as one float; ties keep the earlier page, a NaN ranks lowest. Its row of the page table
  * and its rows of accounts close up in the old order, vacated entries become -1 and 0, and seq_lens loses page_size tokens for each
  * page evicted. (Keys keep the positions that they were given before they were cached.) The other sequences stay as they are.
- * Statistics and 4-bit records go by physical page and need nothing.
+ * Statistics and 4-bit records go by physical page and need nothing, if records are found by the same table. A table of their own has to close up as
+ * well: by a call for that table on the same accounts and lengths, with other arrays for both outputs, before the call that changes them in place.
  *   d_weights_out, d_page_table_out, d_seq_lens_out : d_weights_in, desc->page_table and desc->seq_lens again (in place), or arrays like them
  *                   that do not overlap them; entries at and beyond the pages that the sequence had are left as they are.
  *   d_freed_pages : out, int32 [batch][freed_stride], the PHYSICAL ids of the evicted pages in their order in the sequence, -1 behind them;

@@ -63,9 +63,13 @@ __global__ __launch_bounds__(kAccountThreads) void rank_kernel(CacheView c, cons
 }
 
 constexpr int kEvictMost = 16384;       // pages of the longest sequence that a workgroup holds
-constexpr int64_t kSumsHere = 24576;    // accounts of a sequence up to which its workgroup sums them up and closes their rows
+// Accounts of a sequence up to which its workgroup sums them up and closes their rows, one launch instead of three; above it they are summed up and closed by
+// more workgroups. us of the call so / apart, heads x pages of each of 2 sequences, one page too many: 8 x 1000 9.4 / 16.2, 8 x 2900 8.8 / 14.7, 32 x 700
+// 10.8 / 15.0, 2 x 8188 8.9 / 15.1; half of the pages evicted: 8 x 2900 12.2 / 15.1, 2 x 8188 14.7 / 18.7, but 8 x 5000 20.6 / 17.0, 8 x 8188 23.5 / 18.6 (32
+// sequences 24.7 / 21.9). Rows between would gain by a bound of their own: 8 x 3400, one page too many, 9.6 / 14.6, 4 x 7000 9.5 / 14.9.
+constexpr int64_t kSumsHere = 24576;
 constexpr int kFew = 4;                 // pages that are sought one by one
-constexpr int kGathered = 256;            // keys that one wave searches
+constexpr int kGathered = 256;          // keys that one wave searches (16 x 8 x 8188 pages to 1024, us with 64, 128, 256, 512, 1024: 19.7, 19.3, 19.2, 19.3, 20.4)
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / kWave;
 
 // How many lanes for which pred(j) holds come before each of a wave's kPer rows of 64 lanes, in the order j, wave, lane of the workgroup;

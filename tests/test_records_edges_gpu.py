@@ -202,3 +202,37 @@ def test_a_session_with_accounts_claims_no_lower_bound_on_its_lengths(gpu_lib):
     assert DecodeSession(wl, track_weights=True).desc.min_seq_len_hint == 0
     assert DecodeSession(wl, track_weights=True, min_seq_len_hint=40).desc.min_seq_len_hint == 40
     assert DecodeSession(wl).desc.min_seq_len_hint == 700
+
+
+def test_evict_from_two_tables(gpu_lib):
+    """A pool of records and full-precision pages with a table each: both close up by the same accounts and lengths, which the second call changes."""
+    S, Hkv, budget, lens = 8, 2, 6, [77, 30, 1600]
+    g = torch.Generator().manual_seed(3)
+    (table, pool), (records, _) = (tables(lens, S, g) for _ in range(2))
+    w = torch.rand((3, Hkv, table.shape[1]), generator=g)
+    geo = geometry(Hkv, Hkv, 64, S, torch.bfloat16, pool, table, lens)
+    policy = dict(budget_pages=budget, sink_pages=1, recent_pages=2, weights=w.to(DEV))
+    acc = PageAccounts(**policy, **geo)
+    other = PageAccounts(**policy, **dict(geo, page_table=records.to(DEV)))
+    w_out, l_out = torch.zeros_like(acc.weights), torch.zeros_like(geo["seq_lens"])
+    other.evict_pages(weights_out=w_out, seq_lens_out=l_out)
+    acc.evict_pages()
+    torch.cuda.synchronize()
+    args = torch.tensor(lens), w, S, (budget, 1, 2)
+    check_evict(other, records, *args, other.page_table.cpu(), l_out.cpu(), w_out.cpu())
+    check_evict(acc, table, *args, geo["page_table"].cpu(), geo["seq_lens"].cpu(), acc.weights.cpu())
+
+
+def test_accounts_that_became_infinite_or_nan_stay_so(gpu_lib):
+    """With any decay, for their page alone; from nothing they are finite again."""
+    wl = paged([70, 33], 16, 4, 64, 8, torch.bfloat16, 9).to(DEV)
+    sess = DecodeSession(wl, top_k=2, track_weights=True)
+    for decay in (0.0, 0.5, 1.0):
+        w, out = torch.rand_like(sess.page_weights), torch.zeros_like(sess.page_weights)
+        w[0, 1, 2], w[1, 0, 1] = float("nan"), float("inf")
+        sess.weighted_paged_decode(decay=decay, weights_in=w, weights_out=out)
+        lost = torch.zeros_like(w, dtype=torch.bool)
+        lost[0, 1, 2] = lost[1, 0, 1] = True
+        assert torch.equal(~torch.isfinite(out), lost), decay
+        sess.weighted_paged_decode(decay=decay, weights_out=out)
+        assert torch.isfinite(out).all()
