@@ -106,8 +106,8 @@ __device__ __forceinline__ int lanes_below(unsigned long long mask, int acc) {
 
 // Chooses the pages of a sequence that stay and closes its row of the table, a workgroup a sequence with kPer keys a thread. The key
 // that separates them is sought between the least and the largest, a fourth of the window at a time from the number of keys above three
-// candidates, with comparisons and ballots only, as histograms would be of a few exponents; done as soon as a candidate has exactly as many
-// above it as stay, or few keys are left, which one wave finishes. A round of eight keys a thread takes 1 us (16 waves issue 110 instructions each). kSums: the pages'
+// candidates, with comparisons and ballots only (a histogram of exponents would be a few bins; one of equal bins of the window has not been
+// tried); done as soon as a candidate has exactly as many above it as stay, or few keys are left, which one wave finishes. A round of eight keys a thread takes 1 us (16 waves issue 110 instructions each). kSums: the pages'
 // sums are formed here and the rows of accounts closed, too; else they are in `rank`, and `kept` is for close_kernel.
 template <int kPer, bool kSums>
 __global__ __launch_bounds__(kEvictThreads) void evict_kernel(CacheView c, EvictArgs a, const float* __restrict__ rank, int rank_stride,
