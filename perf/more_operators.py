@@ -309,7 +309,7 @@ def prepare(case, seed):
             size, prefix, _ = _groups(case)
             s["prefixes"] = PrefixGroups(q_heads=H, k_cache=s["k"], v_cache=s["v"], page_table=s["table"], seq_lens=s["seq_lens"],
                                          group_starts=s["starts"], members=s["members"], prefix_pages=s["prefix_pages"], max_members=max(size),
-                                         max_prefix_pages=max(prefix) // S, max_seq_len=int(s["seq_lens"].max()))
+                                         max_prefix_pages=max(prefix) // S, max_own_tokens=case["alone"])
     return s
 
 
