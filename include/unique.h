@@ -296,6 +296,93 @@ int unique_evict_pages(const unique_cache_desc* desc, int32_t budget_pages, int3
                        int32_t* d_seq_lens_out, int32_t* d_freed_pages, int32_t* d_freed_count, int32_t freed_stride, void* d_workspace,
                        size_t workspace_bytes, void* stream);
 
+/* ---- The steps around the cache: places for new tokens, what is written there, contexts that begin alike ---- */
+
+/* Where the new tokens of a step go. Arrays whose names end in _out may be their inputs again (in place), or arrays that do not overlap them.
+ * Free pages are a stack of ids: what comes back is put on its end, what is given out is taken from its end. */
+typedef struct unique_placement {
+  const int32_t* new_tokens;         /* [batch]: tokens that the sequence gets, 0 = none; negative = it has ended and its pages go back */
+  const int32_t* shared_pages;       /* [batch], NULL = 0: so many pages at the beginning of its row are not its own and do not go back */
+  const int32_t* next_positions;     /* [batch], NULL = seq_lens: the position of its next token (evictions shorten a sequence, not its positions) */
+  const int32_t* freed_pages;        /* [batch][freed_stride] and freed_count [batch], both NULL = none: pages that go back, */
+  const int32_t* freed_count;        /*   as unique_evict_pages leaves them */
+  int32_t* free_pages;               /* [free_capacity]: the stack; entries at and beyond the count are unspecified */
+  const int32_t* free_count;         /* one number */
+  int32_t* free_count_out;
+  int32_t* page_table_out;           /* desc->page_table or an array like it that holds its entries; only those that change are written */
+  int32_t* seq_lens_out;             /* [batch] */
+  int32_t* next_positions_out;       /* [batch], NULL exactly where next_positions is */
+  int32_t* placed;                   /* [batch]: tokens that have a place: all of the new ones, or 0 */
+  int32_t* token_starts;             /* [batch + 1]: the rows of a sequence's new tokens are [starts[b], starts[b + 1]) */
+  int32_t* positions;                /* [max_new_tokens]: of each row, -1 = no place, also behind the last sequence's rows */
+  int64_t* slots;                    /* [max_new_tokens]: physical page * page_size + place in the page, or -1 */
+  int32_t freed_stride;
+  int32_t free_capacity;             /* entries of free_pages; what does not fit is lost (num_phys_pages always fit) */
+  int32_t max_new_tokens;            /* rows that there are, at most 2^30 */
+  int32_t reserved0;                 /* 0 */
+} unique_placement;
+
+/* Bytes of device workspace that unique_place_tokens may need for this descriptor and so many rows (256-byte aligned, nothing carried between calls). */
+int unique_place_workspace_bytes(const unique_cache_desc* desc, int32_t max_new_tokens, size_t* out_bytes);
+
+/* Gives the new tokens of every sequence their places, in three steps, each in the order of the batch: pages of freed_pages go back; sequences that
+ * have ended give their pages back, their lengths and positions become 0 and their pages' entries of the table -1; the other
+ * sequences get the pages that their new lengths need, one by one from the end of the stack. A sequence whose new tokens do not fit its row of the table
+ * (max_pages_per_seq) or the max_new_tokens rows gets no place. Of the others, from the first whose pages are not there any more on, none
+ * gets pages; those that need none are not held up. A sequence without a place stays as it is, and its rows get -1.
+ * Page ids are not checked; a sequence that has ended must not be longer than its row. batch * max_pages_per_seq and batch * freed_stride must be below 2^31.
+ * desc's k_cache and v_cache are not used and may be NULL; its max_seq_len_hint does not count. */
+int unique_place_tokens(const unique_cache_desc* desc, const unique_placement* place, void* d_workspace, size_t workspace_bytes, void* stream);
+
+/* What is done with the queries and keys of new tokens before they are used: each head normalised by its root mean square, then turned by
+ * its position. */
+typedef struct unique_head_transform {
+  const void* q_weight;         /* device, [head_dim] dtype, 16-byte aligned, both or none: x / sqrt(mean(x^2) + eps) * weight for each head. NULL = no norm */
+  const void* k_weight;
+  const double* frequencies;    /* device, [rotary_dim / 2]: angle per position of each pair, in radians. NULL if rotary_dim is 0 */
+  float eps;                    /* >= 0 */
+  float magnitude;              /* sine and cosine are multiplied by it (1 = a rotation) */
+  int32_t rotary_dim;           /* the first so many channels of a head are turned: a multiple of 16, at most head_dim; 0 = none */
+  int32_t interleaved;          /* pair i is channels (i, i + rotary_dim / 2); non-zero: channels (2 i, 2 i + 1) */
+} unique_head_transform;
+
+/* Queries, keys and values of new tokens: keys and values go to their slots of desc's k_cache and v_cache (which this call writes), queries to d_q_out.
+ * Norm, angles and rotation are computed in 32 bits or more and rounded once, to desc's dtype.
+ *   d_q, d_k, d_v : row r of num_rows at r * {q,k,v}_stride elements: num_q_heads * head_dim, num_kv_heads * head_dim, num_kv_heads * head_dim
+ *                   elements of desc's dtype (parts of the rows of one projection, for instance). 16-byte aligned, strides multiples of 16 bytes.
+ *   d_positions, d_slots : [num_rows], as unique_place_tokens gives them. A row whose slot is negative or outside the pool is left out: nothing of
+ *                   it is written, its row of d_q_out neither. Rows must have different slots: of two with one slot either may stay, or a mixture of both.
+ *   transform     : NULL = neither norm nor rotation.
+ *   d_q_out       : [num_rows][num_q_heads][head_dim]; may be d_q itself if q_stride is num_q_heads * head_dim, and must not overlap it otherwise.
+ * num_rows 0 is allowed. desc's page_table and seq_lens are not used and may be NULL. Statistics and records of the touched pages are the
+ * business of unique_update_page_stats and unique_quantise_pages. */
+int unique_append_tokens(const unique_cache_desc* desc, int32_t num_rows, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                         const void* d_v, int64_t v_stride, const int32_t* d_positions, const int64_t* d_slots,
+                         const unique_head_transform* transform, void* d_q_out, void* stream);
+
+/* Sequences whose contexts begin with the same pages, in groups. The host's bounds must be true: what lies beyond them is ignored by every kernel. */
+typedef struct unique_prefix_groups {
+  const int32_t* starts;        /* device, [num_groups + 1], ascending from 0: members [starts[g], starts[g + 1]) belong to group g */
+  const int32_t* members;       /* device, [batch]: the sequence of each member; NULL = member i is sequence i */
+  const int32_t* prefix_pages;  /* device, [num_groups]: so many entries at the beginning of all its members' rows of the page table are the same */
+  int32_t num_groups;           /* 1 to batch */
+  int32_t max_members;          /* host upper bound on members of a group */
+  int32_t max_prefix_pages;     /* host upper bound on prefix_pages[] */
+  int32_t max_own_pages;        /* host upper bound on the pages of any member behind its group's prefix; 0 = unknown */
+} unique_prefix_groups;
+
+/* Bytes of device workspace that the call below may need (256-byte aligned, nothing carried between calls, one for each stream that may
+ * overlap another). groups' device pointers are not used. */
+int unique_shared_prefix_workspace_bytes(const unique_cache_desc* desc, const unique_prefix_groups* groups, size_t* out_bytes);
+
+/* unique_dense_paged_decode for sequences that share the beginnings of their contexts: the pages of a group's prefix are read once for all of its
+ * members (from the first member's row of the page table), each member's other pages as always. A member may be shorter than the prefix.
+ * Sequences that no group lists are left out, their rows of d_out and d_lse_out left as they are; one that is listed twice is attended twice. At most
+ * `batch` members in all. Against unique_dense_paged_decode the sums are in another order, and for bf16 caches the probabilities of the prefix's
+ * tokens are rounded to bf16 before they multiply the values (2^-8 of a term at most; the sum that they are divided by is not rounded). */
+int unique_shared_prefix_decode(const unique_cache_desc* desc, const unique_prefix_groups* groups, const void* d_q, float sm_scale, void* d_out,
+                                float* d_lse_out, void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* Static strings; never NULL. */
 const char* unique_status_string(int status);
 const char* unique_last_error(void); /* thread-local detail of the last non-OK return on this thread */

@@ -20,7 +20,9 @@ DTYPE_CODE = {torch.float32: 0, torch.bfloat16: 1}
 EXPORTS = ("unique_workspace_bytes", "unique_page_stats_record_bytes", "unique_update_page_stats", "unique_score_select_topk",
            "unique_page_scores", "unique_select_topk", "unique_decode_step", "unique_decode_step_static", "unique_sparse_paged_decode", "unique_dense_paged_decode",
            "unique_page_record_bytes", "unique_quantise_pages", "unique_restore_pages", "unique_quantised_workspace_bytes", "unique_quantised_paged_decode",
-           "unique_account_workspace_bytes", "unique_weighted_paged_decode", "unique_evict_pages", "unique_status_string",
+           "unique_account_workspace_bytes", "unique_weighted_paged_decode", "unique_evict_pages",
+           "unique_place_workspace_bytes", "unique_place_tokens", "unique_append_tokens", "unique_shared_prefix_workspace_bytes",
+           "unique_shared_prefix_decode", "unique_status_string",
            "unique_last_error", "unique_version")
 
 
@@ -34,6 +36,26 @@ class CacheDesc(C.Structure):
                 ("stats_dtype", C.c_int32), ("force_recent_pages", C.c_int32),
                 ("kv_page_stride", C.c_int64), ("kv_head_stride", C.c_int64),
                 ("min_seq_len_hint", C.c_int32), ("reserved0", C.c_int32)]
+
+
+class Placement(C.Structure):
+    """Mirror of ``unique_placement``."""
+    _fields_ = [(name, C.c_void_p) for name in ("new_tokens", "shared_pages", "next_positions", "freed_pages", "freed_count", "free_pages",
+                                                "free_count", "free_count_out", "page_table_out", "seq_lens_out", "next_positions_out", "placed",
+                                                "token_starts", "positions", "slots")]
+    _fields_ += [(name, C.c_int32) for name in ("freed_stride", "free_capacity", "max_new_tokens", "reserved0")]
+
+
+class HeadTransform(C.Structure):
+    """Mirror of ``unique_head_transform``."""
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("frequencies", C.c_void_p), ("eps", C.c_float),
+                ("magnitude", C.c_float), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class PrefixGroupsDesc(C.Structure):
+    """Mirror of ``unique_prefix_groups``."""
+    _fields_ = [("starts", C.c_void_p), ("members", C.c_void_p), ("prefix_pages", C.c_void_p), ("num_groups", C.c_int32),
+                ("max_members", C.c_int32), ("max_prefix_pages", C.c_int32), ("max_own_pages", C.c_int32)]
 
 
 class UniqueError(RuntimeError):
@@ -101,6 +123,13 @@ class Library:
         self.c.unique_account_workspace_bytes.argtypes = [desc, C.POINTER(C.c_size_t)]
         self.c.unique_weighted_paged_decode.argtypes = [desc, ptr, C.c_float, C.c_float, ptr, ptr, i32, ptr, ptr, ptr, C.c_size_t, ptr]
         self.c.unique_evict_pages.argtypes = [desc, i32, i32, i32, ptr, ptr, i32, ptr, ptr, ptr, ptr, i32, ptr, C.c_size_t, ptr]
+
+        place, groups, i64 = C.POINTER(Placement), C.POINTER(PrefixGroupsDesc), C.c_int64
+        self.c.unique_place_workspace_bytes.argtypes = [desc, i32, C.POINTER(C.c_size_t)]
+        self.c.unique_place_tokens.argtypes = [desc, place, ptr, C.c_size_t, ptr]
+        self.c.unique_append_tokens.argtypes = [desc, i32, ptr, i64, ptr, i64, ptr, i64, ptr, ptr, C.POINTER(HeadTransform), ptr, ptr]
+        self.c.unique_shared_prefix_workspace_bytes.argtypes = [desc, groups, C.POINTER(C.c_size_t)]
+        self.c.unique_shared_prefix_decode.argtypes = [desc, groups, ptr, C.c_float, ptr, ptr, ptr, C.c_size_t, ptr]
 
     # -- helpers -----------------------------------------------------------------------------
     def check(self, rc: int) -> None:
@@ -222,6 +251,33 @@ class Library:
                                        weights_in.shape[-1], page_table_out.data_ptr(), seq_lens_out.data_ptr(),
                                        freed_pages.data_ptr(), freed_count.data_ptr(), freed_pages.shape[-1], workspace.data_ptr(),
                                        workspace.nbytes, _stream())
+        if rc:
+            self.check(rc)
+
+    def place_workspace_bytes(self, desc: CacheDesc, max_new_tokens: int) -> int:
+        n = C.c_size_t(0)
+        self.check(self.c.unique_place_workspace_bytes(C.byref(desc), max_new_tokens, C.byref(n)))
+        return int(n.value)
+
+    def place_tokens(self, desc: CacheDesc, place: Placement, workspace):
+        rc = self.c.unique_place_tokens(desc, place, workspace.data_ptr(), workspace.nbytes, _stream())
+        if rc:
+            self.check(rc)
+
+    def append_tokens(self, desc: CacheDesc, q, k, v, positions, slots, transform: HeadTransform | None, q_out):
+        rc = self.c.unique_append_tokens(desc, slots.shape[0], q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+                                         positions.data_ptr(), slots.data_ptr(), transform, q_out.data_ptr(), _stream())
+        if rc:
+            self.check(rc)
+
+    def shared_prefix_workspace_bytes(self, desc: CacheDesc, groups: PrefixGroupsDesc) -> int:
+        n = C.c_size_t(0)
+        self.check(self.c.unique_shared_prefix_workspace_bytes(C.byref(desc), C.byref(groups), C.byref(n)))
+        return int(n.value)
+
+    def shared_prefix_decode(self, desc: CacheDesc, groups: PrefixGroupsDesc, q, sm_scale: float, out, lse_out, workspace):
+        rc = self.c.unique_shared_prefix_decode(desc, groups, q.data_ptr(), sm_scale, out.data_ptr(), _p(lse_out), workspace.data_ptr(),
+                                                workspace.nbytes, _stream())
         if rc:
             self.check(rc)
 

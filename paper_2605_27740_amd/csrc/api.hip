@@ -11,6 +11,7 @@
 
 #include "kernels.hpp"
 #include "quant.hpp"
+#include "serving.hpp"
 #include "step_rule.hpp"
 #include "weigh.hpp"
 
@@ -275,6 +276,39 @@ int record_call(const unique::CacheView& v, const void* d_records, const int32_t
     return fail(UNIQUE_ERR_INVALID_ARG, "max_pages_touched_per_seq must be >= 0 (got %d)", max_pages_touched_per_seq);
   *pool = {reinterpret_cast<char*>(const_cast<void*>(d_records)), d_record_table ? d_record_table : v.page_table, num_records};
   *touched = std::min(max_pages_touched_per_seq, v.max_pages);
+  return UNIQUE_OK;
+}
+
+// The descriptor of a call that needs neither table nor lengths.
+int make_pool_view(const unique_cache_desc* desc, unique::CacheView* v) {
+  if (!desc) return fail(UNIQUE_ERR_INVALID_ARG, "desc is NULL");
+  static const int32_t dummy = 0;
+  unique_cache_desc d = *desc;
+  if (!d.page_table) d.page_table = &dummy;
+  if (!d.seq_lens) d.seq_lens = &dummy;
+  return make_view(&d, v, false, true);
+}
+
+constexpr int kMostRows = 1 << 24;  // rows that unique_place_tokens can number
+
+int check_rows(int32_t max_new_tokens) {
+  if (max_new_tokens < 0 || max_new_tokens > kMostRows)
+    return fail(UNIQUE_ERR_INVALID_ARG, "max_new_tokens must lie in [0, %d] (got %d)", kMostRows, max_new_tokens);
+  return UNIQUE_OK;
+}
+
+// The host's part of the groups; bounds that exceed those of the batch come back as these.
+int check_groups(const unique::CacheView& v, const unique_prefix_groups* groups, unique_prefix_groups* g) {
+  if (!groups) return fail(UNIQUE_ERR_INVALID_ARG, "groups is NULL");
+  *g = *groups;
+  if (g->num_groups < 1 || g->num_groups > v.B)
+    return fail(UNIQUE_ERR_INVALID_ARG, "num_groups must lie in [1, batch %d] (got %d)", v.B, g->num_groups);
+  if (g->max_members < 1) return fail(UNIQUE_ERR_INVALID_ARG, "max_members must be >= 1 (got %d)", g->max_members);
+  if (g->max_prefix_pages < 0 || g->max_own_pages < 0)
+    return fail(UNIQUE_ERR_INVALID_ARG, "max_prefix_pages and max_own_pages must be >= 0 (got %d, %d)", g->max_prefix_pages, g->max_own_pages);
+  g->max_members = std::min(g->max_members, v.B);
+  g->max_prefix_pages = std::min(g->max_prefix_pages, v.max_pages_hint);
+  g->max_own_pages = g->max_own_pages ? std::min(g->max_own_pages, v.max_pages_hint) : v.max_pages_hint;
   return UNIQUE_OK;
 }
 
@@ -580,6 +614,109 @@ int unique_evict_pages(const unique_cache_desc* desc, int32_t budget_pages, int3
                                d_seq_lens_out, d_freed_pages, d_freed_count, freed_stride, d_workspace};
   const hipError_t e = unique::launch_evict(v, a, (hipStream_t)stream);
   return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "evict launch");
+}
+
+int unique_place_workspace_bytes(const unique_cache_desc* desc, int32_t max_new_tokens, size_t* out_bytes) {
+  if (!out_bytes) return fail(UNIQUE_ERR_INVALID_ARG, "out_bytes is NULL");
+  unique::CacheView v;
+  int rc = make_size_view(desc, &v);
+  if (rc == UNIQUE_OK) rc = check_rows(max_new_tokens);
+  if (rc != UNIQUE_OK) return rc;
+  *out_bytes = round_up(std::max<size_t>(unique::place_bytes(v, max_new_tokens), 1), kAlign);
+  return UNIQUE_OK;
+}
+
+int unique_place_tokens(const unique_cache_desc* desc, const unique_placement* place, void* d_workspace, size_t workspace_bytes, void* stream) {
+  unique::CacheView v;
+  int rc = make_shape_view(desc, &v);
+  if (rc != UNIQUE_OK) return rc;
+  if (!place) return fail(UNIQUE_ERR_INVALID_ARG, "place is NULL");
+  const unique_placement& p = *place;
+  rc = check_rows(p.max_new_tokens);
+  if (rc != UNIQUE_OK) return rc;
+  if (!p.new_tokens || !p.free_pages || !p.free_count || !p.free_count_out || !p.page_table_out || !p.seq_lens_out || !p.placed || !p.token_starts)
+    return fail(UNIQUE_ERR_INVALID_ARG, "new_tokens, free_pages, free_count, free_count_out, page_table_out, seq_lens_out, placed and token_starts "
+                "must be non-NULL");
+  if (p.max_new_tokens > 0 && (!p.positions || !p.slots)) return fail(UNIQUE_ERR_INVALID_ARG, "positions and slots must be non-NULL");
+  if ((p.next_positions == nullptr) != (p.next_positions_out == nullptr))
+    return fail(UNIQUE_ERR_INVALID_ARG, "next_positions and next_positions_out must both be NULL or both be set");
+  if ((p.freed_pages == nullptr) != (p.freed_count == nullptr))
+    return fail(UNIQUE_ERR_INVALID_ARG, "freed_pages and freed_count must both be NULL or both be set");
+  if (p.freed_pages && p.freed_stride < 1) return fail(UNIQUE_ERR_INVALID_ARG, "freed_stride must be >= 1 (got %d)", p.freed_stride);
+  if (p.free_capacity < 1) return fail(UNIQUE_ERR_INVALID_ARG, "free_capacity must be >= 1 (got %d)", p.free_capacity);
+  if ((int64_t)v.B * v.max_pages > INT32_MAX || (p.freed_pages && (int64_t)v.B * p.freed_stride > INT32_MAX))
+    return fail(UNIQUE_ERR_UNSUPPORTED, "batch * max_pages_per_seq and batch * freed_stride must be below 2^31");
+  rc = check_workspace(d_workspace, workspace_bytes, unique::place_bytes(v, p.max_new_tokens));
+  if (rc != UNIQUE_OK) return rc;
+  const hipError_t e = unique::launch_place(v, p, d_workspace, (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "place launch");
+}
+
+int unique_append_tokens(const unique_cache_desc* desc, int32_t num_rows, const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride,
+                         const void* d_v, int64_t v_stride, const int32_t* d_positions, const int64_t* d_slots,
+                         const unique_head_transform* transform, void* d_q_out, void* stream) {
+  unique::CacheView v;
+  const int rc = make_pool_view(desc, &v);
+  if (rc != UNIQUE_OK) return rc;
+  if (num_rows < 0) return fail(UNIQUE_ERR_INVALID_ARG, "num_rows must be >= 0 (got %d)", num_rows);
+  unique_head_transform how = {};
+  if (transform) how = *transform;
+  if ((how.q_weight == nullptr) != (how.k_weight == nullptr))
+    return fail(UNIQUE_ERR_INVALID_ARG, "q_weight and k_weight must both be NULL or both be set");
+  if (((uintptr_t)how.q_weight | (uintptr_t)how.k_weight) & 15u) return fail(UNIQUE_ERR_INVALID_ARG, "q_weight and k_weight must be 16-byte aligned");
+  if (how.rotary_dim < 0 || how.rotary_dim > v.D || how.rotary_dim % 16 != 0)
+    return fail(UNIQUE_ERR_INVALID_ARG, "rotary_dim %d must be a multiple of 16 in [0, head_dim %d]", how.rotary_dim, v.D);
+  if (how.rotary_dim > 0 && !how.frequencies) return fail(UNIQUE_ERR_INVALID_ARG, "frequencies is NULL");
+  if ((uintptr_t)how.frequencies & 7u) return fail(UNIQUE_ERR_INVALID_ARG, "frequencies must be 8-byte aligned");
+  if (!(how.eps >= 0.f)) return fail(UNIQUE_ERR_INVALID_ARG, "eps must be >= 0");
+  if (!(how.magnitude == how.magnitude)) return fail(UNIQUE_ERR_INVALID_ARG, "magnitude is NaN");
+  if (num_rows == 0) return UNIQUE_OK;
+  if (!d_q || !d_k || !d_v || !d_positions || !d_slots || !d_q_out)
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_q, d_k, d_v, d_positions, d_slots and d_q_out must be non-NULL");
+  if (((uintptr_t)d_q | (uintptr_t)d_k | (uintptr_t)d_v | (uintptr_t)d_q_out) & 15u)
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_q, d_k, d_v and d_q_out must be 16-byte aligned");
+  const int64_t vec = v.dtype == UNIQUE_DTYPE_BF16 ? 8 : 4;
+  if (q_stride < (int64_t)v.H * v.D || k_stride < (int64_t)v.Hkv * v.D || v_stride < (int64_t)v.Hkv * v.D || q_stride % vec || k_stride % vec ||
+      v_stride % vec)
+    return fail(UNIQUE_ERR_INVALID_ARG, "q_stride %lld, k_stride %lld, v_stride %lld: at least a row's heads, in multiples of 16 bytes",
+                (long long)q_stride, (long long)k_stride, (long long)v_stride);
+  if (d_q == d_q_out && q_stride != (int64_t)v.H * v.D)
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_q_out may be d_q only if q_stride is num_q_heads * head_dim");
+  const unique::AppendArgs a = {d_q, d_k, d_v, q_stride, k_stride, v_stride, d_positions, d_slots, d_q_out, num_rows, how};
+  const hipError_t e = unique::launch_append(v, a, (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "append launch");
+}
+
+int unique_shared_prefix_workspace_bytes(const unique_cache_desc* desc, const unique_prefix_groups* groups, size_t* out_bytes) {
+  if (!out_bytes) return fail(UNIQUE_ERR_INVALID_ARG, "out_bytes is NULL");
+  unique::CacheView v;
+  int rc = make_size_view(desc, &v);
+  if (rc != UNIQUE_OK) return rc;
+  unique_prefix_groups g;
+  rc = check_groups(v, groups, &g);
+  if (rc != UNIQUE_OK) return rc;
+  *out_bytes = round_up(unique::prefix_floats(v, g) * sizeof(float), kAlign);
+  return UNIQUE_OK;
+}
+
+int unique_shared_prefix_decode(const unique_cache_desc* desc, const unique_prefix_groups* groups, const void* d_q, float sm_scale, void* d_out,
+                                float* d_lse_out, void* d_workspace, size_t workspace_bytes, void* stream) {
+  unique::CacheView v;
+  int rc = make_view(desc, &v, false, true);
+  if (rc != UNIQUE_OK) return rc;
+  unique_prefix_groups g;
+  rc = check_groups(v, groups, &g);
+  if (rc != UNIQUE_OK) return rc;
+  if (!g.starts || !g.prefix_pages) return fail(UNIQUE_ERR_INVALID_ARG, "starts and prefix_pages must be non-NULL");
+  if (!d_q || !d_out) return fail(UNIQUE_ERR_INVALID_ARG, "d_q and d_out must be non-NULL");
+  if (((uintptr_t)d_q | (uintptr_t)d_out) & 15u)
+    return fail(UNIQUE_ERR_INVALID_ARG, "d_q and d_out must be 16-byte aligned");
+  if (!(sm_scale == sm_scale)) return fail(UNIQUE_ERR_INVALID_ARG, "sm_scale is NaN");
+  rc = check_workspace(d_workspace, workspace_bytes, unique::prefix_floats(v, g) * sizeof(float));
+  if (rc != UNIQUE_OK) return rc;
+  const unique::PrefixArgs a = {g, d_q, unique::decode_scale_log2(v, sm_scale), d_out, d_lse_out, reinterpret_cast<float*>(d_workspace)};
+  const hipError_t e = unique::launch_prefix(v, a, (hipStream_t)stream);
+  return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "shared prefix launch");
 }
 
 const char* unique_status_string(int status) {

@@ -1,0 +1,177 @@
+// Queries, keys and values of new tokens: each query and key head normalised by its root mean square and turned by its position, keys and values
+// written to their slots.
+//
+//   y = x / sqrt(mean(x^2) + eps) * w;  a pair (y_1, y_2) becomes m (y_1 cos a - y_2 sin a, y_1 sin a + y_2 cos a), a = position * f
+//
+// Memory bounds it: every element is read and written once. A lane holds two 16-byte pieces of a head, those whose channels are paired if the
+// pairs are halves of the head, so a pair never leaves its lane; D / (2 * 16 bytes) lanes hold a head and a wave 4 to 16 heads at a time. All heads of a token
+// share their angles: lane i of the wave forms those of pair i once, in turns and in 64 bits (a position of 2^20 times a frequency
+// leaves 2^-33 of a turn, where 32 bits would leave 2^-4), and the wave takes them from the LDS.
+#include <type_traits>
+
+#include "decode_core.hpp"
+#include "serving.hpp"
+
+namespace unique {
+namespace {
+
+constexpr int kAppendWaves = 4;
+constexpr int kAppendAhead = 2;  // steps of heads in flight
+
+template <typename T>
+__device__ __forceinline__ Raw16 pack_vec(const float (&x)[Elem<T>::kVec]) {
+  Raw16 r;
+  if constexpr (sizeof(T) == 4) {
+    r.v = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)float_to_bf16(x[2 * i]) | (uint32_t)float_to_bf16(x[2 * i + 1]) << 16;
+    r.v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return r;
+}
+
+// kInterleaved: pairs are neighbours. A wave takes `per` steps of heads of a token, the wave's item = (token, part of its heads).
+template <typename T, int D, bool kInterleaved>
+__global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c, AppendArgs a, int steps, int per) {
+  constexpr int kVec = Elem<T>::kVec;
+  constexpr int kLanes = D / kVec / 2;      // lanes of a head
+  constexpr int kHeads = kWave / kLanes;    // heads of a step
+  __shared__ float2 s_turn[kAppendWaves][D / 2];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int parts = (steps + per - 1) / per;
+  const int64_t item = (int64_t)blockIdx.x * kAppendWaves + wave;
+  const int64_t row = item / parts;
+  if (row >= a.rows) return;  // (no barrier below)
+  const int part = (int)(item - row * parts);
+  const int64_t slot = a.slots[row];
+  if (slot < 0 || slot >= c.num_phys * c.S) return;
+  const int position = a.positions[row];
+  const int64_t page = slot / c.S;
+  const int place = (int)(slot - page * c.S);
+
+  // This lane's two pieces of a head: where halves are paired, one of each half; behind the turned channels neighbours.
+  const int R = a.how.rotary_dim, mine = lane % kLanes, pairs = kInterleaved ? 0 : R / (2 * kVec);
+  const int c0 = mine < pairs ? mine : 2 * pairs + 2 * (mine - pairs), c1 = mine < pairs ? mine + pairs : c0 + 1;
+  if (lane < R / 2) {
+    const double turns = (double)position * (a.how.frequencies[lane] * 0.15915494309189535);
+    const float f = (float)(turns - rint(turns));  // in [-1/2, 1/2]
+    float sn, cs;
+    sincospif(2.f * f, &sn, &cs);
+    s_turn[wave][lane] = make_float2(cs * a.how.magnitude, sn * a.how.magnitude);
+  }
+  __builtin_amdgcn_wave_barrier();  // the LDS serves a wave's accesses in order; the compiler keeps it
+  const bool norm = a.how.q_weight != nullptr;
+  Raw16 wq[2], wk[2];
+  if (norm) {
+    wq[0] = load_raw(reinterpret_cast<const T*>(a.how.q_weight) + c0 * kVec);
+    wq[1] = load_raw(reinterpret_cast<const T*>(a.how.q_weight) + c1 * kVec);
+    wk[0] = load_raw(reinterpret_cast<const T*>(a.how.k_weight) + c0 * kVec);
+    wk[1] = load_raw(reinterpret_cast<const T*>(a.how.k_weight) + c1 * kVec);
+  }
+  const int all = c.H + 2 * c.Hkv;
+  const T* q = reinterpret_cast<const T*>(a.q) + row * a.q_stride;
+  const T* k = reinterpret_cast<const T*>(a.k) + row * a.k_stride;
+  const T* v = reinterpret_cast<const T*>(a.v) + row * a.v_stride;
+  T* q_out = reinterpret_cast<T*>(a.q_out) + row * c.H * D;
+  const int64_t token = page * c.kv_page_stride + (int64_t)place * D;
+  T* kc = reinterpret_cast<T*>(const_cast<void*>(c.k_cache)) + token;
+  T* vc = reinterpret_cast<T*>(const_cast<void*>(c.v_cache)) + token;
+
+  auto load = [&](int step, Raw16(&x)[2]) {
+    const int head = min(step * kHeads + lane / kLanes, all - 1);
+    const T* src = head < c.H ? q + head * D : (head < c.H + c.Hkv ? k + (head - c.H) * D : v + (head - c.H - c.Hkv) * D);
+    x[0] = load_raw(src + c0 * kVec);
+    x[1] = load_raw(src + c1 * kVec);
+  };
+  auto finish = [&](int step, Raw16(&x)[2]) {
+    const int head = step * kHeads + lane / kLanes;
+    const bool is_q = head < c.H, is_v = head >= c.H + c.Hkv;
+    float y[2][kVec];
+    unpack_raw(x[0], y[0], (const T*)nullptr);
+    unpack_raw(x[1], y[1], (const T*)nullptr);
+    if (norm) {  // uniform
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 2 * kVec; ++i) sum = fmaf(y[i / kVec][i % kVec], y[i / kVec][i % kVec], sum);
+      sum = group_allreduce<kLanes>(sum, OpSum());
+      const float scale = 1.f / sqrtf(sum * (1.f / D) + a.how.eps);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float w[kVec];
+        Raw16 raw;
+        raw.v.x = is_q ? wq[u].v.x : wk[u].v.x; raw.v.y = is_q ? wq[u].v.y : wk[u].v.y;
+        raw.v.z = is_q ? wq[u].v.z : wk[u].v.z; raw.v.w = is_q ? wq[u].v.w : wk[u].v.w;
+        unpack_raw(raw, w, (const T*)nullptr);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) y[u][i] *= scale * w[i];
+      }
+    }
+    if constexpr (kInterleaved) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int piece = u == 0 ? c0 : c1;
+        if (piece * kVec < R) {
+#pragma unroll
+          for (int i = 0; i < kVec; i += 2) {
+            const float2 t = s_turn[wave][piece * (kVec / 2) + i / 2];
+            const float y0 = y[u][i], y1 = y[u][i + 1];
+            y[u][i] = y0 * t.x - y1 * t.y;
+            y[u][i + 1] = y0 * t.y + y1 * t.x;
+          }
+        }
+      }
+    } else if (mine < pairs) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const float2 t = s_turn[wave][mine * kVec + i];
+        const float y0 = y[0][i], y1 = y[1][i];
+        y[0][i] = y0 * t.x - y1 * t.y;
+        y[1][i] = y0 * t.y + y1 * t.x;
+      }
+    }
+    if (head >= all) return;
+    T* dst = is_q ? q_out + head * D
+                  : (is_v ? vc + (int64_t)(head - c.H - c.Hkv) * c.kv_head_stride : kc + (int64_t)(head - c.H) * c.kv_head_stride);
+    // values go as they are
+    Raw16 z0 = pack_vec<T>(y[0]), z1 = pack_vec<T>(y[1]);
+    if (is_v) { z0 = x[0]; z1 = x[1]; }
+    *reinterpret_cast<uint4*>(dst + c0 * kVec) = z0.v;
+    *reinterpret_cast<uint4*>(dst + c1 * kVec) = z1.v;
+  };
+
+  const int begin = part * per, end = min(begin + per, steps);
+  Raw16 x[kAppendAhead][2];
+  for (int s0 = begin; s0 < end; s0 += kAppendAhead) {
+#pragma unroll
+    for (int u = 0; u < kAppendAhead; ++u) load(s0 + u, x[u]);
+#pragma unroll
+    for (int u = 0; u < kAppendAhead; ++u)
+      if (s0 + u < end) finish(s0 + u, x[u]);  // uniform
+  }
+}
+
+}  // namespace
+
+hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t st) {
+  auto with = [&](auto elem, auto dim) {
+    using T = decltype(elem);
+    constexpr int D = decltype(dim)::value, kHeads = kWave / (D / Elem<T>::kVec / 2);
+    const int steps = (c.H + 2 * c.Hkv + kHeads - 1) / kHeads;
+    int per = steps;
+    while (per > 1 && (int64_t)a.rows * ((steps + per - 1) / per) < 4096) per = (per + 1) / 2;
+    const int64_t items = (int64_t)a.rows * ((steps + per - 1) / per);
+    auto go = [&](auto kernel) {
+      kernel<<<dim3((unsigned)((items + kAppendWaves - 1) / kAppendWaves)), dim3(kAppendWaves * kWave), 0, st>>>(c, a, steps, per);
+      return hipGetLastError();
+    };
+    return a.how.interleaved ? go(append_kernel<T, D, true>) : go(append_kernel<T, D, false>);
+  };
+  auto with_dim = [&](auto elem) {
+    return c.D == 64 ? with(elem, std::integral_constant<int, 64>()) : with(elem, std::integral_constant<int, 128>());
+  };
+  return c.dtype == 0 ? with_dim(float()) : with_dim(bf16_t());
+}
+
+}  // namespace unique

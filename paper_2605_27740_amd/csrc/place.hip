@@ -1,0 +1,217 @@
+// Places for the new tokens of a step: pages from a stack of free ones, page table, lengths, positions and slots.
+//
+// Sequence b needs need_b = ceil((n_b + t_b) / S) - ceil(n_b / S) pages; with the sums of need over the sequences before it, its pages are known without
+// asking the others: page i of all is entry n - 1 - i of a stack of n. So one workgroup forms four prefix sums over the batch (pages that come back twice,
+// tokens, needs), and everything else is per page or per row. Small calls do all of it in that workgroup; in larger ones the pages that come
+// back and the rows have launches of their own, as the former must be on the stack before the latter read it.
+#include "decode_core.hpp"
+#include "serving.hpp"
+
+namespace unique {
+namespace {
+
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;
+constexpr int kFillThreads = 256, kFillRows = 4;  // rows of a thread
+constexpr int kMostTokens = 1 << 25;              // where sums of tokens saturate, above any number of rows
+
+struct Seat {  // what the rows of a sequence's new tokens need
+  int len, first, position, ok;  // its length, its first page among all that are given out
+};
+struct Back {  // what a sequence gives back
+  int freed_at, own_at, freed, pages;  // places on the stack; evicted pages, pages of its row if it has ended
+};
+struct PlaceArrays {
+  Seat* seat;   // [B]
+  Back* back;   // [B]
+  int* starts;  // [B + 1]
+  int* size;    // the stack's, with what has come back
+};
+
+__device__ __forceinline__ int pages_of(int tokens, int S) { return (tokens + S - 1) / S; }
+
+// Sums over the workgroup of up to 64 Ki values each, whose total fits.
+__device__ __forceinline__ int block_sum(int x, int* scratch) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int upto = wave_inclusive_scan(x);
+  __syncthreads();
+  if (lane == kWave - 1) scratch[wave] = upto;
+  __syncthreads();
+  return __builtin_amdgcn_readlane(wave_inclusive_scan(lane < kPlanWaves ? scratch[lane] : 0), kWave - 1);
+}
+
+// The plan of the whole batch by one workgroup. A thread takes sequences t, t + 1024, ..., so nothing is read that another one writes.
+__device__ __forceinline__ void plan_places(const CacheView& c, const unique_placement& p, const PlaceArrays& to) {
+  __shared__ int s_scan[4][kPlanWaves], s_sum[kPlanWaves];
+  const int t = threadIdx.x, lane = t % kWave, wave = t / kWave, S = c.S;
+  const int capacity = p.free_capacity;
+  const int64_t most = (int64_t)c.max_pages * S;
+  auto freed_of = [&](int b) { return p.freed_count ? min(max(p.freed_count[b], 0), p.freed_stride) : 0; };
+  auto length_of = [&](int b) { return (int)min((int64_t)max(c.seq_lens[b], 0), most); };
+  auto own_of = [&](int b, int pages) { return pages - (p.shared_pages ? min(max(p.shared_pages[b], 0), pages) : 0); };
+
+  int freed_all = 0, own_all = 0;
+  for (int b = t; b < c.B; b += kPlanThreads) {
+    freed_all += freed_of(b);
+    if (p.new_tokens[b] < 0) own_all += own_of(b, pages_of(length_of(b), S));
+  }
+  const int before = min(max(*p.free_count, 0), capacity);
+  freed_all = block_sum(freed_all, s_sum);
+  own_all = block_sum(own_all, s_sum);
+  const int size = (int)min((int64_t)before + freed_all + own_all, (int64_t)capacity);
+
+  int base[4] = {0, 0, 0, 0}, given = 0;  // freed, own, tokens, needs before the strip
+  for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
+    const int b = b0 + t;
+    const bool live = b < c.B;
+    const int len = live ? length_of(b) : 0, asked = live ? p.new_tokens[b] : 0, pages = pages_of(len, S);
+    const bool ended = asked < 0;
+    const int tokens = min(max(asked, 0), kMostTokens);
+    const bool fits = (int64_t)len + tokens <= most;
+    const int freed = live ? freed_of(b) : 0, own = live && ended ? own_of(b, pages) : 0;
+    const int need = fits && !ended ? pages_of(len + tokens, S) - pages : 0;
+    int x[4] = {freed, own, tokens, need}, upto[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      upto[i] = wave_inclusive_scan(x[i]);
+      if (i == 2) upto[i] = (int)min((uint32_t)upto[i], (uint32_t)kMostTokens);
+    }
+    __syncthreads();
+    if (lane == kWave - 1) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_scan[i][wave] = upto[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int waves = wave_inclusive_scan(lane < kPlanWaves ? s_scan[i][lane] : 0);
+      const int mine = base[i] + upto[i] + (wave > 0 ? __builtin_amdgcn_readlane(waves, wave - 1) : 0);
+      upto[i] = i == 2 ? min(mine, kMostTokens) : mine;
+      base[i] += __builtin_amdgcn_readlane(waves, kWave - 1);
+      if (i == 2) base[i] = min(base[i], kMostTokens);
+    }
+    if (live) {
+      // Sequences whose rows are not there are the last ones, so their needs may count.
+      const bool ok = !ended && fits && upto[2] <= p.max_new_tokens && (need == 0 || upto[3] <= size);
+      const int placed = ok ? tokens : 0;
+      const int position = p.next_positions ? p.next_positions[b] : len;
+      to.seat[b] = Seat{len, upto[3] - need, position, ok ? 1 : 0};
+      to.back[b] = Back{before + upto[0] - freed, before + freed_all + upto[1] - own, freed, ended ? pages : 0};
+      to.starts[b] = p.token_starts[b] = upto[2] - tokens;
+      if (b == c.B - 1) to.starts[c.B] = p.token_starts[c.B] = upto[2];
+      p.placed[b] = placed;
+      p.seq_lens_out[b] = ended ? 0 : len + placed;
+      if (p.next_positions_out) p.next_positions_out[b] = ended ? 0 : position + placed;
+      if (ok && need > 0) given = upto[3];  // (the largest is the last)
+    }
+  }
+  __syncthreads();
+  // the most of the workgroup: sums of needs only grow
+  given = (int)wave_allreduce_minmax<true>((uint32_t)given);
+  if (lane == 0) s_sum[wave] = given;
+  __syncthreads();
+  if (t == 0) {
+    for (int w = 0; w < kPlanWaves; ++w) given = max(given, s_sum[w]);
+    *p.free_count_out = size - given;
+    *to.size = size;
+  }
+}
+
+// Pages of sequence b go back, by the threads of a workgroup or wave.
+__device__ __forceinline__ void give_back(const CacheView& c, const unique_placement& p, const Back& k, int b, int from, int step) {
+  for (int i = from; i < k.freed; i += step)
+    if (k.freed_at + i < p.free_capacity) p.free_pages[k.freed_at + i] = p.freed_pages[(int64_t)b * p.freed_stride + i];
+  if (k.pages == 0) return;
+  const int shared = p.shared_pages ? min(max(p.shared_pages[b], 0), k.pages) : 0;
+  const int64_t row = (int64_t)b * c.max_pages;
+  for (int i = from; i < k.pages; i += step) {
+    const int to = k.own_at + i - shared;
+    if (i >= shared && to < p.free_capacity) p.free_pages[to] = c.page_table[row + i];
+    p.page_table_out[row + i] = -1;
+  }
+}
+
+// Position and slot of a row; the first token of a page also writes the page's entry of the table.
+__device__ __forceinline__ void fill_row(const CacheView& c, const unique_placement& p, const PlaceArrays& from, int size, int row) {
+  int position = -1;
+  int64_t slot = -1;
+  if (row < from.starts[c.B]) {
+    int lo = 0, hi = c.B - 1;  // the first sequence whose rows end behind this one
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (from.starts[mid + 1] > row) hi = mid;
+      else lo = mid + 1;
+    }
+    const Seat s = from.seat[lo];
+    if (s.ok) {
+      const int i = row - from.starts[lo], at = s.len + i, lp = at / c.S, have = pages_of(s.len, c.S);
+      const int64_t entry = (int64_t)lo * c.max_pages + lp;
+      const int page = lp < have ? c.page_table[entry] : p.free_pages[size - 1 - (s.first + lp - have)];
+      position = s.position + i;
+      slot = page < 0 ? -1 : (int64_t)page * c.S + at % c.S;
+      if (at % c.S == 0) p.page_table_out[entry] = page;
+    }
+  }
+  p.positions[row] = position;
+  p.slots[row] = slot;
+}
+
+constexpr int kSmallRows = 8192;
+__global__ __launch_bounds__(kPlanThreads) void place_kernel(CacheView c, unique_placement p) {
+  __shared__ Seat s_seat[kPlanThreads];
+  __shared__ Back s_back[kPlanThreads];
+  __shared__ int s_starts[kPlanThreads + 1], s_size;
+  const PlaceArrays at = {s_seat, s_back, s_starts, &s_size};
+  plan_places(c, p, at);
+  __syncthreads();
+  for (int b = threadIdx.x / kWave; b < c.B; b += kPlanWaves) give_back(c, p, s_back[b], b, threadIdx.x % kWave, kWave);
+  __threadfence_block();  // the stack is read by other waves
+  __syncthreads();
+  for (int row = threadIdx.x; row < p.max_new_tokens; row += kPlanThreads) fill_row(c, p, at, s_size, row);
+}
+
+__global__ __launch_bounds__(kPlanThreads) void place_plan_kernel(CacheView c, unique_placement p, PlaceArrays at) { plan_places(c, p, at); }
+
+__global__ __launch_bounds__(kFillThreads) void place_back_kernel(CacheView c, unique_placement p, PlaceArrays at) {
+  for (int b = blockIdx.x; b < c.B; b += gridDim.x) give_back(c, p, at.back[b], b, threadIdx.x, kFillThreads);
+}
+
+__global__ __launch_bounds__(kFillThreads) void place_fill_kernel(CacheView c, unique_placement p, PlaceArrays at) {
+  const int size = *at.size;
+#pragma unroll
+  for (int k = 0; k < kFillRows; ++k) {
+    const int row = (blockIdx.x * kFillRows + k) * kFillThreads + threadIdx.x;
+    if (row < p.max_new_tokens) fill_row(c, p, at, size, row);
+  }
+}
+
+bool place_is_small(const CacheView& c, int max_new_tokens) { return c.B <= kPlanThreads && max_new_tokens <= kSmallRows; }
+
+}  // namespace
+
+size_t place_bytes(const CacheView& c, int max_new_tokens) {
+  if (place_is_small(c, max_new_tokens)) return 0;
+  return (size_t)c.B * (sizeof(Seat) + sizeof(Back)) + ((size_t)c.B + 2) * sizeof(int);
+}
+
+hipError_t launch_place(const CacheView& c, const unique_placement& p, void* workspace, hipStream_t st) {
+  if (place_is_small(c, p.max_new_tokens)) {
+    place_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(c, p);
+    return hipGetLastError();
+  }
+  PlaceArrays at;
+  at.seat = reinterpret_cast<Seat*>(workspace);
+  at.back = reinterpret_cast<Back*>(at.seat + c.B);
+  at.starts = reinterpret_cast<int*>(at.back + c.B);
+  at.size = at.starts + c.B + 1;
+  place_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(c, p, at);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  place_back_kernel<<<dim3(c.B < 2048 ? c.B : 2048), dim3(kFillThreads), 0, st>>>(c, p, at);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.max_new_tokens == 0) return e;
+  constexpr int kRows = kFillThreads * kFillRows;
+  place_fill_kernel<<<dim3((p.max_new_tokens + kRows - 1) / kRows), dim3(kFillThreads), 0, st>>>(c, p, at);
+  return hipGetLastError();
+}
+
+}  // namespace unique

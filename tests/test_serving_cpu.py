@@ -1,0 +1,174 @@
+"""The calls around the cache without a GPU: refusals, sizes, frequencies, and the plain counterparts themselves."""
+import ctypes as C
+import math
+import random
+
+import pytest
+import torch
+
+from paper_2605_27740_amd import binding
+from paper_2605_27740_amd.session import rotary_frequencies
+from tests import serving_ref as R
+from tests.test_boundary_cpu import good_desc
+
+BAD, UNSUPPORTED, WORKSPACE = binding.ERR_INVALID_ARG, binding.ERR_UNSUPPORTED, binding.ERR_WORKSPACE
+A, NWS = 0x10000, 1 << 30
+
+
+@pytest.fixture(scope="module")
+def c():
+    return binding.load().c
+
+
+def placement(**over):
+    f = {name: A for name, kind in binding.Placement._fields_ if kind is C.c_void_p}
+    f.update(freed_stride=4, free_capacity=9, max_new_tokens=7)
+    f.update(over)
+    return binding.Placement(**f)
+
+
+def groups(**over):
+    f = dict(starts=A, members=A, prefix_pages=A, num_groups=1, max_members=2, max_prefix_pages=3, max_own_pages=4)
+    f.update(over)
+    return binding.PrefixGroupsDesc(**f)
+
+
+def transform(**over):
+    f = dict(q_weight=A, k_weight=A, frequencies=A, eps=1e-6, magnitude=1.0, rotary_dim=64, interleaved=0)
+    f.update(over)
+    return binding.HeadTransform(**f)
+
+
+SHAPES = [(dict(dtype=2), BAD), (dict(batch=0), BAD), (dict(num_q_heads=30), BAD), (dict(head_dim=96), UNSUPPORTED), (dict(page_size=12), UNSUPPORTED),
+          (dict(num_q_heads=24), UNSUPPORTED), (dict(max_seq_len_hint=-1), BAD), (dict(kv_head_stride=1024), BAD)]
+
+
+@pytest.mark.parametrize("over,code", SHAPES)
+def test_descriptors_are_refused(c, over, code):
+    d, n = C.byref(good_desc(**over)), C.c_size_t()
+    assert c.unique_place_tokens(d, placement(), A, NWS, None) == code
+    assert c.unique_place_workspace_bytes(d, 7, C.byref(n)) == code
+    assert c.unique_append_tokens(d, 3, A, 4096, A, 1024, A, 1024, A, A, transform(), A, None) == code
+    assert c.unique_shared_prefix_decode(d, groups(), A, 0.0, A, None, A, NWS, None) == code
+    assert c.unique_shared_prefix_workspace_bytes(d, groups(), C.byref(n)) == code
+
+
+def test_place_refuses(c):
+    f, d = c.unique_place_tokens, C.byref(good_desc())
+    n = C.c_size_t()
+    assert f(None, placement(), A, NWS, None) == BAD
+    assert f(d, None, A, NWS, None) == BAD
+    for name in ("new_tokens", "free_pages", "free_count", "free_count_out", "page_table_out", "seq_lens_out", "placed", "token_starts", "positions", "slots",
+                 "next_positions", "next_positions_out", "freed_pages", "freed_count"):
+        assert f(d, placement(**{name: 0}), A, NWS, None) == BAD, name
+    for over in (dict(page_table=0), dict(seq_lens=0)):
+        assert f(C.byref(good_desc(**over)), placement(), A, NWS, None) == BAD
+    for over in (dict(freed_stride=0), dict(free_capacity=0), dict(max_new_tokens=-1), dict(max_new_tokens=(1 << 24) + 1)):
+        assert f(d, placement(**over), A, NWS, None) == BAD, over
+    assert f(C.byref(good_desc(batch=1 << 12)), placement(freed_stride=1 << 20), A, NWS, None) == UNSUPPORTED
+    assert f(d, placement(), None, NWS, None) == WORKSPACE
+    assert f(d, placement(), A + 8, NWS, None) == WORKSPACE
+    assert f(d, placement(max_new_tokens=100_000), A, 64, None) == WORKSPACE
+    assert c.unique_place_workspace_bytes(d, 7, None) == BAD
+    assert c.unique_place_workspace_bytes(None, 7, C.byref(n)) == BAD
+    assert c.unique_place_workspace_bytes(d, -1, C.byref(n)) == BAD
+    assert c.unique_place_workspace_bytes(C.byref(good_desc(page_table=0, seq_lens=0, k_cache=0)), 100_000, C.byref(n)) == 0
+    assert n.value % 256 == 0 and n.value >= 256
+
+
+def test_append_refuses(c):
+    f = c.unique_append_tokens
+    good = dict(desc=good_desc(), rows=3, q=A, qs=4096, k=A, ks=1024, v=A, vs=1024, positions=A, slots=A, how=transform(), out=A + (1 << 20))
+
+    def call(**over):
+        x = dict(good, **over)
+        d = None if x["desc"] is None else C.byref(x["desc"])
+        return f(d, x["rows"], x["q"], x["qs"], x["k"], x["ks"], x["v"], x["vs"], x["positions"], x["slots"], x["how"], x["out"], None)
+
+    for name in ("desc", "q", "k", "v", "positions", "slots", "out"):
+        assert call(**{name: None}) == BAD, name
+    for name in ("q", "k", "v", "out"):
+        assert call(**{name: A + 8}) == BAD, name
+    for over in (dict(rows=-1), dict(qs=4088), dict(ks=1023), dict(vs=1028), dict(qs=4100), dict(out=A, qs=8192), dict(desc=good_desc(k_cache=0)),
+                 dict(desc=good_desc(v_cache=0))):
+        assert call(**over) == BAD, over
+    for over in (dict(q_weight=0), dict(k_weight=0), dict(q_weight=A + 4), dict(rotary_dim=-16), dict(rotary_dim=24), dict(rotary_dim=144), dict(frequencies=0),
+                 dict(frequencies=A + 4), dict(eps=-1.0), dict(eps=math.nan), dict(magnitude=math.nan)):
+        assert call(how=transform(**over)) == BAD, over
+    assert call(rows=0, q=None, out=None) == 0  # nothing to do
+
+
+def test_prefix_refuses(c):
+    f, d = c.unique_shared_prefix_decode, C.byref(good_desc())
+    n = C.c_size_t()
+    assert f(None, groups(), A, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, None, A, 0.0, A, None, A, NWS, None) == BAD
+    for over in (dict(starts=0), dict(prefix_pages=0), dict(num_groups=0), dict(num_groups=good_desc().batch + 1), dict(max_members=0),
+                 dict(max_prefix_pages=-1), dict(max_own_pages=-1)):
+        assert f(d, groups(**over), A, 0.0, A, None, A, NWS, None) == BAD, over
+    for over in (dict(k_cache=0), dict(v_cache=0), dict(page_table=0), dict(seq_lens=0)):
+        assert f(C.byref(good_desc(**over)), groups(), A, 0.0, A, None, A, NWS, None) == BAD, over
+    assert f(d, groups(), None, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, groups(), A, 0.0, None, None, A, NWS, None) == BAD
+    assert f(d, groups(), A + 2, 0.0, A, None, A, NWS, None) == BAD
+    assert f(d, groups(), A, math.nan, A, None, A, NWS, None) == BAD
+    assert f(d, groups(), A, 0.0, A, None, None, NWS, None) == WORKSPACE
+    assert f(d, groups(), A, 0.0, A, None, A, 1, None) == WORKSPACE
+    assert c.unique_shared_prefix_workspace_bytes(d, groups(), None) == BAD
+    assert c.unique_shared_prefix_workspace_bytes(C.byref(good_desc(page_table=0, seq_lens=0, k_cache=0)), groups(starts=0, prefix_pages=0, members=0),
+                                                  C.byref(n)) == 0 and n.value > 0
+
+
+def test_frequencies():
+    f = rotary_frequencies(64, base=1e4)
+    assert f.dtype is torch.float64 and f.shape == (32,) and f[0] == 1.0
+    assert torch.allclose(f, torch.tensor([1e4 ** (-i / 32) for i in range(32)], dtype=torch.float64), rtol=1e-15)
+    assert torch.equal(rotary_frequencies(64, base=1e4, factor=4.0), f / 4)
+    g = rotary_frequencies(64, base=1e4, factor=4.0, trained_len=4096, low_turns=1.0, high_turns=32.0)
+    for a, b in zip(f.tolist(), g.tolist()):
+        turns = 4096 * a / (2 * math.pi)
+        share = min(1.0, max(0.0, (turns - 1) / 31))
+        assert math.isclose(b, a * share + a / 4 * (1 - share), rel_tol=1e-14)
+    assert rotary_frequencies(0).numel() == 0
+
+
+def test_plain_heads_against_complex_numbers():
+    g = torch.Generator().manual_seed(1)
+    x, w = torch.randn((5, 3, 64), generator=g), torch.randn((64,), generator=g)
+    pos, f = torch.arange(5) * 1000, rotary_frequencies(32)
+    for interleaved in (False, True):
+        y, _ = R.heads(x, w, 1e-3, pos, f, 1.5, interleaved)
+        for r in range(5):
+            for h in range(3):
+                z = x[r, h].double()
+                z = z / math.sqrt(float((z * z).sum()) / 64 + 1e-3) * w.double()
+                for i in range(16):
+                    a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + 16)
+                    c = complex(z[a], z[b]) * 1.5 * complex(math.cos(float(pos[r] * f[i])), math.sin(float(pos[r] * f[i])))
+                    assert abs(c - complex(y[r, h, a], y[r, h, b])) < 1e-12
+                assert torch.equal(y[r, h, 32:], z[32:])
+
+
+def test_plain_places_keep_every_page():
+    """No page is lost or given twice, a slot is in its sequence's page, and places follow one another."""
+    for seed in range(200):
+        r = random.Random(seed)
+        S, B, width = r.choice([8, 16]), r.randrange(1, 9), 6
+        lens = [r.randrange(width * S + 1) for _ in range(B)]
+        new = [r.choice([-1, 0, 1, r.randrange(40)]) for _ in range(B)]
+        pages = [-(-n // S) for n in lens]
+        ids = list(range(sum(pages) + r.randrange(10)))
+        r.shuffle(ids)
+        take = iter(ids)
+        table = [[next(take) for _ in range(p)] + [-1] * (width - p) for p in pages]
+        free = list(take)
+        got = R.place(S, table, lens, new, free + [-1] * sum(pages), len(free), 60)
+        held = [p for b in range(B) for p in got["table"][b] if p >= 0]
+        assert sorted(held + got["stack"]) == sorted(ids)
+        for b in range(B):
+            assert sum(p >= 0 for p in got["table"][b]) == -(-got["seq_lens"][b] // S)
+            assert got["seq_lens"][b] == (0 if new[b] < 0 else lens[b] + got["placed"][b])
+            rows = range(got["token_starts"][b], got["token_starts"][b] + got["placed"][b])
+            for i, row in enumerate(rows):
+                at = lens[b] + i
+                assert got["slots"][row] == got["table"][b][at // S] * S + at % S and got["positions"][row] == at

@@ -1,0 +1,295 @@
+"""Places for new tokens, their queries, keys and values, and attention over shared prefixes on the GPU against plain counterparts (serving_ref.py)."""
+import math
+import random
+
+import pytest
+import torch
+
+from paper_2605_27740_amd import binding
+from paper_2605_27740_amd.session import CacheWriter, PageAccounts, PagePool, PrefixGroups, rotary_frequencies
+from tests import serving_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+DTYPES = [torch.bfloat16, torch.float32]
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+# ------------------------------------------------------------------ places
+
+def place_case(seed, B, S, width, most_len, most_new, free_share, *, ended=0.1, evicted=0, shared=True, own_positions=True, spare_rows=5):
+    r = random.Random(seed)
+    lens = [r.choice([0, 1, S - 1, S, r.randrange(most_len + 1)]) for _ in range(B)]
+    lens = [min(n, width * S) for n in lens]
+    new = [-r.randrange(1, 9) if r.random() < ended else r.choice([0, 1, 1, S, r.randrange(most_new + 1)]) for _ in range(B)]
+    pages = [-(-n // S) for n in lens]
+    freed_count = [r.randrange(evicted + 1) for _ in range(B)]
+    need = sum(max(0, -(-(n + max(t, 0)) // S) - -(-n // S)) for n, t in zip(lens, new))
+    free = int(need * free_share)
+    total = sum(pages) + sum(freed_count) + free
+    ids = list(range(total))
+    r.shuffle(ids)
+    take = iter(ids)
+    table = [[next(take) for _ in range(p)] + [-1] * (width - p) for p in pages]
+    freed = [[next(take) for _ in range(n)] + [-1] * (max(evicted, 1) - n) for n in freed_count]
+    stack = list(take)
+    c = dict(S=S, table=table, lens=lens, new=new, free=stack + [-7] * (total - len(stack) + 3), free_count=len(stack),
+             rows=sum(max(t, 0) for t in new) + spare_rows)
+    if shared:
+        c["shared"] = [r.choice([0, 0, 2, p]) for p in pages]
+    if own_positions:
+        c["nxt"] = [n + S * r.randrange(4) for n in lens]
+    if evicted:
+        c.update(freed=freed, freed_count=freed_count)
+    return c, max(total, 1)
+
+
+def run_place(c, total, *, in_place, rows=None):
+    table, lens, nxt, count = i32(c["table"]), i32(c["lens"]), i32(c["nxt"]) if "nxt" in c else None, i32([c["free_count"]])
+    free = i32(c["free"])
+    rows = c["rows"] if rows is None else rows
+    pool = PagePool(q_heads=8, kv_heads=8, head_dim=64, page_size=c["S"], dtype=torch.float32, num_pages=total, page_table=table, seq_lens=lens,
+                    max_new_tokens=rows, free_pages=free, free_count=count, shared_pages=i32(c["shared"]) if "shared" in c else None, next_positions=nxt)
+    freed = {} if "freed" not in c else dict(freed_pages=i32(c["freed"]), freed_count=i32(c["freed_count"]))
+    outs = {}
+    if not in_place:
+        outs = dict(page_table_out=table.clone(), seq_lens_out=torch.full_like(lens, -9), free_count_out=torch.full_like(count, -9))
+        if nxt is not None:
+            outs["next_positions_out"] = torch.full_like(nxt, -9)
+    pool.place_tokens(i32(c["new"]), **freed, **outs)
+    torch.cuda.synchronize()
+    table_out, lens_out = (table, lens) if in_place else (outs["page_table_out"], outs["seq_lens_out"])
+    nxt_out, count_out = (nxt, count) if in_place else (outs.get("next_positions_out"), outs["free_count_out"])
+    if not in_place:
+        assert table.tolist() == c["table"] and lens.tolist() == c["lens"] and count.tolist() == [c["free_count"]]
+    return dict(table=table_out.tolist(), seq_lens=lens_out.tolist(), next=None if nxt_out is None else nxt_out.tolist(), placed=pool.placed.tolist(),
+                token_starts=pool.token_starts.tolist(), positions=pool.positions.tolist(), slots=pool.slots.tolist(),
+                stack=free.tolist()[:int(count_out)])
+
+
+def check_place(c, total, **how):
+    got = run_place(c, total, **how)
+    want = R.place(**{**c, "rows": how.get("rows", c["rows"]) if how.get("rows") is not None else c["rows"]})
+    for key, x in got.items():
+        if x is not None:
+            assert x == want[key], key
+
+
+PLACE = [  # B, S, width, longest, most new, share of the needed pages that are free
+    (1, 16, 40, 100, 1, 1.0), (1, 8, 3, 20, 30, 1.0), (64, 16, 70, 800, 1, 1.1), (257, 32, 20, 300, 70, 0.7), (1024, 8, 12, 60, 9, 0.9),
+    (1025, 16, 9, 60, 40, 0.8), (3000, 8, 30, 100, 20, 1.2), (7, 16, 3000, 9000, 12000, 1.0), (40, 32, 400, 4000, 3000, 0.6), (2100, 16, 5, 64, 3, 0.0)]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("case", PLACE)
+def test_places_as_one_after_the_other(gpu_lib, case, in_place):
+    """Small and large calls; sequences that end, do not fit their row, or find no pages; lengths 0, 1 and around a page."""
+    say(f"place {case} in_place={in_place}")
+    for seed, more in ((1, dict()), (2, dict(evicted=3)), (3, dict(ended=0.0, shared=False, own_positions=False)), (4, dict(ended=0.9, evicted=1))):
+        c, total = place_case(seed + case[0], *case, **more)
+        check_place(c, total, in_place=in_place)
+
+
+@pytest.mark.parametrize("rows", [0, 1, 50, 8192, 8193])
+def test_rows_that_are_not_there(gpu_lib, rows):
+    """Fewer rows than new tokens: the last sequences get no place; more: -1 behind the last."""
+    say(f"rows {rows}")
+    c, total = place_case(5, 60, 16, 40, 200, 30, 2.0)
+    check_place(c, total, in_place=False, rows=rows)
+    check_place(c, total, in_place=True, rows=rows)
+
+
+def test_a_stack_that_is_too_small_loses_what_does_not_fit(gpu_lib):
+    c, total = place_case(6, 50, 8, 30, 200, 10, 0.5, ended=0.6, evicted=2)
+    c["free"] = c["free"][:c["free_count"] + 11]
+    for how in (False, True):
+        check_place(c, total, in_place=how)
+
+
+# ------------------------------------------------------------------ queries, keys and values
+
+def append_bound(y, size, dtype):
+    """The one rounding, and the work in 32 bits. With u = 2^-24: a sum of 128 squares is off by 128 u, so its root by 64 u, division, root and two
+    products 4 u; the angle is off by 2 pi (2^-25 + 2^-33) < 4 u of a radian, sine and cosine by 4 u more, the factor, products and sum by 4 u: 80 u of
+    |y_1| + |y_2| in all. Below the smallest normal number of the type a step is absolute."""
+    return torch.finfo(dtype).eps / 2 * y.abs() + 80 * 2.0 ** -24 * size * (1 + 2.0 ** -7) + torch.finfo(dtype).tiny
+
+
+def run_append(dtype, H, Hkv, D, S, rows, *, rotary, interleaved, norm, magnitude, fused, far=0, in_place=False, strided=False, seed=0, scaled=False):
+    g = torch.Generator().manual_seed(seed + D + rows)
+    pages = rows // S + 7
+    x = torch.randn((rows, H + 2 * Hkv, D), generator=g)
+    x[..., 3] *= 50
+    x = x.to(dtype)
+    q, k, v = x.split([H, Hkv, Hkv], 1)
+    slots = torch.randperm(pages * S, generator=g)[:rows]
+    slots[::5] = -1 - torch.arange(slots[::5].numel())
+    slots[3::11] = pages * S + 1  # outside the pool
+    positions = (torch.randint(0, 5000, (rows,), generator=g) + far).int()
+    shape = (pages, Hkv, 2, S, D) if strided else (pages, Hkv, S, D)
+    caches = [torch.full(shape, -3.0, dtype=dtype, device=DEV) for _ in range(2)]
+    kc, vc = (caches[0][:, :, 0], caches[0][:, :, 1]) if strided else caches
+    w = [(1 + 0.3 * torch.randn((D,), generator=g)).to(dtype) for _ in range(2)] if norm else [None, None]
+    f = rotary_frequencies(rotary, base=5e5, **(dict(factor=8.0, trained_len=4096, low_turns=1.0, high_turns=4.0) if scaled else {}))
+    writer = CacheWriter(q_heads=H, k_cache=kc, v_cache=vc, q_weight=None if w[0] is None else w[0].to(DEV), k_weight=None if w[1] is None else w[1].to(DEV),
+                         eps=1e-5, frequencies=f, magnitude=magnitude, interleaved=interleaved)
+    if fused:
+        parts = x.to(DEV).split([H, Hkv, Hkv], 1)
+    else:
+        parts = [p.contiguous().to(DEV) for p in (q, k, v)]
+    q_out = parts[0] if in_place else torch.full((rows, H, D), -5.0, dtype=dtype, device=DEV)
+    got = writer.append_tokens(*parts, positions.to(DEV), slots.to(DEV), q_out=q_out).cpu()
+    torch.cuda.synchronize()
+    here = (slots >= 0) & (slots < pages * S)
+    (yq, sq), (yk, sk) = (R.heads(t, u, 1e-5, positions, f, magnitude, interleaved) for t, u in ((q, w[0]), (k, w[1])))
+    assert torch.equal(got[~here], q[~here] if in_place else torch.full_like(q[~here], -5.0)), "rows without a slot"
+    assert ((got[here].double() - yq[here]).abs() <= append_bound(yq, sq, dtype)[here]).all()
+    kg, vg = (t.cpu().transpose(1, 2).reshape(pages * S, Hkv, D) for t in (kc, vc))
+    mine = slots[here]
+    assert ((kg[mine].double() - yk[here]).abs() <= append_bound(yk, sk, dtype)[here]).all()
+    assert torch.equal(vg[mine], v[here])
+    others = torch.ones(pages * S, dtype=torch.bool)
+    others[mine] = False
+    assert (kg[others] == -3).all() and (vg[others] == -3).all(), "slots that no row has"
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,H,Hkv,S", [(128, 32, 8, 16), (64, 8, 2, 8), (128, 1, 1, 32), (64, 32, 32, 16), (128, 64, 8, 8), (64, 2, 1, 32)])
+@pytest.mark.parametrize("rows", [1, 37])
+def test_append_every_rotation(gpu_lib, dtype, D, H, Hkv, S, rows):
+    for rotary in [r for r in (0, 16, 48, 64, 96, 128) if r <= D]:
+        for interleaved in (False, True):
+            for norm in (False, True):
+                say(f"append {dtype} {(D, H, Hkv, S)} rows={rows} R={rotary} interleaved={interleaved} norm={norm}")
+                run_append(dtype, H, Hkv, D, S, rows, rotary=rotary, interleaved=interleaved, norm=norm, magnitude=1.0, fused=rotary % 32 == 0)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("far", [1 << 20, (1 << 31) - 6000])
+def test_append_far_positions_scaled(gpu_lib, dtype, far):
+    say(f"append {dtype} far={far}")
+    run_append(dtype, 16, 4, 128, 16, 600, rotary=128, interleaved=False, norm=True, magnitude=1.2, fused=True, far=far, scaled=True)
+    run_append(dtype, 16, 4, 64, 8, 601, rotary=32, interleaved=True, norm=False, magnitude=0.7, fused=False, far=far, scaled=True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_append_in_place_and_into_a_strided_cache(gpu_lib, dtype):
+    say(f"append strides {dtype}")
+    run_append(dtype, 16, 4, 128, 16, 5000, rotary=64, interleaved=False, norm=True, magnitude=1.0, fused=False, in_place=True)
+    run_append(dtype, 8, 8, 64, 32, 333, rotary=64, interleaved=True, norm=True, magnitude=1.0, fused=True, strided=True)
+
+
+def test_append_without_a_transform_copies(gpu_lib):
+    g = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn((9, h, 128), generator=g).bfloat16().to(DEV) for h in (8, 2, 2))
+    kc, vc = (torch.zeros((4, 2, 8, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    slots = torch.arange(9, device=DEV) + 11
+    out = CacheWriter(q_heads=8, k_cache=kc, v_cache=vc).append_tokens(q, k, v, i32(list(range(9))), slots)
+    torch.cuda.synchronize()
+    assert torch.equal(out, q)
+    for cache, x in ((kc, k), (vc, v)):
+        assert torch.equal(cache.transpose(1, 2).reshape(32, 2, 128)[11:20], x)
+
+
+# ------------------------------------------------------------------ shared prefixes
+
+def prefix_case(dtype, H, Hkv, D, S, groups, *, seed=0, loose=0, poison=True, extra_cols=0):
+    """groups: (members' own tokens, prefix pages); a negative number of own tokens makes a member so many tokens shorter than its prefix. `loose`
+    sequences are in no group."""
+    g = torch.Generator().manual_seed(seed + D + S)
+    n = sum(len(own) for own, _ in groups)
+    B = n + loose
+    where = torch.randperm(B, generator=g)
+    lens, rows = [0] * B, [[] for _ in range(B)]
+    ids = iter(torch.randperm(20 + sum(p + sum(-(-max(t, 0) // S) for t in own) for own, p in groups) + 3 * loose, generator=g).tolist())
+    starts, at = [0], 0
+    for own, p in groups:
+        shared = [next(ids) for _ in range(p)]
+        for t in own:
+            b = int(where[at])
+            lens[b] = max(p * S + t, 0)
+            rows[b] = shared + [next(ids) for _ in range(-(-max(t, 0) // S))]
+            at += 1
+        starts.append(at)
+    for b in where[at:].tolist():
+        lens[b], rows[b] = 2 * S + 1, [next(ids) for _ in range(3)]
+    width = max(len(r) for r in rows) + extra_cols
+    table = torch.tensor([r + [-1] * (max(width, 1) - len(r)) for r in rows], dtype=torch.int32)
+    pool = max(max(r, default=0) for r in rows) + 2
+    k, v = (torch.full((pool, Hkv, S, D), math.nan if poison else 0.0) for _ in range(2))
+    for b in range(B):
+        for p, ph in enumerate(rows[b]):
+            used = S if any(p < q and b in where[s:e].tolist() for (_, q), s, e in zip(groups, starts, starts[1:])) else max(0, min(S, lens[b] - p * S))
+            if torch.isnan(k[ph, 0, 0, 0]) or not poison:
+                k[ph, :, :used] = torch.randn((Hkv, used, D), generator=g)
+                v[ph, :, :used] = torch.randn((Hkv, used, D), generator=g)
+    q = torch.randn((B, H, D), generator=g) * 1.5
+    return dict(q=q.to(dtype), k=k.to(dtype), v=v.to(dtype), table=table, lens=torch.tensor(lens, dtype=torch.int32), starts=starts, members=where[:n].int(),
+                pages=[p for _, p in groups], groups=groups, S=S)
+
+
+def make_groups(c, H, **over):
+    args = dict(q_heads=H, k_cache=c["k"].to(DEV), v_cache=c["v"].to(DEV), page_table=c["table"].to(DEV), seq_lens=c["lens"].to(DEV),
+                group_starts=i32(c["starts"]), prefix_pages=i32(c["pages"]), members=torch.cat([c["members"], c["members"].new_zeros(len(c["lens"]))]).to(DEV),
+                max_members=max(len(own) for own, _ in c["groups"]), max_prefix_pages=max(c["pages"]))
+    args.update(over)
+    return PrefixGroups(**args)
+
+
+def prefix_bounds(c, want, dtype):
+    """u = 2^-24. A logit is a sum of D products, off by (D + 2) u of the sum of |q k|, so a weight by twice that relatively (its own and the normaliser's); exponentials and
+    their arguments 2^-21 of a weight, sums of n tokens n u. bf16: probabilities and the output are rounded, half a step each."""
+    out, lse, terms, reach = want
+    n = c["lens"].double()[:, None]
+    rel = 2 * (c["q"].shape[-1] + 2) * 2.0 ** -24 * reach + 2.0 ** -20 + 2 * n * 2.0 ** -24
+    half = 2.0 ** -8 if dtype is torch.bfloat16 else 0.0
+    return (rel + half)[..., None] * terms * (1 + half) + half * out.abs(), rel + 2.0 ** -22 * lse.abs().nan_to_num(posinf=0.0)
+
+
+def check_prefix(c, got, dtype):
+    out, lse = (x.cpu() for x in got)
+    want = R.attend(c["q"], c["k"], c["v"], c["table"], c["lens"])
+    listed = torch.zeros(len(c["lens"]), dtype=torch.bool)
+    listed[c["members"].long()] = True
+    tol, tol_lse = prefix_bounds(c, want, dtype)
+    some = listed & (c["lens"] > 0)
+    assert ((out.double() - want[0]).abs() <= tol)[some].all(), float(((out.double() - want[0]).abs() / tol)[some].max())
+    assert ((lse.double() - want[1]).abs() <= tol_lse)[some].all(), float((lse.double() - want[1])[some].abs().max())
+    none = listed & (c["lens"] == 0)
+    assert (out[none] == 0).all() and torch.isneginf(lse[none]).all()
+    return listed
+
+
+PREFIX = [
+    [([5], 3)],
+    [([0, 1, 40], 1)],
+    [([17] * 9, 20), ([1, 2, 3], 0), ([100], 7)],
+    [([3] * 33, 9), ([0] * 2, 33)],
+    [([-1, 7, -20, 2], 4), ([-10000, 0], 2)],
+    [(list(range(70)), 5)],
+    [([11] * 130, 6)],
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,H,Hkv,S", [(128, 8, 2, 16), (64, 8, 8, 8), (128, 8, 1, 32), (64, 4, 2, 16), (128, 4, 1, 8), (64, 8, 1, 32)])
+@pytest.mark.parametrize("which", range(len(PREFIX)))
+def test_prefix_groups_of_all_kinds(gpu_lib, dtype, D, H, Hkv, S, which):
+    """Few and many members, prefixes of no, one and odd numbers of pages, own parts of 0 tokens and more, members that are shorter than their
+    prefix or empty, sequences in no group; unwritten slots hold NaN."""
+    say(f"prefix {dtype} {(D, H, Hkv, S)} case {which}")
+    c = prefix_case(dtype, H, Hkv, D, S, PREFIX[which], seed=which, loose=2, extra_cols=which % 3)
+    groups = make_groups(c, H)
+    groups.out.fill_(-7.0)
+    groups.lse.fill_(-7.0)
+    got = groups.paged_decode(c["q"].to(DEV))
+    torch.cuda.synchronize()
+    listed = check_prefix(c, got, dtype)
+    assert (got[0][~listed.to(DEV)] == -7).all() and (got[1][~listed.to(DEV)] == -7).all(), "sequences in no group"
