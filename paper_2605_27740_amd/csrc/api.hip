@@ -695,7 +695,7 @@ int unique_shared_prefix_workspace_bytes(const unique_cache_desc* desc, const un
   unique_prefix_groups g;
   rc = check_groups(v, groups, &g);
   if (rc != UNIQUE_OK) return rc;
-  *out_bytes = round_up(unique::prefix_floats(v, g) * sizeof(float), kAlign);
+  *out_bytes = round_up(unique::prefix_bytes(v, g), kAlign);
   return UNIQUE_OK;
 }
 
@@ -712,10 +712,9 @@ int unique_shared_prefix_decode(const unique_cache_desc* desc, const unique_pref
   if (((uintptr_t)d_q | (uintptr_t)d_out) & 15u)
     return fail(UNIQUE_ERR_INVALID_ARG, "d_q and d_out must be 16-byte aligned");
   if (!(sm_scale == sm_scale)) return fail(UNIQUE_ERR_INVALID_ARG, "sm_scale is NaN");
-  rc = check_workspace(d_workspace, workspace_bytes, unique::prefix_floats(v, g) * sizeof(float));
+  rc = check_workspace(d_workspace, workspace_bytes, unique::prefix_bytes(v, g));
   if (rc != UNIQUE_OK) return rc;
-  const unique::PrefixArgs a = {g, d_q, unique::decode_scale_log2(v, sm_scale), d_out, d_lse_out, reinterpret_cast<float*>(d_workspace)};
-  const hipError_t e = unique::launch_prefix(v, a, (hipStream_t)stream);
+  const hipError_t e = unique::launch_prefix(v, g, d_q, unique::decode_scale_log2(v, sm_scale), d_out, d_lse_out, d_workspace, (hipStream_t)stream);
   return e == hipSuccess ? UNIQUE_OK : hip_fail(e, "shared prefix launch");
 }
 

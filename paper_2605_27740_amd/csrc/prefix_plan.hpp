@@ -1,5 +1,5 @@
-// How attention over shared prefixes is cut into workgroups. Host arithmetic on the launch's bounds only (no HIP), so that it can be checked
-// without a GPU.
+// How attention over shared prefixes is cut into work items. Whole numbers only (no HIP), so that it can be checked without a GPU; the kernel that
+// makes the items uses the same functions. (constexpr functions are compiled for the device, too.)
 #pragma once
 #include <stdint.h>
 
@@ -7,37 +7,45 @@
 
 namespace unique {
 
-struct PrefixPlan {
-  int32_t rows;            // query rows of a workgroup: members times heads of the group
-  int32_t blocks;          // of them in a group, at most
-  int32_t chunk_pages;     // prefix pages of a workgroup
-  int32_t chunks;          // of them in a prefix, at most
-  int32_t own_pages;       // a sequence's own pages of a workgroup
-  int32_t own_chunks;
-  constexpr int32_t parts() const { return chunks + own_chunks; }  // of a row, at most
+// Every group is a source of items, its prefix's pages times the blocks of its members' query rows, and every member one, its own pages.
+constexpr int kPrefixSlots = 512;  // items that are wanted per launch: two workgroups to a compute unit
+
+struct PrefixShape {
+  int32_t rows;         // query rows of a workgroup's block
+  int32_t tile_pages;   // pages of a tile of tokens, a power of two
+  int32_t wanted;       // items per KV head
+  int32_t max_items;    // there are at most, per KV head
+  int32_t max_rows;     // rows of partial results at most, per KV head
 };
 
-inline PrefixPlan prefix_plan(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members, int max_prefix_pages,
-                              int max_own_pages) {
-  constexpr int64_t kWorkgroups = 512;
-  PrefixPlan p;
-  const int64_t rows = (int64_t)std::min(max_members, batch) * group;
-  p.rows = elem == 4 ? 128 : (rows <= 64 ? 64 : 128);
-  p.blocks = (int)((rows + p.rows - 1) / p.rows);
-  const int64_t units = (int64_t)num_groups * p.blocks * kv_heads;
-  const int per_tile = std::max(64 / page_size, 1);
-  int64_t chunks = std::max<int64_t>(kWorkgroups / units, 1);
-  int64_t pages = (max_prefix_pages + chunks - 1) / chunks;
-  pages = std::max<int64_t>((pages + per_tile - 1) / per_tile * per_tile, per_tile);
-  p.chunk_pages = (int)pages;
-  p.chunks = (int)((max_prefix_pages + pages - 1) / pages);
-  const int64_t own_units = (int64_t)batch * kv_heads;
-  int64_t own = std::max<int64_t>(kWorkgroups / own_units, 1);
-  own = std::max<int64_t>((max_own_pages + own - 1) / own, 4);
-  own = std::min<int64_t>((own + 3) / 4 * 4, 256);
-  p.own_pages = (int)own;
-  p.own_chunks = (int)((max_own_pages + own - 1) / own);
-  return p;
+inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members) {
+  PrefixShape s;
+  const int64_t most = (int64_t)max_members * group;
+  s.rows = elem == 4 ? 128 : (most <= 64 ? 64 : 128);
+  s.tile_pages = std::max((elem == 4 ? 32 : 64) / page_size, 1);
+  s.wanted = std::max(kPrefixSlots / kv_heads, 1);
+  const int64_t blocks = std::min<int64_t>(num_groups * ((most + s.rows - 1) / s.rows), (int64_t)batch * group / s.rows + num_groups);
+  s.max_items = (int32_t)(s.wanted + blocks + batch);
+  s.max_rows = (int32_t)((s.wanted + blocks) * s.rows + (int64_t)(s.wanted + batch) * group);
+  return s;
+}
+
+// Pages of an item, before the items of a source are made equal: such that there are at most `wanted` items and one for each source's block.
+constexpr int64_t prefix_item_pages(int64_t all_pages, int wanted) { return (all_pages + wanted - 1) / wanted; }
+
+// Items along a source's pages, and the pages of each. A block of many rows gets longer ones: its partial results, 4 bytes times D a row, are written and
+// read again, and tokens are 4 bytes times D (bf16) each as well.
+struct PrefixCut {
+  int32_t count, pages;
+};
+constexpr PrefixCut prefix_cut(int pages, int64_t item_pages, int live_rows, int page_size, int tile_pages) {
+  if (pages <= 0) return PrefixCut{0, tile_pages};
+  const int64_t least = (2ll * live_rows + page_size - 1) / page_size;
+  const int64_t p = item_pages > least ? item_pages : least;
+  const int64_t n = (pages + p - 1) / p;
+  int64_t each = (pages + n - 1) / n;
+  each = (each + tile_pages - 1) / tile_pages * tile_pages;
+  return PrefixCut{(int32_t)((pages + each - 1) / each), (int32_t)each};
 }
 
 }  // namespace unique

@@ -21,21 +21,51 @@ struct AppendArgs {
 };
 hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t stream);
 
+// A prefix of a group, or a member's own pages.
+struct PrefixSource {
+  int32_t first_item, first_row;  // of its items and of their partial results
+  int32_t begin, end, each;       // pages, and those of an item
+  int32_t blocks;                 // of query rows; items of a block follow those of the next, a run of pages after the other
+  int32_t place, rows;            // its first member, and its query rows
+};
+struct PrefixItem {
+  int32_t place, rows;   // first member, query rows
+  int32_t begin, end;    // pages
+  int32_t seq;           // the sequence whose row of the page table it goes by
+  int32_t limit;         // tokens that are there (a prefix's pages are full)
+  int32_t part;          // first row of its partial results
+  int32_t reserved;
+};
+struct PrefixMember {
+  int32_t seq;                       // < 0: left out
+  int32_t count, part, step;         // of the group's items: how many, the row of the first's partial results, rows from one to the next
+  int32_t own_count, own_part;       // of its own
+  int32_t reserved[2];
+};
+struct PrefixWork {
+  int32_t* num_items;    // one number
+  PrefixSource* source;  // [groups + batch]
+  PrefixItem* item;      // [max_items]
+  PrefixMember* member;  // [batch]
+  float* part_o;         // [kv_heads][max_rows][D]
+  float* part_ml;        // [kv_heads][max_rows][2]
+};
 struct PrefixArgs {
   unique_prefix_groups groups;
   const void* q;
   float scale_log2;
   void* out;
   float* lse_out;
-  float* partials;  // prefix_floats
+  PrefixShape shape;
+  PrefixWork work;
 };
-size_t prefix_floats(const CacheView& c, const unique_prefix_groups& g);
-hipError_t launch_prefix(const CacheView& c, const PrefixArgs& a, hipStream_t stream);
+size_t prefix_bytes(const CacheView& c, const unique_prefix_groups& g);
+hipError_t launch_prefix(const CacheView& c, const unique_prefix_groups& g, const void* q, float scale_log2, void* out, float* lse_out, void* workspace,
+                         hipStream_t stream);
 
 template <typename T, int D>
-hipError_t launch_prefix_of(const CacheView& c, const PrefixArgs& a, const PrefixPlan& plan, float* part_ml, bool nt, hipStream_t stream);
-#define UNIQUE_DECLARE(T, D) \
-  template <> hipError_t launch_prefix_of<T, D>(const CacheView&, const PrefixArgs&, const PrefixPlan&, float*, bool, hipStream_t);
+hipError_t launch_prefix_of(const CacheView& c, const PrefixArgs& a, hipStream_t stream);
+#define UNIQUE_DECLARE(T, D) template <> hipError_t launch_prefix_of<T, D>(const CacheView&, const PrefixArgs&, hipStream_t);
 UNIQUE_DECLARE(float, 64) UNIQUE_DECLARE(float, 128) UNIQUE_DECLARE(uint16_t, 64) UNIQUE_DECLARE(uint16_t, 128)
 #undef UNIQUE_DECLARE
 
