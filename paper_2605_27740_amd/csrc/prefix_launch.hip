@@ -171,7 +171,10 @@ size_t prefix_bytes(const CacheView& c, const unique_prefix_groups& g) {
 
 hipError_t launch_prefix(const CacheView& c, const unique_prefix_groups& g, const void* q, float scale_log2, void* out, float* lse_out, void* workspace,
                          hipStream_t st) {
-  PrefixArgs a = {g, q, scale_log2, out, lse_out, shape_of(c, g), {}};
+  // The most that the bounds allow, all groups and members alike.
+  const int64_t pages = std::min<int64_t>((int64_t)g.num_groups * g.max_prefix_pages + (int64_t)c.B * g.max_own_pages, c.num_phys);
+  const bool streams = pages * c.Hkv * c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2) > kStreamNtBytes;
+  PrefixArgs a = {g, q, scale_log2, streams, out, lse_out, shape_of(c, g), {}};
   lay_out(c, g, a.shape, reinterpret_cast<char*>(workspace), &a.work);
   prefix_items_kernel<<<dim3(1), dim3(kItemThreads), 0, st>>>(c, a);
   const hipError_t e = hipGetLastError();

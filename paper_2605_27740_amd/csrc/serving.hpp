@@ -54,6 +54,7 @@ struct PrefixArgs {
   unique_prefix_groups groups;
   const void* q;
   float scale_log2;
+  int32_t streams;  // keys and values are more than the caches hold
   void* out;
   float* lse_out;
   PrefixShape shape;
