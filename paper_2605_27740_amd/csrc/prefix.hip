@@ -7,8 +7,7 @@
 // bf16 caches. A workgroup of four waves takes a chunk of a prefix for a KV head and a tile of rows. Tiles of 64 tokens go straight into the LDS. Both
 // products run on v_mfma_f32_32x32x16_bf16 with the queries as columns: S^T = K Q^T leaves a lane with 16 tokens' logits of ONE query (column lane % 32, rows 8 (i / 4) + 4
 // (lane / 32) + i % 4), so its softmax needs no other lane but lane ^ 32, and these are the k that the lane supplies to O^T = V^T P^T: probabilities never
-// leave their lane. V^T comes out of the LDS by its transposing read. A row of the LDS holds its 16-byte pieces in the order piece ^ f(row), f
-// distinct for 8 consecutive rows and even numbers for 4, so neither read meets a bank twice; the pieces are permuted where they are loaded, within a row of memory.
+// leave their lane. V^T comes out of the LDS by its transposing read. 
 // Probabilities enter the second product rounded to bf16, and their sum does not: 24 bits, in three products, would double the arithmetic, which bounds
 // groups of 32 sequences and more, for an error that is of the size of the output's own rounding.
 // fp32 caches: the same on v_mfma_f32_32x32x2_f32, whose probabilities stay fp32.
@@ -27,24 +26,33 @@ typedef uint32_t lds_addr_t;  // byte address in the LDS
 typedef const __attribute__((address_space(3))) char* lds_char_t;
 typedef __attribute__((address_space(3))) s16x4_t* lds_s16x4_t;
 
-__device__ __forceinline__ int swizzle(int row) { return (row & 3) * 2 + (row >> 2 & 1); }
+// How the eight 16-byte pieces of a row of 128 bytes are permuted (by exclusive or). Two rows lie in the 256 bytes that all banks of the LDS hold: 16 rows at the same
+// piece, and 4 rows at four, then meet no bank twice.
+__device__ __forceinline__ int swizzle(int row) { return (row >> 1 & 1) * 4 + (row >> 2 & 3); }
 
 // 16 bytes a lane from base + off into the LDS, lane after lane from `to` on. In assembly, as the compiler would otherwise wait for all loads before every
 // transposing read; nothing is written but the LDS, and who reads that waits by wait_units.
+// The address comes out of lanes by a vector instruction, after which a memory instruction would have to keep a distance that the compiler does not keep for it here;
+// a scalar one need not, and its copy of the address is also the step between m0 and its use.
 template <bool kNT>
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, lds_addr_t to) {
-  if constexpr (kNT) asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(to) : "memory");
-  else asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(to) : "memory");
+  uint64_t copy;
+  if constexpr (kNT)
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0 nt" : "=&s"(copy) : "v"(off), "s"(base), "s"(to) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %3\n\ts_mov_b64 %0, %2\n\tglobal_load_lds_dwordx4 %1, %0" : "=&s"(copy) : "v"(off), "s"(base), "s"(to) : "memory");
 }
 
-// A unit is a tile of keys or of values: kTokens rows of D elements, the 16-byte pieces of a row permuted.
-template <typename T, int D>
+// A unit is a tile of keys or of values: kTokens rows of D elements, in planes of 128 bytes of each row. kAcross: waves that share the rows of the
+// workgroup; the others take other tokens, 32 each.
+template <typename T, int D, int kAcross>
 struct Unit {
-  static constexpr int kRowBytes = D * (int)sizeof(T), kTokens = sizeof(T) == 2 ? 64 : 32;
-  static constexpr int kBytes = kTokens * kRowBytes, kLoads = kBytes / (kDecWaves * kWave * 16);  // of a wave
-  static constexpr int kLoadTokens = kWave * 16 / kRowBytes;                                      // tokens of a load
-  static constexpr int kPieces = kRowBytes / 16;
-  static constexpr int kRing = 80 * 1024 / kBytes < 6 ? 80 * 1024 / kBytes : 6;                   // units in the LDS
+  static constexpr int kPlanes = D * (int)sizeof(T) / 128, kTokens = 32 * kDecWaves / kAcross;
+  static constexpr int kPlaneBytes = kTokens * 128, kBytes = kPlanes * kPlaneBytes;
+  static constexpr int kRuns = kTokens / 8 / kDecWaves;  // of eight tokens, which a wave loads a kilobyte of each plane of
+  static constexpr int kLoads = kRuns * kPlanes;         // of a wave
+  static constexpr int kMost = kTokens == 64 ? 6 : 10;
+  static constexpr int kRing = 80 * 1024 / kBytes < kMost ? 80 * 1024 / kBytes : kMost;  // units in the LDS
 };
 
 // Until all but the newest `left` units (kMost at most) have arrived.
@@ -54,70 +62,97 @@ __device__ __forceinline__ void wait_units(int left) {
   else if constexpr (kMost > 0) wait_units<kMost - 1, kLoads>(left);
 }
 
-// kAcross: waves that share the rows of the workgroup; the others take other tokens of a tile.
-template <typename T, int D, int kAcross, bool kNT>
-__global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c, PrefixArgs a) {
-  using L = Unit<T, D>;
+// A run of a prefix's pages for a block of query rows. Every wave goes through the tiles, 32 tokens at a time, in steps: the products S = K Q^T of tile t, the softmax
+// of tile t - 1 and O += V P of tile t - 2 do not wait for each other, so that the matrix cores and the vector units both have something to do (bf16:
+// they stand between each other in the code).
+template <typename T, int D, int S, int kAcross, bool kNT>
+__device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixArgs& a, const PrefixItem& item, int hkv, char* ring) {
+  using L = Unit<T, D, kAcross>;
   constexpr bool kBf16 = sizeof(T) == 2;
-  constexpr int kSteps = D / 16;         // q.k products of a 32-token block (bf16)
-  constexpr int kBlocks = D / 32;        // of channels
+  constexpr int kBlocks = D / 32;                    // of channels
   constexpr int kAlong = kDecWaves / kAcross;
-  constexpr int kHalves = L::kTokens / 32 / kAlong;  // 32-token blocks of a wave in a tile
-  static_assert(kHalves >= 1, "a block for every wave");
-  constexpr float kRoom = 6.f;           // log2: how far above the largest logit the reference is put
-  constexpr int kIds = 4;                // page ids in a lane
-  __shared__ __attribute__((aligned(1024))) char ring[L::kRing * L::kBytes];
-
-  const int hkv = blockIdx.x & (c.Hkv - 1), index = blockIdx.x / c.Hkv, G = c.H / c.Hkv;
-  const PrefixItem item = a.work.item[index];
-  if (index >= *a.work.num_items) return;
+  constexpr int kTilePages = L::kTokens / S;
+  constexpr int kLag = 2;
+  constexpr float kRoom = 6.f;                       // log2: how far above the largest logit the reference is put
+  constexpr int kIds = kPrefixMostPages / kWave;     // page ids in a lane
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int col = lane % 32, half = lane / 32;
-  const int across = wave % kAcross, along = wave / kAcross;
+  const int across = wave % kAcross, along = wave / kAcross, G = c.H / c.Hkv;
 
-  // pages of the item, kIds * 64 at a time in the lanes
-  const int shift = __builtin_ctz(c.S), tile_pages = L::kTokens >> shift;
-  const int tiles = (item.end - item.begin + tile_pages - 1) / tile_pages;
-  const int32_t* table = c.page_table + (int64_t)(item.seq >= 0 && item.seq < c.B ? item.seq : 0) * c.max_pages;
-  int held[kIds], ids = -1;
-  auto look_up = [&](int e0) {
+  // The item's pages, looked up once. One that there is not is read from the pool's first page, and does not count.
+  const int pages = item.end - item.begin, tiles = (pages + kTilePages - 1) / kTilePages;
+  const int32_t* table = c.page_table + (int64_t)(item.seq >= 0 && item.seq < c.B ? item.seq : 0) * c.max_pages + item.begin;
+  const uint32_t pool = (uint32_t)min(c.num_phys, (int64_t)INT32_MAX);
+  int ids[kIds];
 #pragma unroll
-    for (int i = 0; i < kIds; ++i) held[i] = e0 + i * kWave + lane < item.end ? table[e0 + i * kWave + lane] : -1;
-    // The wait is here and not where an id is used, where all that is on its way to the LDS would be waited for as well.
-    asm volatile("" : "+v"(held[0]), "+v"(held[1]), "+v"(held[2]), "+v"(held[3]));
+  for (int i = 0; i < kIds; ++i) ids[i] = table[min(i * kWave + lane, pages - 1)];
+  // The wait is here and not where an id is used, where all that is on its way to the LDS would be waited for as well.
+#pragma unroll
+  for (int i = 0; i < kIds; ++i) asm volatile("" : "+v"(ids[i]));
+  bool holes = false;
+#pragma unroll
+  for (int i = 0; i < kIds; ++i) holes |= (uint32_t)ids[i] >= pool;
+  holes = __any(holes);
+  auto ids_of = [&](int window) {
+    int x = 0;
+#pragma unroll
+    for (int i = 0; i < kIds; ++i) x |= ids[i] & -(int)(window == i);  // (a choice becomes an array in memory)
+    return x;
   };
-  look_up(item.begin);
+  constexpr uint32_t kAll = (1u << kTilePages) - 1;
+  auto there_at = [&](int t) {  // pages of tile t that there are, a bit each
+    uint32_t bits = t == tiles - 1 ? (2u << (pages - 1 - t * kTilePages)) - 1 : kAll;
+    if (holes) bits &= (uint32_t)(__ballot((uint32_t)ids_of(t * kTilePages / kWave) < pool) >> (t * kTilePages % kWave));
+    return bits;
+  };
 
-  // Loads of a unit: wave w takes every fourth kilobyte. A page that there is not reads the pool's first page, and does not count. The pieces' order in a
-  // row is the same in all of a wave's loads.
-  const int load_row = lane * 16 / L::kRowBytes;
-  const uint32_t load_off = load_row * L::kRowBytes + ((lane % L::kPieces) ^ (swizzle(wave * L::kLoadTokens + load_row) & (L::kPieces - 1))) * 16;
-  const char* heads[2] = {reinterpret_cast<const char*>(reinterpret_cast<const T*>(c.k_cache) + (int64_t)hkv * c.kv_head_stride),
-                          reinterpret_cast<const char*>(reinterpret_cast<const T*>(c.v_cache) + (int64_t)hkv * c.kv_head_stride)};
-  const int64_t page_bytes = c.kv_page_stride * (int64_t)sizeof(T);
+  // Loads of a unit: wave w takes the tokens 8 w + ..., eight rows of a plane at a time, whose pieces are permuted where they are read, within a line of memory. Where
+  // the pages lie, 64 of them, is in the lanes as well, for the keys and for the values that come behind them.
   const lds_addr_t ring_at = (lds_addr_t)(uintptr_t)(lds_char_t)ring;
-  auto pages_there = [&](int t) {  // of tile t, one bit each (uniform)
-    const int at_page = t * tile_pages;
-    if (at_page % kWave == 0) {
-      if (at_page > 0 && at_page % (kIds * kWave) == 0) look_up(item.begin + at_page);
-      const int i = at_page / kWave % kIds;
-      ids = i == 0 ? held[0] : (i == 1 ? held[1] : (i == 2 ? held[2] : held[3]));
-    }
-    return (uint32_t)(__ballot((uint32_t)ids < (uint32_t)min(c.num_phys, (int64_t)INT32_MAX)) >> (at_page % kWave)) & ((1u << tile_pages) - 1);
-  };
-  uint32_t there_ahead = 0;  // of the newest tile
-  auto issue = [&](int unit, int slot) {
-    const int t = unit / 2;
-    if (unit % 2 == 0) there_ahead = pages_there(t);
-    const lds_addr_t to = ring_at + slot * L::kBytes;
+  const lds_addr_t load_to = ring_at + wave * 1024, load_end = load_to + L::kRing * L::kBytes;
+  const int load_row = 8 * wave + lane / 8;
+  uint32_t load_off[L::kPlanes];
 #pragma unroll
-    for (int j = 0; j < L::kLoads; ++j) {
-      const int at = (j * kDecWaves + wave) * L::kLoadTokens, e = at >> shift;  // token and page of the tile
-      const int id = __builtin_amdgcn_readlane(ids, (t * tile_pages + e) % kWave);
-      const int64_t from = (there_ahead >> e & 1 ? id : 0) * page_bytes + (at & (c.S - 1)) * L::kRowBytes;
-      load_to_lds<kNT>(heads[unit % 2] + from, load_off, to + at * L::kRowBytes);
+  for (int j = 0; j < L::kPlanes; ++j) load_off[j] = load_row % S * (D * (int)sizeof(T)) + j * 128 + (lane % 8 ^ swizzle(load_row)) * 16;
+  const uint64_t head_at = (uint64_t)hkv * c.kv_head_stride * sizeof(T), k_base = (uint64_t)c.k_cache + head_at;
+  const uint64_t v_behind = (uint64_t)c.v_cache - (uint64_t)c.k_cache;
+  uint64_t k_page = 0, v_page = 0;              // addresses of 64 pages' keys and values
+  int next_k = 0, next_v = 0;                   // tiles to load next,
+  int k_lane = 8 * wave / S, v_lane = k_lane;   // their first pages in the lanes
+  lds_addr_t to = load_to;                      // and where to
+  auto load = [&](uint64_t page, int at) {
+#pragma unroll
+    for (int r = 0; r < L::kRuns; ++r) {
+      const int e = at + r * 8 * kDecWaves / S;
+      const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(page >> 32), e) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)page, e);
+#pragma unroll
+      for (int j = 0; j < L::kPlanes; ++j)
+        load_to_lds<kNT>(reinterpret_cast<const char*>(from), load_off[j], to + j * L::kPlaneBytes + r * kDecWaves * 1024);
     }
+    to += L::kBytes;
+    to = to == load_end ? load_to : to;
   };
+  auto load_keys = [&] {
+    if (k_lane < kTilePages) {  // 64 new ones
+      const int id = ids_of(next_k / (kWave / kTilePages));
+      k_page = k_base + ((uint32_t)id < pool ? (uint64_t)(uint32_t)id * (uint64_t)c.kv_page_stride * sizeof(T) : 0);
+    }
+    load(k_page, k_lane);
+    k_lane = (k_lane + kTilePages) % kWave;
+    ++next_k;
+  };
+  auto load_values = [&] {
+    if (v_lane < kTilePages) v_page = k_page + v_behind;  // the keys are at most kLag tiles ahead, and in the same 64 pages as these begin
+    load(v_page, v_lane);
+    v_lane = (v_lane + kTilePages) % kWave;
+    ++next_v;
+  };
+  // Units go into the ring in the order in which the steps need them, K0 K1 K2 V0 K3 V1 ...: step t takes the keys of tile t and the values of tile t - 2.
+  int loaded = 0;
+  for (; loaded < L::kRing && next_v < tiles; ++loaded) {
+    if (next_k < tiles && next_k <= next_v + kLag) load_keys();
+    else load_values();
+  }
 
   // This lane's query row; one that there is not takes another's query, and nobody reads what becomes of it (a column of the products is for itself).
   const int row = across * 32 + col;
@@ -127,30 +162,64 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
   const bool mine = live && seq >= 0 && seq < c.B;
   const int tokens = mine ? c.seq_lens[seq] : 0;  // of this row's sequence
   const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)(mine ? seq : 0) * c.H + hkv * G + row % G) * D;
-  bf16x8_t qb[kBf16 ? kSteps : 1];
-  float qf[kBf16 ? 1 : D / 2];
-  if constexpr (kBf16) {
+  constexpr int kSteps = kBf16 ? D / 16 : D / 8;  // reads of 16 bytes of a key
+  u32x4_t qb[kSteps];  // bf16: the pieces 2 s + half; fp32: the pieces of this half
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) qb[s] = as_bf16x8(load_raw(q + (2 * s + half) * 8));
-  } else {
-#pragma unroll
-    for (int s = 0; s < D / 8; ++s) {
-      const float4 x = *reinterpret_cast<const float4*>(q + half * (D / 2) + 4 * s);
-      qf[4 * s] = x.x; qf[4 * s + 1] = x.y; qf[4 * s + 2] = x.z; qf[4 * s + 3] = x.w;
-    }
-  }
+  for (int s = 0; s < kSteps; ++s) qb[s] = *reinterpret_cast<const u32x4_t*>(reinterpret_cast<const char*>(q) + (kBf16 ? 2 * s + half : half * kSteps + s) * 16);
   // The queries are waited for here, not in every turn of the loop.
-  if constexpr (kBf16) {
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(qb[s]));
-  } else {
-#pragma unroll
-    for (int s = 0; s < D / 2; ++s) asm volatile("" : "+v"(qf[s]));
-  }
-  const bool idle = across * 32 >= item.rows;  // no row of this wave (uniform)
+  for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(qb[s]));
   // tokens that all rows of the wave have
-  const int all_have =
-      __builtin_amdgcn_readfirstlane((int)wave_allreduce_minmax<false>((uint32_t)(live ? min(tokens, item.limit) : INT32_MAX)));
+  const int all_have = __builtin_amdgcn_readfirstlane((int)wave_allreduce_minmax<false>((uint32_t)(live ? tokens : INT32_MAX)));
+  const bool idle = across * 32 >= item.rows;  // no row of this wave (uniform)
+
+  // Where a lane reads, behind a unit's beginning. Keys: token `col`, the pieces of step s, of which four (fp32: eight) are in a plane. Values, bf16: lane i of 16 asks
+  // for token i / 4, channels 4 (i % 4) + ..., and gets channel i of the four tokens; two blocks of channels are in a plane. fp32: channel `col` of a block,
+  // which is a plane.
+  constexpr int kWays = kBf16 ? 4 : 8;
+  lds_addr_t k_at[kWays], v_at[kBf16 ? 4 : 8];
+#pragma unroll
+  for (int s = 0; s < kWays; ++s)
+    k_at[s] = ring_at + (kBf16 ? 0 : half * (kSteps / 8) * L::kPlaneBytes) + (along * 32 + col) * 128 + ((kBf16 ? 2 * s + half : s) ^ swizzle(col)) * 16;
+#pragma unroll
+  for (int i = 0; i < (kBf16 ? 4 : 8); ++i) {
+    const int token = 4 * half + (kBf16 ? lane % 16 / 4 + i / 2 * 8 : i % 4 + i / 4 * 8);
+    const int off = kBf16 ? i % 2 * 64 + lane % 32 / 16 * 32 + lane % 4 * 8 : col * 4;
+    v_at[i] = ring_at + (along * 32 + token) * 128 + ((off / 16) ^ swizzle(token)) * 16 + off % 16;
+  }
+  struct Keys {
+    lds_char_t at[kWays];
+    __device__ __forceinline__ u32x4_t read(int s) const {
+      return *(__attribute__((address_space(3))) const u32x4_t*)(at[s % kWays] + s / kWays * L::kPlaneBytes);
+    }
+  };
+  auto keys_in = [&](int slot) {
+    Keys k;
+#pragma unroll
+    for (int s = 0; s < kWays; ++s) k.at[s] = (lds_char_t)(uintptr_t)(k_at[s] + slot * L::kBytes);
+    return k;
+  };
+  struct Values {
+    lds_char_t at[kBf16 ? 4 : 8];
+    // bf16: of block i % kBlocks, the tokens 4 half + 0..3 and 8 + 4 half + 0..3 of the 16 from 16 (i / kBlocks) on
+    __device__ __forceinline__ bf16x8_t read(int i) const {
+      const int e = i % kBlocks, n = i / kBlocks;
+      s16x4_t part[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) part[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at[e % 2 + 2 * u] + e / 2 * L::kPlaneBytes + n * 16 * 128));
+      return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // fp32: of block e, token 8 (i / 4) + 4 half + i % 4
+    __device__ __forceinline__ float read(int i, int e) const {
+      return *(__attribute__((address_space(3))) const float*)(at[i % 8] + i / 8 * 16 * 128 + e * L::kPlaneBytes);
+    }
+  };
+  auto values_in = [&](int slot) {
+    Values v;
+#pragma unroll
+    for (int i = 0; i < (kBf16 ? 4 : 8); ++i) v.at[i] = (lds_char_t)(uintptr_t)(v_at[i] + slot * L::kBytes);
+    return v;
+  };
 
   float m = kNegBig, l = 0.f;
   f32x16_t acc[kBlocks];
@@ -158,227 +227,246 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
   for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
+  auto zero16 = [] {
+    f32x16_t z;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z[i] = 0.f;
+    return z;
+  };
 
-  // Where a lane reads, behind a unit's beginning. Keys: token `col`, pieces (2 s + half) of step s, of which four follow from each
-  // other by the permutation (fp32: pieces half * D / 8 + s, eight). Values, bf16: lane i of 16 asks for token i / 4, channels 4 (i % 4) + ..., and gets
-  // channel i of the four tokens; blocks of channels two apart follow from each other. fp32: channels `col` of each block, token i % 4 + 4 half.
-  constexpr int kWays = kBf16 ? 4 : 8;
-  const int mine0 = along * kHalves * 32;  // the wave's first token in a tile
-  lds_addr_t k_at[kWays], v_at[kBf16 ? 2 : 4];
+  f32x16_t x;               // logits of a tile: token 8 (i / 4) + 4 half + i % 4 of the wave's 32
+  struct Weights {          // probabilities of the tile before
+    bf16x8_t b[2];          // bf16: as operands
+    float f[kBf16 ? 1 : 16];
+  } p;
+  auto product = [&](u32x4_t k, int s, f32x16_t y) {
+    if constexpr (kBf16) {
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, qb[s]), y, 0, 0, 0);
+    } else {
 #pragma unroll
-  for (int s = 0; s < kWays; ++s) {
-    const int piece = (kBf16 ? 2 * s + half : half * (D / 8) + s) ^ (swizzle(col) & (L::kPieces - 1));
-    k_at[s] = ring_at + (mine0 + col) * L::kRowBytes + piece * 16;
-  }
-  if constexpr (kBf16) {
-    const int token = 4 * half + lane % 16 / 4;
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int channel = e * 32 + lane % 32 / 16 * 16 + lane % 4 * 4;
-      v_at[e] = ring_at + (mine0 + token) * L::kRowBytes + ((channel / 8) ^ (swizzle(token) & (L::kPieces - 1))) * 16 + channel % 8 * 2;
+      for (int i = 0; i < 4; ++i) y = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(k[i]), __uint_as_float(qb[s][i]), y, 0, 0, 0);
+      return y;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int token = 4 * half + i;
-      v_at[i] = ring_at + (mine0 + token) * L::kRowBytes + ((col / 4) ^ swizzle(token)) * 16 + col % 4 * 4;
-    }
-  }
-
-  float p[kHalves][16];  // logits, then probabilities
-  bf16x8_t pb[kBf16 ? kHalves : 1][2];
-  // Products take their operands from the LDS in groups, the next group on its way while one is multiplied (left to itself the compiler reads one operand
-  // at a time and waits for it).
+  };
+  // Operands are read a few ahead (left to itself the compiler reads one at a time and waits for it).
+  constexpr int kFew = kBf16 ? 4 : 2;
   auto keys = [&](int slot) {
-    constexpr int kGroup = kBf16 ? 4 : 2, kGroups = (kBf16 ? kSteps : D / 8) / kGroup;  // reads of 16 bytes
-    u32x4_t ka[2][kGroup];
-    lds_char_t at[kWays];
+    const Keys k = keys_in(slot);
+    u32x4_t few[kFew];
 #pragma unroll
-    for (int s = 0; s < kWays; ++s) at[s] = (lds_char_t)(uintptr_t)(k_at[s] + slot * L::kBytes);
-    auto read = [&](int n, u32x4_t(&to)[kGroup]) {
+    for (int s = 0; s < kFew; ++s) few[s] = k.read(s);
+    x = zero16();
 #pragma unroll
-      for (int u = 0; u < kGroup; ++u) {
-        const int s = n % kGroups * kGroup + u;
-        to[u] = *(__attribute__((address_space(3))) const u32x4_t*)(at[s % kWays] + n / kGroups * 32 * L::kRowBytes + s / kWays * 128);
-      }
-    };
-    read(0, ka[0]);
-    f32x16_t x;
-#pragma unroll
-    for (int n = 0; n < kHalves * kGroups; ++n) {
-      if (n + 1 < kHalves * kGroups) read(n + 1, ka[(n + 1) % 2]);
+    for (int s = 0; s < kSteps; ++s) {
+      x = product(few[s % kFew], s, x);
+      if (s + kFew < kSteps) few[s % kFew] = k.read(s + kFew);
       __builtin_amdgcn_sched_barrier(0);
-      if (n % kGroups == 0) {
+    }
+  };
+  auto values = [&](int slot) {
+    const Values v = values_in(slot);
+    if constexpr (kBf16) {
+      bf16x8_t few[kFew];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      for (int i = 0; i < kFew; ++i) few[i] = v.read(i);
+#pragma unroll
+      for (int i = 0; i < 2 * kBlocks; ++i) {
+        acc[i % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(few[i % kFew], p.b[i / kBlocks], acc[i % kBlocks], 0, 0, 0);
+        if (i + kFew < 2 * kBlocks) few[i % kFew] = v.read(i + kFew);
+        __builtin_amdgcn_sched_barrier(0);
       }
+    } else {
+      float few[kFew][kBlocks];
 #pragma unroll
-      for (int u = 0; u < kGroup; ++u) {
-        const int s = n % kGroups * kGroup + u;
-        if constexpr (kBf16) {
-          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ka[n % 2][u]), qb[s], x, 0, 0, 0);
-        } else {
+      for (int i = 0; i < kFew; ++i)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(ka[n % 2][u][i]), qf[4 * s + i], x, 0, 0, 0);
+        for (int e = 0; e < kBlocks; ++e) few[i][e] = v.read(i, e);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+#pragma unroll
+        for (int e = 0; e < kBlocks; ++e) {
+          acc[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(few[i % kFew][e], p.f[i], acc[e], 0, 0, 0);
+          if (i + kFew < 16) few[i % kFew][e] = v.read(i + kFew, e);
         }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-      if (n % kGroups == kGroups - 1) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[n / kGroups][i] = x[i];
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   };
-  // Softmax of the tile. at0: the number of the wave's first token in it; full: all of its tokens count for all rows (uniform).
-  auto weights = [&](bool full, uint32_t there, int at0) {
-    if (!full) {
+  // Before the exponentials of tile t: tokens that do not count, and the reference. -> what earlier sums are to be multiplied by, as soon as the tile
+  // before, whose probabilities are relative to the old reference, has been added to them.
+  const int whole = holes ? 0 : min(pages / kTilePages, (all_have / S - item.begin) / kTilePages);  // tiles of which all tokens count for all rows
+  auto prepare = [&](int t, f32x16_t& x) {
+    if (t >= whole) {
+      const uint32_t there = there_at(t);
+      const int at0 = (item.begin + t * kTilePages) * S;
 #pragma unroll
-      for (int h = 0; h < kHalves; ++h)
+      for (int n = 0; n < 4; ++n) {  // pages are whole eights of tokens
+        const int end = there >> ((along * 32 + 8 * n) / S) & 1 ? tokens : 0;
 #pragma unroll
-        for (int n = 0; n < 4; ++n) {  // pages are whole eights of tokens
-          const int end = there >> ((mine0 + h * 32 + 8 * n) >> shift) & 1 ? min(tokens, item.limit) : 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[h][4 * n + i] = at0 + h * 32 + 8 * n + 4 * half + i < end ? p[h][4 * n + i] : -INFINITY;
-        }
+        for (int i = 0; i < 4; ++i) x[4 * n + i] = at0 + along * 32 + 8 * n + 4 * half + i < end ? x[4 * n + i] : -INFINITY;
+      }
     }
-    float top = p[0][0];
+    float top = x[0];
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, p[h][i]);
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
     top *= a.scale_log2;
+    float alpha = 1.f;
     if (__any(top > m)) {
       const float mnew = fmaxf(m, with_lane_xor32(top, OpMax()) + kRoom);
-      const float alpha = fast_exp2(m - mnew);
+      alpha = fast_exp2(m - mnew);
       m = mnew;
       l *= alpha;
+    }
+    return alpha;
+  };
+  auto weight = [&](float logit) {
+    const float w = fast_exp2(fmaf(logit, a.scale_log2, -m));
+    l += w;
+    return w;
+  };
+  auto rescale = [&](float alpha) {
+    if (__any(alpha != 1.f)) {
 #pragma unroll
       for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[e][i] *= alpha;
     }
-#pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[h][i] = fast_exp2(fmaf(p[h][i], a.scale_log2, -m));
-        l += p[h][i];
-      }
-      if constexpr (kBf16) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) pb[h][i / 8][i % 8] = (__bf16)p[h][i];
-      }
-    }
   };
-  // Slots without a token may hold anything, so their values are set to zero.
-  auto values = [&](bool full, uint32_t there, int at0, int slot) {
-    auto end_of = [&](int token) { return there >> ((mine0 + token) >> shift) & 1 ? item.limit : 0; };
-    lds_char_t at[kBf16 ? 2 : 4];
+  auto weights = [&] {
 #pragma unroll
-    for (int i = 0; i < (kBf16 ? 2 : 4); ++i) at[i] = (lds_char_t)(uintptr_t)(v_at[i] + slot * L::kBytes);
-    if constexpr (kBf16) {  // a step is 16 tokens, of which 4 half + 0..3 and 8 + 4 half + 0..3 are this lane's
-      s16x4_t va[2][kBlocks][2];
-      auto read = [&](int n, s16x4_t(&to)[kBlocks][2]) {
-#pragma unroll
-        for (int e = 0; e < kBlocks; ++e)
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-            to[e][u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at[e % 2] + e / 2 * 128 + (16 * n + 8 * u) * L::kRowBytes));
-      };
-      read(0, va[0]);
-#pragma unroll
-      for (int n = 0; n < 2 * kHalves; ++n) {
-        if (n + 1 < 2 * kHalves) read(n + 1, va[(n + 1) % 2]);
-        __builtin_amdgcn_sched_barrier(0);
-        if (!full) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const int end = end_of(16 * n + 8 * u) - (at0 + 16 * n + 8 * u + 4 * half);  // of the lane's four tokens
-#pragma unroll
-            for (int e = 0; e < kBlocks; ++e)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) va[n % 2][e][u][i] = i < end ? va[n % 2][e][u][i] : (short)0;
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < kBlocks; ++e) {
-          const s16x8_t v = __builtin_shufflevector(va[n % 2][e][0], va[n % 2][e][1], 0, 1, 2, 3, 4, 5, 6, 7);
-          acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), pb[n / 2][n % 2], acc[e], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    } else {
-      constexpr int kGroup = 2;  // tokens at a time, of each half
-      float va[2][kGroup][kBlocks];
-      auto read = [&](int n, float(&to)[kGroup][kBlocks]) {
-#pragma unroll
-        for (int u = 0; u < kGroup; ++u) {
-          const int i = n * kGroup + u;
-#pragma unroll
-          for (int e = 0; e < kBlocks; ++e)
-            to[u][e] = *(__attribute__((address_space(3))) const float*)(at[i % 4] + 8 * (i / 4) * L::kRowBytes + e * 128);
-        }
-      };
-      constexpr int kTurns = 16 * kHalves / kGroup;
-      read(0, va[0]);
-#pragma unroll
-      for (int n = 0; n < kTurns; ++n) {
-        if (n + 1 < kTurns) read(n + 1, va[(n + 1) % 2]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int u = 0; u < kGroup; ++u) {
-          const int i = n * kGroup + u, token = 8 * (i / 4) + i % 4;
-          if (!full) {
-            const bool here = at0 + token + 4 * half < end_of(token);
-#pragma unroll
-            for (int e = 0; e < kBlocks; ++e) va[n % 2][u][e] = here ? va[n % 2][u][e] : 0.f;
-          }
-#pragma unroll
-          for (int e = 0; e < kBlocks; ++e) acc[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(va[n % 2][u][e], p[i / 16][i % 16], acc[e], 0, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+    for (int i = 0; i < 16; ++i) {
+      const float w = weight(x[i]);
+      if constexpr (kBf16) p.b[i / 8][i % 8] = (__bf16)w;
+      else p.f[i] = w;
     }
   };
 
-  // Unit 2 t holds the keys of tile t, unit 2 t + 1 its values. kRing - 1 units are on their way or in work: a unit that has been worked on by all waves, which the
-  // barrier tells, is loaded again.
-  const int units = 2 * tiles;
-  uint32_t there = 0, there_next[L::kRing / 2 + 1];  // pages of the tile in work, and of those behind it
-#pragma unroll
-  for (int u = 0; u < L::kRing - 1; ++u) {
-    if (u < units) issue(u, u);
-    if (u % 2 == 0) there_next[u / 2] = there_ahead;
-  }
-  constexpr int kAhead = L::kRing - 1;             // units in flight, with the one that is waited for
-  constexpr int kTilesAhead = (kAhead + 1) / 2;    // tiles whose pages have been looked at
-  auto arrive = [&](int unit) {
-    wait_units<kAhead - 1, L::kLoads>(units - 1 - unit);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-  };
   int slot = 0;
   auto next = [&](int s) { return s + 1 == L::kRing ? 0 : s + 1; };
-  auto free_slot = [&](int s) { return s == 0 ? L::kRing - 1 : s - 1; };
-  for (int t = 0; t < tiles; ++t) {
-    there = there_next[0];
-#pragma unroll
-    for (int i = 0; i + 1 < kTilesAhead; ++i) there_next[i] = there_next[i + 1];
-    const int at0 = ((item.begin + t * tile_pages) << shift) + mine0;
-    const bool full = there == (1u << tile_pages) - 1 && at0 - mine0 + L::kTokens <= all_have;
-    arrive(2 * t);
-    if (2 * t + kAhead < units) issue(2 * t + kAhead, free_slot(slot));
-    if (kAhead % 2 == 0) there_next[kTilesAhead - 1] = there_ahead;
+  int taken = 0;  // units, with those of the step
+  auto arrive = [&](int units) {
+    taken += units;
+    const int left = loaded - taken;  // behind them
+    wait_units<L::kRing - 4 < 1 ? 1 : L::kRing - 4, L::kLoads>(left);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
+  // Slots of pages that there are not may hold anything, and a product with zero is not always zero.
+  auto blank = [&](int t, int s) {
+    if (!holes && t < pages / kTilePages) return;
+    const uint32_t there = there_at(t);
+    for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave)
+      if (!(there >> (i * 16 % L::kPlaneBytes / 128 / S) & 1)) *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(ring_at + s * L::kBytes + i * 16) = u32x4_t{0, 0, 0, 0};
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
+
+  arrive(1);
+  if (!idle) keys(slot);
+  slot = next(slot);
+  if (tiles > 1) {
+    arrive(1);
     if (!idle) {
+      prepare(0, x);
+      weights();
       keys(slot);
-      weights(full, there, at0);
     }
     slot = next(slot);
-    arrive(2 * t + 1);
-    if (2 * t + 1 + kAhead < units) issue(2 * t + 1 + kAhead, free_slot(slot));
-    if (kAhead % 2 == 1) there_next[kTilesAhead - 1] = there_ahead;
-    if (!idle) values(full, there, at0, slot);
+  } else if (!idle) {
+    prepare(0, x);
+    weights();
+  }
+  // Step t: from the logits x of tile t - 1 and the probabilities w of tile t - 2 to the logits y of tile t and the probabilities v of tile t - 1.
+  auto step = [&](int t, f32x16_t& x, f32x16_t& y, Weights& w, Weights& v) {
+    arrive(2);
+    // What the step before has used, which all waves are done with, takes the next two units.
+    if constexpr (L::kRing % 2 == 1) {
+      if (next_v < tiles) { load_values(); ++loaded; }
+    }
+    if (next_k < tiles) { load_keys(); ++loaded; }
+    if constexpr (L::kRing % 2 == 0) {
+      if (next_v < tiles) { load_values(); ++loaded; }
+    }
+    const int k_slot = slot, v_slot = next(slot);
+    slot = next(v_slot);
+    if (holes) blank(t - 2, v_slot);
+    if (idle) return;
+    const float alpha = prepare(t - 1, x);
+    constexpr int kEach = 16 / kSteps;  // exponentials between two products
+    const Keys k = keys_in(k_slot);
+    const Values u = values_in(v_slot);
+    u32x4_t kf[kFew];
+    bf16x8_t vf[kFew];
+    y = zero16();
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) {
+      kf[i] = k.read(i);
+      vf[i] = u.read(i);
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      y = product(kf[i % kFew], i, y);
+      if (i + kFew < kSteps) kf[i % kFew] = k.read(i + kFew);
+#pragma unroll
+      for (int j = i * kEach; j < (i + 1) * kEach; ++j) v.b[j / 8][j % 8] = (__bf16)weight(x[j]);
+      asm volatile("" : "+v"(l));  // here, and not where they are used
+      acc[i % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kFew], w.b[i / kBlocks], acc[i % kBlocks], 0, 0, 0);
+      if (i + kFew < kSteps) vf[i % kFew] = u.read(i + kFew);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    rescale(alpha);
+  };
+  if constexpr (kBf16) {
+    f32x16_t y;
+    Weights w;
+    int t = 2;
+    for (; t + 1 < tiles; t += 2) {  // by twos, so that nothing is copied
+      step(t, x, y, p, w);
+      step(t + 1, y, x, w, p);
+    }
+    if (t < tiles) {
+      step(t, x, y, p, w);
+      x = y;
+      p = w;
+    }
+  } else {
+    for (int t = 2; t < tiles; ++t) {
+      arrive(2);
+      if constexpr (L::kRing % 2 == 1) {
+        if (next_v < tiles) { load_values(); ++loaded; }
+      }
+      if (next_k < tiles) { load_keys(); ++loaded; }
+      if constexpr (L::kRing % 2 == 0) {
+        if (next_v < tiles) { load_values(); ++loaded; }
+      }
+      const int k_slot = slot, v_slot = next(slot);
+      slot = next(v_slot);
+      if (holes) blank(t - 2, v_slot);
+      if (!idle) {
+        const float alpha = prepare(t - 1, x);
+        values(v_slot);
+        rescale(alpha);
+        weights();
+        keys(k_slot);
+      }
+    }
+  }
+  auto load_last = [&] {  // the keys are all there
+    if (next_v < tiles) { load_values(); ++loaded; }
+  };
+  if (tiles > 1) {
+    arrive(1);
+    load_last();
+    blank(tiles - 2, slot);
+    if (!idle) {
+      const float alpha = prepare(tiles - 1, x);
+      values(slot);
+      rescale(alpha);
+      weights();
+    }
     slot = next(slot);
   }
+  arrive(1);
+  blank(tiles - 1, slot);
+  if (!idle) values(slot);
 
   l = with_lane_xor32(l, OpSum());
   if constexpr (kAlong > 1) {  // the waves that took other tokens of the same rows
@@ -414,6 +502,35 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
       *reinterpret_cast<float4*>(out + e * 32 + 8 * n + 4 * half) =
           make_float4(acc[e][4 * n], acc[e][4 * n + 1], acc[e][4 * n + 2], acc[e][4 * n + 3]);
   if (half == 0) *reinterpret_cast<float2*>(a.work.part_ml + part * 2) = make_float2(m, l);
+}
+
+// An item: a run of a prefix, or of a member's own pages, which the decode kernels' chunk code takes.
+template <typename T, int D, int S, int G, int kAcross, bool kNT>
+__global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c, PrefixArgs a) {
+  using L = Unit<T, D, kAcross>;
+  constexpr size_t kRingBytes = L::kRing * L::kBytes, kOwnBytes = sizeof(DecodeShared<T, D, G>);
+  __shared__ __attribute__((aligned(1024))) char ring[kRingBytes > kOwnBytes ? kRingBytes : kOwnBytes];
+  const int hkv = blockIdx.x & (c.Hkv - 1), index = blockIdx.x / c.Hkv;
+  const PrefixItem item = a.work.item[index];
+  if (index >= *a.work.num_items) return;
+  if (!item.own) {
+    attend_prefix<T, D, S, kAcross, kNT>(c, a, item, hkv, ring);
+    return;
+  }
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int b = item.seq, N = c.seq_lens[b];
+  const int64_t part = (int64_t)hkv * a.shape.max_rows + item.part;
+  const ChunkOut<T> to = {a.work.part_o + part * D, a.work.part_ml + part * 2, reinterpret_cast<T*>(a.out), a.lse_out, 2};
+  const Chunk chunk = {hkv, b, item.begin, item.end, N, 0};
+  auto lookup = [&](int e, bool, int& phys, int& ntok) {
+    const int ph = c.page_table[(int64_t)b * c.max_pages + e];
+    if (ph >= 0 && (int64_t)ph < c.num_phys) {
+      phys = ph;
+      ntok = min(S, N - e * S);
+    }
+  };
+  decode_chunk<D, S, G, kNT>(c, reinterpret_cast<const T*>(a.q), chunk, wave, lane, lookup, a.scale_log2, to,
+                             *reinterpret_cast<DecodeShared<T, D, G>*>(ring));
 }
 
 // A wave joins the parts of a (member, query head): o = sum of 2^(m_j - M) o_j over sum of 2^(m_j - M) l_j. Lane s takes the pair (m, l) of part s; D / 4 lanes
@@ -472,27 +589,43 @@ __global__ __launch_bounds__(kMergeWaves* kWave) void prefix_merge_kernel(CacheV
   }
 }
 
-}  // namespace
-
 // One translation unit per element type and head dimension: UNIQUE_ELEM, UNIQUE_DIM.
-template <>
-hipError_t launch_prefix_of<UNIQUE_ELEM, UNIQUE_DIM>(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
+template <int S, int G, int kAcross>
+hipError_t launch_items(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
   using T = UNIQUE_ELEM;
   auto go = [&](auto kernel) {
     kernel<<<dim3(c.Hkv * a.shape.max_items), dim3(kDecWaves * kWave), 0, st>>>(c, a);
     return hipGetLastError();
   };
-  hipError_t e;
-  const bool nt = a.streams != 0;
-  if constexpr (sizeof(T) == 2) {
-    if (a.shape.rows == 64) e = nt ? go(prefix_kernel<T, UNIQUE_DIM, 2, true>) : go(prefix_kernel<T, UNIQUE_DIM, 2, false>);
-    else e = nt ? go(prefix_kernel<T, UNIQUE_DIM, 4, true>) : go(prefix_kernel<T, UNIQUE_DIM, 4, false>);
-  } else {
-    e = nt ? go(prefix_kernel<T, UNIQUE_DIM, 4, true>) : go(prefix_kernel<T, UNIQUE_DIM, 4, false>);
+  return a.streams ? go(prefix_kernel<T, UNIQUE_DIM, S, G, kAcross, true>) : go(prefix_kernel<T, UNIQUE_DIM, S, G, kAcross, false>);
+}
+
+template <int S, int G>
+hipError_t launch_rows(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
+  if constexpr (sizeof(UNIQUE_ELEM) == 2)
+    if (a.shape.rows == 64) return launch_items<S, G, 2>(c, a, st);
+  return launch_items<S, G, 4>(c, a, st);
+}
+
+template <int S>
+hipError_t launch_group(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
+  switch (c.H / c.Hkv) {
+    case 1: return launch_rows<S, 1>(c, a, st);
+    case 2: return launch_rows<S, 2>(c, a, st);
+    case 4: return launch_rows<S, 4>(c, a, st);
+    case 8: return launch_rows<S, 8>(c, a, st);
+    default: return hipErrorInvalidValue;
   }
+}
+
+}  // namespace
+
+template <>
+hipError_t launch_prefix_of<UNIQUE_ELEM, UNIQUE_DIM>(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
+  const hipError_t e = c.S == 8 ? launch_group<8>(c, a, st) : (c.S == 16 ? launch_group<16>(c, a, st) : launch_group<32>(c, a, st));
   if (e != hipSuccess) return e;
   const int64_t outs = (int64_t)c.B * c.H;
-  prefix_merge_kernel<T, UNIQUE_DIM><<<dim3((unsigned)((outs + kMergeWaves - 1) / kMergeWaves)), dim3(kMergeWaves * kWave), 0, st>>>(c, a);
+  prefix_merge_kernel<UNIQUE_ELEM, UNIQUE_DIM><<<dim3((unsigned)((outs + kMergeWaves - 1) / kMergeWaves)), dim3(kMergeWaves * kWave), 0, st>>>(c, a);
   return hipGetLastError();
 }
 

@@ -21,6 +21,7 @@ __global__ __launch_bounds__(kItemThreads) void prefix_items_kernel(CacheView c,
   const bool held = sources <= kHeldSources;
   auto start_of = [&](int i) { return min(max(g.starts[i], 0), c.B); };
   auto prefix_of = [&](int i) { return min(max(g.prefix_pages[i], 0), g.max_prefix_pages); };
+  auto size_of = [&](int i) { return min(max(start_of(i + 1) - start_of(i), 0), g.max_members); };
   if (held) {  // ends of the groups, to find the members' in
     for (int i = t; i < n; i += kItemThreads) s_first[i] = g.starts[i + 1];
     __syncthreads();
@@ -30,10 +31,10 @@ __global__ __launch_bounds__(kItemThreads) void prefix_items_kernel(CacheView c,
   for (int i = t; i < sources; i += kItemThreads) {
     PrefixSource s = {};
     if (i < n) {
-      const int start = start_of(i), size = min(max(start_of(i + 1) - start, 0), g.max_members);
-      s.place = start;
+      const int size = size_of(i);
+      s.place = start_of(i);
       s.rows = size * G;
-      s.end = size > 0 ? prefix_of(i) : 0;
+      s.end = size > 1 ? prefix_of(i) : 0;  // (nobody to share it with: all pages are the member's own)
       s.blocks = (s.rows + a.shape.rows - 1) / a.shape.rows;
     } else {
       const int at = i - n;
@@ -53,8 +54,9 @@ __global__ __launch_bounds__(kItemThreads) void prefix_items_kernel(CacheView c,
           s.place = at;
           s.rows = G;
           s.blocks = 1;
-          s.begin = prefix_of(lo);
-          s.end = min(min((c.seq_lens[seq] + c.S - 1) / c.S, c.max_pages_hint), s.begin + g.max_own_pages);
+          const int prefix = prefix_of(lo);
+          s.begin = size_of(lo) > 1 ? prefix : 0;
+          s.end = min(min((c.seq_lens[seq] + c.S - 1) / c.S, c.max_pages_hint), prefix + g.max_own_pages);
         }
       }
       w.member[at] = m;
@@ -75,7 +77,7 @@ __global__ __launch_bounds__(kItemThreads) void prefix_items_kernel(CacheView c,
     const int i = i0 + t;
     PrefixSource s = {};
     if (i < sources) s = w.source[i];
-    const PrefixCut cut = prefix_cut(s.end - s.begin, item_pages, min(s.rows, a.shape.rows), c.S, a.shape.tile_pages);
+    const PrefixCut cut = prefix_cut(s.end - s.begin, item_pages, min(s.rows, a.shape.rows), c.S, a.shape.tile_pages, i >= n);
     const int mine = cut.count * s.blocks;
     int x[2] = {mine, mine * (i < n ? a.shape.rows : G)}, upto[2];
 #pragma unroll
@@ -134,7 +136,7 @@ __global__ __launch_bounds__(kItemThreads) void prefix_items_kernel(CacheView c,
     item.begin = s.begin + run * s.each;
     item.end = min(item.begin + s.each, s.end);
     item.seq = g.members ? g.members[s.place] : s.place;
-    item.limit = lo < n || item.seq < 0 || item.seq >= c.B ? INT32_MAX : c.seq_lens[item.seq];
+    item.own = lo >= n;
     item.part = s.first_row + k * (lo < n ? a.shape.rows : G);
     w.item[i] = item;
   }
@@ -143,7 +145,7 @@ __global__ __launch_bounds__(kItemThreads) void prefix_items_kernel(CacheView c,
 size_t aligned(size_t x) { return (x + 255) / 256 * 256; }
 
 PrefixShape shape_of(const CacheView& c, const unique_prefix_groups& g) {
-  return prefix_shape(c.B, c.Hkv, c.H / c.Hkv, c.dtype == 0 ? 4 : 2, c.S, g.num_groups, g.max_members);
+  return prefix_shape(c.B, c.Hkv, c.H / c.Hkv, c.dtype == 0 ? 4 : 2, c.S, g.num_groups, g.max_members, g.max_prefix_pages);
 }
 
 // Where everything lies in the workspace; -> its size.

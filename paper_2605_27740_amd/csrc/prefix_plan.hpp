@@ -10,6 +10,8 @@ namespace unique {
 // Every group is a source of items, its prefix's pages times the blocks of its members' query rows, and every member one, its own pages.
 constexpr int kPrefixSlots = 512;  // items that are wanted per launch: two workgroups to a compute unit
 
+constexpr int kPrefixMostPages = 512;  // of an item of a prefix, whose page ids are held in registers
+
 struct PrefixShape {
   int32_t rows;         // query rows of a workgroup's block
   int32_t tile_pages;   // pages of a tile of tokens, a power of two
@@ -18,15 +20,17 @@ struct PrefixShape {
   int32_t max_rows;     // rows of partial results at most, per KV head
 };
 
-inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members) {
+inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members, int max_prefix_pages) {
   PrefixShape s;
   const int64_t most = (int64_t)max_members * group;
   s.rows = elem == 4 ? 128 : (most <= 64 ? 64 : 128);
-  s.tile_pages = std::max((elem == 4 ? 32 : 64) / page_size, 1);
+  s.tile_pages = (s.rows == 64 ? 64 : 32) / page_size;
   s.wanted = std::max(kPrefixSlots / kv_heads, 1);
   const int64_t blocks = std::min<int64_t>(num_groups * ((most + s.rows - 1) / s.rows), (int64_t)batch * group / s.rows + num_groups);
-  s.max_items = (int32_t)(s.wanted + blocks + batch);
-  s.max_rows = (int32_t)((s.wanted + blocks) * s.rows + (int64_t)(s.wanted + batch) * group);
+  // of prefixes: the wanted ones or the longest, and one more for each block
+  const int64_t of_prefixes = std::max<int64_t>(s.wanted, blocks * max_prefix_pages / kPrefixMostPages) + blocks;
+  s.max_items = (int32_t)(of_prefixes + s.wanted + batch);
+  s.max_rows = (int32_t)(of_prefixes * s.rows + (int64_t)(s.wanted + batch) * group);
   return s;
 }
 
@@ -38,10 +42,11 @@ constexpr int64_t prefix_item_pages(int64_t all_pages, int wanted) { return (all
 struct PrefixCut {
   int32_t count, pages;
 };
-constexpr PrefixCut prefix_cut(int pages, int64_t item_pages, int live_rows, int page_size, int tile_pages) {
+constexpr PrefixCut prefix_cut(int pages, int64_t item_pages, int live_rows, int page_size, int tile_pages, bool own) {
   if (pages <= 0) return PrefixCut{0, tile_pages};
   const int64_t least = (2ll * live_rows + page_size - 1) / page_size;
-  const int64_t p = item_pages > least ? item_pages : least;
+  int64_t p = item_pages > least ? item_pages : least;
+  if (!own && p > kPrefixMostPages) p = kPrefixMostPages;
   const int64_t n = (pages + p - 1) / p;
   int64_t each = (pages + n - 1) / n;
   each = (each + tile_pages - 1) / tile_pages * tile_pages;

@@ -32,7 +32,7 @@ struct PrefixItem {
   int32_t place, rows;   // first member, query rows
   int32_t begin, end;    // pages
   int32_t seq;           // the sequence whose row of the page table it goes by
-  int32_t limit;         // tokens that are there (a prefix's pages are full)
+  int32_t own;           // 1: a member's own pages
   int32_t part;          // first row of its partial results
   int32_t reserved;
 };
