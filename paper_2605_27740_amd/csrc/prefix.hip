@@ -295,6 +295,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   // Before the exponentials of tile t: tokens that do not count, and the reference. -> what earlier sums are to be multiplied by, as soon as the tile
   // before, whose probabilities are relative to the old reference, has been added to them.
   const int whole = holes ? 0 : min(pages / kTilePages, (all_have / S - item.begin) / kTilePages);  // tiles of which all tokens count for all rows
+  bool moved = false;  // uniform
   auto prepare = [&](int t, f32x16_t& x) {
     if (t >= whole) {
       const uint32_t there = there_at(t);
@@ -311,7 +312,8 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
     top *= a.scale_log2;
     float alpha = 1.f;
-    if (__any(top > m)) {
+    moved = __any(top > m);
+    if (moved) {
       const float mnew = fmaxf(m, with_lane_xor32(top, OpMax()) + kRoom);
       alpha = fast_exp2(m - mnew);
       m = mnew;
@@ -325,7 +327,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     return w;
   };
   auto rescale = [&](float alpha) {
-    if (__any(alpha != 1.f)) {
+    if (moved) {
 #pragma unroll
       for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
@@ -378,17 +380,21 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   auto step = [&](int t, f32x16_t& x, f32x16_t& y, Weights& w, Weights& v) {
     arrive(2);
     // What the step before has used, which all waves are done with, takes the next two units.
-    if constexpr (L::kRing % 2 == 1) {
-      if (next_v < tiles) { load_values(); ++loaded; }
-    }
-    if (next_k < tiles) { load_keys(); ++loaded; }
-    if constexpr (L::kRing % 2 == 0) {
-      if (next_v < tiles) { load_values(); ++loaded; }
-    }
+    auto load_one = [&](bool keys) {
+      if (keys ? next_k < tiles : next_v < tiles) {
+        if (keys) load_keys();
+        else load_values();
+        ++loaded;
+      }
+    };
     const int k_slot = slot, v_slot = next(slot);
     slot = next(v_slot);
     if (holes) blank(t - 2, v_slot);
-    if (idle) return;
+    if (idle) {
+      load_one(L::kRing % 2 == 0);
+      load_one(L::kRing % 2 == 1);
+      return;
+    }
     const float alpha = prepare(t - 1, x);
     constexpr int kEach = 16 / kSteps;  // exponentials between two products
     const Keys k = keys_in(k_slot);
@@ -411,6 +417,8 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       acc[i % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kFew], w.b[i / kBlocks], acc[i % kBlocks], 0, 0, 0);
       if (i + kFew < kSteps) vf[i % kFew] = u.read(i + kFew);
       __builtin_amdgcn_sched_barrier(0);
+      if (i == 0) load_one(L::kRing % 2 == 0);  // while products are in work
+      if (i == kSteps / 2) load_one(L::kRing % 2 == 1);
     }
     rescale(alpha);
   };
@@ -550,23 +558,29 @@ __global__ __launch_bounds__(kMergeWaves* kWave) void prefix_merge_kernel(CacheV
   const float2* ml = reinterpret_cast<const float2*>(a.work.part_ml);
   const float2 none = make_float2(kNegBig, 0.f);
 
+  const int sub = lane / kLanes, channel = lane % kLanes * 4;
+  float4 v[kAhead];
+  auto request = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      if (s0 + u * kParts < n) v[u] = *reinterpret_cast<const float4*>(a.work.part_o + row_of(min(s0 + u * kParts + sub, n - 1)) * D + channel);  // uniform
+  };
   const float2 first = lane < n ? ml[row_of(lane)] : none;
+  request(0);
   float M = first.x;
   for (int s0 = kWave; s0 < n; s0 += kWave) M = fmaxf(M, s0 + lane < n ? ml[row_of(s0 + lane)].x : kNegBig);
   M = group_allreduce<kWave>(M, OpMax());
   float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  const int sub = lane / kLanes, channel = lane % kLanes * 4;
   for (int s0 = 0; s0 < n; s0 += kWave) {
     const float2 p = s0 == 0 ? first : (s0 + lane < n ? ml[row_of(s0 + lane)] : none);
     const float scale = fast_exp2(p.x - M);
     L = fmaf(p.y, scale, L);
     const int here = min(kWave, n - s0);
     for (int j0 = 0; j0 < here; j0 += kParts * kAhead) {
-      float4 v[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) v[u] = *reinterpret_cast<const float4*>(a.work.part_o + row_of(min(s0 + j0 + u * kParts + sub, n - 1)) * D + channel);
+      if (s0 + j0 > 0) request(s0 + j0);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
+        if (j0 + u * kParts >= here) break;  // uniform
         const int j = j0 + u * kParts + sub;
         const float of_j = __shfl(scale, j % kWave, kWave);  // by all lanes, as any may be asked for its own
         const float sc = j < here ? of_j : 0.f;

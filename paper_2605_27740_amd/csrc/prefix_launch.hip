@@ -6,138 +6,159 @@ namespace unique {
 namespace {
 
 constexpr int kItemThreads = 1024, kItemWaves = kItemThreads / kWave;
-constexpr int kHeldSources = 2048;  // sources whose first items are searched in the LDS
+constexpr int kHeldSources = kItemThreads;  // sources that are kept in the LDS
+constexpr int kClasses = 3;                 // items come in this order: prefixes', long ones of members, short ones of members
 
 // One workgroup makes the items: what each source has to read, how long items have to be for the chip to be full, where each source's items and
-// partial results begin, and the items. Groups come first, as theirs have the most to do.
+// partial results begin, and the items. kHeld: there is a thread for every source, and their number is the only loop.
+template <bool kHeld>
 __global__ __launch_bounds__(kItemThreads) void prefix_items_kernel(CacheView c, PrefixArgs a) {
-  __shared__ int s_first[kHeldSources + 1];
-  __shared__ int64_t s_pages[kItemWaves];
-  __shared__ int s_scan[2][kItemWaves];
+  __shared__ PrefixSource s_source[kHeld ? kHeldSources : 1];
+  __shared__ int s_first[kClasses][kHeld ? kHeldSources : 1];  // items of a class before each source's
+  __shared__ int64_t s_cost[kItemWaves];
+  __shared__ int s_scan[kClasses + 1][kItemWaves];
   const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
   const int n = a.groups.num_groups, sources = n + c.B, G = c.H / c.Hkv;
   const unique_prefix_groups& g = a.groups;
   const PrefixWork& w = a.work;
-  const bool held = sources <= kHeldSources;
-  auto start_of = [&](int i) { return min(max(g.starts[i], 0), c.B); };
-  auto prefix_of = [&](int i) { return min(max(g.prefix_pages[i], 0), g.max_prefix_pages); };
-  auto size_of = [&](int i) { return min(max(start_of(i + 1) - start_of(i), 0), g.max_members); };
-  if (held) {  // ends of the groups, to find the members' in
-    for (int i = t; i < n; i += kItemThreads) s_first[i] = g.starts[i + 1];
-    __syncthreads();
-  }
+  PrefixSource* const source = kHeld ? s_source : w.source;
+  auto first_of = [&](int k, int i) -> int& { return kHeld ? s_first[k][i] : w.first[(int64_t)k * sources + i]; };
+  auto bound = [&](int at) { return min(max(at, 0), c.B); };
+  auto prefix_of = [&](int pages) { return min(max(pages, 0), g.max_prefix_pages); };
+  auto size_of = [&](int from, int to) { return min(max(bound(to) - bound(from), 0), g.max_members); };
 
-  int64_t pages = 0;
-  for (int i = t; i < sources; i += kItemThreads) {
+  // What a source has to read. A member's group is the first that ends behind it.
+  auto look_at = [&](int i, PrefixMember& m) {
     PrefixSource s = {};
     if (i < n) {
-      const int size = size_of(i);
-      s.place = start_of(i);
+      const int from = g.starts[i], to = g.starts[i + 1], pages = g.prefix_pages[i], size = size_of(from, to);
+      s.place = bound(from);
       s.rows = size * G;
-      s.end = size > 1 ? prefix_of(i) : 0;  // (nobody to share it with: all pages are the member's own)
+      s.end = size > 1 ? prefix_of(pages) : 0;  // (nobody to share it with: all pages are the member's own)
       s.blocks = (s.rows + a.shape.rows - 1) / a.shape.rows;
-    } else {
-      const int at = i - n;
-      int lo = 0, hi = n;  // the first group that ends behind it
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if ((held ? s_first[mid] : g.starts[mid + 1]) > at) hi = mid;
-        else lo = mid + 1;
-      }
-      PrefixMember m = {};
-      m.seq = -1;
-      if (lo < n && at >= g.starts[lo] && at - g.starts[lo] < g.max_members) {
-        const int seq = g.members ? g.members[at] : at;
-        if (seq >= 0 && seq < c.B) {
-          m.seq = seq;
-          m.reserved[0] = lo;
-          s.place = at;
-          s.rows = G;
-          s.blocks = 1;
-          const int prefix = prefix_of(lo);
-          s.begin = size_of(lo) > 1 ? prefix : 0;
-          s.end = min(min((c.seq_lens[seq] + c.S - 1) / c.S, c.max_pages_hint), prefix + g.max_own_pages);
-        }
-      }
-      w.member[at] = m;
+      return s;
     }
-    w.source[i] = s;
-    pages += (int64_t)max(s.end - s.begin, 0) * s.blocks;
+    const int at = i - n, seq = g.members ? g.members[at] : at;
+    int lo = 0, hi = n;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (g.starts[mid + 1] > at) hi = mid;
+      else lo = mid + 1;
+    }
+    m = {};
+    m.seq = -1;
+    if (lo == n) return s;
+    const int from = g.starts[lo], to = g.starts[lo + 1], prefix = prefix_of(g.prefix_pages[lo]);
+    if (at < from || at - from >= g.max_members || seq < 0 || seq >= c.B) return s;
+    m.seq = seq;
+    m.group = lo;
+    s.place = at;
+    s.rows = G;
+    s.blocks = 1;
+    s.begin = size_of(from, to) > 1 ? prefix : 0;
+    s.end = min(min((c.seq_lens[seq] + c.S - 1) / c.S, c.max_pages_hint), prefix + g.max_own_pages);
+    return s;
+  };
+  auto cost_of = [&](int i, const PrefixSource& s) { return prefix_cost(s.end - s.begin, s.blocks, i >= n, c.S); };
+
+  PrefixSource s = {};
+  PrefixMember m = {};
+  int64_t cost = 0;
+  for (int i = t; i < sources; i += kItemThreads) {
+    s = look_at(i, m);
+    cost += cost_of(i, s);
+    if constexpr (!kHeld) {
+      w.source[i] = s;
+      if (i >= n) w.member[i - n] = m;
+    }
   }
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) pages += __shfl_xor(pages, d, kWave);
-  if (lane == 0) s_pages[wave] = pages;
+  for (int d = 1; d < kWave; d *= 2) cost += __shfl_xor(cost, d, kWave);
+  if (lane == 0) s_cost[wave] = cost;
   __syncthreads();
-  pages = 0;
-  for (int i = 0; i < kItemWaves; ++i) pages += s_pages[i];
-  const int64_t item_pages = prefix_item_pages(pages, a.shape.wanted);
+  cost = lane < kItemWaves ? s_cost[lane] : 0;
+#pragma unroll
+  for (int d = 1; d < kItemWaves; d *= 2) cost += __shfl_xor(cost, d, kWave);
+  const int64_t item_pages = prefix_item_pages(__shfl(cost, 0, kWave), a.shape.wanted);
 
-  int items = 0, rows = 0;  // before the strip
+  int before[kClasses + 1] = {0, 0, 0, 0};  // items of each class and rows before the strip
   for (int i0 = 0; i0 < sources; i0 += kItemThreads) {
     const int i = i0 + t;
-    PrefixSource s = {};
-    if (i < sources) s = w.source[i];
+    if constexpr (!kHeld) s = i < sources ? w.source[i] : PrefixSource{};
     const PrefixCut cut = prefix_cut(s.end - s.begin, item_pages, min(s.rows, a.shape.rows), c.S, a.shape.tile_pages, i >= n);
     const int mine = cut.count * s.blocks;
-    int x[2] = {mine, mine * (i < n ? a.shape.rows : G)}, upto[2];
+    s.kind = i < n ? 0 : (2 * (int64_t)min(cut.pages, s.end - s.begin) >= item_pages ? 1 : 2);
+    int x[kClasses + 1], upto[kClasses + 1];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) upto[k] = wave_inclusive_scan(x[k]);
+    for (int k = 0; k < kClasses; ++k) x[k] = s.kind == k ? mine : 0;
+    x[kClasses] = mine * (i < n ? a.shape.rows : G);
+#pragma unroll
+    for (int k = 0; k <= kClasses; ++k) upto[k] = wave_inclusive_scan(x[k]);
     __syncthreads();
     if (lane == kWave - 1) {
-      s_scan[0][wave] = upto[0];
-      s_scan[1][wave] = upto[1];
+#pragma unroll
+      for (int k = 0; k <= kClasses; ++k) s_scan[k][wave] = upto[k];
     }
     __syncthreads();
-    int all[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k <= kClasses; ++k) {
       const int waves = wave_inclusive_scan(lane < kItemWaves ? s_scan[k][lane] : 0);
-      if (wave > 0) upto[k] += __builtin_amdgcn_readlane(waves, wave - 1);
-      all[k] = __builtin_amdgcn_readlane(waves, kWave - 1);
+      upto[k] += before[k] + (wave > 0 ? __builtin_amdgcn_readlane(waves, wave - 1) : 0);
+      before[k] += __builtin_amdgcn_readlane(waves, kWave - 1);
     }
-    s.first_item = items + upto[0] - x[0];
-    s.first_row = rows + upto[1] - x[1];
+    s.first_row = upto[kClasses] - x[kClasses];
+    s.count = cut.count;
     s.each = cut.pages;
     if (i < sources) {
-      w.source[i] = s;
-      if (held) s_first[i] = s.first_item;
+      source[i] = s;
+#pragma unroll
+      for (int k = 0; k < kClasses; ++k) first_of(k, i) = upto[k] - x[k];
     }
-    items += all[0];
-    rows += all[1];
   }
+  const int items = before[0] + before[1] + before[2];
   if (t == 0) *w.num_items = items;
-  __threadfence_block();
+  if constexpr (!kHeld) __threadfence_block();
   __syncthreads();
 
-  for (int at = t; at < c.B; at += kItemThreads) {
-    PrefixMember m = w.member[at];
-    if (m.seq < 0) continue;
-    const PrefixSource s = w.source[m.reserved[0]], own = w.source[n + at];
-    const int row = (at - s.place) * G;
-    m.count = s.end > 0 ? (s.end + s.each - 1) / s.each : 0;
-    m.part = s.first_row + row;  // blocks follow one another
-    m.step = s.blocks * a.shape.rows;
-    m.own_count = own.end > own.begin ? (own.end - own.begin + own.each - 1) / own.each : 0;
-    m.own_part = own.first_row;
-    w.member[at] = m;
+  for (int i = n + t % kItemThreads - (kHeld ? n : 0); i < sources; i += kItemThreads) {
+    if (i < n) continue;
+    if constexpr (!kHeld) m = w.member[i - n];
+    if (m.seq >= 0) {
+      const PrefixSource of = source[m.group], own = source[i];
+      m.count = of.count;
+      m.part = of.first_row + (i - n - of.place) * G;  // blocks follow one another
+      m.step = of.blocks * a.shape.rows;
+      m.own_count = own.count;
+      m.own_part = own.first_row;
+    }
+    w.member[i - n] = m;
   }
   for (int i = t; i < items; i += kItemThreads) {
-    int lo = 0, hi = sources - 1;  // the last source that begins at or before it and has items
+    int k = 0, y = i;
+    if (y >= before[0]) {
+      y -= before[0];
+      k = 1;
+      if (y >= before[1]) {
+        y -= before[1];
+        k = 2;
+      }
+    }
+    int lo = 0, hi = sources - 1;  // the last source whose items of this class begin at or before it
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
-      if ((held ? s_first[mid] : w.source[mid].first_item) <= i) lo = mid;
+      if (first_of(k, mid) <= y) lo = mid;
       else hi = mid - 1;
     }
-    const PrefixSource s = w.source[lo];
-    const int k = i - s.first_item, run = k / s.blocks, block = k - run * s.blocks;
+    const PrefixSource of = source[lo];
+    const int z = y - first_of(k, lo), run = z / of.blocks, block = z - run * of.blocks;
     PrefixItem item = {};
-    item.place = s.place + block * (a.shape.rows / G);
-    item.rows = min(s.rows - block * a.shape.rows, a.shape.rows);
-    item.begin = s.begin + run * s.each;
-    item.end = min(item.begin + s.each, s.end);
-    item.seq = g.members ? g.members[s.place] : s.place;
-    item.own = lo >= n;
-    item.part = s.first_row + k * (lo < n ? a.shape.rows : G);
+    item.place = of.place + block * (a.shape.rows / G);
+    item.rows = min(of.rows - block * a.shape.rows, a.shape.rows);
+    item.begin = of.begin + run * of.each;
+    item.end = min(item.begin + of.each, of.end);
+    item.seq = g.members ? g.members[of.place] : of.place;
+    item.own = k != 0;
+    item.part = of.first_row + z * (k == 0 ? a.shape.rows : G);
     w.item[i] = item;
   }
 }
@@ -156,7 +177,9 @@ size_t lay_out(const CacheView& c, const unique_prefix_groups& g, const PrefixSh
     at += aligned(count * sizeof(**p));
   };
   take(&w->num_items, 1);
-  take(&w->source, (size_t)g.num_groups + c.B);
+  const size_t sources = (size_t)g.num_groups + c.B, kept = sources > kHeldSources ? sources : 0;
+  take(&w->source, kept);
+  take(&w->first, kept * kClasses);
   take(&w->item, (size_t)s.max_items);
   take(&w->member, (size_t)c.B);
   take(&w->part_o, (size_t)c.Hkv * s.max_rows * c.D);
@@ -178,7 +201,8 @@ hipError_t launch_prefix(const CacheView& c, const unique_prefix_groups& g, cons
   const bool streams = pages * c.Hkv * c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2) > kStreamNtBytes;
   PrefixArgs a = {g, q, scale_log2, streams, out, lse_out, shape_of(c, g), {}};
   lay_out(c, g, a.shape, reinterpret_cast<char*>(workspace), &a.work);
-  prefix_items_kernel<<<dim3(1), dim3(kItemThreads), 0, st>>>(c, a);
+  if (g.num_groups + c.B <= kHeldSources) prefix_items_kernel<true><<<dim3(1), dim3(kItemThreads), 0, st>>>(c, a);
+  else prefix_items_kernel<false><<<dim3(1), dim3(kItemThreads), 0, st>>>(c, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (c.dtype == 0) return c.D == 64 ? launch_prefix_of<float, 64>(c, a, st) : launch_prefix_of<float, 128>(c, a, st);

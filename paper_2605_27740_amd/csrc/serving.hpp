@@ -23,8 +23,10 @@ hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t st
 
 // A prefix of a group, or a member's own pages.
 struct PrefixSource {
-  int32_t first_item, first_row;  // of its items and of their partial results
-  int32_t begin, end, each;       // pages, and those of an item
+  int32_t kind;                   // its items' class
+  int32_t first_row;              // of their partial results
+  int32_t begin, end;             // pages,
+  int32_t each, count;            // those of an item, and items along them
   int32_t blocks;                 // of query rows; items of a block follow those of the next, a run of pages after the other
   int32_t place, rows;            // its first member, and its query rows
 };
@@ -40,11 +42,13 @@ struct PrefixMember {
   int32_t seq;                       // < 0: left out
   int32_t count, part, step;         // of the group's items: how many, the row of the first's partial results, rows from one to the next
   int32_t own_count, own_part;       // of its own
-  int32_t reserved[2];
+  int32_t group;
+  int32_t reserved;
 };
 struct PrefixWork {
   int32_t* num_items;    // one number
-  PrefixSource* source;  // [groups + batch]
+  PrefixSource* source;  // [groups + batch], and the items of each class before theirs, where they are more than the kernel that makes
+  int32_t* first;        // [3][groups + batch]   the items holds
   PrefixItem* item;      // [max_items]
   PrefixMember* member;  // [batch]
   float* part_o;         // [kv_heads][max_rows][D]
