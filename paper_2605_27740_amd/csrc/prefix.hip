@@ -47,12 +47,12 @@ __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, lds_
 // workgroup; the others take other tokens, 32 each.
 template <typename T, int D, int kAcross>
 struct Unit {
-  static constexpr int kPlanes = D * (int)sizeof(T) / 128, kTokens = 32 * kDecWaves / kAcross;
+  static constexpr int kPlanes = D * (int)sizeof(T) / 128, kTokens = sizeof(T) == 2 ? 64 : 32;
   static constexpr int kPlaneBytes = kTokens * 128, kBytes = kPlanes * kPlaneBytes;
   static constexpr int kRuns = kTokens / 8 / kDecWaves;  // of eight tokens, which a wave loads a kilobyte of each plane of
   static constexpr int kLoads = kRuns * kPlanes;         // of a wave
-  static constexpr int kMost = kTokens == 64 ? 6 : 10;
-  static constexpr int kRing = 80 * 1024 / kBytes < kMost ? 80 * 1024 / kBytes : kMost;  // units in the LDS
+  static constexpr int kRing = 80 * 1024 / kBytes;       // units in the LDS
+  static constexpr int kHalves = kTokens * kAcross / kDecWaves / 32;  // blocks of 32 tokens of a tile that a wave takes, one or two
 };
 
 // Until all but the newest `left` units (kMost at most) have arrived.
@@ -72,7 +72,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   constexpr int kBlocks = D / 32;                    // of channels
   constexpr int kAlong = kDecWaves / kAcross;
   constexpr int kTilePages = L::kTokens / S;
-  constexpr int kLag = 2;
+  constexpr int kLag = 3 - L::kHalves;
   constexpr float kRoom = 6.f;                       // log2: how far above the largest logit the reference is put
   constexpr int kIds = kPrefixMostPages / kWave;     // page ids in a lane
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -147,9 +147,9 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     v_lane = (v_lane + kTilePages) % kWave;
     ++next_v;
   };
-  // Units go into the ring in the order in which the steps need them, K0 K1 K2 V0 K3 V1 ...: step t takes the keys of tile t and the values of tile t - 2.
+  // Units go into the ring in the order in which the steps need them, K0 K1 K2 V0 K3 V1 ...: step t takes the keys of tile t and the values of tile t - kLag.
   int loaded = 0;
-  for (; loaded < L::kRing && next_v < tiles; ++loaded) {
+  for (; loaded < L::kRing - (L::kHalves - 1) && next_v < tiles; ++loaded) {
     if (next_k < tiles && next_k <= next_v + kLag) load_keys();
     else load_values();
   }
@@ -193,10 +193,10 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       return *(__attribute__((address_space(3))) const u32x4_t*)(at[s % kWays] + s / kWays * L::kPlaneBytes);
     }
   };
-  auto keys_in = [&](int slot) {
+  auto keys_in = [&](int slot, int h) {
     Keys k;
 #pragma unroll
-    for (int s = 0; s < kWays; ++s) k.at[s] = (lds_char_t)(uintptr_t)(k_at[s] + slot * L::kBytes);
+    for (int s = 0; s < kWays; ++s) k.at[s] = (lds_char_t)(uintptr_t)(k_at[s] + slot * L::kBytes) + h * 32 * 128;
     return k;
   };
   struct Values {
@@ -214,10 +214,10 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       return *(__attribute__((address_space(3))) const float*)(at[i % 8] + i / 8 * 16 * 128 + e * L::kPlaneBytes);
     }
   };
-  auto values_in = [&](int slot) {
+  auto values_in = [&](int slot, int h) {
     Values v;
 #pragma unroll
-    for (int i = 0; i < (kBf16 ? 4 : 8); ++i) v.at[i] = (lds_char_t)(uintptr_t)(v_at[i] + slot * L::kBytes);
+    for (int i = 0; i < (kBf16 ? 4 : 8); ++i) v.at[i] = (lds_char_t)(uintptr_t)(v_at[i] + slot * L::kBytes) + h * 32 * 128;
     return v;
   };
 
@@ -250,8 +250,8 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   };
   // Operands are read a few ahead (left to itself the compiler reads one at a time and waits for it).
   constexpr int kFew = kBf16 ? 4 : 2;
-  auto keys = [&](int slot) {
-    const Keys k = keys_in(slot);
+  auto keys = [&](int slot, int h) {
+    const Keys k = keys_in(slot, h);
     u32x4_t few[kFew];
 #pragma unroll
     for (int s = 0; s < kFew; ++s) few[s] = k.read(s);
@@ -263,8 +263,8 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  auto values = [&](int slot) {
-    const Values v = values_in(slot);
+  auto values = [&](int slot, int h) {
+    const Values v = values_in(slot, h);
     if constexpr (kBf16) {
       bf16x8_t few[kFew];
 #pragma unroll
@@ -292,19 +292,19 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       }
     }
   };
-  // Before the exponentials of tile t: tokens that do not count, and the reference. -> what earlier sums are to be multiplied by, as soon as the tile
+  // Before the exponentials of block h of tile t: tokens that do not count, and the reference. -> what earlier sums are to be multiplied by, as soon as the block
   // before, whose probabilities are relative to the old reference, has been added to them.
   const int whole = holes ? 0 : min(pages / kTilePages, (all_have / S - item.begin) / kTilePages);  // tiles of which all tokens count for all rows
   bool moved = false;  // uniform
-  auto prepare = [&](int t, f32x16_t& x) {
+  auto prepare = [&](int t, int h, f32x16_t& x) {
     if (t >= whole) {
       const uint32_t there = there_at(t);
-      const int at0 = (item.begin + t * kTilePages) * S;
+      const int first = (along + h) * 32, at0 = (item.begin + t * kTilePages) * S + first;
 #pragma unroll
       for (int n = 0; n < 4; ++n) {  // pages are whole eights of tokens
-        const int end = there >> ((along * 32 + 8 * n) / S) & 1 ? tokens : 0;
+        const int end = there >> ((first + 8 * n) / S) & 1 ? tokens : 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * n + i] = at0 + along * 32 + 8 * n + 4 * half + i < end ? x[4 * n + i] : -INFINITY;
+        for (int i = 0; i < 4; ++i) x[4 * n + i] = at0 + 8 * n + 4 * half + i < end ? x[4 * n + i] : -INFINITY;
       }
     }
     float top = x[0];
@@ -361,44 +361,19 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
 
-  arrive(1);
-  if (!idle) keys(slot);
-  slot = next(slot);
-  if (tiles > 1) {
-    arrive(1);
-    if (!idle) {
-      prepare(0, x);
-      weights();
-      keys(slot);
+  // What a step has used, which all waves are done with at the next, takes the next two units, in their order.
+  auto load_one = [&](bool keys) {
+    if (keys ? next_k < tiles : next_v < tiles) {
+      if (keys) load_keys();
+      else load_values();
+      ++loaded;
     }
-    slot = next(slot);
-  } else if (!idle) {
-    prepare(0, x);
-    weights();
-  }
-  // Step t: from the logits x of tile t - 1 and the probabilities w of tile t - 2 to the logits y of tile t and the probabilities v of tile t - 1.
-  auto step = [&](int t, f32x16_t& x, f32x16_t& y, Weights& w, Weights& v) {
-    arrive(2);
-    // What the step before has used, which all waves are done with, takes the next two units.
-    auto load_one = [&](bool keys) {
-      if (keys ? next_k < tiles : next_v < tiles) {
-        if (keys) load_keys();
-        else load_values();
-        ++loaded;
-      }
-    };
-    const int k_slot = slot, v_slot = next(slot);
-    slot = next(v_slot);
-    if (holes) blank(t - 2, v_slot);
-    if (idle) {
-      load_one(L::kRing % 2 == 0);
-      load_one(L::kRing % 2 == 1);
-      return;
-    }
-    const float alpha = prepare(t - 1, x);
+  };
+  constexpr bool kKeysFirst = L::kRing % 2 == 0;
+  // From the logits x of a block (block h of tile t) and the probabilities w of the one before to the logits y of the next and the probabilities v of this one.
+  auto block = [&](int t, int h, const Keys& k, const Values& u, f32x16_t& x, f32x16_t& y, Weights& w, Weights& v, auto load_now) {
+    const float alpha = prepare(t, h, x);
     constexpr int kEach = 16 / kSteps;  // exponentials between two products
-    const Keys k = keys_in(k_slot);
-    const Values u = values_in(v_slot);
     u32x4_t kf[kFew];
     bf16x8_t vf[kFew];
     y = zero16();
@@ -417,64 +392,113 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       acc[i % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kFew], w.b[i / kBlocks], acc[i % kBlocks], 0, 0, 0);
       if (i + kFew < kSteps) vf[i % kFew] = u.read(i + kFew);
       __builtin_amdgcn_sched_barrier(0);
-      if (i == 0) load_one(L::kRing % 2 == 0);  // while products are in work
-      if (i == kSteps / 2) load_one(L::kRing % 2 == 1);
+      load_now(i);  // while products are in work
     }
     rescale(alpha);
   };
-  if constexpr (kBf16) {
+
+  arrive(1);
+  if (!idle) keys(slot, 0);
+  if constexpr (L::kHalves == 2) {
+    if (!idle) {
+      prepare(0, 0, x);
+      weights();
+      keys(slot, 1);
+    }
+    slot = next(slot);
     f32x16_t y;
     Weights w;
-    int t = 2;
-    for (; t + 1 < tiles; t += 2) {  // by twos, so that nothing is copied
-      step(t, x, y, p, w);
-      step(t + 1, y, x, w, p);
+    for (int t = 1; t < tiles; ++t) {
+      arrive(2);
+      const int k_slot = slot, v_slot = next(slot);
+      slot = next(v_slot);
+      if (holes) blank(t - 1, v_slot);
+      if (idle) {
+        load_one(kKeysFirst);
+        load_one(!kKeysFirst);
+        continue;
+      }
+      block(t - 1, 1, keys_in(k_slot, 0), values_in(v_slot, 0), x, y, p, w, [&](int i) { if (i == 0) load_one(kKeysFirst); });
+      block(t, 0, keys_in(k_slot, 1), values_in(v_slot, 1), y, x, w, p, [&](int i) { if (i == 0) load_one(!kKeysFirst); });
     }
-    if (t < tiles) {
-      step(t, x, y, p, w);
-      x = y;
-      p = w;
+    arrive(1);
+    blank(tiles - 1, slot);
+    if (!idle) {
+      const float alpha = prepare(tiles - 1, 1, x);
+      values(slot, 0);
+      rescale(alpha);
+      weights();
+      values(slot, 1);
     }
   } else {
-    for (int t = 2; t < tiles; ++t) {
+    slot = next(slot);
+    if (tiles > 1) {
+      arrive(1);
+      if (!idle) {
+        prepare(0, 0, x);
+        weights();
+        keys(slot, 0);
+      }
+      slot = next(slot);
+    } else if (!idle) {
+      prepare(0, 0, x);
+      weights();
+    }
+    auto step = [&](int t, f32x16_t& x, f32x16_t& y, Weights& w, Weights& v) {
       arrive(2);
-      if constexpr (L::kRing % 2 == 1) {
-        if (next_v < tiles) { load_values(); ++loaded; }
-      }
-      if (next_k < tiles) { load_keys(); ++loaded; }
-      if constexpr (L::kRing % 2 == 0) {
-        if (next_v < tiles) { load_values(); ++loaded; }
-      }
       const int k_slot = slot, v_slot = next(slot);
       slot = next(v_slot);
       if (holes) blank(t - 2, v_slot);
-      if (!idle) {
-        const float alpha = prepare(t - 1, x);
-        values(v_slot);
+      if (!kBf16 || idle) {
+        load_one(kKeysFirst);
+        load_one(!kKeysFirst);
+        if (idle) return;
+      }
+      if constexpr (kBf16) {
+        block(t - 1, 0, keys_in(k_slot, 0), values_in(v_slot, 0), x, y, w, v, [&](int i) {
+          if (i == 0) load_one(kKeysFirst);
+          if (i == kSteps / 2) load_one(!kKeysFirst);
+        });
+      } else {
+        const float alpha = prepare(t - 1, 0, x);
+        values(v_slot, 0);
         rescale(alpha);
         weights();
-        keys(k_slot);
+        keys(k_slot, 0);
       }
+    };
+    if constexpr (kBf16) {
+      f32x16_t y;
+      Weights w;
+      int t = 2;
+      for (; t + 1 < tiles; t += 2) {  // by twos, so that nothing is copied
+        step(t, x, y, p, w);
+        step(t + 1, y, x, w, p);
+      }
+      if (t < tiles) {
+        step(t, x, y, p, w);
+        x = y;
+        p = w;
+      }
+    } else {
+      for (int t = 2; t < tiles; ++t) step(t, x, x, p, p);
     }
-  }
-  auto load_last = [&] {  // the keys are all there
-    if (next_v < tiles) { load_values(); ++loaded; }
-  };
-  if (tiles > 1) {
+    if (tiles > 1) {
+      arrive(1);
+      load_one(false);  // the keys are all there
+      blank(tiles - 2, slot);
+      if (!idle) {
+        const float alpha = prepare(tiles - 1, 0, x);
+        values(slot, 0);
+        rescale(alpha);
+        weights();
+      }
+      slot = next(slot);
+    }
     arrive(1);
-    load_last();
-    blank(tiles - 2, slot);
-    if (!idle) {
-      const float alpha = prepare(tiles - 1, x);
-      values(slot);
-      rescale(alpha);
-      weights();
-    }
-    slot = next(slot);
+    blank(tiles - 1, slot);
+    if (!idle) values(slot, 0);
   }
-  arrive(1);
-  blank(tiles - 1, slot);
-  if (!idle) values(slot);
 
   l = with_lane_xor32(l, OpSum());
   if constexpr (kAlong > 1) {  // the waves that took other tokens of the same rows
@@ -547,13 +571,11 @@ template <typename T, int D>
 __global__ __launch_bounds__(kMergeWaves* kWave) void prefix_merge_kernel(CacheView c, PrefixArgs a) {
   constexpr int kLanes = D / 4, kParts = kWave / kLanes, kAhead = 8;
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t item = (int64_t)blockIdx.x * kMergeWaves + wave;
-  if (item >= (int64_t)c.B * c.H) return;  // (no barrier below)
-  const int i = (int)(item / c.H), h = (int)(item - (int64_t)i * c.H), G = c.H / c.Hkv, hkv = h / G;
-  const PrefixMember of = a.work.member[i];
-  if (of.seq < 0) return;
+  const int h = blockIdx.y * kMergeWaves + wave, shift = __builtin_ctz(c.H / c.Hkv), G = 1 << shift, hkv = h >> shift;
+  const PrefixMember of = a.work.member[blockIdx.x];
+  if (h >= c.H || of.seq < 0) return;  // (no barrier below)
   const int n = of.count + of.own_count;
-  const int64_t base = (int64_t)hkv * a.shape.max_rows + h % G;
+  const int64_t base = (int64_t)hkv * a.shape.max_rows + (h & (G - 1));
   auto row_of = [&](int s) { return base + (s < of.count ? of.part + (int64_t)s * of.step : of.own_part + (int64_t)(s - of.count) * G); };
   const float2* ml = reinterpret_cast<const float2*>(a.work.part_ml);
   const float2 none = make_float2(kNegBig, 0.f);
@@ -638,8 +660,7 @@ template <>
 hipError_t launch_prefix_of<UNIQUE_ELEM, UNIQUE_DIM>(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
   const hipError_t e = c.S == 8 ? launch_group<8>(c, a, st) : (c.S == 16 ? launch_group<16>(c, a, st) : launch_group<32>(c, a, st));
   if (e != hipSuccess) return e;
-  const int64_t outs = (int64_t)c.B * c.H;
-  prefix_merge_kernel<UNIQUE_ELEM, UNIQUE_DIM><<<dim3((unsigned)((outs + kMergeWaves - 1) / kMergeWaves)), dim3(kMergeWaves * kWave), 0, st>>>(c, a);
+  prefix_merge_kernel<UNIQUE_ELEM, UNIQUE_DIM><<<dim3(c.B, (c.H + kMergeWaves - 1) / kMergeWaves), dim3(kMergeWaves * kWave), 0, st>>>(c, a);
   return hipGetLastError();
 }
 

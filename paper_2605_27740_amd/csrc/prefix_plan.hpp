@@ -24,7 +24,7 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   PrefixShape s;
   const int64_t most = (int64_t)max_members * group;
   s.rows = elem == 4 ? 128 : (most <= 64 ? 64 : 128);
-  s.tile_pages = (s.rows == 64 ? 64 : 32) / page_size;
+  s.tile_pages = (elem == 4 ? 32 : 64) / page_size;
   s.wanted = std::max(kPrefixSlots / kv_heads, 1);
   const int64_t blocks = std::min<int64_t>(num_groups * ((most + s.rows - 1) / s.rows), (int64_t)batch * group / s.rows + num_groups);
   // of prefixes: the wanted ones or the longest, and one more for each block
