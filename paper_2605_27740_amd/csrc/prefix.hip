@@ -13,9 +13,7 @@
 // fp32 caches: the same on v_mfma_f32_32x32x2_f32, whose probabilities stay fp32.
 #include <type_traits>
 
-#include "decode_core.hpp"
-#include "prefix_plan.hpp"
-#include "serving.hpp"
+#include "prefix_items.hpp"
 
 namespace unique {
 namespace {
@@ -536,6 +534,11 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   if (half == 0) *reinterpret_cast<float2*>(a.work.part_ml + part * 2) = make_float2(m, l);
 }
 
+__device__ __forceinline__ PrefixItem uniform(const PrefixItem& x) {
+  auto of = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  return {of(x.place), of(x.rows), of(x.begin), of(x.end), of(x.seq), of(x.own), of(x.part), 0};
+}
+
 // An item: a run of a prefix, or of a member's own pages, which the decode kernels' chunk code takes.
 template <typename T, int D, int S, int G, int kAcross, bool kNT>
 __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c, PrefixArgs a) {
@@ -543,8 +546,26 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
   constexpr size_t kRingBytes = L::kRing * L::kBytes, kOwnBytes = sizeof(DecodeShared<T, D, G>);
   __shared__ __attribute__((aligned(1024))) char ring[kRingBytes > kOwnBytes ? kRingBytes : kOwnBytes];
   const int hkv = blockIdx.x & (c.Hkv - 1), index = blockIdx.x / c.Hkv;
-  const PrefixItem item = a.work.item[index];
-  if (index >= *a.work.num_items) return;
+  PrefixItem item;
+  if (a.shape.plans) {  // a thread for every source
+    ItemsPlan<kDecWaves * kWave, true> plan = {c, a, *reinterpret_cast<ItemsShared<kDecWaves * kWave, true>*>(ring)};
+    plan.make();
+    if (blockIdx.x == 0) {  // for the kernel that joins the results
+      if (plan.t < plan.sources) plan.keep(plan.t);
+      __syncthreads();
+      if (plan.t >= plan.n && plan.t < plan.sources) plan.tell_member(plan.t - plan.n, plan.m);
+    }
+    if (index >= plan.items()) return;
+    int y = index;
+    const int k = plan.class_of(y), z = y - plan.at_of(k);
+    if (plan.s.kind == k && z >= 0 && z < plan.mine) plan.sh.item = plan.item_of(plan.s, z, plan.seq_of(plan.s.place));
+    __syncthreads();
+    item = uniform(plan.sh.item);
+    __syncthreads();  // the ring is for keys now
+  } else {
+    item = a.work.item[index];
+    if (index >= *a.work.num_items) return;
+  }
   if (!item.own) {
     attend_prefix<T, D, S, kAcross, kNT>(c, a, item, hkv, ring);
     return;

@@ -8,7 +8,7 @@
 namespace unique {
 
 // Every group is a source of items, its prefix's pages times the blocks of its members' query rows, and every member one, its own pages.
-constexpr int kPrefixSlots = 512;  // items that are wanted per launch: two workgroups to a compute unit
+constexpr int kPrefixSlots = 512;  // items that are wanted per launch: two workgroups to a compute unit, that many run at a time
 
 constexpr int kPrefixMostPages = 512;  // of an item of a prefix, whose page ids are held in registers
 
@@ -18,21 +18,35 @@ struct PrefixShape {
   int32_t wanted;       // items per KV head
   int32_t max_items;    // there are at most, per KV head
   int32_t max_rows;     // rows of partial results at most, per KV head
+  int32_t plans;        // every workgroup of the attention kernel makes the plan for itself
 };
 
-inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members, int max_prefix_pages) {
+inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members, int max_prefix_pages,
+                                int max_own_pages) {
   PrefixShape s;
   const int64_t most = (int64_t)max_members * group;
   s.rows = elem == 4 ? 128 : (most <= 64 ? 64 : 128);
   s.tile_pages = (elem == 4 ? 32 : 64) / page_size;
   s.wanted = std::max(kPrefixSlots / kv_heads, 1);
   const int64_t blocks = std::min<int64_t>(num_groups * ((most + s.rows - 1) / s.rows), (int64_t)batch * group / s.rows + num_groups);
-  // of prefixes: the wanted ones or the longest, and one more for each block
-  const int64_t of_prefixes = std::max<int64_t>(s.wanted, blocks * max_prefix_pages / kPrefixMostPages) + blocks;
-  s.max_items = (int32_t)(of_prefixes + s.wanted + batch);
-  s.max_rows = (int32_t)(of_prefixes * s.rows + (int64_t)(s.wanted + batch) * group);
+  // A source's items are one more than its share of the wanted ones at most, and hold a tile each. A member who is alone in a group has its prefix as their own.
+  const int64_t longest = blocks * max_prefix_pages / kPrefixMostPages, prefix_tiles = blocks * ((max_prefix_pages + s.tile_pages - 1) / s.tile_pages);
+  const int64_t tiles = prefix_tiles + (int64_t)batch * ((max_own_pages + s.tile_pages - 1) / s.tile_pages);
+  const int64_t of_prefixes = std::min(std::max<int64_t>(s.wanted, longest) + blocks, prefix_tiles);
+  // Prefixes may have to be cut for their page ids, when items would be longer.
+  const int64_t cost = blocks * max_prefix_pages + batch * (max_own_pages + 96 / page_size + 1ll);
+  const int64_t most_items = s.wanted + (cost > (int64_t)kPrefixMostPages * s.wanted ? longest : 0) + blocks + batch;
+  s.max_items = (int32_t)std::max<int64_t>(std::min(most_items, tiles), 1);
+  s.max_rows = (int32_t)(of_prefixes * s.rows + std::min<int64_t>(s.wanted + batch, tiles) * group);
+  // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us: 2 x 2048 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, 776 workgroups) 40.0 / 38.6,
+  // 16 x 131072 (648) 107.6 / 107.2, 60 rows in 6 groups (1048) 107.6 / 108.5.
+  s.plans = num_groups + batch < 256 && (int64_t)s.max_items * kv_heads <= 2 * kPrefixSlots;
   return s;
 }
+
+// Kinds of items, in the order in which they are started: the long ones first.
+enum PrefixKind { kPrefixRun = 0, kOwnRun = 1, kShortOwn = 2, kPrefixKinds = 3 };
+constexpr int prefix_kind(bool own, int pages, int64_t item_pages) { return !own ? kPrefixRun : (2 * (int64_t)pages >= item_pages ? kOwnRun : kShortOwn); }
 
 // What a source costs, in pages. An item of few rows takes 3.5 us whatever there is to read, as long as 100 tokens of an 8-headed bf16 cache.
 constexpr int64_t prefix_cost(int pages, int blocks, bool own, int page_size) {
