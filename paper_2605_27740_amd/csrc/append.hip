@@ -33,8 +33,9 @@ __device__ __forceinline__ Raw16 pack_vec(const float (&x)[Elem<T>::kVec]) {
 }
 
 // kInterleaved: pairs are neighbours. A wave takes `per` steps of heads of a token, the wave's item = (token, part of its heads).
+// early: the first heads are asked for before the slot is known.
 template <typename T, int D, bool kInterleaved>
-__global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c, AppendArgs a, int steps, int per) {
+__global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c, AppendArgs a, int steps, int per, bool early) {
   constexpr int kVec = Elem<T>::kVec;
   constexpr int kLanes = D / kVec / 2;      // lanes of a head
   constexpr int kHeads = kWave / kLanes;    // heads of a step
@@ -46,22 +47,10 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c
   if (row >= a.rows) return;  // (no barrier below)
   const int part = (int)(item - row * parts);
   const int64_t slot = a.slots[row];
-  if (slot < 0 || slot >= c.num_phys * c.S) return;
   const int position = a.positions[row];
-  const int64_t page = slot / c.S;
-  const int place = (int)(slot - page * c.S);
-
   // This lane's two pieces of a head: where halves are paired, one of each half; behind the turned channels neighbours.
   const int R = a.how.rotary_dim, mine = lane % kLanes, pairs = kInterleaved ? 0 : R / (2 * kVec);
   const int c0 = mine < pairs ? mine : 2 * pairs + 2 * (mine - pairs), c1 = mine < pairs ? mine + pairs : c0 + 1;
-  if (lane < R / 2) {
-    const double turns = (double)position * (a.how.frequencies[lane] * 0.15915494309189535);
-    const float f = (float)(turns - rint(turns));  // in [-1/2, 1/2]
-    float sn, cs;
-    sincospif(2.f * f, &sn, &cs);
-    s_turn[wave][lane] = make_float2(cs * a.how.magnitude, sn * a.how.magnitude);
-  }
-  __builtin_amdgcn_wave_barrier();  // the LDS serves a wave's accesses in order; the compiler keeps it
   const bool norm = a.how.q_weight != nullptr;
   Raw16 wq[2], wk[2];
   if (norm) {
@@ -74,10 +63,6 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c
   const T* q = reinterpret_cast<const T*>(a.q) + row * a.q_stride;
   const T* k = reinterpret_cast<const T*>(a.k) + row * a.k_stride;
   const T* v = reinterpret_cast<const T*>(a.v) + row * a.v_stride;
-  T* q_out = reinterpret_cast<T*>(a.q_out) + row * c.H * D;
-  const int64_t token = page * c.kv_page_stride + (int64_t)place * D;
-  T* kc = reinterpret_cast<T*>(const_cast<void*>(c.k_cache)) + token;
-  T* vc = reinterpret_cast<T*>(const_cast<void*>(c.v_cache)) + token;
 
   auto load = [&](int step, Raw16(&x)[2]) {
     const int head = min(step * kHeads + lane / kLanes, all - 1);
@@ -85,6 +70,29 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c
     x[0] = load_raw(src + c0 * kVec);
     x[1] = load_raw(src + c1 * kVec);
   };
+  const int begin = part * per, end = min(begin + per, steps);
+  Raw16 x[kAppendAhead][2];
+  auto load_few = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < kAppendAhead; ++u) load(s0 + u, x[u]);
+  };
+  if (early) load_few(begin);
+  if (slot < 0 || slot >= c.num_phys * c.S) return;
+  if (lane < R / 2) {
+    const double turns = (double)position * (a.how.frequencies[lane] * 0.15915494309189535);
+    const float f = (float)(turns - rint(turns));  // in [-1/2, 1/2]
+    float sn, cs;
+    sincospif(2.f * f, &sn, &cs);
+    s_turn[wave][lane] = make_float2(cs * a.how.magnitude, sn * a.how.magnitude);
+  }
+  __builtin_amdgcn_wave_barrier();  // the LDS serves a wave's accesses in order; the compiler keeps it
+
+  const int shift = __builtin_ctz(c.S), place = (int)slot & (c.S - 1);
+  T* q_out = reinterpret_cast<T*>(a.q_out) + row * c.H * D;
+  const int64_t token = (slot >> shift) * c.kv_page_stride + (int64_t)place * D;
+  T* kc = reinterpret_cast<T*>(const_cast<void*>(c.k_cache)) + token;
+  T* vc = reinterpret_cast<T*>(const_cast<void*>(c.v_cache)) + token;
+
   auto finish = [&](int step, Raw16(&x)[2]) {
     const int head = step * kHeads + lane / kLanes;
     const bool is_q = head < c.H, is_v = head >= c.H + c.Hkv;
@@ -141,11 +149,9 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c
     *reinterpret_cast<uint4*>(dst + c1 * kVec) = z1.v;
   };
 
-  const int begin = part * per, end = min(begin + per, steps);
-  Raw16 x[kAppendAhead][2];
+  if (!early) load_few(begin);
   for (int s0 = begin; s0 < end; s0 += kAppendAhead) {
-#pragma unroll
-    for (int u = 0; u < kAppendAhead; ++u) load(s0 + u, x[u]);
+    if (s0 > begin) load_few(s0);
 #pragma unroll
     for (int u = 0; u < kAppendAhead; ++u)
       if (s0 + u < end) finish(s0 + u, x[u]);  // uniform
@@ -159,11 +165,16 @@ hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t st
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value, kHeads = kWave / (D / Elem<T>::kVec / 2);
     const int steps = (c.H + 2 * c.Hkv + kHeads - 1) / kHeads;
+    // A wave takes all of a token, or less where there are few. What it does before its first head, the angles and weights, is little of fp32 heads' time and of a call's without norm:
+    // there, in long calls, a step each. us, all of a token / parts that make 16384 items / a step: 8192 bf16 tokens of 48 heads 44.2 / 41.0 / 44.6, without norm 43.4 / 40.2 / 41.9; 65536 of
+    // 80 heads 511 / 511 / 538, without norm 505 / 506 / 482; 16384 fp32 tokens of 48 heads 157 / 157 / 144. (Parts that make 4096 items, for 16384: 44.2 of the first.)
     int per = steps;
-    while (per > 1 && (int64_t)a.rows * ((steps + per - 1) / per) < 4096) per = (per + 1) / 2;
+    if (a.rows >= 16384 && (!a.how.q_weight || c.dtype == 0)) per = 1;
+    while (per > 1 && (int64_t)a.rows * ((steps + per - 1) / per) < 16384) per = (per + 1) / 2;
     const int64_t items = (int64_t)a.rows * ((steps + per - 1) / per);
+    const bool early = items <= 8192;  // all waves at once: otherwise tokens without a slot would be read in vain
     auto go = [&](auto kernel) {
-      kernel<<<dim3((unsigned)((items + kAppendWaves - 1) / kAppendWaves)), dim3(kAppendWaves * kWave), 0, st>>>(c, a, steps, per);
+      kernel<<<dim3((unsigned)((items + kAppendWaves - 1) / kAppendWaves)), dim3(kAppendWaves * kWave), 0, st>>>(c, a, steps, per, early);
       return hipGetLastError();
     };
     return a.how.interleaved ? go(append_kernel<T, D, true>) : go(append_kernel<T, D, false>);

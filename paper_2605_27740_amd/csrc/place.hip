@@ -1,9 +1,10 @@
 // Places for the new tokens of a step: pages from a stack of free ones, page table, lengths, positions and slots.
 //
 // Sequence b needs need_b = ceil((n_b + t_b) / S) - ceil(n_b / S) pages; with the sums of need over the sequences before it, its pages are known without
-// asking the others: page i of all is entry n - 1 - i of a stack of n. So one workgroup forms four prefix sums over the batch (pages that come back twice,
-// tokens, needs), and everything else is per page or per row. Small calls do all of it in that workgroup; in larger ones the pages that come
-// back and the rows have launches of their own, as the former must be on the stack before the latter read it.
+// asking the others: page i of all is entry n - 1 - i of a stack of n. So a workgroup forms four prefix sums over the batch (pages that come back twice,
+// tokens, needs), and everything else is per page or per row. Small calls do all of it in one workgroup. In larger ones the rows have a launch of their own, as pages that
+// come back must be on the stack before they are given out, and what the outputs may lie over (lengths, positions, the count of pages) is written there too: in the launch
+// before it, all workgroups of which make the plan, it is still read.
 #include "decode_core.hpp"
 #include "serving.hpp"
 
@@ -14,8 +15,9 @@ constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;
 constexpr int kFillThreads = 256, kFillRows = 4;  // rows of a thread
 constexpr int kMostTokens = 1 << 25;              // where sums of tokens saturate, above any number of rows
 
+enum SeatState { kUnplaced = 0, kPlaced = 1, kEnded = 2 };
 struct Seat {  // what the rows of a sequence's new tokens need
-  int len, first, position, ok;  // its length, its first page among all that are given out
+  int len, first, position, state;  // its length, its first page among all that are given out
 };
 struct Back {  // what a sequence gives back
   int freed_at, own_at, freed, pages;  // places on the stack; evicted pages, pages of its row if it has ended
@@ -24,7 +26,7 @@ struct PlaceArrays {
   Seat* seat;   // [B]
   Back* back;   // [B]
   int* starts;  // [B + 1]
-  int* size;    // the stack's, with what has come back
+  int* size;    // the stack's, with what has come back, and how many pages are given out
 };
 
 __device__ __forceinline__ int pages_of(int tokens, int S) { return (tokens + S - 1) / S; }
@@ -92,15 +94,11 @@ __device__ __forceinline__ void plan_places(const CacheView& c, const unique_pla
     if (live) {
       // Sequences whose rows are not there are the last ones, so their needs may count.
       const bool ok = !ended && fits && upto[2] <= p.max_new_tokens && (need == 0 || upto[3] <= size);
-      const int placed = ok ? tokens : 0;
       const int position = p.next_positions ? p.next_positions[b] : len;
-      to.seat[b] = Seat{len, upto[3] - need, position, ok ? 1 : 0};
+      to.seat[b] = Seat{len, upto[3] - need, position, ended ? kEnded : (ok ? kPlaced : kUnplaced)};
       to.back[b] = Back{before + upto[0] - freed, before + freed_all + upto[1] - own, freed, ended ? pages : 0};
-      to.starts[b] = p.token_starts[b] = upto[2] - tokens;
-      if (b == c.B - 1) to.starts[c.B] = p.token_starts[c.B] = upto[2];
-      p.placed[b] = placed;
-      p.seq_lens_out[b] = ended ? 0 : len + placed;
-      if (p.next_positions_out) p.next_positions_out[b] = ended ? 0 : position + placed;
+      to.starts[b] = upto[2] - tokens;
+      if (b == c.B - 1) to.starts[c.B] = upto[2];
       if (ok && need > 0) given = upto[3];  // (the largest is the last)
     }
   }
@@ -111,8 +109,8 @@ __device__ __forceinline__ void plan_places(const CacheView& c, const unique_pla
   __syncthreads();
   if (t == 0) {
     for (int w = 0; w < kPlanWaves; ++w) given = max(given, s_sum[w]);
-    *p.free_count_out = size - given;
-    *to.size = size;
+    to.size[0] = size;
+    to.size[1] = given;
   }
 }
 
@@ -130,21 +128,57 @@ __device__ __forceinline__ void give_back(const CacheView& c, const unique_place
   }
 }
 
-// Position and slot of a row; the first token of a page also writes the page's entry of the table.
-__device__ __forceinline__ void fill_row(const CacheView& c, const unique_placement& p, const PlaceArrays& from, int size, int row) {
+// What the caller is told of sequence b, and of the stack.
+__device__ __forceinline__ void tell_sequence(const CacheView& c, const unique_placement& p, const PlaceArrays& from, int b) {
+  const Seat s = from.seat[b];
+  const int start = from.starts[b], end = from.starts[b + 1], placed = s.state == kPlaced ? end - start : 0;
+  p.token_starts[b] = start;
+  if (b == c.B - 1) p.token_starts[c.B] = end;
+  p.placed[b] = placed;
+  p.seq_lens_out[b] = s.state == kEnded ? 0 : s.len + placed;
+  if (p.next_positions_out) p.next_positions_out[b] = s.state == kEnded ? 0 : s.position + placed;
+  if (b == 0) *p.free_count_out = from.size[0] - from.size[1];
+}
+
+// The first sequence from lo on whose rows end behind `row`; there is one.
+__device__ __forceinline__ int sequence_of(const int* starts, int lo, int B, int row) {
+  int hi = B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (starts[mid + 1] > row) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
+
+// The same for 64 rows of a wave, lane after lane, of which the first has a sequence: all lanes look for that one's, in 64 places at a time, and the ends of 64 sequences from there on answer
+// the others. Two trips to memory for 4096 sequences and one more, where a search by every lane makes twelve. With one launch fewer: 500 sequences of 1 to 2048 tokens 18.1 / 13.2 us,
+// 32 prompts of 8000 to 32768 13.7 / 12.1.
+__device__ __forceinline__ int sequence_of_lane(const int* starts, int B, int first, int lane) {
+  int lo = 0, hi = B - 1;  // uniform
+  while (lo < hi) {
+    const int step = (hi - lo + kWave) / kWave, last = lo + (lane + 1) * step - 1;
+    const bool behind = last >= hi || starts[last + 1] > first;
+    lo += __builtin_ctzll(__ballot(behind)) * step;
+    hi = min(lo + step - 1, hi);
+  }
+  const int end = starts[min(lo + 1 + lane, B)], row = first + lane;
+  int at = 0;  // sequences of the 64 that end at or before the row
+#pragma unroll
+  for (int d = kWave / 2; d > 0; d /= 2) at += __shfl(end, at + d - 1, kWave) <= row ? d : 0;
+  if (__builtin_amdgcn_readlane(end, kWave - 1) <= row) return sequence_of(starts, min(lo + kWave, B - 1), B, row);
+  return min(lo + at, B - 1);
+}
+
+// Position and slot of a row, of sequence b if it has one; the first token of a page also writes the page's entry of the table.
+__device__ __forceinline__ void fill_row(const CacheView& c, const unique_placement& p, const PlaceArrays& from, int size, int row, int b) {
   int position = -1;
   int64_t slot = -1;
-  if (row < from.starts[c.B]) {
-    int lo = 0, hi = c.B - 1;  // the first sequence whose rows end behind this one
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      if (from.starts[mid + 1] > row) hi = mid;
-      else lo = mid + 1;
-    }
-    const Seat s = from.seat[lo];
-    if (s.ok) {
-      const int i = row - from.starts[lo], at = s.len + i, lp = at / c.S, have = pages_of(s.len, c.S);
-      const int64_t entry = (int64_t)lo * c.max_pages + lp;
+  if (b >= 0) {
+    const Seat s = from.seat[b];
+    if (s.state == kPlaced) {
+      const int i = row - from.starts[b], at = s.len + i, lp = at / c.S, have = pages_of(s.len, c.S);
+      const int64_t entry = (int64_t)b * c.max_pages + lp;
       const int page = lp < have ? c.page_table[entry] : p.free_pages[size - 1 - (s.first + lp - have)];
       position = s.position + i;
       slot = page < 0 ? -1 : (int64_t)page * c.S + at % c.S;
@@ -155,32 +189,63 @@ __device__ __forceinline__ void fill_row(const CacheView& c, const unique_placem
   p.slots[row] = slot;
 }
 
+struct PlaceShared {
+  Seat seat[kPlanThreads];
+  Back back[kPlanThreads];
+  int starts[kPlanThreads + 1], size[2];
+};
+
 constexpr int kSmallRows = 8192;
 __global__ __launch_bounds__(kPlanThreads) void place_kernel(CacheView c, unique_placement p) {
-  __shared__ Seat s_seat[kPlanThreads];
-  __shared__ Back s_back[kPlanThreads];
-  __shared__ int s_starts[kPlanThreads + 1], s_size;
-  const PlaceArrays at = {s_seat, s_back, s_starts, &s_size};
+  __shared__ PlaceShared sh;
+  const PlaceArrays at = {sh.seat, sh.back, sh.starts, sh.size};
   plan_places(c, p, at);
   __syncthreads();
-  for (int b = threadIdx.x / kWave; b < c.B; b += kPlanWaves) give_back(c, p, s_back[b], b, threadIdx.x % kWave, kWave);
+  for (int b = threadIdx.x / kWave; b < c.B; b += kPlanWaves) give_back(c, p, sh.back[b], b, threadIdx.x % kWave, kWave);
+  for (int b = threadIdx.x; b < c.B; b += kPlanThreads) tell_sequence(c, p, at, b);
   __threadfence_block();  // the stack is read by other waves
   __syncthreads();
-  for (int row = threadIdx.x; row < p.max_new_tokens; row += kPlanThreads) fill_row(c, p, at, s_size, row);
+  for (int row = threadIdx.x; row < p.max_new_tokens; row += kPlanThreads)
+    fill_row(c, p, at, sh.size[0], row, row < sh.starts[c.B] ? sequence_of(sh.starts, 0, c.B, row) : -1);
 }
 
-__global__ __launch_bounds__(kPlanThreads) void place_plan_kernel(CacheView c, unique_placement p, PlaceArrays at) { plan_places(c, p, at); }
+// The plan, by every workgroup, and what its sequences give back.
+__global__ __launch_bounds__(kPlanThreads) void place_back_kernel(CacheView c, unique_placement p, PlaceArrays to) {
+  __shared__ PlaceShared sh;
+  const PlaceArrays at = {sh.seat, sh.back, sh.starts, sh.size};
+  plan_places(c, p, at);
+  __syncthreads();
+  const int t = threadIdx.x;
+  if (blockIdx.x == 0) {
+    if (t < c.B) to.seat[t] = sh.seat[t];
+    for (int b = t; b <= c.B; b += kPlanThreads) to.starts[b] = sh.starts[b];
+    if (t < 2) to.size[t] = sh.size[t];
+  }
+  for (int b = blockIdx.x; b < c.B; b += gridDim.x) give_back(c, p, sh.back[b], b, t, kPlanThreads);
+}
 
-__global__ __launch_bounds__(kFillThreads) void place_back_kernel(CacheView c, unique_placement p, PlaceArrays at) {
+// The same in two, where the LDS does not hold the plan.
+__global__ __launch_bounds__(kPlanThreads) void place_many_plan_kernel(CacheView c, unique_placement p, PlaceArrays at) { plan_places(c, p, at); }
+
+__global__ __launch_bounds__(kFillThreads) void place_many_back_kernel(CacheView c, unique_placement p, PlaceArrays at) {
   for (int b = blockIdx.x; b < c.B; b += gridDim.x) give_back(c, p, at.back[b], b, threadIdx.x, kFillThreads);
 }
 
+// The first workgroups take sequences, the others rows.
 __global__ __launch_bounds__(kFillThreads) void place_fill_kernel(CacheView c, unique_placement p, PlaceArrays at) {
-  const int size = *at.size;
+  const int tells = (c.B + kFillThreads - 1) / kFillThreads;
+  if ((int)blockIdx.x < tells) {
+    const int b = blockIdx.x * kFillThreads + threadIdx.x;
+    if (b < c.B) tell_sequence(c, p, at, b);
+    return;
+  }
+  const int size = at.size[0], all = at.starts[c.B];
 #pragma unroll
   for (int k = 0; k < kFillRows; ++k) {
-    const int row = (blockIdx.x * kFillRows + k) * kFillThreads + threadIdx.x;
-    if (row < p.max_new_tokens) fill_row(c, p, at, size, row);
+    const int row = ((blockIdx.x - tells) * kFillRows + k) * kFillThreads + threadIdx.x, lane = row % kWave;
+    if (row - lane >= p.max_new_tokens) return;  // uniform, as below
+    const int b = row - lane < all ? sequence_of_lane(at.starts, c.B, row - lane, lane) : -1;
+    if (row < p.max_new_tokens) fill_row(c, p, at, size, row, row < all ? b : -1);
   }
 }
 
@@ -190,7 +255,7 @@ bool place_is_small(const CacheView& c, int max_new_tokens) { return c.B <= kPla
 
 size_t place_bytes(const CacheView& c, int max_new_tokens) {
   if (place_is_small(c, max_new_tokens)) return 0;
-  return (size_t)c.B * (sizeof(Seat) + sizeof(Back)) + ((size_t)c.B + 2) * sizeof(int);
+  return (size_t)c.B * (sizeof(Seat) + sizeof(Back)) + ((size_t)c.B + 3) * sizeof(int);
 }
 
 hipError_t launch_place(const CacheView& c, const unique_placement& p, void* workspace, hipStream_t st) {
@@ -203,14 +268,19 @@ hipError_t launch_place(const CacheView& c, const unique_placement& p, void* wor
   at.back = reinterpret_cast<Back*>(at.seat + c.B);
   at.starts = reinterpret_cast<int*>(at.back + c.B);
   at.size = at.starts + c.B + 1;
-  place_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(c, p, at);
-  hipError_t e = hipGetLastError();
+  if (c.B <= kPlanThreads) {
+    place_back_kernel<<<dim3(c.B < 256 ? c.B : 256), dim3(kPlanThreads), 0, st>>>(c, p, at);
+  } else {
+    place_many_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(c, p, at);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    place_many_back_kernel<<<dim3(c.B < 2048 ? c.B : 2048), dim3(kFillThreads), 0, st>>>(c, p, at);
+  }
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  place_back_kernel<<<dim3(c.B < 2048 ? c.B : 2048), dim3(kFillThreads), 0, st>>>(c, p, at);
-  e = hipGetLastError();
-  if (e != hipSuccess || p.max_new_tokens == 0) return e;
   constexpr int kRows = kFillThreads * kFillRows;
-  place_fill_kernel<<<dim3((p.max_new_tokens + kRows - 1) / kRows), dim3(kFillThreads), 0, st>>>(c, p, at);
+  const int tells = (c.B + kFillThreads - 1) / kFillThreads, rows = (p.max_new_tokens + kRows - 1) / kRows;
+  place_fill_kernel<<<dim3(tells + rows), dim3(kFillThreads), 0, st>>>(c, p, at);
   return hipGetLastError();
 }
 
