@@ -318,7 +318,7 @@ typedef struct unique_placement {
   int64_t* slots;                    /* [max_new_tokens]: physical page * page_size + place in the page, or -1 */
   int32_t freed_stride;
   int32_t free_capacity;             /* entries of free_pages; what does not fit is lost (num_phys_pages always fit) */
-  int32_t max_new_tokens;            /* rows that there are, at most 2^30 */
+  int32_t max_new_tokens;            /* rows that there are, at most 2^24 */
   int32_t reserved0;                 /* 0 */
 } unique_placement;
 
@@ -362,8 +362,9 @@ int unique_append_tokens(const unique_cache_desc* desc, int32_t num_rows, const 
 
 /* Sequences whose contexts begin with the same pages, in groups. The host's bounds must be true: what lies beyond them is ignored by every kernel. */
 typedef struct unique_prefix_groups {
-  const int32_t* starts;        /* device, [num_groups + 1], ascending from 0: members [starts[g], starts[g + 1]) belong to group g */
-  const int32_t* members;       /* device, [batch]: the sequence of each member; NULL = member i is sequence i */
+  const int32_t* starts;        /* device, [num_groups + 1], ascending from 0: members [starts[g], starts[g + 1]) belong to group g. If they do not
+                                 * ascend, no row is written */
+  const int32_t* members;       /* device, [batch]: the sequence of each member, -1 = none; NULL = member i is sequence i */
   const int32_t* prefix_pages;  /* device, [num_groups]: so many entries at the beginning of all its members' rows of the page table are the same */
   int32_t num_groups;           /* 1 to batch */
   int32_t max_members;          /* host upper bound on members of a group */
@@ -376,9 +377,10 @@ typedef struct unique_prefix_groups {
 int unique_shared_prefix_workspace_bytes(const unique_cache_desc* desc, const unique_prefix_groups* groups, size_t* out_bytes);
 
 /* unique_dense_paged_decode for sequences that share the beginnings of their contexts: the pages of a group's prefix are read once for all of its
- * members (from the first member's row of the page table), each member's other pages as always. A member may be shorter than the prefix.
+ * members (from the row of the first of them that is not empty), each member's other pages as always. A member may be shorter than the prefix: the
+ * tokens behind its length do not count for it (if values of longer members' tokens there are not finite, its results may not be, either). The group of one member has nothing to share, and its prefix is read as its other pages.
  * Sequences that no group lists are left out, their rows of d_out and d_lse_out left as they are; one that is listed twice is attended twice. At most
- * `batch` members in all. Against unique_dense_paged_decode the sums are in another order, and for bf16 caches the probabilities of the prefix's
+ * `batch` members in all. sm_scale and the results of empty sequences are those of unique_dense_paged_decode. Against it the sums are in another order, and for bf16 caches the probabilities of the prefix's
  * tokens are rounded to bf16 before they multiply the values (2^-8 of a term at most; the sum that they are divided by is not rounded). */
 int unique_shared_prefix_decode(const unique_cache_desc* desc, const unique_prefix_groups* groups, const void* d_q, float sm_scale, void* d_out,
                                 float* d_lse_out, void* d_workspace, size_t workspace_bytes, void* stream);

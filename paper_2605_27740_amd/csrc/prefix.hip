@@ -170,6 +170,14 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   // tokens that all rows of the wave have
   const int all_have = __builtin_amdgcn_readfirstlane((int)wave_allreduce_minmax<false>((uint32_t)(live ? tokens : INT32_MAX)));
   const bool idle = across * 32 >= item.rows;  // no row of this wave (uniform)
+  // tokens that any row of the item has, which are not the wave's alone
+  int most = 0;
+#pragma unroll
+  for (int i = 0; i < kAcross * 32 / kWave; ++i) {
+    const int r = i * kWave + lane, at = item.place + min(r, item.rows - 1) / G, s = a.groups.members ? a.groups.members[at] : at;
+    most = max(most, s >= 0 && s < c.B ? c.seq_lens[s] : 0);
+  }
+  const int longest = __builtin_amdgcn_readfirstlane((int)wave_allreduce_minmax<true>((uint32_t)most));
 
   // Where a lane reads, behind a unit's beginning. Keys: token `col`, the pieces of step s, of which four (fp32: eight) are in a plane. Values, bf16: lane i of 16 asks
   // for token i / 4, channels 4 (i % 4) + ..., and gets channel i of the four tokens; two blocks of channels are in a plane. fp32: channel `col` of a block,
@@ -350,12 +358,16 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     wait_units<L::kRing - 4 < 1 ? 1 : L::kRing - 4, L::kLoads>(left);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
-  // Slots of pages that there are not may hold anything, and a product with zero is not always zero.
+  // Slots of pages that there are not, and of tokens behind the longest row, may hold anything, and a product with zero is not always zero.
+  const int clean = holes ? 0 : min(pages / kTilePages, (longest / S - item.begin) / kTilePages);  // tiles that have none
   auto blank = [&](int t, int s) {
-    if (!holes && t < pages / kTilePages) return;
+    if (t < clean) return;
     const uint32_t there = there_at(t);
-    for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave)
-      if (!(there >> (i * 16 % L::kPlaneBytes / 128 / S) & 1)) *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(ring_at + s * L::kBytes + i * 16) = u32x4_t{0, 0, 0, 0};
+    const int end = longest - (item.begin + t * kTilePages) * S;
+    for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave) {
+      const int token = i * 16 % L::kPlaneBytes / 128;
+      if (token >= end || !(there >> (token / S) & 1)) *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(ring_at + s * L::kBytes + i * 16) = u32x4_t{0, 0, 0, 0};
+    }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
 
@@ -410,7 +422,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       arrive(2);
       const int k_slot = slot, v_slot = next(slot);
       slot = next(v_slot);
-      if (holes) blank(t - 1, v_slot);
+      blank(t - 1, v_slot);
       if (idle) {
         load_one(kKeysFirst);
         load_one(!kKeysFirst);
@@ -446,7 +458,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       arrive(2);
       const int k_slot = slot, v_slot = next(slot);
       slot = next(v_slot);
-      if (holes) blank(t - 2, v_slot);
+      blank(t - 2, v_slot);
       if (!kBf16 || idle) {
         load_one(kKeysFirst);
         load_one(!kKeysFirst);
@@ -558,7 +570,7 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
     if (index >= plan.items()) return;
     int y = index;
     const int k = plan.class_of(y), z = y - plan.at_of(k);
-    if (plan.s.kind == k && z >= 0 && z < plan.mine) plan.sh.item = plan.item_of(plan.s, z, plan.seq_of(plan.s.place));
+    if (plan.s.kind == k && z >= 0 && z < plan.mine) plan.sh.item = plan.item_of(plan.s, z, plan.leader_of(plan.s));
     __syncthreads();
     item = uniform(plan.sh.item);
     __syncthreads();  // the ring is for keys now

@@ -15,7 +15,7 @@ struct ItemsShared {
   static constexpr int kWaves = kThreads / kWave;
   PrefixSource source[kHeld ? kThreads : 1];
   int first[kClasses][kHeld ? kThreads : 1];  // items of a class before each source's
-  int starts[kHeld ? kThreads : 1], prefix[kHeld ? kThreads : 1];
+  int starts[kHeld ? kThreads : 1], prefix[kHeld ? kThreads : 1], full[kHeld ? kThreads : 1];  // full: a member's sequence that is not empty, or -1
   int64_t cost[kWaves];
   int scan[kClasses + 1][kWaves];
   PrefixItem item;
@@ -78,6 +78,15 @@ struct ItemsPlan {
   }
   __device__ __forceinline__ int seq_of(int i) const { return a.groups.members ? a.groups.members[i] : i; }
   __device__ __forceinline__ int len_of(int seq) const { return seq >= 0 && seq < c.B ? c.seq_lens[seq] : 0; }
+  // The first sequence of a source that is not empty (one that has ended has lost its pages): its row of the page table is that of the others, as far as their prefix goes.
+  __device__ __forceinline__ int leader_of(const PrefixSource& of) const {
+    for (int i = of.place, end = of.place + of.rows / G; i < end; ++i) {
+      int seq = kHeld ? sh.full[i] : seq_of(i);
+      if (!kHeld && len_of(seq) <= 0) seq = -1;
+      if (seq >= 0) return seq;
+    }
+    return -1;
+  }
 
   __device__ __forceinline__ void make() {
     int64_t cost = 0;
@@ -87,6 +96,7 @@ struct ItemsPlan {
       if (t <= n) sh.starts[t] = a.groups.starts[t];
       if (t < n) sh.prefix[t] = a.groups.prefix_pages[t];
       const int len = len_of(seq);
+      if (t >= n && t < sources) sh.full[t - n] = len > 0 ? seq : -1;
       __syncthreads();
       if (t < sources) s = look_at(t, seq, len, m);
       cost = prefix_cost(s.end - s.begin, s.blocks, t >= n, c.S);

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kThreads) void prefix_items_kernel(CacheView c, Pre
       else hi = mid - 1;
     }
     const PrefixSource of = plan.source()[lo];
-    a.work.item[i] = plan.item_of(of, y - plan.first_of(k, lo), plan.seq_of(of.place));
+    a.work.item[i] = plan.item_of(of, y - plan.first_of(k, lo), plan.leader_of(of));
   }
 }
 

@@ -1,0 +1,22 @@
+// C interface of the cut of attention over shared prefixes for the CPU tests.
+#include "../../paper_2605_27740_amd/csrc/prefix_plan.hpp"
+
+// Sources (pages, rows, own) of a KV head -> items' sources and pages; the shape's bounds.
+extern "C" int prefix_items(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members, int max_prefix, int max_own, int sources,
+                            const int* pages, const int* rows, const int* own, int* shape, int* count, int* each, int* blocks) {
+  const unique::PrefixShape s = unique::prefix_shape(batch, kv_heads, group, elem, page_size, num_groups, max_members, max_prefix, max_own);
+  int64_t cost = 0;
+  for (int i = 0; i < sources; ++i) {
+    blocks[i] = (rows[i] + s.rows - 1) / s.rows;
+    cost += unique::prefix_cost(pages[i], blocks[i], own[i], page_size);
+  }
+  const int64_t item_pages = unique::prefix_item_pages(cost, s.wanted);
+  for (int i = 0; i < sources; ++i) {
+    const unique::PrefixCut cut = unique::prefix_cut(pages[i], item_pages, rows[i] < s.rows ? rows[i] : s.rows, page_size, s.tile_pages, own[i]);
+    count[i] = cut.count;
+    each[i] = cut.pages;
+  }
+  const int out[] = {s.rows, s.tile_pages, s.wanted, s.max_items, s.max_rows, s.plans, unique::kPrefixSlots, unique::kPrefixMostPages};
+  for (int i = 0; i < 8; ++i) shape[i] = out[i];
+  return 0;
+}

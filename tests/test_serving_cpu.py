@@ -1,7 +1,9 @@
 """The calls around the cache without a GPU: refusals, sizes, frequencies, and the plain counterparts themselves."""
 import ctypes as C
 import math
+import os
 import random
+import subprocess
 
 import pytest
 import torch
@@ -172,3 +174,60 @@ def test_plain_places_keep_every_page():
             for i, row in enumerate(rows):
                 at = lens[b] + i
                 assert got["slots"][row] == got["table"][b][at // S] * S + at % S and got["positions"][row] == at
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("rules") / "prefix_rules.so")
+    here = os.path.dirname(os.path.abspath(__file__))
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-ftrapv", "-shared", "-fPIC", "-o", so, os.path.join(here, "c_abi", "prefix_rules.cpp")], check=True)
+    return C.CDLL(so)
+
+
+def prefix_items(rules, kv_heads, group, elem, S, sizes, prefix, own, max_members, max_prefix, max_own, batch):
+    """Sources of a batch as the kernels see them, cut -> shape, sources and their (count, pages each, blocks)."""
+    src = [(p if n > 1 else 0, n * group, 0) for n, p in zip(sizes, prefix)]
+    at = 0
+    for n, p in zip(sizes, prefix):
+        src += [(own[at + i] + (p if n == 1 else 0), group, 1) for i in range(n)]
+        at += n
+    n = len(src)
+    arr = [(C.c_int * n)(*col) for col in zip(*src)]
+    shape, outs = (C.c_int * 8)(), [(C.c_int * n)() for _ in range(3)]
+    rules.prefix_items(batch, kv_heads, group, elem, S, len(sizes), max_members, max_prefix, max_own, n, *arr, shape, *outs)
+    return dict(zip("rows tile wanted max_items max_rows plans slots most".split(), shape)), src, list(zip(*outs))
+
+
+def test_prefix_items_fit_their_arrays(rules):
+    """Whatever true bounds the host knows: items cover every page once, whole tiles but the last, page ids fit the registers, and items and rows of
+    partial results are no more than the workspace has."""
+    for seed in range(3000):
+        r = random.Random(seed)
+        S, group, kv, elem = r.choice([8, 16, 32]), r.choice([1, 2, 4, 8]), r.choice([1, 2, 8, 32]), r.choice([2, 4])
+        n = r.choice([1, 1, 2, 5, 40])
+        longest, alone = r.choice([0, 1, 30, 3000, 70_000]), r.choice([0, 1, 20, 5000])
+        sizes = [r.choice([0, 1, 1, 2, r.randrange(200)]) for _ in range(n)]
+        sizes[0] = max(sizes[0], 1)
+        prefix = [r.choice([0, longest, r.randrange(longest + 1)]) for _ in sizes]
+        own = [r.choice([0, alone, r.randrange(alone + 1)]) for _ in range(sum(sizes))]
+        slack = r.choice([0, 0, 3])
+        batch = max(sum(sizes), n) + slack
+        shape, src, cuts = prefix_items(rules, kv, group, elem, S, sizes, prefix, own, max(sizes) + slack, max(prefix) + slack, max(own) + slack, batch)
+        items = rows = 0
+        for (pages, live, mine), (count, each, blocks) in zip(src, cuts):
+            assert count * each >= pages and (count - 1) * each < max(pages, 1), "every page, no item without pages"
+            assert each % shape["tile"] == 0 or count <= 1
+            assert mine or count == 0 or each <= shape["most"]
+            items += count * blocks
+            rows += count * blocks * (group if mine else shape["rows"])
+        assert items <= shape["max_items"] and rows <= shape["max_rows"], seed
+        if shape["plans"]:
+            assert len(src) < 256 and len(sizes) + batch < 256 and shape["max_items"] * kv <= 2 * shape["slots"]
+
+
+def test_prefix_items_fill_the_chip(rules):
+    """Where there is much to read, items are about as many as run at a time."""
+    for kv, group, n, pages, own in ((8, 4, 16, 8192, 60), (8, 4, 256, 2048, 20), (8, 8, 10, 1500, 180), (1, 8, 4, 100_000, 10)):
+        shape, src, cuts = prefix_items(rules, kv, group, 2, 16, [n], [pages], [own] * n, n, pages, own, n)
+        assert shape["wanted"] * kv == shape["slots"]
+        assert 0.5 * shape["wanted"] <= sum(n * b for n, _, b in cuts) <= shape["max_items"]

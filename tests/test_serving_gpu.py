@@ -106,6 +106,22 @@ def test_rows_that_are_not_there(gpu_lib, rows):
     check_place(c, total, in_place=True, rows=rows)
 
 
+@pytest.mark.parametrize("B", [900, 1024, 5000])
+def test_places_of_few_among_many(gpu_lib, B):
+    """Long runs of sequences without new tokens between those that have some, and rows of one sequence over many workgroups."""
+    for where in ([3, B - 20], [0, 1, 2, 70, 71, 500, B - 1], [B // 2]):
+        r = random.Random(B)
+        c, total = place_case(B, B, 16, 4, 60, 1, 0.0, ended=0.0, shared=False)
+        c["table"] = [row + [-1] * 600 for row in c["table"]]
+        c["new"] = [0] * B
+        for b in where:
+            c["new"][b] = r.choice([1, 9000])
+        c["new"][where[0]] = 9000
+        need = sum(-(-(n + t) // 16) - -(-n // 16) for n, t in zip(c["lens"], c["new"]))
+        c.update(free=list(range(total, total + need)), free_count=need, rows=sum(c["new"]) + 3)
+        check_place(c, total + need, in_place=True)
+
+
 def test_a_stack_that_is_too_small_loses_what_does_not_fit(gpu_lib):
     c, total = place_case(6, 50, 8, 30, 200, 10, 0.5, ended=0.6, evicted=2)
     c["free"] = c["free"][:c["free_count"] + 11]
@@ -293,3 +309,327 @@ def test_prefix_groups_of_all_kinds(gpu_lib, dtype, D, H, Hkv, S, which):
     torch.cuda.synchronize()
     listed = check_prefix(c, got, dtype)
     assert (got[0][~listed.to(DEV)] == -7).all() and (got[1][~listed.to(DEV)] == -7).all(), "sequences in no group"
+
+
+def holes(c, seed):
+    """Entries of prefixes and of own pages that are no pages: -1 and ids beyond the pool."""
+    r = random.Random(seed)
+    pool, S = c["k"].shape[0], c["S"]
+    for g, (own, p) in enumerate(c["groups"]):
+        rows = c["members"][c["starts"][g]:c["starts"][g + 1]].tolist()
+        for i in r.sample(range(p), min(p, max(1, p // 5))):
+            c["table"][rows, i] = r.choice([-1, -7, pool, 2 ** 31 - 1])
+        for b in rows:
+            n = -(-int(c["lens"][b]) // S)
+            if n > p and r.random() < 0.7:
+                c["table"][b, r.randrange(p, n)] = r.choice([-1, pool + 3])
+    return c
+
+
+def check_holes(c, got, dtype):
+    """A sequence all of whose pages are missing is as an empty one."""
+    S, pool = c["S"], c["k"].shape[0]
+    lens = c["lens"].clone()
+    for b, n in enumerate(lens.tolist()):
+        ids = c["table"][b, :-(-n // S)]
+        if not bool(((ids >= 0) & (ids < pool)).any()):
+            lens[b] = 0
+    check_prefix(dict(c, lens=lens), got, dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,H,Hkv,S", [(128, 8, 2, 16), (64, 8, 8, 8), (128, 8, 1, 32)])
+@pytest.mark.parametrize("which", range(len(PREFIX)))
+def test_prefix_pages_that_are_not_there(gpu_lib, dtype, D, H, Hkv, S, which):
+    say(f"holes {dtype} {(D, H, Hkv, S)} case {which}")
+    c = holes(prefix_case(dtype, H, Hkv, D, S, PREFIX[which], seed=40 + which, loose=1), which)
+    check_holes(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("S,pages", [(16, 511), (16, 513), (8, 1500), (8, 4100), (32, 700)])
+def test_prefix_windows_and_long_items(gpu_lib, dtype, S, pages):
+    """One KV head and few or many rows: items of many windows of page ids, their last tiles cut; two groups of different lengths."""
+    say(f"long {dtype} S={S} pages={pages}")
+    for own, H in (([3, 50], 2), ([9] * 20, 8), ([1] * 70, 8)):
+        c = prefix_case(dtype, H, 1, 64, S, [(own, pages), ([2, 2], pages // 3)], seed=pages, poison=False)
+        check_prefix(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+    c = holes(c, 1)
+    check_holes(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+
+
+@pytest.mark.parametrize("own_tokens", [0, 90])
+def test_prefix_items_of_the_most_pages(gpu_lib, own_tokens):
+    """So many groups that an item may be as long as its page ids reach: 20 prefixes of 2000 pages with 8 heads."""
+    c = prefix_case(torch.bfloat16, 8, 8, 64, 8, [([7, 5], 2000)] * 20, seed=3, poison=False)
+    want = make_groups(c, 8, max_own_tokens=own_tokens)
+    check_prefix(c, want.paged_decode(c["q"].to(DEV)), torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("H,D,S", [(8, 128, 16), (2, 64, 32), (8, 64, 8)])
+def test_prefix_that_nobody_fills(gpu_lib, dtype, H, D, S):
+    """Samples of one prompt before their first token: the last page of the prefix is not full, and what lies behind its tokens is NaN; then members that all end
+    pages before the prefix does, and by different amounts in different blocks of rows."""
+    for owns in ([-1] * 3, [-S + 1] * 40, [-3 * S - 5] * 5, [-9 - i for i in range(2 * S)], [-7 * S - i for i in range(70)], [-10 ** 6, -10 ** 6]):
+        for pages in (9, 40):
+            c = prefix_case(dtype, H, 2, D, S, [(owns, pages)], seed=pages)
+            for key in ("k", "v"):
+                row = c["table"][c["members"][0].long()].long()[:pages]
+                flat = c[key][row].transpose(1, 2).reshape(pages * S, 2, D)
+                flat[int(c["lens"].max()):] = math.nan
+                c[key][row] = flat.view(pages, S, 2, D).transpose(1, 2)
+            check_prefix(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+
+
+@pytest.mark.parametrize("n,each", [(120, 2), (300, 2), (700, 2), (1030, 1), (600, 3)])
+def test_prefix_many_groups(gpu_lib, n, each):
+    """Plans of up to 255 sources, up to 1023, and more."""
+    say(f"groups {n} of {each}")
+    r = random.Random(n)
+    c = prefix_case(torch.float32, 2, 1, 64, 8, [([r.randrange(30) for _ in range(each)], r.randrange(4)) for _ in range(n)], seed=n, loose=3, poison=False)
+    check_prefix(c, make_groups(c, 2).paged_decode(c["q"].to(DEV)), torch.float32)
+
+
+@pytest.mark.parametrize("loose", [0, 300, 1100])
+def test_prefix_members_that_are_none(gpu_lib, loose):
+    """-1 and numbers outside the batch among the members, also as a group's first; without a list; the number of groups' bounds used up."""
+    c = prefix_case(torch.bfloat16, 8, 2, 128, 16, [([17] * 5, 9), ([100, 3, 40], 20), ([5, 6], 0)], seed=8, loose=loose)
+    listed = c["members"].tolist()
+    for at, gone in ((0, -1), (5, len(c["lens"]) + 4), (6, -1), (9, -5)):
+        c["members"][at] = gone
+    groups = make_groups(c, 8)
+    groups.out.fill_(-7.0)
+    got = groups.paged_decode(c["q"].to(DEV))
+    torch.cuda.synchronize()
+    out = got[0].cpu()
+    there = [b for b in c["members"].tolist() if 0 <= b < len(c["lens"])]
+    gone = sorted(set(listed) - set(there))
+    assert (out[gone] == -7).all()
+    c["members"] = torch.tensor(there, dtype=torch.int32)
+    check_prefix(c, got, torch.bfloat16)
+
+
+def test_prefix_without_a_list_of_members(gpu_lib):
+    c = prefix_case(torch.bfloat16, 8, 2, 128, 16, [([17] * 5, 9), ([100, 3, 40], 20)], seed=9)
+    order = c["members"].long()
+    for key in ("q", "table", "lens"):
+        c[key] = c[key][order]
+    c["members"] = torch.arange(8, dtype=torch.int32)
+    check_prefix(c, make_groups(c, 8, members=None).paged_decode(c["q"].to(DEV)), torch.bfloat16)
+
+
+@pytest.mark.parametrize("loose", [0, 400, 1200])
+def test_prefix_starts_that_do_not_ascend_write_nothing(gpu_lib, loose):
+    """Refused on the device: the plan sees it, there are no items and no members."""
+    c = prefix_case(torch.float32, 8, 2, 64, 16, [([17] * 5, 9), ([100, 3, 40], 20), ([4, 4], 2)], seed=9, loose=loose)
+    n = c["starts"][-1]
+    for starts in ([0, n, 0, n], [0, 5, 4, n], [n, 0, 0, 0]):
+        groups = make_groups(c, 8, group_starts=i32(starts), max_members=n)
+        groups.out.fill_(-7.0)
+        groups.lse.fill_(-7.0)
+        out, lse = groups.paged_decode(c["q"].to(DEV))
+        torch.cuda.synchronize()
+        assert (out == -7).all() and (lse == -7).all()
+
+
+def test_prefix_bounds_hold(gpu_lib):
+    """What lies beyond the host's bounds does not count: members, pages of prefixes, own pages."""
+    c = prefix_case(torch.float32, 8, 2, 64, 16, [([30, 100, 70, 1], 6), ([200, 90], 3)], seed=4, poison=False)
+    first = c["members"][:2].tolist() + c["members"][4:].tolist()
+    groups = make_groups(c, 8, max_members=2)
+    groups.out.fill_(-7.0)
+    out, _ = groups.paged_decode(c["q"].to(DEV))
+    rest = [b for b in c["members"].tolist() if b not in first]
+    assert (out[rest] == -7).all()
+    d = dict(c, members=torch.tensor(first, dtype=torch.int32))
+    check_prefix(d, (groups.out, groups.lse), torch.float32)
+    # own pages: two of each
+    d = dict(c, lens=torch.minimum(c["lens"], torch.tensor([96 + 32 if b in c["members"][:4].tolist() else 48 + 32 for b in range(6)], dtype=torch.int32)))
+    got = make_groups(c, 8, max_own_tokens=32).paged_decode(c["q"].to(DEV))
+    check_prefix(d, got, torch.float32)
+
+
+def test_prefix_a_member_listed_twice_and_other_scales(gpu_lib):
+    c = prefix_case(torch.bfloat16, 8, 2, 128, 16, [([30, 100, 30], 6)], seed=5, loose=3)
+    twice = c["members"].tolist() + [c["members"][1].item()]
+    want = [x.clone() for x in make_groups(c, 8).paged_decode(c["q"].to(DEV), sm_scale=1.0 / math.sqrt(128))]
+    groups = make_groups(c, 8, group_starts=i32([0, 4]), members=i32(twice + [0] * 6), max_members=4)
+    check_prefix(c, groups.paged_decode(c["q"].to(DEV)), torch.bfloat16)
+    small = make_groups(c, 8)
+    half = dict(c, q=c["q"] * 0.5)  # exact
+    got = small.paged_decode(half["q"].to(DEV), sm_scale=2.0 / math.sqrt(128))
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prefix_strided_caches(gpu_lib, dtype):
+    """Keys and values of a page next to each other, and heads apart."""
+    c = prefix_case(dtype, 8, 2, 128, 16, [([30, 100, 0], 70), ([5] * 9, 3)], seed=6)
+    P, Hkv, S, D = c["k"].shape
+    both = torch.full((P, Hkv, 2, S, D), math.nan, dtype=dtype, device=DEV)
+    both[:, :, 0], both[:, :, 1] = c["k"].to(DEV), c["v"].to(DEV)
+    groups = make_groups(c, 8, k_cache=both[:, :, 0], v_cache=both[:, :, 1])
+    check_prefix(c, groups.paged_decode(c["q"].to(DEV)), dtype)
+    apart = [torch.full((P + 1, Hkv, S, D), math.nan, dtype=dtype, device=DEV) for _ in range(2)]
+    room = torch.cat([apart[1], apart[0]])  # values before keys
+    k, v = room[P + 1:2 * P + 1], room[:P]
+    k.copy_(c["k"]), v.copy_(c["v"])
+    check_prefix(c, make_groups(c, 8, k_cache=k, v_cache=v).paged_decode(c["q"].to(DEV)), dtype)
+
+
+def test_prefix_without_lse_and_far_pages(gpu_lib):
+    """No lse is wanted; pages beyond 2^31 elements of the cache, 2^32 bytes."""
+    c = prefix_case(torch.bfloat16, 8, 2, 128, 16, [([30, 100, 0], 40)], seed=7, poison=False)
+    P, Hkv, S, D = c["k"].shape
+    pages = (1 << 31) // (Hkv * S * D) + P + 9
+    k, v = (torch.empty((pages, Hkv, S, D), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    k[-P:], v[-P:] = c["k"].to(DEV), c["v"].to(DEV)
+    table = torch.where(c["table"] < 0, -1, c["table"] + (pages - P))
+    groups = make_groups(c, 8, k_cache=k, v_cache=v, page_table=table.to(DEV))
+    check_prefix(c, groups.paged_decode(c["q"].to(DEV)), torch.bfloat16)
+    want = groups.out.clone()
+    groups.out.zero_()
+    lib = groups.lib
+    lib.shared_prefix_decode(groups.desc, groups.groups, c["q"].to(DEV), 0.0, groups.out, None, groups.workspace)
+    torch.cuda.synchronize()
+    assert torch.equal(groups.out, want)
+
+
+# ------------------------------------------------------------------ together
+
+class Server:
+    """A batch that decodes: places for the new tokens, heads into the cache, statistics of the touched pages, attention over the prefix that all of its
+    sequences share; with a plain copy of everything on the host."""
+
+    def __init__(self, seed, dtype=torch.bfloat16, H=16, Hkv=4, D=128, S=16, B=6, prefix=5, pages=400, rows=64):
+        self.geo = H, Hkv, D, S, B, prefix
+        self.dtype, self.g = dtype, torch.Generator().manual_seed(seed)
+        self.r = random.Random(seed)
+        self.kc, self.vc = (torch.zeros((pages, Hkv, S, D), dtype=dtype, device=DEV) for _ in range(2))
+        ids = list(range(pages))
+        self.r.shuffle(ids)
+        self.prefix = [ids.pop() for _ in range(prefix)]
+        for cache in (self.kc, self.vc):
+            cache[self.prefix] = torch.randn((prefix, Hkv, S, D), generator=self.g).to(dtype).to(DEV)
+        self.k, self.v = self.kc.cpu(), self.vc.cpu()  # the plain copies
+        width = 40
+        self.host = dict(S=S, table=[self.prefix + [-1] * (width - prefix) for _ in range(B)], lens=[prefix * S] * B, free=ids, free_count=len(ids),
+                         rows=rows, capacity=len(ids), shared=[prefix] * B, nxt=[prefix * S + 1000 * b for b in range(B)])
+        h = self.host
+        self.table, self.lens, self.nxt, self.shared = i32(h["table"]), i32(h["lens"]), i32(h["nxt"]), i32(h["shared"])
+        self.pool = PagePool(q_heads=H, kv_heads=Hkv, head_dim=D, page_size=S, dtype=dtype, num_pages=pages, page_table=self.table, seq_lens=self.lens,
+                             max_new_tokens=rows, free_pages=i32(ids), free_count=i32([len(ids)]), shared_pages=self.shared, next_positions=self.nxt)
+        self.weights = [(1 + 0.2 * torch.randn((D,), generator=self.g)).to(dtype) for _ in range(2)]
+        self.f = rotary_frequencies(D // 2, base=5e5)
+        self.writer = CacheWriter(q_heads=H, k_cache=self.kc, v_cache=self.vc, q_weight=self.weights[0].to(DEV), k_weight=self.weights[1].to(DEV),
+                                  frequencies=self.f)
+        self.groups = PrefixGroups(q_heads=H, k_cache=self.kc, v_cache=self.vc, page_table=self.table, seq_lens=self.lens, group_starts=i32([0, B]),
+                                   prefix_pages=i32([prefix]), max_members=B, max_prefix_pages=prefix)
+        self.new = torch.zeros((B,), dtype=torch.int32, device=DEV)
+        self.x = torch.zeros((rows, H + 2 * Hkv, D), dtype=dtype, device=DEV)
+        self.q_out = torch.zeros((rows, H, D), dtype=dtype, device=DEV)
+        self.q = torch.zeros((B, H, D), dtype=dtype, device=DEV)
+        self.out, self.lse = torch.zeros_like(self.groups.out), torch.zeros_like(self.groups.lse)
+
+    def step(self):
+        """What the server launches, and a graph records."""
+        H, Hkv = self.geo[:2]
+        self.pool.place_tokens(self.new)
+        self.writer.append_tokens(*self.x.split([H, Hkv, Hkv], 1), self.pool.positions, self.pool.slots, q_out=self.q_out)
+        last = (self.pool.token_starts[1:] - 1).clamp(min=0).long()  # each sequence's last new token asks
+        torch.index_select(self.q_out, 0, last, out=self.q)
+        self.groups.paged_decode(self.q)
+
+    def inputs(self, new):
+        rows = self.x.shape[0]
+        self.asked = new
+        self.xh = torch.randn(self.x.shape, generator=self.g).to(self.dtype)
+        self.new.copy_(i32(new))
+        self.x.copy_(self.xh)
+
+    def check(self):
+        H, Hkv, D, S, B, prefix = self.geo
+        torch.cuda.synchronize()
+        h = self.host
+        want = R.place(**{**h, "new": self.asked})
+        assert self.table.tolist() == want["table"] and self.lens.tolist() == want["seq_lens"] and self.nxt.tolist() == want["next"]
+        assert self.pool.slots.tolist() == want["slots"] and self.pool.positions.tolist() == want["positions"] and self.pool.placed.tolist() == want["placed"]
+        assert self.pool.free_pages[:int(self.pool.free_count)].tolist() == want["stack"]
+        h.update(table=want["table"], lens=want["seq_lens"], nxt=want["next"], free=want["stack"], free_count=len(want["stack"]))
+        slots, positions = torch.tensor(want["slots"]), torch.tensor(want["positions"])
+        here = slots >= 0
+        q, k, v = self.xh.split([H, Hkv, Hkv], 1)
+        got_k, got_v = self.kc.cpu(), self.vc.cpu()
+        for x, w, got in ((q, self.weights[0], self.q_out.cpu()), (k, self.weights[1], got_k.transpose(1, 2).reshape(-1, Hkv, D)[slots.clamp(min=0)])):
+            y, size = R.heads(x, w, 1e-6, positions, self.f, 1.0, False)
+            assert ((got.double() - y).abs() <= append_bound(y, size, self.dtype))[here].all()
+        # the keys as they were rounded, from here on
+        at = slots[here]
+        self.k[at // S, :, at % S] = got_k[at // S, :, at % S]
+        self.v[at // S, :, at % S] = v[here]
+        assert torch.equal(got_k, self.k) and torch.equal(got_v, self.v)
+        c = dict(q=self.q.cpu(), k=self.k, v=self.v, table=self.table.cpu(), lens=self.lens.cpu(), members=torch.arange(B))
+        check_prefix(c, (self.groups.out, self.groups.lse), self.dtype)
+
+
+    def admit(self):
+        """Sequences that have ended make room for others with the same prefix."""
+        S, prefix, h = self.geo[3], self.geo[5], self.host
+        for b, n in enumerate(self.asked):
+            if n < 0:
+                h["table"][b][:prefix] = self.prefix
+                h["lens"][b], h["nxt"][b] = prefix * S, prefix * S + 7
+                self.table[b, :prefix] = i32(self.prefix)
+                self.lens[b], self.nxt[b] = prefix * S, prefix * S + 7
+
+
+def asked(r, i, B):
+    """Tokens of a step: most decode, some bring a few, in some steps one ends."""
+    new = [r.choice([1, 1, 1, 5, 0]) for _ in range(B)]
+    if i % 5 == 4:
+        new[i // 5 % B] = -1  # also the first
+    return new
+
+
+@pytest.mark.parametrize("captured", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_server_places_appends_and_attends(gpu_lib, dtype, captured):
+    """Thirty steps, every one against the host's copy; eager, or one HIP graph replayed with work of other kinds between the replays."""
+    s = Server(11, dtype)
+    graph = None
+    for i in range(30):
+        new = asked(s.r, i, s.geo[4])
+        s.inputs(new)
+        if captured and graph is None and i == 2:
+            graph = torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph):
+                s.step()
+        if graph is not None:
+            graph.replay()
+        else:
+            s.step()
+        s.check()
+        s.admit()
+        if i % 4 == 0:
+            (torch.randn((512, 512), device=DEV) @ torch.randn((512, 512), device=DEV)).sum().item()
+
+
+def test_two_servers_on_two_streams(gpu_lib):
+    """Each behind a long kernel of its own stream, with objects of its own."""
+    servers = [Server(21), Server(22, prefix=30, B=9)]
+    streams = [torch.cuda.Stream() for _ in servers]
+    big = torch.randn((4096, 4096), device=DEV)
+    for i in range(3):
+        for s in servers:
+            s.inputs(asked(s.r, 0, s.geo[4]))
+        torch.cuda.synchronize()
+        for s, stream in zip(servers, streams):
+            with torch.cuda.stream(stream):
+                big @ big
+                s.step()
+        torch.cuda.synchronize()
+        for s in servers:
+            s.check()
