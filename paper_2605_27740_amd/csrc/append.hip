@@ -16,7 +16,6 @@ namespace unique {
 namespace {
 
 constexpr int kAppendWaves = 4;
-constexpr int kAppendAhead = 2;  // steps of heads in flight
 
 template <typename T>
 __device__ __forceinline__ Raw16 pack_vec(const float (&x)[Elem<T>::kVec]) {
@@ -32,16 +31,14 @@ __device__ __forceinline__ Raw16 pack_vec(const float (&x)[Elem<T>::kVec]) {
   return r;
 }
 
-// kInterleaved: pairs are neighbours. A wave takes `per` steps of heads of a token, the wave's item = (token, part of its heads).
-// early: the first heads are asked for before the slot is known.
-template <typename T, int D, bool kInterleaved>
-__global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c, AppendArgs a, int steps, int per, bool early) {
+// kInterleaved: pairs are neighbours. A wave takes kAhead steps of a token's heads, of which there are `parts`. early: the first heads are asked for before the slot is known.
+template <typename T, int D, bool kInterleaved, int kAhead>
+__global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c, AppendArgs a, int parts, bool early) {
   constexpr int kVec = Elem<T>::kVec;
   constexpr int kLanes = D / kVec / 2;      // lanes of a head
   constexpr int kHeads = kWave / kLanes;    // heads of a step
   __shared__ float2 s_turn[kAppendWaves][D / 2];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int parts = (steps + per - 1) / per;
   const int64_t item = (int64_t)blockIdx.x * kAppendWaves + wave;
   const int64_t row = item / parts;
   if (row >= a.rows) return;  // (no barrier below)
@@ -70,13 +67,13 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c
     x[0] = load_raw(src + c0 * kVec);
     x[1] = load_raw(src + c1 * kVec);
   };
-  const int begin = part * per, end = min(begin + per, steps);
-  Raw16 x[kAppendAhead][2];
-  auto load_few = [&](int s0) {
+  const int begin = part * kAhead;
+  Raw16 x[kAhead][2];
+  auto load_all = [&] {
 #pragma unroll
-    for (int u = 0; u < kAppendAhead; ++u) load(s0 + u, x[u]);
+    for (int u = 0; u < kAhead; ++u) load(begin + u, x[u]);  // (of a step that there is not: the last head again)
   };
-  if (early) load_few(begin);
+  if (early) load_all();
   if (slot < 0 || slot >= c.num_phys * c.S) return;
   if (lane < R / 2) {
     const double turns = (double)position * (a.how.frequencies[lane] * 0.15915494309189535);
@@ -149,13 +146,9 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c
     *reinterpret_cast<uint4*>(dst + c1 * kVec) = z1.v;
   };
 
-  if (!early) load_few(begin);
-  for (int s0 = begin; s0 < end; s0 += kAppendAhead) {
-    if (s0 > begin) load_few(s0);
+  if (!early) load_all();
 #pragma unroll
-    for (int u = 0; u < kAppendAhead; ++u)
-      if (s0 + u < end) finish(s0 + u, x[u]);  // uniform
-  }
+  for (int u = 0; u < kAhead; ++u) finish(begin + u, x[u]);
 }
 
 }  // namespace
@@ -165,19 +158,19 @@ hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t st
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value, kHeads = kWave / (D / Elem<T>::kVec / 2);
     const int steps = (c.H + 2 * c.Hkv + kHeads - 1) / kHeads;
-    // A wave takes all of a token, or less where there are few. What it does before its first head, the angles and weights, is little of fp32 heads' time and of a call's without norm:
-    // there, in long calls, a step each. us, all of a token / parts that make 16384 items / a step: 8192 bf16 tokens of 48 heads 44.2 / 41.0 / 44.6, without norm 43.4 / 40.2 / 41.9; 65536 of
-    // 80 heads 511 / 511 / 538, without norm 505 / 506 / 482; 16384 fp32 tokens of 48 heads 157 / 157 / 144. (Parts that make 4096 items, for 16384: 44.2 of the first.)
-    int per = steps;
-    if (a.rows >= 16384 && (!a.how.q_weight || c.dtype == 0)) per = 1;
-    while (per > 1 && (int64_t)a.rows * ((steps + per - 1) / per) < 16384) per = (per + 1) / 2;
-    const int64_t items = (int64_t)a.rows * ((steps + per - 1) / per);
+    // Two steps a wave, whose angles and weights are formed once, or one where they are little of the time: fp32 heads and calls without norm, in long calls. us, all of a token /
+    // two steps / one: 8192 bf16 tokens of 48 heads 45.5 / 41.2 / 44.6; 24000 of 80 heads 196 / 173 / 187, 65536 511 / 470 / 505, without norm 507 / 472 / 448; 16384 fp32 tokens of 48
+    // heads 157 / 147 / 142. Three steps: 44.1, 177, 482.
+    const bool one = a.rows >= 16384 && (!a.how.q_weight || c.dtype == 0);
+    const int per = one ? 1 : 2, parts = (steps + per - 1) / per;
+    const int64_t items = (int64_t)a.rows * parts;
     const bool early = items <= 8192;  // all waves at once: otherwise tokens without a slot would be read in vain
     auto go = [&](auto kernel) {
-      kernel<<<dim3((unsigned)((items + kAppendWaves - 1) / kAppendWaves)), dim3(kAppendWaves * kWave), 0, st>>>(c, a, steps, per, early);
+      kernel<<<dim3((unsigned)((items + kAppendWaves - 1) / kAppendWaves)), dim3(kAppendWaves * kWave), 0, st>>>(c, a, parts, early);
       return hipGetLastError();
     };
-    return a.how.interleaved ? go(append_kernel<T, D, true>) : go(append_kernel<T, D, false>);
+    if (one) return a.how.interleaved ? go(append_kernel<T, D, true, 1>) : go(append_kernel<T, D, false, 1>);
+    return a.how.interleaved ? go(append_kernel<T, D, true, 2>) : go(append_kernel<T, D, false, 2>);
   };
   auto with_dim = [&](auto elem) {
     return c.D == 64 ? with(elem, std::integral_constant<int, 64>()) : with(elem, std::integral_constant<int, 128>());
