@@ -12,7 +12,7 @@ namespace unique {
 namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / kWave;
-constexpr int kFillThreads = 256, kFillRows = 4;  // rows of a thread
+constexpr int kFillThreads = 256;
 constexpr int kMostTokens = 1 << 25;              // where sums of tokens saturate, above any number of rows
 
 enum SeatState { kUnplaced = 0, kPlaced = 1, kEnded = 2 };
@@ -152,8 +152,8 @@ __device__ __forceinline__ int sequence_of(const int* starts, int lo, int B, int
 }
 
 // The same for 64 rows of a wave, lane after lane, of which the first has a sequence: all lanes look for that one's, in 64 places at a time, and the ends of 64 sequences from there on answer
-// the others. Two trips to memory for 4096 sequences and one more, where a search by every lane makes twelve. With one launch fewer: 500 sequences of 1 to 2048 tokens 18.1 / 13.2 us,
-// 32 prompts of 8000 to 32768 13.7 / 12.1.
+// the others. Two trips to memory for 4096 sequences and one more, where a search by every lane makes twelve. With one launch fewer: 500 sequences of 1 to 2048 tokens 18.1 / 13.1 us,
+// 32 prompts of 8000 to 32768 13.7 / 11.8.
 __device__ __forceinline__ int sequence_of_lane(const int* starts, int B, int first, int lane) {
   int lo = 0, hi = B - 1;  // uniform
   while (lo < hi) {
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(kFillThreads) void place_many_back_kernel(CacheView
   for (int b = blockIdx.x; b < c.B; b += gridDim.x) give_back(c, p, at.back[b], b, threadIdx.x, kFillThreads);
 }
 
-// The first workgroups take sequences, the others rows.
+// The first workgroups take sequences, the others rows, one a thread (four: 13.1 and 11.8 us where one takes 10.2 and 9.9).
 __global__ __launch_bounds__(kFillThreads) void place_fill_kernel(CacheView c, unique_placement p, PlaceArrays at) {
   const int tells = (c.B + kFillThreads - 1) / kFillThreads;
   if ((int)blockIdx.x < tells) {
@@ -240,13 +240,10 @@ __global__ __launch_bounds__(kFillThreads) void place_fill_kernel(CacheView c, u
     return;
   }
   const int size = at.size[0], all = at.starts[c.B];
-#pragma unroll
-  for (int k = 0; k < kFillRows; ++k) {
-    const int row = ((blockIdx.x - tells) * kFillRows + k) * kFillThreads + threadIdx.x, lane = row % kWave;
-    if (row - lane >= p.max_new_tokens) return;  // uniform, as below
-    const int b = row - lane < all ? sequence_of_lane(at.starts, c.B, row - lane, lane) : -1;
-    if (row < p.max_new_tokens) fill_row(c, p, at, size, row, row < all ? b : -1);
-  }
+  const int row = (blockIdx.x - tells) * kFillThreads + threadIdx.x, lane = row % kWave;
+  if (row - lane >= p.max_new_tokens) return;  // uniform, as below
+  const int b = row - lane < all ? sequence_of_lane(at.starts, c.B, row - lane, lane) : -1;
+  if (row < p.max_new_tokens) fill_row(c, p, at, size, row, row < all ? b : -1);
 }
 
 bool place_is_small(const CacheView& c, int max_new_tokens) { return c.B <= kPlanThreads && max_new_tokens <= kSmallRows; }
@@ -278,8 +275,7 @@ hipError_t launch_place(const CacheView& c, const unique_placement& p, void* wor
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int kRows = kFillThreads * kFillRows;
-  const int tells = (c.B + kFillThreads - 1) / kFillThreads, rows = (p.max_new_tokens + kRows - 1) / kRows;
+  const int tells = (c.B + kFillThreads - 1) / kFillThreads, rows = (p.max_new_tokens + kFillThreads - 1) / kFillThreads;
   place_fill_kernel<<<dim3(tells + rows), dim3(kFillThreads), 0, st>>>(c, p, at);
   return hipGetLastError();
 }
