@@ -160,8 +160,8 @@ hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t st
     const int steps = (c.H + 2 * c.Hkv + kHeads - 1) / kHeads;
     // Two steps a wave, whose angles and weights are formed once, or one where they are little of the time: fp32 heads and calls without norm, in long calls. us, all of a token /
     // two steps / one: 8192 bf16 tokens of 48 heads 45.5 / 41.2 / 44.6; 24000 of 80 heads 196 / 173 / 187, 65536 511 / 470 / 505, without norm 507 / 472 / 448; 16384 fp32 tokens of 48
-    // heads 157 / 147 / 142. Three steps: 44.1, 177, 482.
-    const bool one = a.rows >= 16384 && (!a.how.q_weight || c.dtype == 0);
+    // heads 157 / 147 / 142. Three steps: 44.1, 177, 482. And one where all waves of one step run at once: 32 tokens 5.0 / 4.1 (the kernel).
+    const bool one = (int64_t)a.rows * steps <= 8192 || (a.rows >= 16384 && (!a.how.q_weight || c.dtype == 0));
     const int per = one ? 1 : 2, parts = (steps + per - 1) / per;
     const int64_t items = (int64_t)a.rows * parts;
     const bool early = items <= 8192;  // all waves at once: otherwise tokens without a slot would be read in vain
