@@ -373,7 +373,8 @@ typedef struct unique_prefix_groups {
 } unique_prefix_groups;
 
 /* Bytes of device workspace that the call below may need (256-byte aligned, nothing carried between calls, one for each stream that may
- * overlap another). groups' device pointers are not used. */
+ * overlap another). groups' device pointers are not used. Partial results grow with num_groups * max_prefix_pages, and UNIQUE_ERR_UNSUPPORTED says that they
+ * would be more than 2^31 rows. */
 int unique_shared_prefix_workspace_bytes(const unique_cache_desc* desc, const unique_prefix_groups* groups, size_t* out_bytes);
 
 /* unique_dense_paged_decode for sequences that share the beginnings of their contexts: the pages of a group's prefix are read once for all of its

@@ -309,6 +309,9 @@ int check_groups(const unique::CacheView& v, const unique_prefix_groups* groups,
   g->max_members = std::min(g->max_members, v.B);
   g->max_prefix_pages = std::min(g->max_prefix_pages, v.max_pages_hint);
   g->max_own_pages = g->max_own_pages ? std::min(g->max_own_pages, v.max_pages_hint) : v.max_pages_hint;
+  if (!unique::prefix_fits(v, *g))
+    return fail(UNIQUE_ERR_UNSUPPORTED, "num_groups %d, max_members %d and max_prefix_pages %d leave more work than a launch has room for: give closer bounds",
+                g->num_groups, g->max_members, g->max_prefix_pages);
   return UNIQUE_OK;
 }
 

@@ -2,15 +2,21 @@
 //
 // softmax(q K^T) V over a prefix and a sequence's own tokens is joined from parts (o, m, l): sums relative to the part's own reference m. The parts of the
 // prefix are products: all query heads of a group's members that use a KV head, up to hundreds of rows, times the prefix's keys, read once for all of them. A
-// sequence's own pages are the same with the few rows of one member. What a workgroup takes is an item (prefix_launch.hip): a run of pages times a block of rows.
+// sequence's own pages are the same with the few rows of one member, and the decode kernels' chunk code takes them. What a workgroup takes is an item (prefix_items.hpp): a run of
+// pages times a block of up to 128 query rows, or of a member's own pages.
 //
-// bf16 caches. A workgroup of four waves takes a chunk of a prefix for a KV head and a tile of rows. Tiles of 64 tokens go straight into the LDS. Both
+// bf16 caches. Tiles of 64 tokens go straight into the LDS, 80 KB of them on their way at a time. Both
 // products run on v_mfma_f32_32x32x16_bf16 with the queries as columns: S^T = K Q^T leaves a lane with 16 tokens' logits of ONE query (column lane % 32, rows 8 (i / 4) + 4
 // (lane / 32) + i % 4), so its softmax needs no other lane but lane ^ 32, and these are the k that the lane supplies to O^T = V^T P^T: probabilities never
-// leave their lane. V^T comes out of the LDS by its transposing read. 
+// leave their lane. V^T comes out of the LDS by its transposing read.
 // Probabilities enter the second product rounded to bf16, and their sum does not: 24 bits, in three products, would double the arithmetic, which bounds
 // groups of 32 sequences and more, for an error that is of the size of the output's own rounding.
-// fp32 caches: the same on v_mfma_f32_32x32x2_f32, whose probabilities stay fp32.
+// fp32 caches: the same on v_mfma_f32_32x32x2_f32, whose probabilities stay fp32, with tiles of 32 tokens.
+//
+// What bounds it, at 8 KV heads of 128 channels, bf16, pages of 16 or 32: the stream of keys and values up to some 30 sequences in a group (16 behind 131072 tokens: 552 MB in 94 us, 5.9 TB/s; six groups of
+// 10 with 8 heads each, 1000 to 50000 tokens, 95 us, 5.6), behind it the matrix cores and vector units together (256 behind 32768 tokens: 138 GFLOP in 159 to 168 us, of which the last 20 are the
+// members' own 128 MB; matrix cores 36 % busy, vector units as much, and the clock falls with the power that they take: 198 us in a long run). 512 items are one for each workgroup that fits.
+// Own pages by the same way through the LDS as prefixes: 32 x 8192 tokens with 50 to 2000 of their own 39.4 / 45.0 us; four members with few pages in a workgroup: 39.3 / 43.5.
 #include <type_traits>
 
 #include "prefix_items.hpp"
@@ -145,7 +151,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     v_lane = (v_lane + kTilePages) % kWave;
     ++next_v;
   };
-  // Units go into the ring in the order in which the steps need them, K0 K1 K2 V0 K3 V1 ...: step t takes the keys of tile t and the values of tile t - kLag.
+  // Units go into the ring in the order in which the steps need them (with a lag of two tiles K0 K1 K2 V0 K3 V1 ...): step t takes the keys of tile t and the values of tile t - kLag.
   int loaded = 0;
   for (; loaded < L::kRing - (L::kHalves - 1) && next_v < tiles; ++loaded) {
     if (next_k < tiles && next_k <= next_v + kLag) load_keys();
@@ -158,7 +164,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   const int place = item.place + (live ? row : 0) / G;
   const int seq = a.groups.members ? a.groups.members[place] : place;
   const bool mine = live && seq >= 0 && seq < c.B;
-  const int tokens = mine ? c.seq_lens[seq] : 0;  // of this row's sequence
+  const int tokens = mine ? max(c.seq_lens[seq], 0) : 0;  // of this row's sequence
   const T* q = reinterpret_cast<const T*>(a.q) + ((int64_t)(mine ? seq : 0) * c.H + hkv * G + row % G) * D;
   constexpr int kSteps = kBf16 ? D / 16 : D / 8;  // reads of 16 bytes of a key
   u32x4_t qb[kSteps];  // bf16: the pieces 2 s + half; fp32: the pieces of this half

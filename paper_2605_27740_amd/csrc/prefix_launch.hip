@@ -64,6 +64,8 @@ size_t lay_out(const CacheView& c, const unique_prefix_groups& g, const PrefixSh
 
 }  // namespace
 
+bool prefix_fits(const CacheView& c, const unique_prefix_groups& g) { return shape_of(c, g).fits; }
+
 size_t prefix_bytes(const CacheView& c, const unique_prefix_groups& g) {
   PrefixWork w;
   return lay_out(c, g, shape_of(c, g), nullptr, &w);

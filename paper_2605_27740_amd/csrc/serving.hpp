@@ -64,6 +64,7 @@ struct PrefixArgs {
   PrefixShape shape;
   PrefixWork work;
 };
+bool prefix_fits(const CacheView& c, const unique_prefix_groups& g);  // bounds that a launch can serve
 size_t prefix_bytes(const CacheView& c, const unique_prefix_groups& g);
 hipError_t launch_prefix(const CacheView& c, const unique_prefix_groups& g, const void* q, float scale_log2, void* out, float* lse_out, void* workspace,
                          hipStream_t stream);

@@ -5,6 +5,7 @@
 extern "C" int prefix_items(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members, int max_prefix, int max_own, int sources,
                             const int* pages, const int* rows, const int* own, int* shape, int* count, int* each, int* blocks) {
   const unique::PrefixShape s = unique::prefix_shape(batch, kv_heads, group, elem, page_size, num_groups, max_members, max_prefix, max_own);
+  if (!s.fits) return 1;
   int64_t cost = 0;
   for (int i = 0; i < sources; ++i) {
     blocks[i] = (rows[i] + s.rows - 1) / s.rows;

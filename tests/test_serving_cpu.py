@@ -116,6 +116,11 @@ def test_prefix_refuses(c):
     assert f(d, groups(), A, math.nan, A, None, A, NWS, None) == BAD
     assert f(d, groups(), A, 0.0, A, None, None, NWS, None) == WORKSPACE
     assert f(d, groups(), A, 0.0, A, None, A, 1, None) == WORKSPACE
+    # bounds by which there would be 2^31 rows of partial results and more
+    wide = good_desc(batch=65535, max_pages_per_seq=1 << 20)
+    assert f(C.byref(wide), groups(num_groups=65535, max_members=65535, max_prefix_pages=1 << 20), A, 0.0, A, None, A, 1 << 62, None) == UNSUPPORTED
+    assert c.unique_shared_prefix_workspace_bytes(C.byref(wide), groups(num_groups=65535, max_members=65535, max_prefix_pages=1 << 20), C.byref(n)) == UNSUPPORTED
+    assert c.unique_shared_prefix_workspace_bytes(C.byref(wide), groups(num_groups=65535, max_members=2, max_prefix_pages=100), C.byref(n)) == 0
     assert c.unique_shared_prefix_workspace_bytes(d, groups(), None) == BAD
     assert c.unique_shared_prefix_workspace_bytes(C.byref(good_desc(page_table=0, seq_lens=0, k_cache=0)), groups(starts=0, prefix_pages=0, members=0),
                                                   C.byref(n)) == 0 and n.value > 0
@@ -194,7 +199,7 @@ def prefix_items(rules, kv_heads, group, elem, S, sizes, prefix, own, max_member
     n = len(src)
     arr = [(C.c_int * n)(*col) for col in zip(*src)]
     shape, outs = (C.c_int * 8)(), [(C.c_int * n)() for _ in range(3)]
-    rules.prefix_items(batch, kv_heads, group, elem, S, len(sizes), max_members, max_prefix, max_own, n, *arr, shape, *outs)
+    assert rules.prefix_items(batch, kv_heads, group, elem, S, len(sizes), max_members, max_prefix, max_own, n, *arr, shape, *outs) == 0
     return dict(zip("rows tile wanted max_items max_rows plans slots most".split(), shape)), src, list(zip(*outs))
 
 
