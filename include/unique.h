@@ -322,7 +322,8 @@ typedef struct unique_placement {
   int32_t reserved0;                 /* 0 */
 } unique_placement;
 
-/* Bytes of device workspace that unique_place_tokens may need for this descriptor and so many rows (256-byte aligned, nothing carried between calls). */
+/* Bytes of device workspace that unique_place_tokens may need for this descriptor and so many rows (256-byte aligned, nothing carried between calls, one for
+ * each stream that may overlap another). */
 int unique_place_workspace_bytes(const unique_cache_desc* desc, int32_t max_new_tokens, size_t* out_bytes);
 
 /* Gives the new tokens of every sequence their places, in three steps, each in the order of the batch: pages of freed_pages go back; sequences that

@@ -165,8 +165,10 @@ hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t st
     const int per = one ? 1 : 2, parts = (steps + per - 1) / per;
     const int64_t items = (int64_t)a.rows * parts;
     const bool early = items <= 8192;  // all waves at once: otherwise tokens without a slot would be read in vain
+    const int64_t blocks = (items + kAppendWaves - 1) / kAppendWaves;
+    if (blocks >= (1ll << 32) / (kAppendWaves * kWave)) return hipErrorInvalidConfiguration;  // threads are counted in 32 bits
     auto go = [&](auto kernel) {
-      kernel<<<dim3((unsigned)((items + kAppendWaves - 1) / kAppendWaves)), dim3(kAppendWaves * kWave), 0, st>>>(c, a, parts, early);
+      kernel<<<dim3((unsigned)blocks), dim3(kAppendWaves * kWave), 0, st>>>(c, a, parts, early);
       return hipGetLastError();
     };
     if (one) return a.how.interleaved ? go(append_kernel<T, D, true, 1>) : go(append_kernel<T, D, false, 1>);

@@ -37,7 +37,7 @@ __device__ __forceinline__ int swizzle(int row) { return (row >> 1 & 1) * 4 + (r
 // 16 bytes a lane from base + off into the LDS, lane after lane from `to` on. In assembly, as the compiler would otherwise wait for all loads before every
 // transposing read; nothing is written but the LDS, and who reads that waits by wait_units.
 // The address comes out of lanes by a vector instruction, after which a memory instruction would have to keep a distance that the compiler does not keep for it here;
-// a scalar one need not, and its copy of the address is also the step between m0 and its use.
+// a scalar one need not, and its copy of the address is also the step between m0 and its use. (Nothing else in these kernels uses m0: accesses to the LDS do not here.)
 template <bool kNT>
 __device__ __forceinline__ void load_to_lds(const char* base, uint32_t off, lds_addr_t to) {
   uint64_t copy;

@@ -11,6 +11,7 @@ namespace unique {
 constexpr int kPrefixSlots = 512;  // items that are wanted per launch: two workgroups to a compute unit, that many run at a time
 
 constexpr int kPrefixMostPages = 512;  // of an item of a prefix, whose page ids are held in registers
+constexpr int kPrefixMostWorkgroups = (1 << 24) - 1;  // of 256 threads, of which a launch has fewer than 2^32
 
 struct PrefixShape {
   int32_t rows;         // query rows of a workgroup's block
@@ -18,7 +19,7 @@ struct PrefixShape {
   int32_t wanted;       // items per KV head
   int32_t max_items;    // there are at most, per KV head
   int32_t max_rows;     // rows of partial results at most, per KV head
-  int32_t fits;         // these are numbers of 32 bits, as launches and arrays need them; if not, the call is refused
+  int32_t fits;         // a launch has room for that many; if not, the call is refused
   int32_t plans;        // every workgroup of the attention kernel makes the plan for itself
 };
 
@@ -38,7 +39,7 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   const int64_t cost = blocks * max_prefix_pages + batch * (max_own_pages + 96 / page_size + 1ll);
   const int64_t most_items = s.wanted + (cost > (int64_t)kPrefixMostPages * s.wanted ? longest : 0) + blocks + batch;
   const int64_t items = std::max<int64_t>(std::min(most_items, tiles), 1), all_rows = of_prefixes * s.rows + std::min<int64_t>(s.wanted + batch, tiles) * group;
-  s.fits = items <= INT32_MAX / kv_heads && all_rows <= INT32_MAX;
+  s.fits = items <= kPrefixMostWorkgroups / kv_heads && all_rows <= INT32_MAX;
   s.max_items = s.fits ? (int32_t)items : 0;
   s.max_rows = s.fits ? (int32_t)all_rows : 0;
   // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us: 2 x 2048 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, 776 workgroups) 40.0 / 38.6,

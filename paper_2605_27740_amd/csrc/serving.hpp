@@ -39,11 +39,10 @@ struct PrefixItem {
   int32_t reserved;
 };
 struct PrefixMember {
-  int32_t seq;                       // < 0: left out
-  int32_t count, part, step;         // of the group's items: how many, the row of the first's partial results, rows from one to the next
-  int32_t own_count, own_part;       // of its own
-  int32_t group;
-  int32_t reserved;
+  int32_t seq;                  // < 0: left out
+  int32_t count, part, step;    // of the group's items: how many, the row of the first's partial results, rows from one to the next
+  int32_t own_count, own_part;  // of its own
+  int32_t reserved[2];
 };
 struct PrefixWork {
   int32_t* num_items;    // one number

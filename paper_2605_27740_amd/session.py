@@ -277,7 +277,7 @@ class PagePool:
                      free_count_out=None):
         """``new_tokens`` [batch]: how many each sequence gets, negative: it has ended. ``freed_pages`` and ``freed_count``: what an eviction left, which
         goes back first. In place by default; outputs that are given are written instead (a page table that is given must hold the
-        table's entries: only those that change are written). -> ``positions``, ``slots``, ``token_starts``, ``placed``."""
+        table's entries: only those that change are written). -> ``positions``, ``slots``, ``token_starts``, ``placed`` (the same tensors every time)."""
         assert _current_device() == self._device
         self._check(new_tokens, self._batch)
         place = binding.Placement.from_buffer_copy(self._place)

@@ -633,3 +633,104 @@ def test_two_servers_on_two_streams(gpu_lib):
         torch.cuda.synchronize()
         for s in servers:
             s.check()
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_evicted_pages_are_given_out_again(gpu_lib, captured):
+    """Placement and eviction in turn on one table: what an eviction frees goes back at the next placement, no page is lost or held twice, and positions run on."""
+    B, S, Hkv, budget, width, pages = 5, 8, 2, 6, 16, 60
+    r = random.Random(3)
+    table, lens, nxt = torch.full((B, width), -1, dtype=torch.int32, device=DEV), i32([0] * B), i32([0] * B)
+    geo = dict(q_heads=4, kv_heads=Hkv, head_dim=64, page_size=S, dtype=torch.float32, num_pages=pages, page_table=table, seq_lens=lens)
+    pool = PagePool(max_new_tokens=64, next_positions=nxt, **geo)
+    acc = PageAccounts(budget_pages=budget, sink_pages=1, recent_pages=2, **geo)
+    new = i32([0] * B)
+    host = dict(S=S, table=table.tolist(), lens=[0] * B, nxt=[0] * B, free=list(range(pages)), free_count=pages, rows=64, capacity=pages)
+
+    def step():
+        pool.place_tokens(new, acc.freed_pages, acc.freed_count)
+
+    graph = None
+    for i in range(60):
+        asked = [r.choice([1, 1, 9, 3, 0, -1 if i % 7 == 6 else 1]) for _ in range(B)]
+        new.copy_(i32(asked))
+        freed, count = acc.freed_pages.tolist(), acc.freed_count.tolist()
+        if captured and graph is None and i == 3:
+            graph = torch.cuda.CUDAGraph()
+            torch.cuda.synchronize()
+            with torch.cuda.graph(graph):
+                step()
+        if graph is not None:
+            graph.replay()
+        else:
+            step()
+        torch.cuda.synchronize()
+        want = R.place(**{**host, "new": asked, "freed": freed, "freed_count": count})
+        for key, x in (("table", table), ("seq_lens", lens), ("next", nxt), ("placed", pool.placed), ("slots", pool.slots), ("positions", pool.positions)):
+            assert x.tolist() == want[key], (i, key)
+        assert pool.free_pages[:int(pool.free_count)].tolist() == want["stack"]
+        acc.weights.copy_(torch.rand(acc.weights.shape))
+        acc.evict_pages()
+        torch.cuda.synchronize()
+        held = [p for row, n in zip(table.tolist(), lens.tolist()) for p in row[:-(-n // S)]]
+        back = [p for row, n in zip(acc.freed_pages.tolist(), acc.freed_count.tolist()) for p in row[:n]]
+        assert sorted(held + back + want["stack"]) == list(range(pages)) and max(lens.tolist()) <= budget * S
+        host.update(table=table.tolist(), lens=lens.tolist(), nxt=want["next"], free=want["stack"], free_count=len(want["stack"]))
+        if i % 10 == 0:
+            torch.randn((256, 256), device=DEV).sum().item()
+
+
+def test_prefix_random_batches(gpu_lib):
+    """Shapes, groups and bounds drawn together."""
+    for seed in range(40):
+        r = random.Random(seed)
+        dtype, D, S, Hkv, G = r.choice(DTYPES), r.choice([64, 128]), r.choice([8, 16, 32]), r.choice([1, 2, 4, 8]), r.choice([1, 2, 4, 8])
+        groups = [([r.choice([0, 1, r.randrange(300), -r.randrange(3 * S)]) for _ in range(r.choice([1, 1, 2, 3, 20, 60]))], r.choice([0, 1, r.randrange(60), r.randrange(300)]))
+                  for _ in range(r.choice([1, 2, 6]))]
+        say(f"random {seed}: {dtype} D={D} S={S} Hkv={Hkv} G={G} groups={[(len(o), p) for o, p in groups]}")
+        c = prefix_case(dtype, G * Hkv, Hkv, D, S, groups, seed=seed, loose=r.randrange(3), extra_cols=r.randrange(4), poison=r.random() < 0.7)
+        most = max(max(o) for o, _ in groups)
+        bounds = r.choice([{}, dict(max_own_tokens=max(most, 1)), dict(max_seq_len=max(int(c["lens"].max()), 1)),
+                           dict(max_members=len(c["lens"]) + 3, max_prefix_pages=c["table"].shape[1] + 7)])
+        check_prefix(c, make_groups(c, G * Hkv, **bounds).paged_decode(c["q"].to(DEV)), dtype)
+
+
+def test_objects_refuse_what_does_not_fit(gpu_lib):
+    """Types, shapes and strides that the calls cannot see."""
+    table, lens = torch.full((2, 8), -1, dtype=torch.int32, device=DEV), i32([0, 0])
+    geo = dict(q_heads=4, kv_heads=2, head_dim=64, page_size=8, dtype=torch.float32, num_pages=16, page_table=table, seq_lens=lens, max_new_tokens=4)
+    with pytest.raises(AssertionError):
+        PagePool(free_pages=i32([1, 2]), **geo)
+    with pytest.raises(AssertionError):
+        PagePool(shared_pages=i32([1]), **geo)
+    pool = PagePool(**geo)
+    for bad in (i32([1]), torch.tensor([1, 1], device=DEV), torch.tensor([1, 1], dtype=torch.int32)):
+        with pytest.raises(AssertionError):
+            pool.place_tokens(bad)
+    for over in (dict(freed_count=i32([0, 0])), dict(freed_pages=i32([[1], [2]]), freed_count=i32([0])), dict(seq_lens_out=i32([0])), dict(next_positions_out=i32([0, 0])),
+                 dict(page_table_out=table[:, :4])):
+        with pytest.raises(AssertionError):
+            pool.place_tokens(i32([1, 1]), **over)
+    k, v = (torch.zeros((16, 2, 8, 64), device=DEV) for _ in range(2))
+    for over in (dict(frequencies=torch.ones((32,))), dict(frequencies=torch.ones((33,), dtype=torch.float64)), dict(q_weight=torch.ones((64,), device=DEV)),
+                 dict(q_weight=torch.ones((32,), device=DEV), k_weight=torch.ones((64,), device=DEV)), dict(v_cache=v.bfloat16())):
+        with pytest.raises(AssertionError):
+            CacheWriter(**{**dict(q_heads=4, k_cache=k, v_cache=v), **over})
+    writer = CacheWriter(q_heads=4, k_cache=k, v_cache=v)
+    good = dict(q=torch.zeros((3, 4, 64), device=DEV), k=torch.zeros((3, 2, 64), device=DEV), v=torch.zeros((3, 2, 64), device=DEV), positions=i32([0, 1, 2]),
+                slots=torch.arange(3, device=DEV))
+    writer.append_tokens(**good)
+    for over in (dict(q=good["q"].bfloat16()), dict(k=good["q"]), dict(slots=i32([0, 1, 2])), dict(positions=good["slots"]), dict(v=good["v"][:2]),
+                 dict(q=torch.zeros((3, 64, 4), device=DEV).transpose(1, 2)), dict(q_out=torch.zeros((3, 4, 64))), dict(q=torch.zeros((3, 8, 64), device=DEV)[:, ::2])):
+        with pytest.raises(AssertionError):
+            writer.append_tokens(**{**good, **over})
+    args = dict(q_heads=4, k_cache=k, v_cache=v, page_table=table, seq_lens=lens, group_starts=i32([0, 2]), prefix_pages=i32([1]), max_members=2, max_prefix_pages=1)
+    for over in (dict(group_starts=i32([0])), dict(members=i32([0])), dict(prefix_pages=torch.ones((1,), device=DEV, dtype=torch.int64)), dict(seq_lens=i32([0]))):
+        with pytest.raises(AssertionError):
+            PrefixGroups(**{**args, **over})
+    groups = PrefixGroups(**args)
+    for bad in (torch.zeros((2, 4, 64), device=DEV).bfloat16(), torch.zeros((1, 4, 64), device=DEV), torch.zeros((4, 2, 64), device=DEV).transpose(0, 1)):
+        with pytest.raises(AssertionError):
+            groups.paged_decode(bad)
+    with pytest.raises(RuntimeError):
+        PrefixGroups(**{**args, "max_members": 0})
