@@ -625,6 +625,50 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
                              *reinterpret_cast<DecodeShared<T, D, G>*>(ring));
 }
 
+// A chunk of a member's pages, prefix and own: calls with little to read (prefix_plan.hpp). A member's group is the first that ends behind it.
+template <typename T, int D, int S, int G>
+__global__ __launch_bounds__(kDecWaves* kWave) void prefix_alone_kernel(CacheView c, PrefixArgs a) {
+  __shared__ DecodeShared<T, D, G> sh;
+  const int hkv = blockIdx.x, z = blockIdx.y, place = blockIdx.z;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, n = a.groups.num_groups;
+  const int seq = a.groups.members ? a.groups.members[place] : place;
+  const bool valid = seq >= 0 && seq < c.B;
+  const int N = valid ? max(c.seq_lens[seq], 0) : 0;
+  int group = 0;
+  bool down = false;
+  for (int i0 = 0; i0 < n; i0 += kWave) {
+    const int i = min(i0 + lane, n - 1), from = a.groups.starts[i], to = a.groups.starts[i + 1];
+    down |= to < from;
+    group += __popcll(__ballot(i0 + lane < n && to <= place));
+  }
+  const int of = min(group, n - 1), from = a.groups.starts[of], prefix = min(max(a.groups.prefix_pages[of], 0), a.groups.max_prefix_pages);
+  const bool listed = valid && !__any(down) && group < n && place >= from && place - from < a.groups.max_members;
+  const int end = min(min((N + S - 1) / S, c.max_pages_hint), prefix + a.groups.max_own_pages), chunks = (end + a.shape.chunk_pages - 1) / a.shape.chunk_pages;
+  if (hkv == 0 && z == 0 && threadIdx.x == 0) {
+    PrefixMember m = {};
+    m.seq = listed && chunks > 1 ? seq : -1;  // of one chunk there is nothing to join
+    m.own_count = chunks;
+    m.own_part = place * a.shape.chunks * G;
+    a.work.member[place] = m;
+  }
+  if (!listed || z >= max(chunks, 1)) return;
+  const int64_t part = (int64_t)hkv * a.shape.max_rows + (int64_t)(place * a.shape.chunks + z) * G;
+  const ChunkOut<T> to = {a.work.part_o + part * D, a.work.part_ml + part * 2, reinterpret_cast<T*>(a.out), a.lse_out, max(chunks, 1)};
+  if (chunks == 0) {
+    write_empty<T, D, G>(c, to, seq, hkv);
+    return;
+  }
+  const Chunk chunk = {hkv, seq, z * a.shape.chunk_pages, min((z + 1) * a.shape.chunk_pages, end), N, 0};
+  auto lookup = [&](int e, bool, int& phys, int& ntok) {
+    const int ph = c.page_table[(int64_t)seq * c.max_pages + e];
+    if (ph >= 0 && (int64_t)ph < c.num_phys) {
+      phys = ph;
+      ntok = min(S, N - e * S);
+    }
+  };
+  decode_chunk<D, S, G, false>(c, reinterpret_cast<const T*>(a.q), chunk, wave, lane, lookup, a.scale_log2, to, sh);
+}
+
 // A wave joins the parts of a (member, query head): o = sum of 2^(m_j - M) o_j over sum of 2^(m_j - M) l_j. Lane s takes the pair (m, l) of part s; D / 4 lanes
 // read a part's row, so that a load covers 2 or 4 parts, and eight loads are in flight.
 template <typename T, int D>
@@ -698,6 +742,10 @@ hipError_t launch_items(const CacheView& c, const PrefixArgs& a, hipStream_t st)
 
 template <int S, int G>
 hipError_t launch_rows(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
+  if (a.shape.chunks > 0) {
+    prefix_alone_kernel<UNIQUE_ELEM, UNIQUE_DIM, S, G><<<dim3(c.Hkv, a.shape.chunks, c.B), dim3(kDecWaves * kWave), 0, st>>>(c, a);
+    return hipGetLastError();
+  }
   if constexpr (sizeof(UNIQUE_ELEM) == 2)
     if (a.shape.rows == 64) return launch_items<S, G, 2>(c, a, st);
   return launch_items<S, G, 4>(c, a, st);
@@ -719,7 +767,7 @@ hipError_t launch_group(const CacheView& c, const PrefixArgs& a, hipStream_t st)
 template <>
 hipError_t launch_prefix_of<UNIQUE_ELEM, UNIQUE_DIM>(const CacheView& c, const PrefixArgs& a, hipStream_t st) {
   const hipError_t e = c.S == 8 ? launch_group<8>(c, a, st) : (c.S == 16 ? launch_group<16>(c, a, st) : launch_group<32>(c, a, st));
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.shape.chunks == 1) return e;
   prefix_merge_kernel<UNIQUE_ELEM, UNIQUE_DIM><<<dim3(c.B, (c.H + kMergeWaves - 1) / kMergeWaves), dim3(kMergeWaves * kWave), 0, st>>>(c, a);
   return hipGetLastError();
 }

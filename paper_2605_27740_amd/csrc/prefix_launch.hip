@@ -41,7 +41,7 @@ __global__ __launch_bounds__(kThreads) void prefix_items_kernel(CacheView c, Pre
 size_t aligned(size_t x) { return (x + 255) / 256 * 256; }
 
 PrefixShape shape_of(const CacheView& c, const unique_prefix_groups& g) {
-  return prefix_shape(c.B, c.Hkv, c.H / c.Hkv, c.dtype == 0 ? 4 : 2, c.S, g.num_groups, g.max_members, g.max_prefix_pages, g.max_own_pages);
+  return prefix_shape(c.B, c.Hkv, c.H / c.Hkv, c.dtype == 0 ? 4 : 2, c.S, c.S * c.D * 2 * (c.dtype == 0 ? 4 : 2), c.max_pages_hint, g.num_groups, g.max_members, g.max_prefix_pages, g.max_own_pages);
 }
 
 // Where everything lies in the workspace; -> its size.
@@ -79,7 +79,7 @@ hipError_t launch_prefix(const CacheView& c, const unique_prefix_groups& g, cons
   const int sources = g.num_groups + c.B;
   PrefixArgs a = {g, q, scale_log2, streams, out, lse_out, shape_of(c, g), {}};
   lay_out(c, g, a.shape, reinterpret_cast<char*>(workspace), &a.work);
-  if (!a.shape.plans) {
+  if (!a.shape.plans && !a.shape.chunks) {
     auto make = [&](auto kernel, int threads) { kernel<<<dim3(1), dim3(threads), 0, st>>>(c, a); };
     if (sources < kFewThreads) make(prefix_items_kernel<kFewThreads, true>, kFewThreads);
     else if (sources <= kHeldSources) make(prefix_items_kernel<kItemThreads, true>, kItemThreads);

@@ -13,6 +13,13 @@ constexpr int kPrefixSlots = 512;  // items that are wanted per launch: two work
 constexpr int kPrefixMostPages = 512;  // of an item of a prefix, whose page ids are held in registers
 constexpr int kPrefixMostWorkgroups = (1 << 24) - 1;  // of 256 threads, of which a launch has fewer than 2^32
 
+// Where there is little to read, every member reads its prefix for itself, in chunks that the host cuts, mostly out of the caches: there is no plan, and nothing to join if a chunk is all. Shared / each
+// for itself, us: 2 x 2148 tokens (fp32, 2 heads of 64, 4 MB) 15.6 / 9.4, 2 x 300 (8 heads, bf16) 13.1 / 7.1, 8 x 1100 (34 MB) 15.4 / 11.5, 16 x 1500 (94 MB) 17.4 / 17.3, 4 x 8500 (133 MB) 22.3 / 24.1.
+constexpr int64_t kPrefixAloneBytes = 64ll << 20;
+// Tokens of such a chunk at least, and half as many again if that is all of them: 2 x 600 tokens in one chunk or two 9.5 / 10.5 us, 900 12.3 / 11.9; chunks of 256, 512 and 1024 tokens at least, 8 x 1100
+// 13.4 / 11.5 / 13.8. fp32, 2 x 2148 tokens of 64 channels, by 128 and 512: 9.8 / 12.7.
+constexpr int prefix_alone_tokens(int elem) { return elem == 4 ? 128 : 512; }
+
 struct PrefixShape {
   int32_t rows;         // query rows of a workgroup's block
   int32_t tile_pages;   // pages of a tile of tokens, a power of two
@@ -21,11 +28,23 @@ struct PrefixShape {
   int32_t max_rows;     // rows of partial results at most, per KV head
   int32_t fits;         // a launch has room for that many; if not, the call is refused
   int32_t plans;        // every workgroup of the attention kernel makes the plan for itself
+  int32_t chunks;       // of a member's pages, at most, where every member reads the prefix for itself; 0: it is shared
+  int32_t chunk_pages;  // pages of such a chunk
 };
 
-inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, int page_size, int num_groups, int max_members, int max_prefix_pages,
-                                int max_own_pages) {
-  PrefixShape s;
+// page_bytes: keys and values of a page and head; max_pages: the most that a sequence has.
+inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, int page_size, int page_bytes, int max_pages, int num_groups, int max_members,
+                                int max_prefix_pages, int max_own_pages) {
+  PrefixShape s = {};
+  const int64_t pages = std::max<int64_t>(std::min<int64_t>((int64_t)max_prefix_pages + max_own_pages, max_pages), 1), members = (int64_t)batch * kv_heads;
+  if (members * pages * page_bytes <= kPrefixAloneBytes) {
+    const int64_t least = prefix_alone_tokens(elem) / page_size, n = 2 * pages <= 3 * least ? 1 : std::min((pages + least - 1) / least, std::max<int64_t>(2 * kPrefixSlots / members, 1));
+    s.chunk_pages = (int32_t)((pages + n - 1) / n);
+    s.chunks = (int32_t)((pages + s.chunk_pages - 1) / s.chunk_pages);
+    s.max_rows = (int32_t)((int64_t)batch * s.chunks * group);
+    s.fits = 1;
+    return s;
+  }
   const int64_t most = (int64_t)max_members * group;
   s.rows = elem == 4 ? 128 : (most <= 64 ? 64 : 128);
   s.tile_pages = (elem == 4 ? 32 : 64) / page_size;
@@ -42,7 +61,7 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   s.fits = items <= kPrefixMostWorkgroups / kv_heads && all_rows <= INT32_MAX;
   s.max_items = s.fits ? (int32_t)items : 0;
   s.max_rows = s.fits ? (int32_t)all_rows : 0;
-  // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us: 2 x 2048 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, 776 workgroups) 40.0 / 38.6,
+  // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us: 2 x 2148 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, 776 workgroups) 40.0 / 38.6,
   // 16 x 131072 (648) 107.6 / 107.2, 60 rows in 6 groups (1048) 107.6 / 108.5.
   s.plans = num_groups + batch < 256 && (int64_t)s.max_items * kv_heads <= 2 * kPrefixSlots;
   return s;

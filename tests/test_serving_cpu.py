@@ -236,3 +236,20 @@ def test_prefix_items_fill_the_chip(rules):
         shape, src, cuts = prefix_items(rules, kv, group, 2, 16, [n], [pages], [own] * n, n, pages, own, n)
         assert shape["wanted"] * kv == shape["slots"]
         assert 0.5 * shape["wanted"] <= sum(n * b for n, _, b in cuts) <= shape["max_items"]
+
+
+def test_prefix_members_for_themselves(rules):
+    """Where there is little to read: chunks cover the most pages that a member may have, every one has some, and they are no more than launches and arrays are made for."""
+    out = (C.c_int * 3)()
+    for seed in range(3000):
+        r = random.Random(seed)
+        batch, kv, group, elem, S, D = r.choice([1, 2, 9, 64, 4096]), r.choice([1, 2, 8, 32]), r.choice([1, 4, 8]), r.choice([2, 4]), r.choice([8, 16, 32]), r.choice([64, 128])
+        width, prefix, own = r.choice([1, 40, 300, 5000, 1 << 22]), r.choice([0, 1, 30, 400, 10_000]), r.choice([0, 1, 50, 5000])
+        page = S * D * 2 * elem
+        rules.prefix_alone(batch, kv, group, elem, S, page, width, prefix, own, out)
+        chunks, pages, rows = out
+        most = max(min(width, prefix + own), 1)
+        assert (chunks > 0) == (most * batch * kv * page <= 64 << 20), seed
+        if chunks:
+            assert chunks * pages >= most > (chunks - 1) * pages and rows == batch * chunks * group
+            assert chunks == 1 or (chunks * batch * kv <= 1024 and pages * S >= (64 if elem == 4 else 256))

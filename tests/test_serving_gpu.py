@@ -251,8 +251,14 @@ def prefix_case(dtype, H, Hkv, D, S, groups, *, seed=0, loose=0, poison=True, ex
                 pages=[p for _, p in groups], groups=groups, S=S)
 
 
-def make_groups(c, H, **over):
-    args = dict(q_heads=H, k_cache=c["k"].to(DEV), v_cache=c["v"].to(DEV), page_table=c["table"].to(DEV), seq_lens=c["lens"].to(DEV),
+def make_groups(c, H, wide=True, **over):
+    """wide: rows of the page table that are long enough (by entries that no sequence reaches) for the batch not to be one of little to read, where every member reads its prefix
+    for itself."""
+    table = c["table"]
+    if wide:
+        columns = (64 << 20) // (len(c["lens"]) * c["k"][0].numel() * 2 * c["k"].element_size()) + 1
+        table = torch.nn.functional.pad(table, (0, max(0, columns - table.shape[1])), value=-1)
+    args = dict(q_heads=H, k_cache=c["k"].to(DEV), v_cache=c["v"].to(DEV), page_table=table.to(DEV), seq_lens=c["lens"].to(DEV),
                 group_starts=i32(c["starts"]), prefix_pages=i32(c["pages"]), members=torch.cat([c["members"], c["members"].new_zeros(len(c["lens"]))]).to(DEV),
                 max_members=max(len(own) for own, _ in c["groups"]), max_prefix_pages=max(c["pages"]))
     args.update(over)
@@ -269,9 +275,9 @@ def prefix_bounds(c, want, dtype):
     return (rel + half)[..., None] * terms * (1 + half) + half * out.abs(), rel + 2.0 ** -22 * lse.abs().nan_to_num(posinf=0.0)
 
 
-def check_prefix(c, got, dtype):
+def check_prefix(c, got, dtype, want=None):
     out, lse = (x.cpu() for x in got)
-    want = R.attend(c["q"], c["k"], c["v"], c["table"], c["lens"])
+    want = want or R.attend(c["q"], c["k"], c["v"], c["table"], c["lens"])
     listed = torch.zeros(len(c["lens"]), dtype=torch.bool)
     listed[c["members"].long()] = True
     tol, tol_lse = prefix_bounds(c, want, dtype)
@@ -281,6 +287,13 @@ def check_prefix(c, got, dtype):
     none = listed & (c["lens"] == 0)
     assert (out[none] == 0).all() and torch.isneginf(lse[none]).all()
     return listed
+
+
+def check_both(c, H, dtype, check=None, **over):
+    """Prefixes shared, and read by every member for itself."""
+    want = R.attend(c["q"], c["k"], c["v"], c["table"], c["lens"])
+    for wide in (True, False):
+        (check or check_prefix)(c, make_groups(c, H, wide=wide, **over).paged_decode(c["q"].to(DEV)), dtype, want)
 
 
 PREFIX = [
@@ -302,13 +315,15 @@ def test_prefix_groups_of_all_kinds(gpu_lib, dtype, D, H, Hkv, S, which):
     prefix or empty, sequences in no group; unwritten slots hold NaN."""
     say(f"prefix {dtype} {(D, H, Hkv, S)} case {which}")
     c = prefix_case(dtype, H, Hkv, D, S, PREFIX[which], seed=which, loose=2, extra_cols=which % 3)
-    groups = make_groups(c, H)
-    groups.out.fill_(-7.0)
-    groups.lse.fill_(-7.0)
-    got = groups.paged_decode(c["q"].to(DEV))
-    torch.cuda.synchronize()
-    listed = check_prefix(c, got, dtype)
-    assert (got[0][~listed.to(DEV)] == -7).all() and (got[1][~listed.to(DEV)] == -7).all(), "sequences in no group"
+    want = R.attend(c["q"], c["k"], c["v"], c["table"], c["lens"])
+    for wide in (True, False):
+        groups = make_groups(c, H, wide=wide)
+        groups.out.fill_(-7.0)
+        groups.lse.fill_(-7.0)
+        got = groups.paged_decode(c["q"].to(DEV))
+        torch.cuda.synchronize()
+        listed = check_prefix(c, got, dtype, want)
+        assert (got[0][~listed.to(DEV)] == -7).all() and (got[1][~listed.to(DEV)] == -7).all(), "sequences in no group"
 
 
 def holes(c, seed):
@@ -326,7 +341,7 @@ def holes(c, seed):
     return c
 
 
-def check_holes(c, got, dtype):
+def check_holes(c, got, dtype, want=None):
     """A sequence all of whose pages are missing is as an empty one."""
     S, pool = c["S"], c["k"].shape[0]
     lens = c["lens"].clone()
@@ -334,7 +349,7 @@ def check_holes(c, got, dtype):
         ids = c["table"][b, :-(-n // S)]
         if not bool(((ids >= 0) & (ids < pool)).any()):
             lens[b] = 0
-    check_prefix(dict(c, lens=lens), got, dtype)
+    check_prefix(dict(c, lens=lens), got, dtype, want)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -343,7 +358,7 @@ def check_holes(c, got, dtype):
 def test_prefix_pages_that_are_not_there(gpu_lib, dtype, D, H, Hkv, S, which):
     say(f"holes {dtype} {(D, H, Hkv, S)} case {which}")
     c = holes(prefix_case(dtype, H, Hkv, D, S, PREFIX[which], seed=40 + which, loose=1), which)
-    check_holes(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+    check_both(c, H, dtype, check_holes)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -353,9 +368,9 @@ def test_prefix_windows_and_long_items(gpu_lib, dtype, S, pages):
     say(f"long {dtype} S={S} pages={pages}")
     for own, H in (([3, 50], 2), ([9] * 20, 8), ([1] * 70, 8)):
         c = prefix_case(dtype, H, 1, 64, S, [(own, pages), ([2, 2], pages // 3)], seed=pages, poison=False)
-        check_prefix(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+        check_both(c, H, dtype)
     c = holes(c, 1)
-    check_holes(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+    check_both(c, H, dtype, check_holes)
 
 
 @pytest.mark.parametrize("own_tokens", [0, 90])
@@ -379,7 +394,7 @@ def test_prefix_that_nobody_fills(gpu_lib, dtype, H, D, S):
                 flat = c[key][row].transpose(1, 2).reshape(pages * S, 2, D)
                 flat[int(c["lens"].max()):] = math.nan
                 c[key][row] = flat.view(pages, S, 2, D).transpose(1, 2)
-            check_prefix(c, make_groups(c, H).paged_decode(c["q"].to(DEV)), dtype)
+            check_both(c, H, dtype)
 
 
 @pytest.mark.parametrize("n,each", [(120, 2), (300, 2), (700, 2), (1030, 1), (600, 3)])
@@ -388,7 +403,7 @@ def test_prefix_many_groups(gpu_lib, n, each):
     say(f"groups {n} of {each}")
     r = random.Random(n)
     c = prefix_case(torch.float32, 2, 1, 64, 8, [([r.randrange(30) for _ in range(each)], r.randrange(4)) for _ in range(n)], seed=n, loose=3, poison=False)
-    check_prefix(c, make_groups(c, 2).paged_decode(c["q"].to(DEV)), torch.float32)
+    check_both(c, 2, torch.float32)
 
 
 @pytest.mark.parametrize("loose", [0, 300, 1100])
@@ -398,16 +413,15 @@ def test_prefix_members_that_are_none(gpu_lib, loose):
     listed = c["members"].tolist()
     for at, gone in ((0, -1), (5, len(c["lens"]) + 4), (6, -1), (9, -5)):
         c["members"][at] = gone
-    groups = make_groups(c, 8)
-    groups.out.fill_(-7.0)
-    got = groups.paged_decode(c["q"].to(DEV))
-    torch.cuda.synchronize()
-    out = got[0].cpu()
     there = [b for b in c["members"].tolist() if 0 <= b < len(c["lens"])]
     gone = sorted(set(listed) - set(there))
-    assert (out[gone] == -7).all()
-    c["members"] = torch.tensor(there, dtype=torch.int32)
-    check_prefix(c, got, torch.bfloat16)
+    for wide in (True, False):
+        groups = make_groups(c, 8, wide=wide)
+        groups.out.fill_(-7.0)
+        got = groups.paged_decode(c["q"].to(DEV))
+        torch.cuda.synchronize()
+        assert (got[0].cpu()[gone] == -7).all()
+        check_prefix(dict(c, members=torch.tensor(there, dtype=torch.int32)), got, torch.bfloat16)
 
 
 def test_prefix_without_a_list_of_members(gpu_lib):
@@ -416,7 +430,7 @@ def test_prefix_without_a_list_of_members(gpu_lib):
     for key in ("q", "table", "lens"):
         c[key] = c[key][order]
     c["members"] = torch.arange(8, dtype=torch.int32)
-    check_prefix(c, make_groups(c, 8, members=None).paged_decode(c["q"].to(DEV)), torch.bfloat16)
+    check_both(c, 8, torch.bfloat16, members=None)
 
 
 @pytest.mark.parametrize("loose", [0, 400, 1200])
@@ -424,8 +438,8 @@ def test_prefix_starts_that_do_not_ascend_write_nothing(gpu_lib, loose):
     """Refused on the device: the plan sees it, there are no items and no members."""
     c = prefix_case(torch.float32, 8, 2, 64, 16, [([17] * 5, 9), ([100, 3, 40], 20), ([4, 4], 2)], seed=9, loose=loose)
     n = c["starts"][-1]
-    for starts in ([0, n, 0, n], [0, 5, 4, n], [n, 0, 0, 0]):
-        groups = make_groups(c, 8, group_starts=i32(starts), max_members=n)
+    for starts, wide in [(x, w) for x in ([0, n, 0, n], [0, 5, 4, n], [n, 0, 0, 0]) for w in (True, False)]:
+        groups = make_groups(c, 8, wide=wide, group_starts=i32(starts), max_members=n)
         groups.out.fill_(-7.0)
         groups.lse.fill_(-7.0)
         out, lse = groups.paged_decode(c["q"].to(DEV))
@@ -437,25 +451,24 @@ def test_prefix_bounds_hold(gpu_lib):
     """What lies beyond the host's bounds does not count: members, pages of prefixes, own pages."""
     c = prefix_case(torch.float32, 8, 2, 64, 16, [([30, 100, 70, 1], 6), ([200, 90], 3)], seed=4, poison=False)
     first = c["members"][:2].tolist() + c["members"][4:].tolist()
-    groups = make_groups(c, 8, max_members=2)
-    groups.out.fill_(-7.0)
-    out, _ = groups.paged_decode(c["q"].to(DEV))
     rest = [b for b in c["members"].tolist() if b not in first]
-    assert (out[rest] == -7).all()
-    d = dict(c, members=torch.tensor(first, dtype=torch.int32))
-    check_prefix(d, (groups.out, groups.lse), torch.float32)
+    for wide in (True, False):
+        groups = make_groups(c, 8, wide=wide, max_members=2)
+        groups.out.fill_(-7.0)
+        out, _ = groups.paged_decode(c["q"].to(DEV))
+        assert (out[rest] == -7).all()
+        check_prefix(dict(c, members=torch.tensor(first, dtype=torch.int32)), (groups.out, groups.lse), torch.float32)
     # own pages: two of each
     d = dict(c, lens=torch.minimum(c["lens"], torch.tensor([96 + 32 if b in c["members"][:4].tolist() else 48 + 32 for b in range(6)], dtype=torch.int32)))
-    got = make_groups(c, 8, max_own_tokens=32).paged_decode(c["q"].to(DEV))
-    check_prefix(d, got, torch.float32)
+    for more in ({}, dict(max_prefix_pages=1 << 14)):  # (the latter: prefixes are shared)
+        check_prefix(d, make_groups(c, 8, max_own_tokens=32, **more).paged_decode(c["q"].to(DEV)), torch.float32)
 
 
 def test_prefix_a_member_listed_twice_and_other_scales(gpu_lib):
     c = prefix_case(torch.bfloat16, 8, 2, 128, 16, [([30, 100, 30], 6)], seed=5, loose=3)
     twice = c["members"].tolist() + [c["members"][1].item()]
     want = [x.clone() for x in make_groups(c, 8).paged_decode(c["q"].to(DEV), sm_scale=1.0 / math.sqrt(128))]
-    groups = make_groups(c, 8, group_starts=i32([0, 4]), members=i32(twice + [0] * 6), max_members=4)
-    check_prefix(c, groups.paged_decode(c["q"].to(DEV)), torch.bfloat16)
+    check_both(c, 8, torch.bfloat16, group_starts=i32([0, 4]), members=i32(twice + [0] * 6), max_members=4)
     small = make_groups(c, 8)
     half = dict(c, q=c["q"] * 0.5)  # exact
     got = small.paged_decode(half["q"].to(DEV), sm_scale=2.0 / math.sqrt(128))
@@ -470,13 +483,12 @@ def test_prefix_strided_caches(gpu_lib, dtype):
     P, Hkv, S, D = c["k"].shape
     both = torch.full((P, Hkv, 2, S, D), math.nan, dtype=dtype, device=DEV)
     both[:, :, 0], both[:, :, 1] = c["k"].to(DEV), c["v"].to(DEV)
-    groups = make_groups(c, 8, k_cache=both[:, :, 0], v_cache=both[:, :, 1])
-    check_prefix(c, groups.paged_decode(c["q"].to(DEV)), dtype)
+    check_both(c, 8, dtype, k_cache=both[:, :, 0], v_cache=both[:, :, 1])
     apart = [torch.full((P + 1, Hkv, S, D), math.nan, dtype=dtype, device=DEV) for _ in range(2)]
     room = torch.cat([apart[1], apart[0]])  # values before keys
     k, v = room[P + 1:2 * P + 1], room[:P]
     k.copy_(c["k"]), v.copy_(c["v"])
-    check_prefix(c, make_groups(c, 8, k_cache=k, v_cache=v).paged_decode(c["q"].to(DEV)), dtype)
+    check_both(c, 8, dtype, k_cache=k, v_cache=v)
 
 
 def test_prefix_without_lse_and_far_pages(gpu_lib):
@@ -503,7 +515,7 @@ class Server:
     """A batch that decodes: places for the new tokens, heads into the cache, statistics of the touched pages, attention over the prefix that all of its
     sequences share; with a plain copy of everything on the host."""
 
-    def __init__(self, seed, dtype=torch.bfloat16, H=16, Hkv=4, D=128, S=16, B=6, prefix=5, pages=400, rows=64):
+    def __init__(self, seed, dtype=torch.bfloat16, H=16, Hkv=4, D=128, S=16, B=6, prefix=5, pages=400, rows=64, width=400):
         self.geo = H, Hkv, D, S, B, prefix
         self.dtype, self.g = dtype, torch.Generator().manual_seed(seed)
         self.r = random.Random(seed)
@@ -514,7 +526,6 @@ class Server:
         for cache in (self.kc, self.vc):
             cache[self.prefix] = torch.randn((prefix, Hkv, S, D), generator=self.g).to(dtype).to(DEV)
         self.k, self.v = self.kc.cpu(), self.vc.cpu()  # the plain copies
-        width = 40
         self.host = dict(S=S, table=[self.prefix + [-1] * (width - prefix) for _ in range(B)], lens=[prefix * S] * B, free=ids, free_count=len(ids),
                          rows=rows, capacity=len(ids), shared=[prefix] * B, nxt=[prefix * S + 1000 * b for b in range(B)])
         h = self.host
@@ -595,9 +606,11 @@ def asked(r, i, B):
 
 @pytest.mark.parametrize("captured", [False, True])
 @pytest.mark.parametrize("dtype", DTYPES)
-def test_a_server_places_appends_and_attends(gpu_lib, dtype, captured):
-    """Thirty steps, every one against the host's copy; eager, or one HIP graph replayed with work of other kinds between the replays."""
-    s = Server(11, dtype)
+@pytest.mark.parametrize("width", [40, 400])
+def test_a_server_places_appends_and_attends(gpu_lib, dtype, captured, width):
+    """Thirty steps, every one against the host's copy; eager, or one HIP graph replayed with work of other kinds between the replays. Tables of 40 pages: every sequence reads
+    the prefix for itself; of 400: it is shared."""
+    s = Server(11, dtype, width=width)
     graph = None
     for i in range(30):
         new = asked(s.r, i, s.geo[4])
@@ -692,7 +705,7 @@ def test_prefix_random_batches(gpu_lib):
         most = max(max(o) for o, _ in groups)
         bounds = r.choice([{}, dict(max_own_tokens=max(most, 1)), dict(max_seq_len=max(int(c["lens"].max()), 1)),
                            dict(max_members=len(c["lens"]) + 3, max_prefix_pages=c["table"].shape[1] + 7)])
-        check_prefix(c, make_groups(c, G * Hkv, **bounds).paged_decode(c["q"].to(DEV)), dtype)
+        check_both(c, G * Hkv, dtype, **bounds)
 
 
 def test_objects_refuse_what_does_not_fit(gpu_lib):
