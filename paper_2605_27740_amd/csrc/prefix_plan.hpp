@@ -8,7 +8,7 @@
 namespace unique {
 
 // Every group is a source of items, its prefix's pages times the blocks of its members' query rows, and every member one, its own pages.
-constexpr int kPrefixSlots = 512;  // items that are wanted per launch: two workgroups to a compute unit, that many run at a time
+constexpr int kPrefixSlots = 512;  // workgroups that run at a time, two to a compute unit
 
 constexpr int kPrefixMostPages = 512;  // of an item of a prefix, whose page ids are held in registers
 constexpr int kPrefixMostWorkgroups = (1 << 24) - 1;  // of 256 threads, of which a launch has fewer than 2^32
@@ -48,8 +48,10 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   const int64_t most = (int64_t)max_members * group;
   s.rows = elem == 4 ? 128 : (most <= 64 ? 64 : 128);
   s.tile_pages = (elem == 4 ? 32 : 64) / page_size;
-  s.wanted = std::max(kPrefixSlots / kv_heads, 1);
   const int64_t blocks = std::min<int64_t>(num_groups * ((most + s.rows - 1) / s.rows), (int64_t)batch * group / s.rows + num_groups);
+  // An eighth fewer items than fit leave room for the short ones, unless a prefix's items are many blocks' anyway. 512 / 448, us: 16 x 131072 tokens 108.5 / 101.8, 24 x 100000 103.7 / 97.2, 32 x 8192 40.2 /
+  // 38.8, 60 rows in 6 groups 107.2 / 105.1, 12 x 30000 with up to 3000 of their own 53.8 / 54.9; 256 x 32768, eight blocks, 182 / 193.
+  s.wanted = std::max((blocks > 2 * num_groups ? kPrefixSlots : kPrefixSlots / 8 * 7) / kv_heads, 1);
   // A source's items are one more than its share of the wanted ones at most, and hold a tile each. A member who is alone in a group has its prefix as their own.
   const int64_t longest = blocks * max_prefix_pages / kPrefixMostPages, prefix_tiles = blocks * ((max_prefix_pages + s.tile_pages - 1) / s.tile_pages);
   const int64_t tiles = prefix_tiles + (int64_t)batch * ((max_own_pages + s.tile_pages - 1) / s.tile_pages);
@@ -61,7 +63,7 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   s.fits = items <= kPrefixMostWorkgroups / kv_heads && all_rows <= INT32_MAX;
   s.max_items = s.fits ? (int32_t)items : 0;
   s.max_rows = s.fits ? (int32_t)all_rows : 0;
-  // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us: 2 x 2148 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, 776 workgroups) 40.0 / 38.6,
+  // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us (512 items wanted): 2 x 2148 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, 776 workgroups) 40.0 / 38.6,
   // 16 x 131072 (648) 107.6 / 107.2, 60 rows in 6 groups (1048) 107.6 / 108.5.
   s.plans = num_groups + batch < 256 && (int64_t)s.max_items * kv_heads <= 2 * kPrefixSlots;
   return s;

@@ -234,7 +234,7 @@ def test_prefix_items_fill_the_chip(rules):
     """Where there is much to read, items are about as many as run at a time."""
     for kv, group, n, pages, own in ((8, 4, 16, 8192, 60), (8, 4, 256, 2048, 20), (8, 8, 10, 1500, 180), (1, 8, 4, 100_000, 10)):
         shape, src, cuts = prefix_items(rules, kv, group, 2, 16, [n], [pages], [own] * n, n, pages, own, n)
-        assert shape["wanted"] * kv == shape["slots"]
+        assert shape["slots"] * 7 // 8 <= shape["wanted"] * kv <= shape["slots"]
         assert 0.5 * shape["wanted"] <= sum(n * b for n, _, b in cuts) <= shape["max_items"]
 
 
