@@ -584,7 +584,7 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
   using L = Unit<T, D, kAcross>;
   constexpr size_t kRingBytes = L::kRing * L::kBytes, kOwnBytes = sizeof(DecodeShared<T, D, G>);
   __shared__ __attribute__((aligned(1024))) char ring[kRingBytes > kOwnBytes ? kRingBytes : kOwnBytes];
-  const int hkv = blockIdx.x & (c.Hkv - 1), index = blockIdx.x / c.Hkv;
+  const int hkv = blockIdx.x & (c.Hkv - 1), index = blockIdx.x >> __builtin_ctz(c.Hkv);
   PrefixItem item;
   if (a.shape.plans) {  // a thread for every source
     ItemsPlan<kDecWaves * kWave, true> plan = {c, a, *reinterpret_cast<ItemsShared<kDecWaves * kWave, true>*>(ring)};

@@ -28,7 +28,7 @@ struct ItemsPlan {
   const PrefixArgs& a;
   ItemsShared<kThreads, kHeld>& sh;
   const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
-  const int n = a.groups.num_groups, sources = n + c.B, G = c.H / c.Hkv;
+  const int n = a.groups.num_groups, sources = n + c.B, shift = __builtin_ctz(c.H) - __builtin_ctz(c.Hkv), G = 1 << shift;
   int before[kClasses + 1] = {};  // items of each class and rows, in the end all
   PrefixSource s = {};            // of this thread's source (kHeld)
   PrefixMember m = {};            // and its member, if it is one
@@ -52,7 +52,7 @@ struct ItemsPlan {
       s.place = bound(from);
       s.rows = size * G;
       s.end = size > 1 ? pages(i) : 0;  // (nobody to share it with: all pages are the member's own)
-      s.blocks = (s.rows + a.shape.rows - 1) / a.shape.rows;
+      s.blocks = (s.rows + a.shape.rows - 1) >> __builtin_ctz(a.shape.rows);  // (a power of two)
       return s;
     }
     const int place = i - n;
@@ -73,14 +73,14 @@ struct ItemsPlan {
     s.rows = G;
     s.blocks = 1;
     s.begin = size_of(from, to) > 1 ? prefix : 0;
-    s.end = min(min((len + c.S - 1) / c.S, c.max_pages_hint), prefix + a.groups.max_own_pages);
+    s.end = min(min(prefix_pages_of(len, c.S), c.max_pages_hint), prefix + a.groups.max_own_pages);
     return s;
   }
   __device__ __forceinline__ int seq_of(int i) const { return a.groups.members ? a.groups.members[i] : i; }
   __device__ __forceinline__ int len_of(int seq) const { return seq >= 0 && seq < c.B ? c.seq_lens[seq] : 0; }
   // The first sequence of a source that is not empty (one that has ended has lost its pages): its row of the page table is that of the others, as far as their prefix goes.
   __device__ __forceinline__ int leader_of(const PrefixSource& of) const {
-    for (int i = of.place, end = of.place + of.rows / G; i < end; ++i) {
+    for (int i = of.place, end = of.place + (of.rows >> shift); i < end; ++i) {
       int seq = kHeld ? sh.full[i] : seq_of(i);
       if (!kHeld && len_of(seq) <= 0) seq = -1;
       if (seq >= 0) return seq;
@@ -111,19 +111,20 @@ struct ItemsPlan {
         if (i >= n) a.work.member[i - n] = m;
       }
     }
-    auto sum = [](int64_t x, int over) {
-#pragma unroll
-      for (int d = 1; d < over; d *= 2) x += __shfl_xor(x, d, kWave);
-      return x;
-    };
-    cost = sum(cost, kWave);
-    if (__any(down)) cost = -(1ll << 56);  // more than all the rest
-    if (lane == 0) sh.cost[wave] = cost;
+    // The sum over the workgroup, in two parts of 24 and more bits within a wave.
+    const int low = __builtin_amdgcn_readlane(wave_inclusive_scan((int)(cost & 0xffffff)), kWave - 1);
+    const int high = __builtin_amdgcn_readlane(wave_inclusive_scan((int)(cost >> 24)), kWave - 1);
+    const bool bad = __any(down);
+    if (lane == 0) sh.cost[wave] = bad ? -1 : ((int64_t)high << 24) + low;
     __syncthreads();
-    cost = __shfl(sum(lane < kWaves ? sh.cost[lane] : 0, kWaves), 0, kWave);
-    ok = cost >= 0;
+    cost = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      ok = ok && sh.cost[w] >= 0;
+      cost += sh.cost[w];
+    }
     if (!ok) return;
-    const int64_t item_pages = prefix_item_pages(cost, a.shape.wanted);
+    const int item_pages = prefix_item_pages(cost, a.shape.wanted);
 
     for (int i0 = 0; i0 < sources; i0 += kThreads) {
       const int i = i0 + t;
@@ -193,7 +194,7 @@ struct ItemsPlan {
     const int run = z / of.blocks, block = z - run * of.blocks;
     PrefixItem item = {};
     item.own = of.kind != kPrefixRun;
-    item.place = of.place + block * (a.shape.rows / G);
+    item.place = of.place + block * (a.shape.rows >> shift);
     item.rows = min(of.rows - block * a.shape.rows, a.shape.rows);
     item.begin = of.begin + run * of.each;
     item.end = min(item.begin + of.each, of.end);

@@ -69,31 +69,38 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   return s;
 }
 
+// (Page sizes are powers of two, and divisions in 64 bits take a workgroup as long as a trip to memory.)
+constexpr int prefix_pages_of(int tokens, int page_size) { return tokens <= 0 ? 0 : (int)(((uint32_t)tokens + page_size - 1) >> __builtin_ctz(page_size)); }
+
 // Kinds of items, in the order in which they are started: the long ones first.
 enum PrefixKind { kPrefixRun = 0, kOwnRun = 1, kShortOwn = 2, kPrefixKinds = 3 };
-constexpr int prefix_kind(bool own, int pages, int64_t item_pages) { return !own ? kPrefixRun : (2 * (int64_t)pages >= item_pages ? kOwnRun : kShortOwn); }
+constexpr int prefix_kind(bool own, int pages, int item_pages) { return !own ? kPrefixRun : (2 * pages >= item_pages ? kOwnRun : kShortOwn); }
 
 // What a source costs, in pages. An item of few rows takes 3.5 us whatever there is to read, as long as 100 tokens of an 8-headed bf16 cache.
 constexpr int64_t prefix_cost(int pages, int blocks, bool own, int page_size) {
-  return pages <= 0 ? 0 : (int64_t)pages * blocks + (own ? 96 / page_size : 0);
+  return pages <= 0 ? 0 : (int64_t)pages * blocks + (own ? prefix_pages_of(96, page_size) : 0);
 }
 
-// Pages of an item, before the items of a source are made equal: such that there are at most `wanted` items and one for each source's block.
-constexpr int64_t prefix_item_pages(int64_t all_pages, int wanted) { return (all_pages + wanted - 1) / wanted; }
+// Pages of an item, before the items of a source are made equal: such that there are at most `wanted` items and one for each source's block. (No source has 2^29 pages.)
+constexpr int prefix_item_pages(int64_t all_pages, int wanted) {
+  if (all_pages <= INT32_MAX / 2) return (int)(((uint32_t)all_pages + (uint32_t)wanted - 1) / (uint32_t)wanted);
+  const int64_t each = (all_pages + wanted - 1) / wanted;
+  return each < (1 << 29) ? (int)each : 1 << 29;
+}
 
 // Items along a source's pages, and the pages of each. A block of many rows gets longer ones: its partial results, 4 bytes times D a row, are written and
 // read again, and tokens are 4 bytes times D (bf16) each as well.
 struct PrefixCut {
   int32_t count, pages;
 };
-constexpr PrefixCut prefix_cut(int pages, int64_t item_pages, int live_rows, int page_size, int tile_pages, bool own) {
+constexpr PrefixCut prefix_cut(int pages, int item_pages, int live_rows, int page_size, int tile_pages, bool own) {
   if (pages <= 0) return PrefixCut{0, tile_pages};
-  const int64_t least = (2ll * live_rows + page_size - 1) / page_size;
-  int64_t p = item_pages > least ? item_pages : least;
+  const int least = prefix_pages_of(2 * live_rows, page_size);
+  uint32_t p = item_pages > least ? item_pages : least;
   if (!own && p > kPrefixMostPages) p = kPrefixMostPages;
-  const int64_t n = (pages + p - 1) / p;
-  int64_t each = (pages + n - 1) / n;
-  each = (each + tile_pages - 1) / tile_pages * tile_pages;
+  const uint32_t n = (pages + p - 1) / p;
+  uint32_t each = (pages + n - 1) / n;
+  each = (each + tile_pages - 1) & ~(uint32_t)(tile_pages - 1);
   return PrefixCut{(int32_t)((pages + each - 1) / each), (int32_t)each};
 }
 

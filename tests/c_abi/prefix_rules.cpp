@@ -18,7 +18,7 @@ extern "C" int prefix_items(int batch, int kv_heads, int group, int elem, int pa
     blocks[i] = (rows[i] + s.rows - 1) / s.rows;
     cost += unique::prefix_cost(pages[i], blocks[i], own[i], page_size);
   }
-  const int64_t item_pages = unique::prefix_item_pages(cost, s.wanted);
+  const int item_pages = unique::prefix_item_pages(cost, s.wanted);
   for (int i = 0; i < sources; ++i) {
     const unique::PrefixCut cut = unique::prefix_cut(pages[i], item_pages, rows[i] < s.rows ? rows[i] : s.rows, page_size, s.tile_pages, own[i]);
     count[i] = cut.count;
