@@ -253,9 +253,12 @@ __global__ __launch_bounds__(kFillThreads) void place_fill_kernel(CacheView c, u
   if (row < p.max_new_tokens) fill_row(c, p, at, size, row, row < all ? b : -1);
 }
 
-// One workgroup takes 5 us, 1 for 1024 rows and 1 for 120 sequences, two launches 10 whatever there is: 64 sequences and 2048 rows 7.1 / 10.1, 4096 rows 9.4 / 10.5, 8192 rows 13.9 / 10.5; 1000
-// sequences and 2000 rows 15.4 / 9.7.
-bool place_is_small(const CacheView& c, int max_new_tokens) { return c.B <= kPlanThreads && max_new_tokens + 8ll * c.B <= 5120; }
+// One workgroup takes 5 us, 1 for 1024 rows, 1 for 120 sequences and 1 for 5600 pages that ended sequences give back; two launches take 10 whatever there is: 64 sequences and 2048 rows 7.1 / 10.1, 4096 rows
+// 9.4 / 10.5, 8192 rows 13.9 / 10.5; 1000 sequences and 2000 rows 15.4 / 9.7; 360 sequences of up to 13600 pages, 66 of which end, 163 / 11.1. Which sequences end the host does not know:
+// rows of the table that hold 2^18 pages in all are 47 us at the very worst.
+bool place_is_small(const CacheView& c, int max_new_tokens) {
+  return c.B <= kPlanThreads && max_new_tokens + 8ll * c.B <= 5120 && (int64_t)c.B * c.max_pages <= 1 << 18;
+}
 
 }  // namespace
 

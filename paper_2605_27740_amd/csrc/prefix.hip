@@ -13,9 +13,9 @@
 // groups of 32 sequences and more, for an error that is of the size of the output's own rounding.
 // fp32 caches: the same on v_mfma_f32_32x32x2_f32, whose probabilities stay fp32, with tiles of 32 tokens.
 //
-// What bounds it, at 8 KV heads of 128 channels, bf16, pages of 16 or 32: the stream of keys and values up to some 30 sequences in a group (16 behind 131072 tokens: 552 MB in 94 us, 5.9 TB/s; six groups of
-// 10 with 8 heads each, 1000 to 50000 tokens, 95 us, 5.6), behind it the matrix cores and vector units together (256 behind 32768 tokens: 138 GFLOP in 159 to 168 us, of which the last 20 are the
-// members' own 128 MB; matrix cores 36 % busy, vector units as much, and the clock falls with the power that they take: 198 us in a long run). 512 items are one for each workgroup that fits.
+// What bounds it, at 8 KV heads of 128 channels, bf16, pages of 16 or 32: the stream of keys and values up to some 30 sequences in a group (16 behind 131072 tokens: 552 MB in 94 us with the plan in
+// front, 6.1 TB/s behind it; six groups of 10 with 8 heads each, 1000 to 50000 tokens, 95 us, 5.8), behind it the matrix cores and vector units together (256 behind 32768 tokens: 138 GFLOP in 159 to 170 us, of
+// which the last 20 are the members' own 128 MB; matrix cores 45 % busy, vector units as much, and the clock falls with the power that they take: 197 us in a long run).
 // Own pages by the same way through the LDS as prefixes: 32 x 8192 tokens with 50 to 2000 of their own 39.4 / 45.0 us; four members with few pages in a workgroup: 39.3 / 43.5.
 #include <type_traits>
 

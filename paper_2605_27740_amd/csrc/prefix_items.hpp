@@ -129,7 +129,7 @@ struct ItemsPlan {
     for (int i0 = 0; i0 < sources; i0 += kThreads) {
       const int i = i0 + t;
       if constexpr (!kHeld) s = i < sources ? a.work.source[i] : PrefixSource{};
-      const PrefixCut cut = prefix_cut(s.end - s.begin, item_pages, min(s.rows, a.shape.rows), c.S, a.shape.tile_pages, i >= n);
+      const PrefixCut cut = prefix_cut(s.end - s.begin, item_pages, min(s.rows, a.shape.rows), a.shape.row_tokens, c.S, a.shape.tile_pages, i >= n);
       mine = cut.count * s.blocks;
       s.kind = prefix_kind(i >= n, min(cut.pages, s.end - s.begin), item_pages);
       int x[kClasses + 1], upto[kClasses + 1];

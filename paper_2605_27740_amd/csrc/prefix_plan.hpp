@@ -24,6 +24,7 @@ struct PrefixShape {
   int32_t rows;         // query rows of a workgroup's block
   int32_t tile_pages;   // pages of a tile of tokens, a power of two
   int32_t wanted;       // items per KV head
+  int32_t row_tokens;   // tokens of an item at least, for four of its rows
   int32_t max_items;    // there are at most, per KV head
   int32_t max_rows;     // rows of partial results at most, per KV head
   int32_t fits;         // a launch has room for that many; if not, the call is refused
@@ -48,6 +49,7 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   const int64_t most = (int64_t)max_members * group;
   s.rows = elem == 4 ? 128 : (most <= 64 ? 64 : 128);
   s.tile_pages = (elem == 4 ? 32 : 64) / page_size;
+  s.row_tokens = elem == 4 ? 2 : 8;
   const int64_t blocks = std::min<int64_t>(num_groups * ((most + s.rows - 1) / s.rows), (int64_t)batch * group / s.rows + num_groups);
   // An eighth fewer items than fit leave room for the short ones, unless a prefix's items are many blocks' anyway. 512 / 448, us: 16 x 131072 tokens 108.5 / 101.8, 24 x 100000 103.7 / 97.2, 32 x 8192 40.2 /
   // 38.8, 60 rows in 6 groups 107.2 / 105.1, 12 x 30000 with up to 3000 of their own 53.8 / 54.9; 256 x 32768, eight blocks, 182 / 193.
@@ -89,13 +91,13 @@ constexpr int prefix_item_pages(int64_t all_pages, int wanted) {
 }
 
 // Items along a source's pages, and the pages of each. A block of many rows gets longer ones: its partial results, 4 bytes times D a row, are written and
-// read again, and tokens are 4 bytes times D (bf16) each as well.
+// read again, and tokens are 4 bytes times D (bf16) each as well. In fp32, whose products take four times as long for each byte, a quarter as long: 70 rows behind 4722 tokens (one KV head) 50.7 / 28.2 us.
 struct PrefixCut {
   int32_t count, pages;
 };
-constexpr PrefixCut prefix_cut(int pages, int item_pages, int live_rows, int page_size, int tile_pages, bool own) {
+constexpr PrefixCut prefix_cut(int pages, int item_pages, int live_rows, int row_tokens, int page_size, int tile_pages, bool own) {
   if (pages <= 0) return PrefixCut{0, tile_pages};
-  const int least = prefix_pages_of(2 * live_rows, page_size);
+  const int least = prefix_pages_of((live_rows * row_tokens + 3) >> 2, page_size);
   uint32_t p = item_pages > least ? item_pages : least;
   if (!own && p > kPrefixMostPages) p = kPrefixMostPages;
   const uint32_t n = (pages + p - 1) / p;

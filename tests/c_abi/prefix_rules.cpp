@@ -20,7 +20,7 @@ extern "C" int prefix_items(int batch, int kv_heads, int group, int elem, int pa
   }
   const int item_pages = unique::prefix_item_pages(cost, s.wanted);
   for (int i = 0; i < sources; ++i) {
-    const unique::PrefixCut cut = unique::prefix_cut(pages[i], item_pages, rows[i] < s.rows ? rows[i] : s.rows, page_size, s.tile_pages, own[i]);
+    const unique::PrefixCut cut = unique::prefix_cut(pages[i], item_pages, rows[i] < s.rows ? rows[i] : s.rows, s.row_tokens, page_size, s.tile_pages, own[i]);
     count[i] = cut.count;
     each[i] = cut.pages;
   }
