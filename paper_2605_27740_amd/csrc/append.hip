@@ -77,10 +77,11 @@ __global__ __launch_bounds__(kAppendWaves* kWave) void append_kernel(CacheView c
   if (slot < 0 || slot >= c.num_phys * c.S) return;
   if (lane < R / 2) {
     const double turns = (double)position * (a.how.frequencies[lane] * 0.15915494309189535);
-    const float f = (float)(turns - rint(turns));  // in [-1/2, 1/2]
+    const double part = turns - rint(turns);
+    const float f = (float)part, rest = (float)(part - (double)f) * 6.2831853f;  // f in [-1/2, 1/2], rest: 2^-23 of a radian at most
     float sn, cs;
     sincospif(2.f * f, &sn, &cs);
-    s_turn[wave][lane] = make_float2(cs * a.how.magnitude, sn * a.how.magnitude);
+    s_turn[wave][lane] = make_float2(fmaf(-sn, rest, cs) * a.how.magnitude, fmaf(cs, rest, sn) * a.how.magnitude);
   }
   __builtin_amdgcn_wave_barrier();  // the LDS serves a wave's accesses in order; the compiler keeps it
 
