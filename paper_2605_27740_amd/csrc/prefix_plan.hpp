@@ -15,7 +15,9 @@ constexpr int kPrefixMostWorkgroups = (1 << 24) - 1;  // of 256 threads, of whic
 
 // Where there is little to read, every member reads its prefix for itself, in chunks that the host cuts, mostly out of the caches: there is no plan, and nothing to join if a chunk is all. Shared / each
 // for itself, us: 2 x 2148 tokens (fp32, 2 heads of 64, 4 MB) 15.6 / 9.4, 2 x 300 (8 heads, bf16) 13.1 / 7.1, 8 x 1100 (34 MB) 15.4 / 11.5, 16 x 1500 (94 MB) 17.4 / 17.3, 4 x 8500 (133 MB) 22.3 / 24.1.
-constexpr int64_t kPrefixAloneBytes = 64ll << 20;
+// If a chunk is all, up to 256 MB: 245 x 57 tokens (32 heads, 245 MB) 78.5 / 60.5, 64 x 768 in 8 groups (192 MB) 21.5 / 20.0, 128 x 520 (264 MB) 25.2 / 27.7. In fp32, whose products take long, up to 160:
+// 57 x 1769 (one head, 99 MB) 24.0 / 20.7, 67 x 2039 in 5 groups (134 MB) 25.4 / 25.5, 4 x 4500 (141 MB) 35.2 / 28.7, 20 x 2865 of 64 channels (225 MB) 23.2 / 29.1, 2 x 14065 (220 MB) 57.3 / 45.7.
+constexpr int64_t prefix_alone_bytes(bool one_chunk, int elem) { return (one_chunk ? 256ll : (elem == 4 ? 160ll : 64ll)) << 20; }
 // Tokens of such a chunk at least, and half as many again if that is all of them: 2 x 600 tokens in one chunk or two 9.5 / 10.5 us, 900 12.3 / 11.9; chunks of 256, 512 and 1024 tokens at least, 8 x 1100
 // 13.4 / 11.5 / 13.8. fp32, 2 x 2148 tokens of 64 channels, by 128 and 512: 9.8 / 12.7.
 constexpr int prefix_alone_tokens(int elem) { return elem == 4 ? 128 : 512; }
@@ -38,8 +40,10 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
                                 int max_prefix_pages, int max_own_pages) {
   PrefixShape s = {};
   const int64_t pages = std::max<int64_t>(std::min<int64_t>((int64_t)max_prefix_pages + max_own_pages, max_pages), 1), members = (int64_t)batch * kv_heads;
-  if (members * pages * page_bytes <= kPrefixAloneBytes) {
-    const int64_t least = prefix_alone_tokens(elem) / page_size, n = 2 * pages <= 3 * least ? 1 : std::min((pages + least - 1) / least, std::max<int64_t>(2 * kPrefixSlots / members, 1));
+  const int64_t least = prefix_alone_tokens(elem) / page_size;
+  const bool one = 2 * pages <= 3 * least;
+  if (members * pages * page_bytes <= prefix_alone_bytes(one, elem)) {
+    const int64_t n = one ? 1 : std::min((pages + least - 1) / least, std::max<int64_t>(2 * kPrefixSlots / members, 1));
     s.chunk_pages = (int32_t)((pages + n - 1) / n);
     s.chunks = (int32_t)((pages + s.chunk_pages - 1) / s.chunk_pages);
     s.max_rows = (int32_t)((int64_t)batch * s.chunks * group);

@@ -249,7 +249,8 @@ def test_prefix_members_for_themselves(rules):
         rules.prefix_alone(batch, kv, group, elem, S, page, width, prefix, own, out)
         chunks, pages, rows = out
         most = max(min(width, prefix + own), 1)
-        assert (chunks > 0) == (most * batch * kv * page <= 64 << 20), seed
+        one = 2 * most * S <= 3 * (128 if elem == 4 else 512)
+        assert (chunks > 0) == (most * batch * kv * page <= (256 if one else 160 if elem == 4 else 64) << 20) and (chunks <= 1 or not one), seed
         if chunks:
             assert chunks * pages >= most > (chunks - 1) * pages and rows == batch * chunks * group
             assert chunks == 1 or (chunks * batch * kv <= 1024 and pages * S >= (64 if elem == 4 else 256))

@@ -256,7 +256,7 @@ def make_groups(c, H, wide=True, **over):
     for itself."""
     table = c["table"]
     if wide:
-        columns = (64 << 20) // (len(c["lens"]) * c["k"][0].numel() * 2 * c["k"].element_size()) + 1
+        columns = max((256 << 20) // (len(c["lens"]) * c["k"][0].numel() * 2 * c["k"].element_size()), 768 // c["S"]) + 1
         table = torch.nn.functional.pad(table, (0, max(0, columns - table.shape[1])), value=-1)
     args = dict(q_heads=H, k_cache=c["k"].to(DEV), v_cache=c["v"].to(DEV), page_table=table.to(DEV), seq_lens=c["lens"].to(DEV),
                 group_starts=i32(c["starts"]), prefix_pages=i32(c["pages"]), members=torch.cat([c["members"], c["members"].new_zeros(len(c["lens"]))]).to(DEV),
@@ -460,7 +460,7 @@ def test_prefix_bounds_hold(gpu_lib):
         check_prefix(dict(c, members=torch.tensor(first, dtype=torch.int32)), (groups.out, groups.lse), torch.float32)
     # own pages: two of each
     d = dict(c, lens=torch.minimum(c["lens"], torch.tensor([96 + 32 if b in c["members"][:4].tolist() else 48 + 32 for b in range(6)], dtype=torch.int32)))
-    for more in ({}, dict(max_prefix_pages=1 << 14)):  # (the latter: prefixes are shared)
+    for more in ({}, dict(max_prefix_pages=1 << 16)):  # (the latter: prefixes are shared)
         check_prefix(d, make_groups(c, 8, max_own_tokens=32, **more).paged_decode(c["q"].to(DEV)), torch.float32)
 
 
@@ -515,7 +515,7 @@ class Server:
     """A batch that decodes: places for the new tokens, heads into the cache, statistics of the touched pages, attention over the prefix that all of its
     sequences share; with a plain copy of everything on the host."""
 
-    def __init__(self, seed, dtype=torch.bfloat16, H=16, Hkv=4, D=128, S=16, B=6, prefix=5, pages=400, rows=64, width=400):
+    def __init__(self, seed, dtype=torch.bfloat16, H=16, Hkv=4, D=128, S=16, B=6, prefix=5, pages=400, rows=64, width=1600):
         self.geo = H, Hkv, D, S, B, prefix
         self.dtype, self.g = dtype, torch.Generator().manual_seed(seed)
         self.r = random.Random(seed)
@@ -606,10 +606,10 @@ def asked(r, i, B):
 
 @pytest.mark.parametrize("captured", [False, True])
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("width", [40, 400])
+@pytest.mark.parametrize("width", [40, 1600])
 def test_a_server_places_appends_and_attends(gpu_lib, dtype, captured, width):
     """Thirty steps, every one against the host's copy; eager, or one HIP graph replayed with work of other kinds between the replays. Tables of 40 pages: every sequence reads
-    the prefix for itself; of 400: it is shared."""
+    the prefix for itself; of 1600: it is shared."""
     s = Server(11, dtype, width=width)
     graph = None
     for i in range(30):
