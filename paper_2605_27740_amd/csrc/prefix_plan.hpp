@@ -21,6 +21,8 @@ constexpr int64_t prefix_alone_bytes(bool one_chunk, int elem) { return (one_chu
 // Tokens of such a chunk at least, and half as many again if that is all of them: 2 x 600 tokens in one chunk or two 9.5 / 10.5 us, 900 12.3 / 11.9; chunks of 256, 512 and 1024 tokens at least, 8 x 1100
 // 13.4 / 11.5 / 13.8. fp32, 2 x 2148 tokens of 64 channels, by 128 and 512: 9.8 / 12.7.
 constexpr int prefix_alone_tokens(int elem) { return elem == 4 ? 128 : 512; }
+// Every workgroup goes through the groups' starts, 64 at a time, for its member's: shared / each for itself 1024 x 70 tokens in 512 groups 50.4 / 27.7 us, 4096 in 2048 (or one more) 175 / 159.
+constexpr int kPrefixAloneGroups = 2048;
 
 struct PrefixShape {
   int32_t rows;         // query rows of a workgroup's block
@@ -42,7 +44,7 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   const int64_t pages = std::max<int64_t>(std::min<int64_t>((int64_t)max_prefix_pages + max_own_pages, max_pages), 1), members = (int64_t)batch * kv_heads;
   const int64_t least = prefix_alone_tokens(elem) / page_size;
   const bool one = 2 * pages <= 3 * least;
-  if (members * pages * page_bytes <= prefix_alone_bytes(one, elem)) {
+  if (num_groups <= kPrefixAloneGroups && members * pages * page_bytes <= prefix_alone_bytes(one, elem)) {
     const int64_t n = one ? 1 : std::min((pages + least - 1) / least, std::max<int64_t>(2 * kPrefixSlots / members, 1));
     s.chunk_pages = (int32_t)((pages + n - 1) / n);
     s.chunks = (int32_t)((pages + s.chunk_pages - 1) / s.chunk_pages);
