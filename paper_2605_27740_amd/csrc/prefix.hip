@@ -9,8 +9,10 @@
 // products run on v_mfma_f32_32x32x16_bf16 with the queries as columns: S^T = K Q^T leaves a lane with 16 tokens' logits of ONE query (column lane % 32, rows 8 (i / 4) + 4
 // (lane / 32) + i % 4), so its softmax needs no other lane but lane ^ 32, and these are the k that the lane supplies to O^T = V^T P^T: probabilities never
 // leave their lane. V^T comes out of the LDS by its transposing read.
-// Probabilities enter the second product rounded to bf16, and their sum does not: 24 bits, in three products, would double the arithmetic, which bounds
-// groups of 32 sequences and more, for an error that is of the size of the output's own rounding.
+// Probabilities enter the second product with all 24 bits, as three parts of 8 (exactly), three products instead of one: with 8 bits an output whose terms cancel was off by 2^-9 of the
+// terms, and two tokens of opposite values whose weights are nearly the same gave 0. us with one product / three: 256 sequences behind 32768 tokens 182 / 285, 16 behind 131072 100.5 / 107 to 113, 32 behind 8192
+// 37.2 / 42.7, six groups of 10 102 / 107. The parts are made just before they are used, for 8 of a lane's 16 tokens at a time; between the products before, where registers end at 64 rows,
+// 119 instead of 112 us behind 131072 tokens, 284 instead of 291 behind 32768.
 // fp32 caches: the same on v_mfma_f32_32x32x2_f32, whose probabilities stay fp32, with tiles of 32 tokens.
 //
 // What bounds it, at 8 KV heads of 128 channels, bf16, pages of 16 or 32: the stream of keys and values up to some 30 sequences in a group (16 behind 131072 tokens: 552 MB in 94 us with the plan in
@@ -248,14 +250,30 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
 
   f32x16_t x;               // logits of a tile: token 8 (i / 4) + 4 half + i % 4 of the wave's 32
   struct Weights {          // probabilities of the tile before
-    bf16x8_t b[2];          // bf16: as operands
-    float f[kBf16 ? 1 : 16];
+    float f[16];
   } p;
+  struct Parts {            // of 8 of them, as operands: three parts of 8 bits, the largest first, whose sum they are
+    u32x4_t b[3];
+  };
+  // Probabilities 2 j and 2 j + 1 of eight.
+  auto split = [](const float* f, int j, Parts& to) {
+    float r[2] = {f[2 * j], f[2 * j + 1]};
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      to.b[u][j] = pack_hi(__float_as_uint(r[0]), __float_as_uint(r[1]));
+#pragma unroll
+      for (int i = 0; i < 2; ++i) r[i] -= bf16_part(r[i]);  // exact
+    }
+  };
   auto product = [&](u32x4_t k, int s, f32x16_t y) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), __builtin_bit_cast(bf16x8_t, qb[s]), y, 0, 0, 0);
   };
   // Operands are read a few ahead (left to itself the compiler reads one at a time and waits for it).
-  constexpr int kFew = kBf16 ? 4 : 2;
+  constexpr int kFew = 2;
+  auto add = [&](bf16x8_t v, const Parts& w, int e) {
+#pragma unroll
+    for (int u = 2; u >= 0; --u) acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8_t, w.b[u]), acc[e], 0, 0, 0);
+  };
   auto keys = [&](int slot, int h) {
     const Keys k = keys_in(slot, h);
     u32x4_t few[kFew];
@@ -297,9 +315,14 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       bf16x8_t few[kFew];
 #pragma unroll
       for (int i = 0; i < kFew; ++i) few[i] = v.read(i);
+      Parts parts;
 #pragma unroll
       for (int i = 0; i < 2 * kBlocks; ++i) {
-        acc[i % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(few[i % kFew], p.b[i / kBlocks], acc[i % kBlocks], 0, 0, 0);
+        if (i % kBlocks == 0) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) split(p.f + i / kBlocks * 8, j, parts);
+        }
+        add(few[i % kFew], parts, i % kBlocks);
         if (i + kFew < 2 * kBlocks) few[i % kFew] = v.read(i + kFew);
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -365,7 +388,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   auto weights = [&] {
     if constexpr (kBf16) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) p.b[i / 8][i % 8] = (__bf16)weight(x[i]);
+      for (int i = 0; i < 16; ++i) p.f[i] = weight(x[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < 16; ++i) p.f[i] = fast_exp2(fmaf(x[i], a.scale_log2, -m));
@@ -415,18 +438,22 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     bf16x8_t vf[kFew];
     y = zero16();
 #pragma unroll
-    for (int i = 0; i < kFew; ++i) {
-      kf[i] = k.read(i);
-      vf[i] = u.read(i);
-    }
+    for (int i = 0; i < kFew; ++i) kf[i] = k.read(i);
+#pragma unroll
+    for (int i = 0; i < kFew; ++i) vf[i] = u.read(i);
+    Parts parts;
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
       y = product(kf[i % kFew], i, y);
       if (i + kFew < kSteps) kf[i % kFew] = k.read(i + kFew);
 #pragma unroll
-      for (int j = i * kEach; j < (i + 1) * kEach; ++j) v.b[j / 8][j % 8] = (__bf16)weight(x[j]);
+      for (int j = i * kEach; j < (i + 1) * kEach; ++j) v.f[j] = weight(x[j]);
       asm volatile("" : "+v"(l));  // here, and not where they are used
-      acc[i % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kFew], w.b[i / kBlocks], acc[i % kBlocks], 0, 0, 0);
+      if (i % kBlocks == 0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) split(w.f + i / kBlocks * 8, j, parts);
+      }
+      add(vf[i % kFew], parts, i % kBlocks);
       if (i + kFew < kSteps) vf[i % kFew] = u.read(i + kFew);
       __builtin_amdgcn_sched_barrier(0);
       load_now(i);  // while products are in work

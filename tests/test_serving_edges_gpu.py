@@ -1,0 +1,45 @@
+"""Values of placement, append and attention over shared prefixes where they can go wrong: terms that cancel, sums near their type's end, values that are not finite."""
+import math
+
+import pytest
+import torch
+
+from tests import test_serving_gpu as G
+
+pytestmark = pytest.mark.gpu
+DEV, DTYPES, i32, say = G.DEV, G.DTYPES, G.i32, G.say
+
+
+# ------------------------------------------------------------------ shared prefixes
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,H,Hkv,S,members", [(128, 8, 1, 16, 3), (128, 8, 1, 16, 20), (64, 8, 2, 8, 5), (64, 8, 1, 32, 40), (128, 2, 2, 32, 50)])
+def test_prefix_terms_that_cancel(gpu_lib, dtype, D, H, Hkv, S, members):
+    """Two tokens of opposite values whose weights are within some 2^-12 of each other, all others' weights 0: out = v tanh(d / 2) with the difference d of the logits.
+    A weight is off by 2^-20 of itself (its argument, below 16, by 2^-21 twice, the exponential by 2^-23), the sums of two by 2^-24, so out by
+    2^-19 of |v| and its rounding. Probabilities of 8 bits would be equal and leave 0."""
+    say(f"cancel {dtype} {(D, H, Hkv, S)} members={members}")
+    pages = 200 // S
+    c = G.prefix_case(dtype, H, Hkv, D, S, [([0] * members, pages)], seed=members, poison=False)
+    g = torch.Generator().manual_seed(D + S)
+    ids = c["table"][c["members"][0].long(), :pages].long()
+    pool = c["k"].shape[0]
+    half = torch.finfo(dtype).eps / 2
+    for i, j in ((0, 1), (3, 30), (7, 40), (33, 70), (66, 190), (150, 199 // S * S - 1)):
+        k = torch.zeros((pool, Hkv, S, D))
+        k[..., 0] = -2.0 ** 14
+        v = torch.randn((pool, Hkv, S, D), generator=g)
+        q = torch.zeros((members, H, D))
+        q[..., 0] = torch.tensor([1.0, 0.5, 2.0, 1.0])[torch.arange(members * H).view(members, H) % 4]
+        value = torch.randn((Hkv, D), generator=g).to(dtype).float()
+        for t, logit, sign in ((i, 0.0, -1.0), (j, 2.0 ** -8, 1.0)):
+            k[ids[t // S], :, t % S, 0] = logit
+            v[ids[t // S], :, t % S] = sign * value
+        x = dict(c, q=q.to(dtype), k=k.to(dtype), v=v.to(dtype))
+        d = q[..., 0].double() * 2.0 ** -8 / math.sqrt(D)
+        of = value.double().repeat_interleave(H // Hkv, 0)
+        want = of * torch.tanh(d / 2)[..., None]
+        for wide in (True, False):
+            out = G.make_groups(x, H, wide=wide).paged_decode(x["q"].to(DEV))[0].cpu().double()
+            tol = 2.0 ** -19 * of.abs() * (1 + half) + half * want.abs()
+            assert ((out - want).abs() <= tol).all(), (i, j, wide, float(((out - want).abs() / tol).max()))
