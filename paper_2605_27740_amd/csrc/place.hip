@@ -6,6 +6,7 @@
 // come back must be on the stack before they are given out, and what the outputs may lie over (lengths, positions, the count of pages) is written there too: in the launch
 // before it, all workgroups of which make the plan, it is still read.
 #include "decode_core.hpp"
+#include "place_plan.hpp"
 #include "serving.hpp"
 
 namespace unique {
@@ -59,7 +60,7 @@ __device__ __forceinline__ void plan_places(const CacheView& c, const unique_pla
   const int before = min(max(*p.free_count, 0), capacity);
   freed_all = block_sum(freed_all, s_sum);
   own_all = block_sum(own_all, s_sum);
-  const int size = (int)min((int64_t)before + freed_all + own_all, (int64_t)capacity);
+  const int size = stack_place(before, (int64_t)freed_all + own_all, capacity);
 
   int base[4] = {0, 0, 0, 0}, given = 0;  // freed, own, tokens, needs before the strip
   for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
@@ -96,7 +97,7 @@ __device__ __forceinline__ void plan_places(const CacheView& c, const unique_pla
       const bool ok = !ended && fits && upto[2] <= p.max_new_tokens && (need == 0 || upto[3] <= size);
       const int position = p.next_positions ? p.next_positions[b] : len;
       to.seat[b] = Seat{len, upto[3] - need, position, ended ? kEnded : (ok ? kPlaced : kUnplaced)};
-      to.back[b] = Back{before + upto[0] - freed, before + freed_all + upto[1] - own, freed, ended ? pages : 0};
+      to.back[b] = Back{stack_place(before, upto[0] - freed, capacity), stack_place(before, (int64_t)freed_all + (upto[1] - own), capacity), freed, ended ? pages : 0};
       to.starts[b] = upto[2] - tokens;
       if (b == c.B - 1) to.starts[c.B] = upto[2];
       if (ok && need > 0) given = upto[3];  // (the largest is the last)
@@ -116,8 +117,8 @@ __device__ __forceinline__ void plan_places(const CacheView& c, const unique_pla
 
 // Pages of sequence b go back, by the threads of a workgroup or wave.
 __device__ __forceinline__ void give_back(const CacheView& c, const unique_placement& p, const Back& k, int b, int from, int step) {
-  for (int i = from; i < k.freed; i += step)
-    if (k.freed_at + i < p.free_capacity) p.free_pages[k.freed_at + i] = p.freed_pages[(int64_t)b * p.freed_stride + i];
+  for (int64_t i = from; i < k.freed; i += step)
+    if (stack_has(k.freed_at, (int)i, p.free_capacity)) p.free_pages[k.freed_at + i] = p.freed_pages[(int64_t)b * p.freed_stride + i];
   if (k.pages == 0) return;
   const int shared = p.shared_pages ? min(max(p.shared_pages[b], 0), k.pages) : 0;
   const int64_t row = (int64_t)b * c.max_pages;
@@ -128,9 +129,9 @@ __device__ __forceinline__ void give_back(const CacheView& c, const unique_place
     for (int u = 0; u < kFew; ++u) page[u] = c.page_table[row + (i0 + u * step < k.pages ? i0 + u * step : i0)];  // this thread's own
 #pragma unroll
     for (int u = 0; u < kFew; ++u) {
-      const int i = i0 + u * step, to = k.own_at + i - shared;
+      const int i = i0 + u * step;
       if (i >= k.pages) break;
-      if (i >= shared && to < p.free_capacity) p.free_pages[to] = page[u];
+      if (i >= shared && stack_has(k.own_at, i - shared, p.free_capacity)) p.free_pages[k.own_at + i - shared] = page[u];
       p.page_table_out[row + i] = -1;
     }
   }

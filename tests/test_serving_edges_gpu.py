@@ -4,6 +4,8 @@ import math
 import pytest
 import torch
 
+from paper_2605_27740_amd.session import PagePool
+from tests import serving_ref as R
 from tests import test_serving_gpu as G
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +45,28 @@ def test_prefix_terms_that_cancel(gpu_lib, dtype, D, H, Hkv, S, members):
             out = G.make_groups(x, H, wide=wide).paged_decode(x["q"].to(DEV))[0].cpu().double()
             tol = 2.0 ** -19 * of.abs() * (1 + half) + half * want.abs()
             assert ((out - want).abs() <= tol).all(), (i, j, wide, float(((out - want).abs() / tol).max()))
+
+
+# ------------------------------------------------------------------ places
+
+@pytest.mark.parametrize("B,rows", [(50, 100), (50, 9000), (1100, 100)])
+def test_a_stack_of_2_31_entries(gpu_lib, B, rows):
+    """Pages that come back to a nearly full stack whose capacity is the largest there is: those that do not fit are lost, and nothing is written in front of the stack. One launch, two, three."""
+    say(f"stack of 2^31 - 1 entries, B={B} rows={rows}")
+    most, window, guard = 2 ** 31 - 1, 60, 1024
+    c, total = G.place_case(B, B, 8, 30, 200, 1, 0.0, ended=0.7, evicted=3)
+    c.update(free=list(range(total, total + window)), free_count=window - 5, rows=rows)
+    c["new"] = [min(t, 1) for t in c["new"]]
+    want = R.place(**c)
+    buf = torch.empty((guard + most,), dtype=torch.int32, device=DEV)
+    buf[:guard] = -5
+    stack = buf[guard:]
+    stack[most - window:] = i32(c["free"])
+    table, lens, nxt, count = i32(c["table"]), i32(c["lens"]), i32(c["nxt"]), i32([most - 5])
+    pool = PagePool(q_heads=8, kv_heads=8, head_dim=64, page_size=8, dtype=torch.float32, num_pages=total + window, page_table=table, seq_lens=lens, max_new_tokens=rows,
+                    free_pages=stack, free_count=count, shared_pages=i32(c["shared"]), next_positions=nxt)
+    pool.place_tokens(i32(c["new"]), i32(c["freed"]), i32(c["freed_count"]))
+    torch.cuda.synchronize()
+    assert (buf[:guard] == -5).all()
+    assert table.tolist() == want["table"] and lens.tolist() == want["seq_lens"] and pool.slots.tolist() == want["slots"] and pool.placed.tolist() == want["placed"]
+    assert stack[most - window:int(count)].tolist() == want["stack"]
