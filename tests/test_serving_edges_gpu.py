@@ -4,7 +4,7 @@ import math
 import pytest
 import torch
 
-from paper_2605_27740_amd.session import PagePool
+from paper_2605_27740_amd.session import CacheWriter, PagePool, rotary_frequencies
 from tests import serving_ref as R
 from tests import test_serving_gpu as G
 
@@ -70,3 +70,28 @@ def test_a_stack_of_2_31_entries(gpu_lib, B, rows):
     assert (buf[:guard] == -5).all()
     assert table.tolist() == want["table"] and lens.tolist() == want["seq_lens"] and pool.slots.tolist() == want["slots"] and pool.placed.tolist() == want["placed"]
     assert stack[most - window:int(count)].tolist() == want["stack"]
+
+
+# ------------------------------------------------------------------ queries, keys and values
+
+@pytest.mark.parametrize("D,interleaved", [(128, False), (128, True), (64, False), (64, True)])
+@pytest.mark.parametrize("magnitude", [1.0, 1.25])
+def test_sine_and_cosine_are_rounded_once(gpu_lib, D, interleaved, magnitude):
+    """fp32 heads whose pairs are (1, 0) come out as m (cos a, sin a): half a step from 64 bits. The angle of a position below 2^20 is off by three roundings in 64 bits, 2^-31
+    of a radian, and the reference's by one, 2^-33."""
+    rows, g = 4000, torch.Generator().manual_seed(D)
+    x = torch.zeros((rows, 4, D))
+    lo, hi = (slice(0, D, 2), slice(1, D, 2)) if interleaved else (slice(0, D // 2), slice(D // 2, D))
+    x[..., lo] = 1.0
+    positions = torch.randint(0, 1 << 20, (rows,), generator=g).int()
+    positions[:64] = torch.arange(64)
+    kc, vc = (torch.zeros((rows // 16, 2, 16, D), device=DEV) for _ in range(2))
+    f = rotary_frequencies(D, base=5e5)
+    writer = CacheWriter(q_heads=4, k_cache=kc, v_cache=vc, frequencies=f, magnitude=magnitude, interleaved=interleaved)
+    q = writer.append_tokens(x.to(DEV), x[:, :2].contiguous().to(DEV), x[:, :2].contiguous().to(DEV), positions.to(DEV), torch.arange(rows, device=DEV))
+    torch.cuda.synchronize()
+    a = (positions.double()[:, None] * f)[:, None]
+    for got in (q.cpu(), kc.cpu().transpose(1, 2).reshape(rows, 2, D)):
+        for part, want in ((lo, magnitude * torch.cos(a)), (hi, magnitude * torch.sin(a))):
+            off = (got[..., part].double() - want).abs()
+            assert (off <= 2.0 ** -24 * want.abs() + magnitude * 2.0 ** -30.5).all(), float((off - 2.0 ** -24 * want.abs()).max())
