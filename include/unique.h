@@ -380,7 +380,7 @@ int unique_shared_prefix_workspace_bytes(const unique_cache_desc* desc, const un
 
 /* unique_dense_paged_decode for sequences that share the beginnings of their contexts: the pages of a group's prefix are read once for all of its
  * members (from the row of the first of them that is not empty; where there is little to read, from every member's own), each member's other pages as always. A member may be shorter than the prefix: the
- * tokens behind its length do not count for it (if values of longer members' tokens there are not finite, its results may not be, either). The group of one member has nothing to share, and its prefix is read as its other pages.
+ * tokens behind its length do not count for it, whatever they hold. The group of one member has nothing to share, and its prefix is read as its other pages.
  * Sequences that no group lists are left out, their rows of d_out and d_lse_out left as they are; one that is listed twice is attended twice. At most
  * `batch` members in all. sm_scale and the results of empty sequences are those of unique_dense_paged_decode. Against it the sums are in another order. */
 int unique_shared_prefix_decode(const unique_cache_desc* desc, const unique_prefix_groups* groups, const void* d_q, float sm_scale, void* d_out,

@@ -178,14 +178,17 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
   // tokens that all rows of the wave have
   const int all_have = __builtin_amdgcn_readfirstlane((int)wave_allreduce_minmax<false>((uint32_t)(live ? tokens : INT32_MAX)));
   const bool idle = across * 32 >= item.rows;  // no row of this wave (uniform)
-  // tokens that any row of the item has, which are not the wave's alone
-  int most = 0;
+  // tokens that any row of the item has, which are not the wave's alone, and tokens that all rows have that have any here
+  int most = 0, least = INT32_MAX;
 #pragma unroll
   for (int i = 0; i < kAcross * 32 / kWave; ++i) {
     const int r = i * kWave + lane, at = item.place + min(r, item.rows - 1) / G, s = a.groups.members ? a.groups.members[at] : at;
-    most = max(most, s >= 0 && s < c.B ? c.seq_lens[s] : 0);
+    const int n = s >= 0 && s < c.B ? c.seq_lens[s] : 0;
+    most = max(most, n);
+    if (n > item.begin * S) least = min(least, n);
   }
   const int longest = __builtin_amdgcn_readfirstlane((int)wave_allreduce_minmax<true>((uint32_t)most));
+  const int shortest = __builtin_amdgcn_readfirstlane((int)wave_allreduce_minmax<false>((uint32_t)least));
 
   // Where a lane reads, behind a unit's beginning. Keys: token `col`, the pieces of step s, of which four (fp32: eight) are in a plane. Values, bf16: lane i of 16 asks
   // for token i / 4, channels 4 (i % 4) + ..., and gets channel i of the four tokens; two blocks of channels are in a plane. fp32: channel `col` of a block,
@@ -408,19 +411,67 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     wait_units<L::kRing - 4 < 1 ? 1 : L::kRing - 4, L::kLoads>(left);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
-  // Slots of pages that there are not, and of tokens behind the longest row, may hold anything, and a product with zero is not always zero.
-  const int clean = holes ? 0 : min(pages / kTilePages, (longest / S - item.begin) / kTilePages);  // tiles that have none
+  // Slots of pages that there are not, and of tokens behind the longest row, may hold anything, and a product with zero is not always zero. Neither is it for the values of tokens that some rows have
+  // and others have not: where one of these is not finite, the rows that have its token get their NaN here, and the products 0.
+  const int clean = holes ? 0 : min(pages / kTilePages, (longest / S - item.begin) / kTilePages);  // tiles without the first kind,
+  const int even = (shortest / S - item.begin) / kTilePages;                                       // and without the second
   auto blank = [&](int t, int s) {
-    if (t < clean) return;
+    if (t < clean && t < even) return;
     const uint32_t there = there_at(t);
-    const int end = longest - (item.begin + t * kTilePages) * S;
-    for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave) {
-      const int token = i * 16 % L::kPlaneBytes / 128;
-      if (token >= end || !(there >> (token / S) & 1)) *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(ring_at + s * L::kBytes + i * 16) = u32x4_t{0, 0, 0, 0};
+    const int at0 = (item.begin + t * kTilePages) * S, end = longest - at0;
+    const lds_addr_t unit = ring_at + s * L::kBytes;
+    auto piece = [&](int i) { return (__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(unit + i * 16); };
+    auto token_of = [](int i) { return i * 16 % L::kPlaneBytes / 128; };
+    auto has = [&](int token) { return token < end && (there >> (token / S) & 1); };
+    auto in_lanes = [&](uint32_t w, uint32_t bits) { return (w & bits) == bits; };
+    constexpr uint32_t kHigh = 0x7f800000u, kLow = 0x7f80u;  // exponents of infinities and NaN; bf16: two elements to a word
+    bool odd = false;
+    if (t >= even) {  // every wave looks at the whole tile, so that all go the same way
+      const int from = shortest - at0;
+#pragma unroll 1
+      for (int i = lane; i < L::kBytes / 16; i += kWave) {
+        if (token_of(i) < from || !has(token_of(i))) continue;
+        const u32x4_t w = *piece(i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) odd |= in_lanes(w[j], kHigh) || (kBf16 && in_lanes(w[j], kLow));
+      }
+      odd = __any(odd);
+      if (odd) {
+        const int stop = min(end, L::kTokens);
+#pragma unroll 1
+        for (int token = max(from, 0); token < stop; ++token) {
+          if (!has(token)) continue;  // uniform
+          const bool counts = at0 + token < tokens;
+#pragma unroll
+          for (int e = 0; e < kBlocks; ++e)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {  // four channels
+              const int off = (e * 32 + 8 * n + 4 * half) * (int)sizeof(T);
+              const lds_addr_t from4 = unit + off / 128 * L::kPlaneBytes + token * 128 + ((off % 128 / 16) ^ swizzle(token)) * 16 + off % 16;
+              const __attribute__((address_space(3))) uint32_t* w = (const __attribute__((address_space(3))) uint32_t*)(uintptr_t)from4;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                if (counts && in_lanes(w[kBf16 ? j / 2 : j], kBf16 && j % 2 == 0 ? kLow : kHigh)) acc[e][4 * n + j] = __builtin_nanf("");
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave) {
+          if (token_of(i) < from || !has(token_of(i))) continue;
+          u32x4_t w = *piece(i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if (in_lanes(w[j], kHigh)) w[j] &= kBf16 ? 0xffffu : 0u;
+            if (kBf16 && in_lanes(w[j], kLow)) w[j] &= 0xffff0000u;
+          }
+          *piece(i) = w;
+        }
+      }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (t >= clean)
+      for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave)
+        if (!has(token_of(i))) *piece(i) = u32x4_t{0, 0, 0, 0};
+    if (odd || t >= clean) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
-
   // What a step has used, which all waves are done with at the next, takes the next two units, in their order.
   auto load_one = [&](bool keys) {
     if (keys ? next_k < tiles : next_v < tiles) {
@@ -726,8 +777,9 @@ __global__ __launch_bounds__(kMergeWaves* kWave) void prefix_merge_kernel(CacheV
   float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   for (int s0 = 0; s0 < n; s0 += kWave) {
     const float2 p = s0 == 0 ? first : (s0 + lane < n ? ml[row_of(s0 + lane)] : none);
-    const float scale = fast_exp2(p.x - M);
-    L = fmaf(p.y, scale, L);
+    // (a part without tokens that count for this row may have sums that are not finite, from tokens of others)
+    const float scale = p.y == 0.f ? -1.f : fast_exp2(p.x - M);
+    L = p.y == 0.f ? L : fmaf(p.y, scale, L);
     const int here = min(kWave, n - s0);
     for (int j0 = 0; j0 < here; j0 += kParts * kAhead) {
       if (s0 + j0 > 0) request(s0 + j0);
@@ -736,11 +788,11 @@ __global__ __launch_bounds__(kMergeWaves* kWave) void prefix_merge_kernel(CacheV
         if (j0 + u * kParts >= here) break;  // uniform
         const int j = j0 + u * kParts + sub;
         const float of_j = __shfl(scale, j % kWave, kWave);  // by all lanes, as any may be asked for its own
-        const float sc = j < here ? of_j : 0.f;
-        o[0] = fmaf(v[u].x, sc, o[0]);
-        o[1] = fmaf(v[u].y, sc, o[1]);
-        o[2] = fmaf(v[u].z, sc, o[2]);
-        o[3] = fmaf(v[u].w, sc, o[3]);
+        if (j >= here || of_j < 0.f) continue;
+        o[0] = fmaf(v[u].x, of_j, o[0]);
+        o[1] = fmaf(v[u].y, of_j, o[1]);
+        o[2] = fmaf(v[u].z, of_j, o[2]);
+        o[3] = fmaf(v[u].w, of_j, o[3]);
       }
     }
   }

@@ -95,3 +95,46 @@ def test_sine_and_cosine_are_rounded_once(gpu_lib, D, interleaved, magnitude):
         for part, want in ((lo, magnitude * torch.cos(a)), (hi, magnitude * torch.sin(a))):
             off = (got[..., part].double() - want).abs()
             assert (off <= 2.0 ** -24 * want.abs() + magnitude * 2.0 ** -30.5).all(), float((off - 2.0 ** -24 * want.abs()).max())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,H,Hkv,S", [(128, 8, 2, 16), (64, 8, 1, 8), (128, 4, 4, 32), (64, 2, 2, 16)])
+@pytest.mark.parametrize("members", [2, 5, 45])
+def test_prefix_values_that_are_not_finite_are_their_own_members(gpu_lib, dtype, D, H, Hkv, S, members):
+    """Infinities and NaN among the values of a prefix: members that are shorter get their results as ever, the others have no finite number in those channels, and theirs in all
+    other channels. Members end before the prefix does, in its first pages, at a page's end, or are empty; a page in the middle is missing in one case."""
+    say(f"not finite {dtype} {(D, H, Hkv, S)} members={members}")
+    pages = 1200 // S
+    N = pages * S
+    lens = [N + 9, N - 700, 0, N, 1, N - 64, N - 65, S, N - 300, 130]
+    own = [lens[i % 10] - N - (i // 10 if i % 10 > 3 and lens[i % 10] > 9 else 0) for i in range(members)]
+    for seed, hole in ((1, False), (2, True)):
+        c = G.prefix_case(dtype, H, Hkv, D, S, [(own, pages), ([3], 1)], seed=seed + members)
+        row = c["table"][c["members"][0].long(), :pages].long()
+        if hole:
+            c["table"][c["members"][:members].long(), 30] = -1
+        bad = [(0, 5, math.nan), (64, 7, math.inf), (129, 8, -math.inf), (130, D - 1, math.inf), (131, D - 2, math.nan), (N - 701, 0, math.nan), (N - 700, 33, math.nan),
+               (N - 300, 34, -math.inf), (N - 66, 1, math.nan), (N - 40, 2, math.inf), (N - 1, 3, math.nan)]
+        if seed == 2:
+            bad = bad[-5:]
+        clean = dict(c, v=c["v"].clone())
+        lost = torch.zeros((len(c["lens"]), H, D), dtype=torch.bool)
+        for at, channel, x in bad:
+            kv = at % Hkv
+            c["v"][row[at // S], kv, at % S, channel] = x
+            clean["v"][row[at // S], kv, at % S, channel] = 0.0
+            heads = torch.arange(kv * (H // Hkv), (kv + 1) * (H // Hkv))
+            if at // S != 30 or not hole:
+                for b in c["members"][:members].tolist():
+                    if c["lens"][b] > at:
+                        lost[b, heads, channel] = True
+        want = R.attend(clean["q"], clean["k"], clean["v"], clean["table"], clean["lens"])
+        tol, tol_lse = G.prefix_bounds(clean, want, dtype)
+        some = c["lens"] > 0
+        for wide in (True, False):
+            out, lse = (x.cpu() for x in G.make_groups(c, H, wide=wide).paged_decode(c["q"].to(DEV)))
+            fine = ((out.double() - want[0]).abs() <= tol) | ~some[:, None, None]
+            assert (fine | lost).all(), (seed, wide, (~(fine | lost)).nonzero()[:5].tolist())
+            assert not out[lost].isfinite().any(), (seed, wide)
+            assert ((lse.double() - want[1]).abs() <= tol_lse)[some].all()
+            assert (out[~some] == 0).all() and torch.isneginf(lse[~some]).all()
