@@ -144,7 +144,7 @@ __device__ __forceinline__ void tell_sequence(const CacheView& c, const unique_p
   p.token_starts[b] = start;
   if (b == c.B - 1) p.token_starts[c.B] = end;
   p.placed[b] = placed;
-  p.seq_lens_out[b] = s.state == kEnded ? 0 : s.len + placed;
+  p.seq_lens_out[b] = s.state == kEnded ? 0 : (placed > 0 ? s.len + placed : c.seq_lens[b]);  // (as it was, also where that is no length of this row)
   if (p.next_positions_out) p.next_positions_out[b] = s.state == kEnded ? 0 : s.position + placed;
   if (b == 0) *p.free_count_out = from.size[0] - from.size[1];
 }

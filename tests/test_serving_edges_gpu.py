@@ -72,6 +72,32 @@ def test_a_stack_of_2_31_entries(gpu_lib, B, rows):
     assert stack[most - window:int(count)].tolist() == want["stack"]
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,rows", [(40, 300), (40, 9000), (1100, 9000)])
+def test_sequences_without_a_place_stay_as_they_are(gpu_lib, B, rows, in_place):
+    """Also those whose length is more than their row holds, or none: theirs was cut to the row's."""
+    say(f"stay {B} {rows} {in_place}")
+    c, total = G.place_case(B, B, 16, 6, 90, 5, 1.0, ended=0.1, evicted=1)
+    lens = list(c["lens"])
+    for b, n in ((3, 97), (8, 5000), (17, 2 ** 31 - 1), (21, -4), (30, -2 ** 31)):
+        lens[b], c["new"][b] = n, 0 if b in (8, 21, 30) else 2
+    c["lens"] = [n if 0 <= n <= 96 else 0 for n in lens]
+    c["new"] = [0 if not 0 <= n <= 96 else t for n, t in zip(lens, c["new"])]
+    new = [2 if n > 96 and b != 8 else t for b, (n, t) in enumerate(zip(lens, c["new"]))]
+    c["rows"] = rows
+    table, lens_in, nxt, count = i32(c["table"]), i32(lens), i32(c["nxt"]), i32([c["free_count"]])
+    pool = PagePool(q_heads=8, kv_heads=8, head_dim=64, page_size=16, dtype=torch.float32, num_pages=total, page_table=table, seq_lens=lens_in, max_new_tokens=rows,
+                    free_pages=i32(c["free"]), free_count=count, shared_pages=i32(c["shared"]), next_positions=nxt)
+    outs = {} if in_place else dict(seq_lens_out=torch.full_like(lens_in, -9), next_positions_out=torch.full_like(nxt, -9))
+    pool.place_tokens(i32(new), i32(c["freed"]), i32(c["freed_count"]), **outs)
+    torch.cuda.synchronize()
+    want = R.place(**c)
+    got = (lens_in if in_place else outs["seq_lens_out"]).tolist()
+    assert got == [n if not 0 <= n <= 96 else w for n, w in zip(lens, want["seq_lens"])]
+    assert (nxt if in_place else outs["next_positions_out"]).tolist() == want["next"]
+    assert pool.placed.tolist() == want["placed"] and table.tolist() == want["table"] and pool.free_pages[:int(count)].tolist() == want["stack"]
+
+
 # ------------------------------------------------------------------ queries, keys and values
 
 @pytest.mark.parametrize("D,interleaved", [(128, False), (128, True), (64, False), (64, True)])
