@@ -361,7 +361,9 @@ int unique_append_tokens(const unique_cache_desc* desc, int32_t num_rows, const 
                          const void* d_v, int64_t v_stride, const int32_t* d_positions, const int64_t* d_slots,
                          const unique_head_transform* transform, void* d_q_out, void* stream);
 
-/* Sequences whose contexts begin with the same pages, in groups. The host's bounds must be true: what lies beyond them is ignored by every kernel. */
+/* Sequences whose contexts begin with the same pages, in groups. The host's bounds must be true. Beyond them: members are left out; of a prefix the pages behind the first
+ * max_prefix_pages count as the members' own; own pages behind the first max_own_pages do not count. Bounds that are close matter: they decide which kernels run (a batch that could have
+ * much to read is not served as one that has little) and how large the workspace is. */
 typedef struct unique_prefix_groups {
   const int32_t* starts;        /* device, [num_groups + 1], ascending from 0: members [starts[g], starts[g + 1]) belong to group g. If they do not
                                  * ascend, no row is written */

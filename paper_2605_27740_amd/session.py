@@ -371,7 +371,8 @@ class PrefixGroups:
     """Sequences of a paged cache whose contexts begin with the same pages, and attention over such a batch: group ``g`` has the members
     ``members[group_starts[g]:group_starts[g + 1]]`` (without ``members`` the sequences of these numbers), whose rows of ``page_table`` begin with the same
     ``prefix_pages[g]`` full pages. The bounds must be true: at most ``max_members`` of a group, ``max_prefix_pages`` pages of a prefix and, if it is
-    known, ``max_own_tokens`` tokens of any member behind its prefix."""
+    known, ``max_own_tokens`` tokens of any member behind its prefix (without it, as many as a row of ``page_table`` or ``max_seq_len`` has room for: a small batch in a wide table is
+    then served as a large one, two sequences of 300 tokens in 13 instead of 7 us)."""
 
     def __init__(self, *, q_heads: int, k_cache, v_cache, page_table, seq_lens, group_starts, prefix_pages, members=None, max_members: int,
                  max_prefix_pages: int, max_own_tokens: int = 0, max_seq_len: int = 0, lib: binding.Library | None = None):

@@ -125,6 +125,22 @@ def test_prefix_many_kv_heads(gpu_lib, dtype, H, Hkv, D, S):
     G.check_both(c, H, dtype)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_prefix_bounds_that_are_too_low(gpu_lib, dtype):
+    """Of a prefix that is longer than the host's bound, the pages behind that count as own ones, as far as those go."""
+    S, first, second = 16, 6, 3
+    c = G.prefix_case(dtype, 8, 2, 64, S, [([30, 100, 70, 1], first), ([200, 90], second)], seed=4, poison=False)
+    G.check_both(c, 8, dtype, max_prefix_pages=4)
+    G.check_both(c, 8, dtype, max_prefix_pages=0)
+    for bound in (4, 1):
+        lens = c["lens"].clone()
+        for members, pages in ((c["members"][:4], first), (c["members"][4:], second)):
+            lens[members.long()] = lens[members.long()].clamp(max=(min(pages, bound) + 4) * S)
+        d = dict(c, lens=lens)
+        want = R.attend(d["q"], d["k"], d["v"], d["table"], lens)
+        G.check_prefix(d, G.make_groups(c, 8, max_prefix_pages=bound, max_own_tokens=4 * S).paged_decode(c["q"].to(DEV)), dtype, want)
+
+
 # ------------------------------------------------------------------ together
 
 class SparseServer(G.Server):
