@@ -71,8 +71,11 @@ __device__ __forceinline__ void wait_units(int left) {
 // A run of a prefix's pages for a block of query rows. Every wave goes through the tiles, 32 tokens at a time, in steps: the products S = K Q^T of tile t, the softmax
 // of tile t - 1 and O += V P of tile t - 2 do not wait for each other, so that the matrix cores and the vector units both have something to do (bf16:
 // they stand between each other in the code).
+// -> true: nothing has been written, and each member has to be attended by itself. A sum is not finite, and some rows have tokens here that others have not: a product of the others'
+// probability, 0, with an infinity or NaN among the values is not 0. (Looking at the values of such tiles beforehand took 216 us for 105, 16 sequences behind 131072 tokens, one of
+// them of one token.)
 template <typename T, int D, int S, int kAcross, bool kNT>
-__device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixArgs& a, const PrefixItem& item, int hkv, char* ring) {
+__device__ __forceinline__ bool attend_prefix(const CacheView& c, const PrefixArgs& a, const PrefixItem& item, int hkv, char* ring) {
   using L = Unit<T, D, kAcross>;
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int kBlocks = D / 32;                    // of channels
@@ -411,67 +414,19 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     wait_units<L::kRing - 4 < 1 ? 1 : L::kRing - 4, L::kLoads>(left);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
-  // Slots of pages that there are not, and of tokens behind the longest row, may hold anything, and a product with zero is not always zero. Neither is it for the values of tokens that some rows have
-  // and others have not: where one of these is not finite, the rows that have its token get their NaN here, and the products 0.
-  const int clean = holes ? 0 : min(pages / kTilePages, (longest / S - item.begin) / kTilePages);  // tiles without the first kind,
-  const int even = (shortest / S - item.begin) / kTilePages;                                       // and without the second
+  // Slots of pages that there are not, and of tokens behind the longest row, may hold anything, and a product with zero is not always zero.
+  const int clean = holes ? 0 : min(pages / kTilePages, (longest / S - item.begin) / kTilePages);  // tiles that have none
   auto blank = [&](int t, int s) {
-    if (t < clean && t < even) return;
+    if (t < clean) return;
     const uint32_t there = there_at(t);
-    const int at0 = (item.begin + t * kTilePages) * S, end = longest - at0;
-    const lds_addr_t unit = ring_at + s * L::kBytes;
-    auto piece = [&](int i) { return (__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(unit + i * 16); };
-    auto token_of = [](int i) { return i * 16 % L::kPlaneBytes / 128; };
-    auto has = [&](int token) { return token < end && (there >> (token / S) & 1); };
-    auto in_lanes = [&](uint32_t w, uint32_t bits) { return (w & bits) == bits; };
-    constexpr uint32_t kHigh = 0x7f800000u, kLow = 0x7f80u;  // exponents of infinities and NaN; bf16: two elements to a word
-    bool odd = false;
-    if (t >= even) {  // every wave looks at the whole tile, so that all go the same way
-      const int from = shortest - at0;
-#pragma unroll 1
-      for (int i = lane; i < L::kBytes / 16; i += kWave) {
-        if (token_of(i) < from || !has(token_of(i))) continue;
-        const u32x4_t w = *piece(i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) odd |= in_lanes(w[j], kHigh) || (kBf16 && in_lanes(w[j], kLow));
-      }
-      odd = __any(odd);
-      if (odd) {
-        const int stop = min(end, L::kTokens);
-#pragma unroll 1
-        for (int token = max(from, 0); token < stop; ++token) {
-          if (!has(token)) continue;  // uniform
-          const bool counts = at0 + token < tokens;
-#pragma unroll
-          for (int e = 0; e < kBlocks; ++e)
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {  // four channels
-              const int off = (e * 32 + 8 * n + 4 * half) * (int)sizeof(T);
-              const lds_addr_t from4 = unit + off / 128 * L::kPlaneBytes + token * 128 + ((off % 128 / 16) ^ swizzle(token)) * 16 + off % 16;
-              const __attribute__((address_space(3))) uint32_t* w = (const __attribute__((address_space(3))) uint32_t*)(uintptr_t)from4;
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (counts && in_lanes(w[kBf16 ? j / 2 : j], kBf16 && j % 2 == 0 ? kLow : kHigh)) acc[e][4 * n + j] = __builtin_nanf("");
-            }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave) {
-          if (token_of(i) < from || !has(token_of(i))) continue;
-          u32x4_t w = *piece(i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (in_lanes(w[j], kHigh)) w[j] &= kBf16 ? 0xffffu : 0u;
-            if (kBf16 && in_lanes(w[j], kLow)) w[j] &= 0xffff0000u;
-          }
-          *piece(i) = w;
-        }
-      }
+    const int end = longest - (item.begin + t * kTilePages) * S;
+    for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave) {
+      const int token = i * 16 % L::kPlaneBytes / 128;
+      if (token >= end || !(there >> (token / S) & 1)) *(__attribute__((address_space(3))) u32x4_t*)(uintptr_t)(ring_at + s * L::kBytes + i * 16) = u32x4_t{0, 0, 0, 0};
     }
-    if (t >= clean)
-      for (int i = threadIdx.x; i < L::kBytes / 16; i += kDecWaves * kWave)
-        if (!has(token_of(i))) *piece(i) = u32x4_t{0, 0, 0, 0};
-    if (odd || t >= clean) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
+
   // What a step has used, which all waves are done with at the next, takes the next two units, in their order.
   auto load_one = [&](bool keys) {
     if (keys ? next_k < tiles : next_v < tiles) {
@@ -615,6 +570,22 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
     if (!idle) values(slot, 0);
   }
 
+  if (shortest < min(item.end * S, longest)) {  // (the same in all waves)
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < kBlocks; ++e)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd |= !(fabsf(acc[e][i]) < INFINITY);
+    int* any = reinterpret_cast<int*>(ring);
+    __syncthreads();
+    if (threadIdx.x == 0) *any = 0;
+    __syncthreads();
+    if (__any(odd) && lane == 0) *any = 1;
+    __syncthreads();
+    const bool alone = __builtin_amdgcn_readfirstlane(*any) != 0;
+    __syncthreads();
+    if (alone) return true;
+  }
   l = with_lane_xor32(l, OpSum());
   if constexpr (kAlong > 1) {  // the waves that took other tokens of the same rows
     static_assert(kAlong == 2, "two waves");
@@ -629,7 +600,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       if (half == 0) { o[32 * D + col] = m; o[32 * D + 32 + col] = l; }
     }
     __syncthreads();
-    if (along == 1) return;
+    if (along == 1) return false;
     const float m2 = o[32 * D + col], l2 = o[32 * D + 32 + col], M = fmaxf(m, m2);
     const float s1 = fast_exp2(m - M), s2 = fast_exp2(m2 - M);
     m = M;
@@ -639,7 +610,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[e][i] = acc[e][i] * s1 + o[(e * 16 + i) * 64 + lane] * s2;
   }
-  if (!live) return;
+  if (!live) return false;
   const int64_t part = (int64_t)hkv * a.shape.max_rows + item.part + row;
   float* out = a.work.part_o + part * D;
 #pragma unroll
@@ -649,6 +620,7 @@ __device__ __forceinline__ void attend_prefix(const CacheView& c, const PrefixAr
       *reinterpret_cast<float4*>(out + e * 32 + 8 * n + 4 * half) =
           make_float4(acc[e][4 * n], acc[e][4 * n + 1], acc[e][4 * n + 2], acc[e][4 * n + 3]);
   if (half == 0) *reinterpret_cast<float2*>(a.work.part_ml + part * 2) = make_float2(m, l);
+  return false;
 }
 
 __device__ __forceinline__ PrefixItem uniform(const PrefixItem& x) {
@@ -683,24 +655,34 @@ __global__ __launch_bounds__(kDecWaves* kWave, 2) void prefix_kernel(CacheView c
     item = a.work.item[index];
     if (index >= *a.work.num_items) return;
   }
-  if (!item.own) {
-    attend_prefix<T, D, S, kAcross, kNT>(c, a, item, hkv, ring);
-    return;
-  }
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int b = item.seq, N = c.seq_lens[b];
-  const int64_t part = (int64_t)hkv * a.shape.max_rows + item.part;
-  const ChunkOut<T> to = {a.work.part_o + part * D, a.work.part_ml + part * 2, reinterpret_cast<T*>(a.out), a.lse_out, 2};
-  const Chunk chunk = {hkv, b, item.begin, item.end, N, 0};
-  auto lookup = [&](int e, bool, int& phys, int& ntok) {
-    const int ph = c.page_table[(int64_t)b * c.max_pages + e];
-    if (ph >= 0 && (int64_t)ph < c.num_phys) {
-      phys = ph;
-      ntok = min(S, N - e * S);
+  const bool alone = item.own || attend_prefix<T, D, S, kAcross, kNT>(c, a, item, hkv, ring);
+  asm volatile("" ::: "memory");  // (one way on; with two, values of the chunk code are formed in front of the products and take their registers)
+  if (!alone) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+#pragma unroll 1
+  for (int i = 0, members = item.own ? 1 : item.rows / G; i < members; ++i) {
+    if (i > 0) __syncthreads();  // the LDS is the next one's
+    int lane = threadIdx.x % kWave;
+    asm volatile("" : "+v"(lane));  // nothing of a turn is formed before the loop, where it would take registers
+    int b = item.seq;
+    if (!item.own) {
+      b = a.groups.members ? a.groups.members[item.place + i] : item.place + i;
+      if (b < 0 || b >= c.B) continue;  // (uniform)
     }
-  };
-  decode_chunk<D, S, G, kNT>(c, reinterpret_cast<const T*>(a.q), chunk, wave, lane, lookup, a.scale_log2, to,
-                             *reinterpret_cast<DecodeShared<T, D, G>*>(ring));
+    const int N = c.seq_lens[b], end = item.own ? item.end : min(item.end, prefix_pages_of(N, S));
+    const int64_t part = (int64_t)hkv * a.shape.max_rows + item.part + i * G;
+    const ChunkOut<T> to = {a.work.part_o + part * D, a.work.part_ml + part * 2, reinterpret_cast<T*>(a.out), a.lse_out, 2};
+    const Chunk chunk = {hkv, b, item.begin, end, N, 0};
+    auto lookup = [&](int e, bool, int& phys, int& ntok) {
+      const int ph = c.page_table[(int64_t)b * c.max_pages + e];
+      if (ph >= 0 && (int64_t)ph < c.num_phys) {
+        phys = ph;
+        ntok = min(S, N - e * S);
+      }
+    };
+    decode_chunk<D, S, G, kNT>(c, reinterpret_cast<const T*>(a.q), chunk, wave, lane, lookup, a.scale_log2, to,
+                               *reinterpret_cast<DecodeShared<T, D, G>*>(ring));
+  }
 }
 
 // A chunk of a member's pages, prefix and own: calls with little to read (prefix_plan.hpp). A member's group is the first that ends behind it.
