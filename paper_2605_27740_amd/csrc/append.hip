@@ -6,8 +6,8 @@
 // Memory bounds it: every element is read and written once. A lane holds two 16-byte pieces of a head, those whose channels are paired if the
 // pairs are halves of the head, so a pair never leaves its lane; D / (2 * 16 bytes) lanes hold a head and a wave 4 to 16 heads at a time. All heads of a token
 // share their angles: lane i of the wave forms those of pair i once, in turns and in 64 bits (a position of 2^20 times a frequency
-// leaves 2^-33 of a turn, where 32 bits would leave 2^-4), and the wave takes them from the LDS. Sine and cosine are formed in 64 bits, too, and rounded once: that takes
-// as long as 32-bit ones (us: 8192 tokens of 48 bf16 heads 40.1 / 40.4, 65536 of 80 453 / 448), which left fp32 heads 1.6 times as far from 64 bits as a plain form.
+// leaves 2^-33 of a turn, where 32 bits would leave 2^-4), and the wave takes them from the LDS. Sine and cosine are formed in 64 bits as well, and rounded once: by a
+// function of 32 bits fp32 heads were 1.6 times as far from 64 bits as a plain form's. us in 64 / 32 bits: 8192 tokens of 48 bf16 heads 40.1 / 40.4, 65536 of 80 453 / 448.
 #include <type_traits>
 
 #include "decode_core.hpp"
@@ -174,9 +174,9 @@ hipError_t launch_append(const CacheView& c, const AppendArgs& a, hipStream_t st
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value, kHeads = kWave / (D / Elem<T>::kVec / 2);
     const int steps = (c.H + 2 * c.Hkv + kHeads - 1) / kHeads;
-    // Two steps a wave, whose angles and weights are formed once, or one where they are little of the time: fp32 heads and calls without norm, in long calls. us, all of a token /
-    // two steps / one: 8192 bf16 tokens of 48 heads 45.5 / 41.2 / 44.6; 24000 of 80 heads 196 / 173 / 187, 65536 511 / 470 / 505, without norm 507 / 472 / 448; 16384 fp32 tokens of 48
-    // heads 157 / 147 / 142. Three steps: 44.1, 177, 482. And one where all waves of one step run at once: 32 tokens 5.0 / 4.1 (the kernel).
+    // Two steps a wave, whose angles and weights are formed once, or one where they are little of the time: fp32 heads and calls without norm, in long calls. us, two
+    // steps / one, back to back on one set of rows: 8192 bf16 tokens of 48 heads 33.4 / 33.3, 24000 of 80 heads 165 / 177, 65536 445 / 479, without norm 473 / 430; 16384 fp32 tokens of 48 heads
+    // 138 / 134. And one where all waves of one step run at once: 32 tokens 5.0 / 4.1 (the kernel).
     const bool one = (int64_t)a.rows * steps <= 8192 || (a.rows >= 16384 && (!a.how.q_weight || c.dtype == 0));
     const int per = one ? 1 : 2, parts = (steps + per - 1) / per;
     const int64_t items = (int64_t)a.rows * parts;

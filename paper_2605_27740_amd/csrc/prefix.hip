@@ -10,15 +10,16 @@
 // (lane / 32) + i % 4), so its softmax needs no other lane but lane ^ 32, and these are the k that the lane supplies to O^T = V^T P^T: probabilities never
 // leave their lane. V^T comes out of the LDS by its transposing read.
 // Probabilities enter the second product with all 24 bits, as three parts of 8 (exactly), three products instead of one: with 8 bits an output whose terms cancel was off by 2^-9 of the
-// terms, and two tokens of opposite values whose weights are nearly the same gave 0. us with one product / three: 256 sequences behind 32768 tokens 182 / 285, 16 behind 131072 100.5 / 107 to 113, 32 behind 8192
-// 37.2 / 42.7, six groups of 10 102 / 107. The parts are made just before they are used, for 8 of a lane's 16 tokens at a time; between the products before, where registers end at 64 rows,
+// terms, and two tokens of opposite values whose weights are nearly the same gave 0. us with one product / three: 256 sequences behind 32768 tokens 182 / 271 to 281, 16 behind 131072 100.5 / 108 to 110, 32 behind 8192
+// 37.2 / 41.6, six groups of 10 102 / 106. The parts are made just before they are used, for 8 of a lane's 16 tokens at a time; between the products before, where registers end at 64 rows,
 // 119 instead of 112 us behind 131072 tokens, 284 instead of 291 behind 32768.
 // fp32 caches: the same on v_mfma_f32_32x32x2_f32, whose probabilities stay fp32, with tiles of 32 tokens.
 //
-// What bounds it, at 8 KV heads of 128 channels, bf16, pages of 16 or 32: the stream of keys and values up to some 30 sequences in a group (16 behind 131072 tokens: 552 MB in 94 us with the plan in
-// front, 6.1 TB/s behind it; six groups of 10 with 8 heads each, 1000 to 50000 tokens, 95 us, 5.8), behind it the matrix cores and vector units together (256 behind 32768 tokens: 138 GFLOP in 159 to 170 us, of
-// which the last 20 are the members' own 128 MB; matrix cores 45 % busy, vector units as much, and the clock falls with the power that they take: 197 us in a long run).
-// Own pages by the same way through the LDS as prefixes: 32 x 8192 tokens with 50 to 2000 of their own 39.4 / 45.0 us; four members with few pages in a workgroup: 39.3 / 43.5.
+// What bounds it, at 8 KV heads of 128 channels, bf16, pages of 16 or 32: the stream of keys and values up to some 30 sequences in a group (16 behind 131072 tokens: 552 MB in 97 us with the plan in
+// front, 5.7 TB/s, matrix cores and vector units 36 % busy; six groups of 10 with 8 heads each, 1000 to 50000 tokens, 100 us, 5.4 TB/s), behind it the matrix cores and vector units together (256 behind 32768 tokens:
+// 138 GFLOP, with three parts of a probability 276 of products, in 265 to 280 us, of which the last 20 are the members' own 128 MB; matrix cores 58 % busy, vector units 52, and the clock falls with the power that
+// they take: 312 us in a long run).
+// Own pages by the same way through the LDS as prefixes (measured with one part): 32 x 8192 tokens with 50 to 2000 of their own 39.4 / 45.0 us; four members with few pages in a workgroup: 39.3 / 43.5.
 #include <type_traits>
 
 #include "prefix_items.hpp"
@@ -73,7 +74,7 @@ __device__ __forceinline__ void wait_units(int left) {
 // they stand between each other in the code).
 // -> true: nothing has been written, and each member has to be attended by itself. A sum is not finite, and some rows have tokens here that others have not: a product of the others'
 // probability, 0, with an infinity or NaN among the values is not 0. (Looking at the values of such tiles beforehand took 216 us for 105, 16 sequences behind 131072 tokens, one of
-// them of one token.)
+// them of one token. Where such a value is, behind the end of one of them: 588 us; 256 behind 32768 tokens 2175 for 287.)
 template <typename T, int D, int S, int kAcross, bool kNT>
 __device__ __forceinline__ bool attend_prefix(const CacheView& c, const PrefixArgs& a, const PrefixItem& item, int hkv, char* ring) {
   using L = Unit<T, D, kAcross>;

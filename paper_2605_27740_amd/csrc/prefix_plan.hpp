@@ -14,8 +14,8 @@ constexpr int kPrefixMostPages = 512;  // of an item of a prefix, whose page ids
 constexpr int kPrefixMostWorkgroups = (1 << 24) - 1;  // of 256 threads, of which a launch has fewer than 2^32
 
 // Where there is little to read, every member reads its prefix for itself, in chunks that the host cuts, mostly out of the caches: there is no plan, and nothing to join if a chunk is all. Shared / each
-// for itself, us: 2 x 2148 tokens (fp32, 2 heads of 64, 4 MB) 15.6 / 9.4, 2 x 300 (8 heads, bf16) 13.1 / 7.1, 8 x 1100 (34 MB) 15.4 / 11.5, 16 x 1500 (94 MB) 17.4 / 17.3, 4 x 8500 (133 MB) 22.3 / 24.1.
-// If a chunk is all, up to 256 MB: 245 x 57 tokens (32 heads, 245 MB) 78.5 / 60.5, 64 x 768 in 8 groups (192 MB) 21.5 / 20.0, 128 x 520 (264 MB) 25.2 / 27.7. In fp32, whose products take long, up to 160:
+// for itself, us: 2 x 2148 tokens (fp32, 2 heads of 64, 4 MB) 15.6 / 9.4, 2 x 300 (8 heads, bf16) 12.5 / 6.8, 8 x 1100 (34 MB) 14.3 / 10.8, 16 x 1500 (94 MB) 15.8 / 17.4, 4 x 8500 (133 MB) 21.7 / 24.4.
+// If a chunk is all, up to 256 MB: 245 x 57 tokens (32 heads, 245 MB) 70.4 / 59.1, 64 x 768 in 8 groups (192 MB) 21.6 / 19.2, 128 x 520 (264 MB) 27.2 / 25.8. In fp32, whose products take long, up to 160:
 // 57 x 1769 (one head, 99 MB) 24.0 / 20.7, 67 x 2039 in 5 groups (134 MB) 25.4 / 25.5, 4 x 4500 (141 MB) 35.2 / 28.7, 20 x 2865 of 64 channels (225 MB) 23.2 / 29.1, 2 x 14065 (220 MB) 57.3 / 45.7.
 constexpr int64_t prefix_alone_bytes(bool one_chunk, int elem) { return (one_chunk ? 256ll : (elem == 4 ? 160ll : 64ll)) << 20; }
 // Tokens of such a chunk at least, and half as many again if that is all of them: 2 x 600 tokens in one chunk or two 9.5 / 10.5 us, 900 12.3 / 11.9; chunks of 256, 512 and 1024 tokens at least, 8 x 1100
@@ -57,8 +57,8 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   s.tile_pages = (elem == 4 ? 32 : 64) / page_size;
   s.row_tokens = elem == 4 ? 2 : 8;
   const int64_t blocks = std::min<int64_t>(num_groups * ((most + s.rows - 1) / s.rows), (int64_t)batch * group / s.rows + num_groups);
-  // An eighth fewer items than fit leave room for the short ones, unless a prefix's items are many blocks' anyway. 512 / 448, us: 16 x 131072 tokens 108.5 / 101.8, 24 x 100000 103.7 / 97.2, 32 x 8192 40.2 /
-  // 38.8, 60 rows in 6 groups 107.2 / 105.1, 12 x 30000 with up to 3000 of their own 53.8 / 54.9; 256 x 32768, eight blocks, 182 / 193.
+  // An eighth fewer items than fit leave room for the short ones, unless a prefix's items are many blocks' anyway. 512 / 448, us: 16 x 131072 tokens 110.6 / 107.8, 24 x 100000 107 / 110, 32 x 8192 40.4 / 41.6,
+  // 60 rows in 6 groups 106.4 / 105.9 (with one bf16 part of a probability instead of three 108.5 / 101.8, 103.7 / 97.2, 40.2 / 38.8, 107.2 / 105.1; 256 x 32768, eight blocks, 182 / 193).
   s.wanted = std::max((blocks > 2 * num_groups ? kPrefixSlots : kPrefixSlots / 8 * 7) / kv_heads, 1);
   // A source's items are one more than its share of the wanted ones at most, and hold a tile each. A member who is alone in a group has its prefix as their own.
   const int64_t longest = blocks * max_prefix_pages / kPrefixMostPages, prefix_tiles = blocks * ((max_prefix_pages + s.tile_pages - 1) / s.tile_pages);
@@ -71,8 +71,8 @@ inline PrefixShape prefix_shape(int batch, int kv_heads, int group, int elem, in
   s.fits = items <= kPrefixMostWorkgroups / kv_heads && all_rows <= INT32_MAX;
   s.max_items = s.fits ? (int32_t)items : 0;
   s.max_rows = s.fits ? (int32_t)all_rows : 0;
-  // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us (512 items wanted): 2 x 2148 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, 776 workgroups) 40.0 / 38.6,
-  // 16 x 131072 (648) 107.6 / 107.2, 60 rows in 6 groups (1048) 107.6 / 108.5.
+  // The plan takes a workgroup 2.5 us, and a kernel of its own 5. By a kernel / by all, us (512 items wanted): 2 x 2148 tokens (fp32, 2 heads) 17.5 / 15.0, 32 x 8192 (8 heads, with 1000 of their own) 47.6 /
+  // 43.6, 16 x 131072 108.1 / 105.8, 60 rows in 6 groups of 20000 tokens 158.9 / 157.8.
   s.plans = num_groups + batch < 256 && (int64_t)s.max_items * kv_heads <= 2 * kPrefixSlots;
   return s;
 }
